@@ -59,6 +59,10 @@ extern "C" {
 #define CADD_STATUS_COST_NONPOSITIVE    32   /* C_d + C_v(n) <= 0 (or not finite) was met; expansion stopped there */
 #define CADD_STATUS_BAD_N_NODES         64   /* verify: n_nodes[b] was outside [0, R-1] and was clamped */
 #define CADD_STATUS_BAD_TABLE_IDX      256   /* build, CADD_COST_TABLE: table_idx[b] was outside [0, n_tables); the request returns the empty tree */
+#define CADD_STATUS_BAD_PAGE           512   /* cache: an entry of block_table in use was outside [0, n_pages); its tokens are neither read nor written */
+#define CADD_STATUS_BAD_LENGTH        1024   /* cache: length / base_length / start / count / n_rows / path_len was out of range and was clamped */
+#define CADD_STATUS_CACHE_FULL        2048   /* cache append: the request's pages could not hold every row; those beyond were dropped */
+#define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out */
 #define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax */
 
 #define CADD_DTYPE_BF16 0
@@ -297,6 +301,177 @@ typedef struct cadd_fit_args {
     int32_t* status;               /* [n_tables] out: CADD_FIT_STATUS_* bits, 0 = optimal; may be NULL */
 } cadd_fit_args;
 
+/*
+ * A paged key/value cache, as the cadd_cache_* calls and cadd_tree_attention see it.  The token at place p of request b
+ * lives in page block_table[b, p / page_size], slot p % page_size.  Keys and values are pools of token rows of head_dim
+ * elements; the row of (page, head, slot) is number  page * stride_page + head * stride_head + slot * stride_slot  of
+ * every pool (so [n_pages, heads, page_size, ...] and [n_pages, page_size, heads, ...] both fit).  Requests may share
+ * pages that are only read.
+ *   CADD_CACHE_BF16  k, v: bf16, head_dim elements a row.
+ *   CADD_CACHE_FP4   k, v: e2m1 codes, two to a byte (the even element in the low four bits), head_dim / 2 bytes a row;
+ *                    k_scale, v_scale: one e4m3 scale (never negative) for 16 elements along the row, head_dim / 16 bytes.
+ *                    An element stands for  code * scale * 2^-k_exp  (2^-v_exp for values).  Stored is, of x * 2^k_exp:
+ *                    scale = e4m3(max|x| / 6) over the 16, code = e2m1(x / scale), both to nearest even and saturating;
+ *                    a zero scale has zero codes; NaN is stored as zero.  The exponents, -16..16, move a model's values
+ *                    into e4m3's range (blocks whose largest value is below 2^-9 lose precision otherwise).
+ * Unused slots and pages are never read.
+ */
+#define CADD_CACHE_BF16 0
+#define CADD_CACHE_FP4  1
+typedef struct cadd_cache {
+    uint32_t struct_size;          /* = sizeof(cadd_cache) */
+    int32_t  format;               /* CADD_CACHE_* */
+    int32_t  batch;
+    int32_t  heads;                /* key/value heads */
+    int32_t  head_dim;             /* 64 or 128 */
+    int32_t  page_size;            /* a power of two, 1..65536 */
+    int32_t  max_pages;            /* columns of block_table; max_pages * page_size < 2^30 */
+    int32_t  k_exp, v_exp;         /* FP4: -16..16; BF16: 0 */
+    int32_t  reserved0;
+    int64_t  n_pages;              /* pages in the pools, < 2^31 */
+    int64_t  stride_page, stride_head, stride_slot;   /* in rows, >= 1 */
+    void*    k;                    /* 16-byte aligned */
+    void*    v;                    /* 16-byte aligned */
+    void*    k_scale;              /* FP4: 8-byte aligned; BF16: ignored */
+    void*    v_scale;
+    const int32_t* block_table;    /* [batch, max_pages]; an entry in use outside [0, n_pages) is never followed: CADD_STATUS_BAD_PAGE */
+    const int32_t* length;         /* [batch] tokens in the cache, clamped to [0, max_pages * page_size] */
+} cadd_cache;
+
+/*
+ * Arguments of cadd_cache_append: rows of k and v are written behind each request's `length` tokens.  With `path`
+ * (accepted_nodes and accepted_len of a verification): row 0, the root, then rows path[b, 0 .. path_len[b]-1].  Without:
+ * rows 0 .. n_rows[b]-1 (a prompt, or one decoded token).
+ */
+typedef struct cadd_append_args {
+    uint32_t struct_size;          /* = sizeof(cadd_append_args) */
+    uint32_t flags;                /* reserved, 0 */
+    int32_t  R;                    /* rows of k and v per request */
+    int32_t  L;                    /* columns of path */
+    const void* k;                 /* bf16 [batch, R, heads, head_dim], last axis contiguous, 16-byte aligned */
+    const void* v;
+    int64_t  stride_b, stride_row, stride_head;      /* of k and of v, in elements, multiples of 8 */
+    const int32_t* n_rows;         /* [batch], NULL => R; ignored with path */
+    const int32_t* path;           /* [batch, L] or NULL */
+    const int32_t* path_len;       /* [batch], required with path */
+    int32_t* new_length;           /* [batch] out: length + rows written; may be cache.length itself */
+    int32_t* status;               /* [batch] CADD_STATUS_* bits, may be NULL */
+    cadd_cache cache;
+} cadd_append_args;
+
+/*
+ * Arguments of cadd_cache_read: places start[b] .. start[b]+count[b]-1 of the cache as bf16 rows (of a 4-bit cache: what
+ * the codes stand for, which bf16 holds exactly).  Row i of the output is place start[b] + i; output rows from the number
+ * of rows read on are left as they were.
+ */
+typedef struct cadd_read_args {
+    uint32_t struct_size;          /* = sizeof(cadd_read_args) */
+    uint32_t flags;                /* reserved, 0 */
+    int32_t  n_max;                /* rows of the outputs per request */
+    int32_t  reserved0;
+    const int32_t* start;          /* [batch], NULL => 0 */
+    const int32_t* count;          /* [batch], NULL => up to length; at most n_max and length - start are read */
+    void*    k;                    /* out: bf16 [batch, n_max, heads, head_dim], last axis contiguous, 16-byte aligned */
+    void*    v;
+    int64_t  stride_b, stride_row, stride_head;      /* of k and of v, in elements, multiples of 8 */
+    int32_t* status;               /* [batch], may be NULL */
+    cadd_cache cache;
+} cadd_read_args;
+
+/*
+ * Arguments of cadd_tree_attention: what the target's forward pass over a draft tree needs between building the tree and
+ * verifying it (Section 3.3: a node attends to the context and to its own ancestors).  For every live row r and query
+ * head h, with g = h / (heads_q / heads) its key/value head:
+ *     out[r,h] = sum_p softmax_p(scale * q[r,h] . k[p,g]) v[p,g],     lse[r,h] = log sum_p exp(scale * q[r,h] . k[p,g])
+ * over the cached places p = 0 .. length-1 and the tree's own rows c (k, v), as far as r sees them:
+ *     cached place p: window = 0, or p < n_sinks, or p > length + depth[r] - window;
+ *     tree row c:     bit c of mask_bits row r (mask_bits NULL: c <= r, the rows of a prompt chunk), and
+ *                     window = 0, or depth[r] - depth[c] < window, or length + depth[c] < n_sinks.
+ * One decoded token is R = 1.  A row that sees nothing (or only scores of -Inf) gets 0 and lse -Inf.  What a row does not
+ * see has no influence on it, whatever it holds.  Products are bf16 with fp32 sums, the softmax is fp32, its weights are
+ * rounded to bf16 for the product with the values (relative error at most 2^-8 each).
+ * Rows above n_nodes[b] are left as they were in out and lse.
+ */
+typedef struct cadd_attention_args {
+    uint32_t struct_size;          /* = sizeof(cadd_attention_args) */
+    uint32_t flags;                /* 0, or CADD_ATTENTION_TILED_PATH */
+    int32_t  R;                    /* row capacity, 1..65536 */
+    int32_t  heads_q;              /* a multiple of cache.heads */
+    int32_t  window;               /* 0: none */
+    int32_t  n_sinks;              /* 0..2^30 */
+    float    scale;                /* > 0 */
+    int32_t  reserved0;
+    const void* q;                 /* bf16 [batch, R, heads_q, head_dim]; strides in elements, multiples of 8; 16-byte aligned */
+    int64_t  q_stride_b, q_stride_row, q_stride_head;
+    const void* k;                 /* bf16 [batch, R, heads, head_dim], the tree's own rows */
+    const void* v;
+    int64_t  kv_stride_b, kv_stride_row, kv_stride_head;
+    const int32_t* n_nodes;        /* [batch] as from cadd_build_tree: rows 0..n_nodes[b] are live; NULL => R-1; -1: none.
+                                      Outside [-1, R-1]: clamped, CADD_STATUS_BAD_N_NODES */
+    const uint32_t* mask_bits;     /* [batch, R, ceil(R/32)] as from cadd_build_tree, or NULL */
+    const int32_t* depth;          /* [batch, R]; NULL => the row's number (allowed where mask_bits is NULL or window is 0) */
+    void*    out;                  /* bf16 [batch, R, heads_q, head_dim] */
+    int64_t  out_stride_b, out_stride_row, out_stride_head;
+    float*   lse;                  /* [batch, R, heads_q], natural logarithm; may be NULL */
+    int32_t* status;               /* [batch], may be NULL */
+    void*    workspace;            /* >= cadd_tree_attention_workspace_bytes, 256-byte aligned */
+    size_t   workspace_bytes;
+    cadd_cache cache;              /* length: the tokens before the tree */
+} cadd_attention_args;
+
+/*
+ * Arguments of cadd_cache_weights: the attention weight that a round's accepted rows spent on each cached place, added to
+ * a running total, from which cadd_cache_evict chooses.  Called after the rows have been appended: accepted row i (row 0,
+ * then path) sits at place base_length[b] + i.  For every place p < length[b], with E_i(p) = sum over the heads of the
+ * group of exp(scale * q[i] . k[p] - lse[i]) for rows i that see p (p <= base_length + i; window, n_sinks as above with
+ * base_length + i as the row's place):
+ *     weights_out[b, head, p] = (p < base_length[b] ? weights[b, head, p] : 0) + sum_i E_i(p).
+ * Places from length[b] on are left as they were.  A row whose lse is -Inf or +Inf adds nothing.
+ */
+typedef struct cadd_weights_args {
+    uint32_t struct_size;          /* = sizeof(cadd_weights_args) */
+    uint32_t flags;                /* reserved, 0 */
+    int32_t  R, L, heads_q;
+    int32_t  window, n_sinks;
+    float    scale;                /* > 0 */
+    const void* q;                 /* as in cadd_attention_args */
+    int64_t  q_stride_b, q_stride_row, q_stride_head;
+    const float* lse;              /* [batch, R, heads_q] */
+    const int32_t* n_rows;         /* [batch] without path: rows 0..n_rows-1; NULL => R */
+    const int32_t* path;           /* [batch, L] or NULL */
+    const int32_t* path_len;       /* [batch], required with path */
+    const int32_t* base_length;    /* [batch] tokens before the append, at most length */
+    const float* weights;          /* [batch, heads, stride >= max_pages * page_size] */
+    float*   weights_out;          /* the same shape; may be weights itself */
+    int64_t  weights_stride;       /* elements from one head to the next, of both */
+    int32_t* status;               /* [batch], may be NULL */
+    cadd_cache cache;
+} cadd_weights_args;
+
+/*
+ * Arguments of cadd_cache_evict: every (request, head) keeps at most `budget` of its places: the first n_sinks, the last
+ * n_recent and, of the places between, those with the largest weights (equal weights: the lower place; NaN counts as the
+ * lowest).  The rows that stay are copied, in order, to the places 0, 1, ... of new pages (new_block_table), their weights
+ * with them; the old pages stay as they are, for requests that share them.  A request with at most `budget` tokens keeps
+ * all.  New pages must not be among the pages in use.
+ */
+typedef struct cadd_evict_args {
+    uint32_t struct_size;          /* = sizeof(cadd_evict_args) */
+    uint32_t flags;                /* reserved, 0 */
+    int32_t  budget;               /* 1 .. new_max_pages * page_size, >= n_sinks + n_recent */
+    int32_t  n_sinks, n_recent;
+    int32_t  new_max_pages;        /* columns of new_block_table */
+    const float* weights;          /* [batch, heads, weights_stride >= max_pages * page_size] */
+    int64_t  weights_stride;       /* elements from one head to the next */
+    const int32_t* new_block_table;/* [batch, new_max_pages] */
+    int32_t* new_length;           /* [batch] out; may be cache.length itself */
+    int32_t* kept;                 /* [batch, heads, budget] out: the places that stay, ascending, -1 behind them */
+    float*   weights_out;          /* [batch, heads, weights_out_stride >= budget] out, may be NULL; not weights itself */
+    int64_t  weights_out_stride;
+    int32_t* status;               /* [batch], may be NULL */
+    cadd_cache cache;
+} cadd_evict_args;
+
 /* ABI version of the loaded library (CADD_ABI_VERSION it was built with). */
 int cadd_version(void);
 
@@ -349,6 +524,26 @@ int cadd_verify_tree_sampled(const cadd_sample_args* a, void* cuda_stream);
 /* Convex, non-decreasing least-squares fit of every row (see cadd_fit_args).  Asynchronous on `cuda_stream`: one
  * kernel, one CTA per row, fp64.  CADD_ERR_SHAPE if N > CADD_FIT_MAX_N. */
 int cadd_fit_cost_tables(const cadd_fit_args* a, void* cuda_stream);
+
+/* Rows into a paged cache (see cadd_append_args) and back out of it (see cadd_read_args).  Asynchronous on `cuda_stream`:
+ * one kernel (a second, tiny one where new_length is cache.length). */
+int cadd_cache_append(const cadd_append_args* a, void* cuda_stream);
+int cadd_cache_read(const cadd_read_args* a, void* cuda_stream);
+
+/* Scratch size of cadd_tree_attention: pure host arithmetic on R, heads_q and the cache's shape. */
+int cadd_tree_attention_workspace_bytes(const cadd_attention_args* a, size_t* out);
+
+/* Attention of tree rows over the paged cache and the tree (see cadd_attention_args).  Asynchronous on `cuda_stream`:
+ * two kernels (attention over equal shares of all keys, then the join of the rows whose keys were shared out). */
+int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream);
+
+/* Attention weight of the accepted rows, added up per cached place (see cadd_weights_args).  Asynchronous on
+ * `cuda_stream`: one kernel.  The same inputs give the same bits. */
+int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream);
+
+/* Eviction by accumulated weight into new pages (see cadd_evict_args).  Asynchronous on `cuda_stream`: two kernels
+ * (choice, copy). */
+int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream);
 
 /*
  * cadd_build_tree for callers that cannot provide scratch memory.  (The paper has no counterpart to

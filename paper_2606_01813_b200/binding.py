@@ -21,6 +21,8 @@ ERR_NULL, ERR_STRUCT_SIZE, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_WORKSPACE, ERR_L
 STATUS_NONFINITE_INPUT, STATUS_FEWER_THAN_K_FINITE, STATUS_CAP_HIT, STATUS_FRONTIER_EXHAUSTED = 1, 2, 4, 8
 STATUS_L_EFF_CLAMPED, STATUS_COST_NONPOSITIVE, STATUS_BAD_N_NODES, STATUS_INTERNAL_TIMEOUT = 16, 32, 64, 128
 STATUS_BAD_TABLE_IDX = 256
+STATUS_BAD_PAGE, STATUS_BAD_LENGTH, STATUS_CACHE_FULL, STATUS_BAD_PATH = 512, 1024, 2048, 4096
+CACHE_BF16, CACHE_FP4 = 0, 1
 DTYPE_BF16, DTYPE_FP32 = 0, 1
 COST_QUADRATIC, COST_TABLE, COST_TABLE_INTERP = 0, 1, 2
 FLAG_EMIT_DENSE_MASK, FLAG_EMIT_TOPK, FLAG_FIXED_BUDGET = 1, 2, 4
@@ -35,7 +37,9 @@ ROWS_LIVE, ROWS_DENSE = 0, 1
 EXPORTS = ("cadd_version", "cadd_status_string", "cadd_build_workspace_bytes", "cadd_verify_workspace_bytes",
            "cadd_build_tree", "cadd_verify_tree", "cadd_build_tree_static_scratch", "cadd_build_launches", "cadd_verify_launches",
            "cadd_head_workspace_bytes", "cadd_verify_tree_fused_head", "cadd_fit_cost_tables",
-           "cadd_build_head_workspace_bytes", "cadd_build_tree_fused_head", "cadd_verify_tree_sampled")
+           "cadd_build_head_workspace_bytes", "cadd_build_tree_fused_head", "cadd_verify_tree_sampled",
+           "cadd_cache_append", "cadd_cache_read", "cadd_tree_attention_workspace_bytes", "cadd_tree_attention",
+           "cadd_cache_weights", "cadd_cache_evict")
 ERR_STATIC_SCRATCH = -8
 STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -115,6 +119,67 @@ class FitArgs(C.Structure):
     ]
 
 
+class CacheArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("format", C.c_int32), ("batch", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+        ("page_size", C.c_int32), ("max_pages", C.c_int32), ("k_exp", C.c_int32), ("v_exp", C.c_int32), ("reserved0", C.c_int32),
+        ("n_pages", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_slot", C.c_int64),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("block_table", C.c_void_p), ("length", C.c_void_p),
+    ]
+
+
+class AppendArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("R", C.c_int32), ("L", C.c_int32),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("stride_b", C.c_int64), ("stride_row", C.c_int64), ("stride_head", C.c_int64),
+        ("n_rows", C.c_void_p), ("path", C.c_void_p), ("path_len", C.c_void_p), ("new_length", C.c_void_p), ("status", C.c_void_p),
+        ("cache", CacheArgs),
+    ]
+
+
+class ReadArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("n_max", C.c_int32), ("reserved0", C.c_int32),
+        ("start", C.c_void_p), ("count", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+        ("stride_b", C.c_int64), ("stride_row", C.c_int64), ("stride_head", C.c_int64), ("status", C.c_void_p),
+        ("cache", CacheArgs),
+    ]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("R", C.c_int32), ("heads_q", C.c_int32),
+        ("window", C.c_int32), ("n_sinks", C.c_int32), ("scale", C.c_float), ("reserved0", C.c_int32),
+        ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64),
+        ("k", C.c_void_p), ("v", C.c_void_p), ("kv_stride_b", C.c_int64), ("kv_stride_row", C.c_int64), ("kv_stride_head", C.c_int64),
+        ("n_nodes", C.c_void_p), ("mask_bits", C.c_void_p), ("depth", C.c_void_p),
+        ("out", C.c_void_p), ("out_stride_b", C.c_int64), ("out_stride_row", C.c_int64), ("out_stride_head", C.c_int64),
+        ("lse", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("cache", CacheArgs),
+    ]
+
+
+class WeightsArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("R", C.c_int32), ("L", C.c_int32), ("heads_q", C.c_int32),
+        ("window", C.c_int32), ("n_sinks", C.c_int32), ("scale", C.c_float),
+        ("q", C.c_void_p), ("q_stride_b", C.c_int64), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64),
+        ("lse", C.c_void_p), ("n_rows", C.c_void_p), ("path", C.c_void_p), ("path_len", C.c_void_p), ("base_length", C.c_void_p),
+        ("weights", C.c_void_p), ("weights_out", C.c_void_p), ("weights_stride", C.c_int64), ("status", C.c_void_p),
+        ("cache", CacheArgs),
+    ]
+
+
+class EvictArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("budget", C.c_int32), ("n_sinks", C.c_int32), ("n_recent", C.c_int32),
+        ("new_max_pages", C.c_int32), ("weights", C.c_void_p), ("weights_stride", C.c_int64), ("new_block_table", C.c_void_p),
+        ("new_length", C.c_void_p), ("kept", C.c_void_p), ("weights_out", C.c_void_p), ("weights_out_stride", C.c_int64),
+        ("status", C.c_void_p), ("cache", CacheArgs),
+    ]
+
+
 _lib = None
 
 
@@ -142,6 +207,12 @@ def lib() -> C.CDLL:
         l.cadd_build_tree_static_scratch.argtypes = [C.POINTER(BuildArgs), C.c_void_p]
         l.cadd_build_launches.argtypes = [C.POINTER(BuildArgs)]
         l.cadd_verify_launches.argtypes = [C.POINTER(VerifyArgs)]
+        l.cadd_cache_append.argtypes = [C.POINTER(AppendArgs), C.c_void_p]
+        l.cadd_cache_read.argtypes = [C.POINTER(ReadArgs), C.c_void_p]
+        l.cadd_tree_attention_workspace_bytes.argtypes = [C.POINTER(AttentionArgs), C.POINTER(C.c_size_t)]
+        l.cadd_tree_attention.argtypes = [C.POINTER(AttentionArgs), C.c_void_p]
+        l.cadd_cache_weights.argtypes = [C.POINTER(WeightsArgs), C.c_void_p]
+        l.cadd_cache_evict.argtypes = [C.POINTER(EvictArgs), C.c_void_p]
         _lib = l
     return _lib
 
@@ -605,4 +676,312 @@ def cadd_build_tree_static_scratch(draft_logits: torch.Tensor, K: int, B_max: in
     for t in keep:
         if t is not None:
             t.record_stream(st)
+    return out
+
+
+# ---- the paged key/value cache and the tree attention over it ----
+
+def _need(ok: bool, message: str) -> None:
+    if not ok:
+        raise ValueError(message)
+
+
+def _need_i32(t: Optional[torch.Tensor], shape, dev, name: str) -> Optional[int]:
+    """Pointer of an int32 input of the given shape on the call's device (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _need_rows(t: torch.Tensor, shape, dev, name: str):
+    """Pointer and (batch, row, head) strides of a bf16 operand [batch, rows, heads, head_dim]."""
+    if t.dtype != torch.bfloat16 or t.device != dev or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a bfloat16 tensor {list(shape)} on {dev}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name} must have a contiguous last axis")
+    # an axis of length one may carry any stride; it is never stepped along
+    return t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))
+
+
+def _enqueue(fn, args, dev, stream) -> torch.cuda.Stream:
+    st = _stream_of(stream, dev)
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(C.byref(args), st.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(C.byref(args), st.cuda_stream)
+    if rc != OK:
+        raise CaddError(rc)
+    return st
+
+
+@dataclass(frozen=True)
+class KvCache:
+    """A paged key/value cache (cadd_cache): the pools and a batch's view of them.
+
+    k, v: CUDA tensors [n_pages, heads, page_size, head_dim] in bf16, or in 4 bits as uint8 codes [..., head_dim / 2] with
+    k_scale, v_scale uint8 (e4m3) [..., head_dim / 16].  A token's row must be contiguous; the other axes may be strided
+    alike in all pools (permuted views fit).  block_table [batch, max_pages] and length [batch] are int32 on the same device.
+    In the 4-bit form k_exp and v_exp are the powers of two that rows are multiplied by before they are stored."""
+    k: torch.Tensor
+    v: torch.Tensor
+    block_table: torch.Tensor
+    length: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    k_exp: int = 0
+    v_exp: int = 0
+
+    def __post_init__(self):
+        k, v = self.k, self.v
+        _need(k.is_cuda, "the cache must be on a CUDA device (there is no CPU path)")
+        dev, fp4 = k.device, k.dtype == torch.uint8
+        if k.dtype not in (torch.uint8, torch.bfloat16):
+            raise TypeError(f"unsupported cache dtype {k.dtype}")
+        _need(k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and v.device == dev, "k and v must be alike, [n_pages, heads, page_size, ...]")
+        pools = [k, v]
+        if fp4:
+            ks, vs = self.k_scale, self.v_scale
+            _need(ks is not None and vs is not None, "a 4-bit cache needs k_scale and v_scale")
+            for t in (ks, vs):
+                _need(t.dtype == torch.uint8 and t.device == dev and t.shape == (*k.shape[:3], k.shape[3] // 8) and k.shape[3] % 8 == 0,
+                      "k_scale and v_scale must be uint8 with one scale for 8 bytes of codes")
+            pools += [ks, vs]
+        else:
+            _need(self.k_scale is None and self.v_scale is None, "a bf16 cache has no scales")
+        rows = None
+        for t in pools:
+            _need(t.stride(3) == 1, "a token's row must be contiguous")
+            n = t.shape[3]
+            _need(all(t.stride(i) % n == 0 for i in range(3) if t.shape[i] > 1), "the pools' strides must be whole rows")
+            mine = tuple(t.stride(i) // n if t.shape[i] > 1 else 1 for i in range(3))
+            _need(rows in (None, mine), "all pools must be laid out alike")
+            rows = mine
+        bt = self.block_table
+        _need(bt.dim() == 2 and bt.dtype == torch.int32 and bt.device == dev and bt.is_contiguous(),
+              "block_table must be a contiguous int32 tensor [batch, max_pages] on the cache's device")
+        a = CacheArgs()
+        a.struct_size = C.sizeof(CacheArgs)
+        a.format = CACHE_FP4 if fp4 else CACHE_BF16
+        a.batch, a.max_pages = bt.shape
+        a.n_pages, a.heads, a.page_size = k.shape[:3]
+        a.head_dim = k.shape[3] * (2 if fp4 else 1)
+        a.k_exp, a.v_exp = self.k_exp, self.v_exp
+        a.stride_page, a.stride_head, a.stride_slot = rows
+        a.k, a.v, a.k_scale, a.v_scale = k.data_ptr(), v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale)
+        a.block_table = bt.data_ptr()
+        a.length = _need_i32(self.length, (a.batch,), dev, "length")
+        object.__setattr__(self, "args", a)
+        object.__setattr__(self, "device", dev)
+
+
+@dataclass
+class Attention:
+    """Outputs of cadd_tree_attention (device tensors): out bf16 [batch, R, heads_q, head_dim]; lse fp32 [batch, R, heads_q]
+    and status int32 [batch], which may be None (not written then)."""
+    out: torch.Tensor
+    lse: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None
+
+
+@dataclass
+class Evicted:
+    """Outputs of cadd_cache_evict (device tensors); weights and status may be None (not written then)."""
+    new_length: torch.Tensor
+    kept: torch.Tensor
+    weights: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None
+
+
+def _marshal_rows(a, cache: KvCache, R: int, n_rows, path, path_len) -> None:
+    a.R = R
+    B, dev = cache.args.batch, cache.device
+    if path is not None:
+        _need(path_len is not None and n_rows is None, "path comes with path_len and without n_rows")
+        _need(path.dim() == 2, "path must be [batch, L]")
+        a.L = path.shape[1]
+        a.path = _need_i32(path, (B, a.L), dev, "path")
+        a.path_len = _need_i32(path_len, (B,), dev, "path_len")
+    else:
+        _need(path_len is None, "path_len comes with path")
+        a.n_rows = _need_i32(n_rows, (B,), dev, "n_rows")
+
+
+def cadd_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, n_rows=None, path=None, path_len=None,
+                      new_length: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Write rows of k and v (bf16 [batch, R, heads, head_dim]) behind each request's cached tokens: rows 0..n_rows[b]-1
+    (all R without n_rows), or with path / path_len (a verification's accepted_nodes / accepted_len) the root and the accepted
+    path.  Returns new_length (which may be given, cache.length itself included: the cache then goes on from there)."""
+    c, dev = cache.args, cache.device
+    _need(k.dim() == 4 and k.shape[0] == c.batch, "k must be [batch, R, heads, head_dim]")
+    shape = (c.batch, k.shape[1], c.heads, c.head_dim)
+    a = AppendArgs()
+    a.struct_size = C.sizeof(AppendArgs)
+    a.cache = c
+    a.k, *strides = _need_rows(k, shape, dev, "k")
+    a.v, *vs = _need_rows(v, shape, dev, "v")
+    _need(strides == vs, "k and v must have the same strides")
+    a.stride_b, a.stride_row, a.stride_head = strides
+    _marshal_rows(a, cache, k.shape[1], n_rows, path, path_len)
+    if new_length is None:
+        new_length = torch.empty(c.batch, dtype=torch.int32, device=dev)
+    a.new_length = _need_i32(new_length, (c.batch,), dev, "new_length")
+    a.status = _need_i32(status, (c.batch,), dev, "status")
+    _enqueue(lib().cadd_cache_append, a, dev, stream)
+    return new_length
+
+
+def cadd_cache_read(cache: KvCache, n_max: int, *, start=None, count=None, out=None, status: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None):
+    """Cached rows as bf16: out = (k, v), each [batch, n_max, heads, head_dim], row i being place start[b] + i (start 0 and
+    count up to the length unless given).  Rows that are not read keep what `out` held (zeros if it is made here)."""
+    c, dev = cache.args, cache.device
+    shape = (c.batch, n_max, c.heads, c.head_dim)
+    if out is None:
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    a = ReadArgs()
+    a.struct_size = C.sizeof(ReadArgs)
+    a.cache = c
+    a.n_max = n_max
+    a.start = _need_i32(start, (c.batch,), dev, "start")
+    a.count = _need_i32(count, (c.batch,), dev, "count")
+    a.k, *strides = _need_rows(out[0], shape, dev, "out k")
+    a.v, *vs = _need_rows(out[1], shape, dev, "out v")
+    _need(strides == vs, "both outputs must have the same strides")
+    a.stride_b, a.stride_row, a.stride_head = strides
+    a.status = _need_i32(status, (c.batch,), dev, "status")
+    _enqueue(lib().cadd_cache_read, a, dev, stream)
+    return out
+
+
+def cadd_tree_attention_workspace_bytes(batch: int, R: int, heads_q: int, cache: KvCache) -> int:
+    a = AttentionArgs()
+    a.struct_size = C.sizeof(AttentionArgs)
+    a.R, a.heads_q = R, heads_q
+    a.cache = cache.args
+    a.cache.batch = batch
+    n = C.c_size_t(0)
+    rc = lib().cadd_tree_attention_workspace_bytes(C.byref(a), C.byref(n))
+    if rc != OK:
+        raise CaddError(rc)
+    return int(n.value)
+
+
+def cadd_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache: KvCache, *, mask_bits=None, n_nodes=None,
+                        depth=None, scale: Optional[float] = None, window: int = 0, n_sinks: int = 0, flags: int = 0,
+                        out: Optional[Attention] = None, workspace: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> Attention:
+    """Attention of a tree's rows (q bf16 [batch, R, heads_q, head_dim]) over the cache and over the tree's own rows (k, v bf16
+    [batch, R, heads, head_dim]) through mask_bits, n_nodes and depth as cadd_build_tree returns them (Section 3.3).
+    Without mask_bits row r sees rows 0..r (a prompt chunk; one decoded token is R = 1).  window > 0: the last `window`
+    places and the first n_sinks only.  scale is 1/sqrt(head_dim) unless given.  Rows above n_nodes keep what `out` held
+    (zeros if it is made here, lse too)."""
+    c, dev = cache.args, cache.device
+    _need(q.is_cuda, "q must be a CUDA tensor (there is no CPU path)")
+    _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
+    R, hq = q.shape[1], q.shape[2]
+    qshape, kvshape = (c.batch, R, hq, c.head_dim), (c.batch, R, c.heads, c.head_dim)
+    a = AttentionArgs()
+    a.struct_size = C.sizeof(AttentionArgs)
+    a.flags = flags
+    a.cache = c
+    a.R, a.heads_q, a.window, a.n_sinks = R, hq, window, n_sinks
+    a.scale = c.head_dim ** -0.5 if scale is None else scale
+    a.q, a.q_stride_b, a.q_stride_row, a.q_stride_head = _need_rows(q, qshape, dev, "q")
+    a.k, *strides = _need_rows(k, kvshape, dev, "k")
+    a.v, *vs = _need_rows(v, kvshape, dev, "v")
+    _need(strides == vs, "k and v must have the same strides")
+    a.kv_stride_b, a.kv_stride_row, a.kv_stride_head = strides
+    a.n_nodes = _need_i32(n_nodes, (c.batch,), dev, "n_nodes")
+    a.mask_bits = _need_i32(mask_bits, (c.batch, R, (R + 31) // 32), dev, "mask_bits")
+    a.depth = _need_i32(depth, (c.batch, R), dev, "depth")
+    if out is None:
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            out = Attention(out=torch.zeros(qshape, dtype=torch.bfloat16, device=dev), lse=torch.zeros(qshape[:3], device=dev),
+                            status=torch.zeros(c.batch, dtype=torch.int32, device=dev))
+    a.out, a.out_stride_b, a.out_stride_row, a.out_stride_head = _need_rows(out.out, qshape, dev, "out")
+    if out.lse is not None:
+        _need(out.lse.dtype == torch.float32 and out.lse.device == dev and tuple(out.lse.shape) == qshape[:3] and out.lse.is_contiguous(),
+              "lse must be a contiguous float32 tensor [batch, R, heads_q]")
+        a.lse = out.lse.data_ptr()
+    a.status = _need_i32(out.status, (c.batch,), dev, "status")
+    made = workspace is None
+    if made:
+        workspace = torch.empty(cadd_tree_attention_workspace_bytes(c.batch, R, hq, cache), dtype=torch.uint8, device=dev)
+    _need(workspace.device == dev and workspace.is_contiguous(), "workspace must be on the call's device")
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = _enqueue(lib().cadd_tree_attention, a, dev, stream)
+    if made:
+        workspace.record_stream(st)
+    return out
+
+
+def _need_weights(w: torch.Tensor, B: int, H: int, n: int, dev, name: str):
+    _need(w.dtype == torch.float32 and w.device == dev and w.dim() == 3 and w.shape[0] == B and w.shape[1] == H and w.shape[2] >= n and w.stride(2) == 1
+          and (B == 1 or w.stride(0) == H * w.stride(1)), f"{name} must be a float32 tensor [batch, heads, >= {n}] with rows of equal stride")
+    return w.data_ptr(), w.stride(1) if B * H > 1 else w.shape[2]
+
+
+def cadd_cache_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache, base_length: torch.Tensor, weights: torch.Tensor, *,
+                       n_rows=None, path=None, path_len=None, scale: Optional[float] = None, window: int = 0, n_sinks: int = 0,
+                       out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Add the attention weight that the accepted rows (rows and lse as in cadd_tree_attention, path / path_len / n_rows as in
+    cadd_cache_append, the rows being in the cache by now) spent on every cached place to weights fp32 [batch, heads, capacity].
+    base_length is the length before the append.  Works in place unless `out` is given."""
+    c, dev = cache.args, cache.device
+    _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
+    R, hq = q.shape[1], q.shape[2]
+    a = WeightsArgs()
+    a.struct_size = C.sizeof(WeightsArgs)
+    a.cache = c
+    _marshal_rows(a, cache, R, n_rows, path, path_len)
+    a.heads_q, a.window, a.n_sinks = hq, window, n_sinks
+    a.scale = c.head_dim ** -0.5 if scale is None else scale
+    a.q, a.q_stride_b, a.q_stride_row, a.q_stride_head = _need_rows(q, (c.batch, R, hq, c.head_dim), dev, "q")
+    _need(lse.dtype == torch.float32 and lse.device == dev and tuple(lse.shape) == (c.batch, R, hq) and lse.is_contiguous(),
+          "lse must be a contiguous float32 tensor [batch, R, heads_q]")
+    a.lse = lse.data_ptr()
+    a.base_length = _need_i32(base_length, (c.batch,), dev, "base_length")
+    out = weights if out is None else out
+    cap = c.max_pages * c.page_size
+    a.weights, a.weights_stride = _need_weights(weights, c.batch, c.heads, cap, dev, "weights")
+    a.weights_out, so = _need_weights(out, c.batch, c.heads, cap, dev, "out")
+    _need(so == a.weights_stride, "weights and out must have the same strides")
+    a.status = _need_i32(status, (c.batch,), dev, "status")
+    _enqueue(lib().cadd_cache_weights, a, dev, stream)
+    return out
+
+
+def cadd_cache_evict(cache: KvCache, weights: torch.Tensor, new_block_table: torch.Tensor, budget: int, *, n_sinks: int = 0,
+                     n_recent: int = 0, out: Optional[Evicted] = None, stream: Optional[torch.cuda.Stream] = None) -> Evicted:
+    """Keep `budget` places of every (request, head): the first n_sinks, the last n_recent and the heaviest between them by
+    weights (as cadd_cache_weights keeps them).  Their rows go, in order, to the pages of new_block_table [batch, pages] in the same
+    pools; the old pages are not changed.  The cache goes on as KvCache(..., block_table=new_block_table,
+    length=result.new_length) with result.weights."""
+    c, dev = cache.args, cache.device
+    B, H = c.batch, c.heads
+    a = EvictArgs()
+    a.struct_size = C.sizeof(EvictArgs)
+    a.cache = c
+    a.budget, a.n_sinks, a.n_recent = budget, n_sinks, n_recent
+    _need(new_block_table.dim() == 2, "new_block_table must be [batch, pages]")
+    a.new_max_pages = new_block_table.shape[1]
+    a.new_block_table = _need_i32(new_block_table, (B, a.new_max_pages), dev, "new_block_table")
+    a.weights, a.weights_stride = _need_weights(weights, B, H, c.max_pages * c.page_size, dev, "weights")
+    if out is None:
+        _need(budget >= 1, "budget must be at least 1")
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            out = Evicted(new_length=torch.empty(B, dtype=torch.int32, device=dev), kept=torch.empty(B, H, budget, dtype=torch.int32, device=dev),
+                          weights=torch.zeros(B, H, a.new_max_pages * c.page_size, device=dev), status=torch.empty(B, dtype=torch.int32, device=dev))
+    a.new_length = _need_i32(out.new_length, (B,), dev, "new_length")
+    a.kept = _need_i32(out.kept, (B, H, budget), dev, "kept")
+    if out.weights is not None:
+        a.weights_out, a.weights_out_stride = _need_weights(out.weights, B, H, budget, dev, "out.weights")
+    a.status = _need_i32(out.status, (B,), dev, "status")
+    _enqueue(lib().cadd_cache_evict, a, dev, stream)
     return out
