@@ -1,0 +1,256 @@
+// How the attention kernels share out their work.
+//
+// An item is (request, key/value head, block of BM rows), a row being one (tree row, query head of the group) pair: all
+// query heads of a group use the same keys, so they stand in one block.  An item's keys are cut into units of 128: the
+// cached places that any of its rows can see (all, or with a window the sinks' units and the window's), then the tree's
+// rows.  All units of all items, one after the other, are cut into equal ranges, one per CTA, whatever the requests'
+// lengths: a CTA works through the ends and wholes of items that its range covers.  An item that lies in one range is
+// finished there; of an item that does not, every range leaves sums (m, l, o) relative to its own maximum, and
+// attn_join_kernel adds them up in range order: the same inputs give the same bits.
+#pragma once
+#include "cache.cuh"
+#include "tile_ring.cuh"
+#include "tree_attention.cuh"
+
+namespace cadd {
+
+constexpr int kUnit = 128;                               // keys per unit
+
+struct AttnWork {
+    AttnParams p;
+    float* records;                                      // [grid][2] partial records of BM x (D + 2) floats
+    int4* items;                                         // [grid] what each range begins with
+};
+
+// The cached units of an item: `sink_units` from place 0 on, then up to the length from unit `win_first` on.
+struct CtxUnits {
+    int sink_units, win_first, total;
+};
+__device__ __forceinline__ CtxUnits ctx_units(const AttnParams& p, int len) {
+    CtxUnits c;
+    const int all = (len + kUnit - 1) / kUnit;
+    c.sink_units = 0;
+    c.win_first = 0;
+    if (p.window > 0) {
+        const int lowest = max(0, len - p.window + 1);                  // no row of depth >= 0 sees below it but for the sinks
+        const int sinks = (min(p.n_sinks, lowest) + kUnit - 1) / kUnit;
+        if (sinks < lowest / kUnit) { c.sink_units = sinks; c.win_first = lowest / kUnit; }
+    }
+    c.total = c.sink_units + all - c.win_first;
+    return c;
+}
+// Tree rows that row block mb can see: all live ones, or without a mask those up to its last row.
+template <int BM>
+__device__ __forceinline__ int tree_rows(const AttnParams& p, int live, int mb) {
+    if (p.mask_bits) return live;
+    const int64_t last = ((int64_t)(mb + 1) * BM - 1) / p.group;
+    return last + 1 < live ? (int)(last + 1) : live;
+}
+template <int BM>
+__device__ __forceinline__ int row_blocks(const AttnParams& p, int live) { return (int)(((int64_t)live * p.group + BM - 1) / BM); }
+template <int BM>
+__device__ __forceinline__ int64_t units_per_head(const AttnParams& p, int len, int live) {
+    const int mbs = row_blocks<BM>(p, live), ctx = ctx_units(p, len).total;
+    if (p.mask_bits) return (int64_t)mbs * (ctx + (live + kUnit - 1) / kUnit);
+    int64_t n = (int64_t)mbs * ctx;
+    for (int mb = 0; mb < mbs; ++mb) n += (tree_rows<BM>(p, live, mb) + kUnit - 1) / kUnit;
+    return n;
+}
+
+struct PlanShared {
+    int64_t part[32];
+    int64_t total, first_off;
+    int first_b;
+};
+
+// Range c of G: [T c / G, T (c+1) / G).
+__device__ __forceinline__ int64_t range_begin(int64_t total, int c, int G) { return total * c / G; }
+
+// The CTA's walk through its range; every warp keeps one of its own and all of them agree.
+template <int BM>
+struct WorkIter {
+    int64_t left;                // units of the range not yet handed out
+    int b, h, mb, mbs, live, len;
+    CtxUnits ctx;
+    int n_units;                 // of the item
+    int u0, u1;                  // the CTA's part of it
+
+    __device__ __forceinline__ void item_size(const AttnParams& p) {
+        n_units = ctx.total + (tree_rows<BM>(p, live, mb) + kUnit - 1) / kUnit;
+    }
+    __device__ __forceinline__ void load_request(const AttnParams& p) {
+        len = cache_length(p.c, b);
+        live = attn_live(p, b);
+        ctx = ctx_units(p, len);
+        mbs = row_blocks<BM>(p, live);
+    }
+    // Whole CTA (barriers inside).  False: the range is empty.
+    __device__ __forceinline__ bool init(const AttnParams& p, PlanShared& sh, int64_t& begin, int64_t& total) {
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = (int)blockDim.x >> 5;
+        int64_t mine = 0;
+        for (int i = tid; i < p.c.batch; i += (int)blockDim.x) mine += p.c.heads * units_per_head<BM>(p, cache_length(p.c, i), attn_live(p, i));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(kFullMask, mine, o);
+        if (lane == 0) sh.part[warp] = mine;
+        __syncthreads();
+        total = 0;
+        for (int i = 0; i < nw; ++i) total += sh.part[i];
+        begin = range_begin(total, blockIdx.x, gridDim.x);
+        left = range_begin(total, blockIdx.x + 1, gridDim.x) - begin;
+        __syncthreads();
+        int64_t base = 0;                                            // units of the requests before this chunk of requests
+        for (int i0 = 0; i0 < p.c.batch && base <= begin; i0 += (int)blockDim.x) {
+            const int i = i0 + tid;
+            const int64_t n = i < p.c.batch ? p.c.heads * units_per_head<BM>(p, cache_length(p.c, i), attn_live(p, i)) : 0;
+            int64_t upto = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(kFullMask, upto, o);
+                if (lane >= o) upto += x;
+            }
+            if (lane == 31) sh.part[warp] = upto;
+            __syncthreads();
+            int64_t before = base, all = 0;
+            for (int j = 0; j < nw; ++j) {
+                if (j < warp) before += sh.part[j];
+                all += sh.part[j];
+            }
+            upto += before;
+            if (begin < upto && begin >= upto - n) { sh.first_b = i; sh.first_off = begin - (upto - n); }
+            base += all;
+            __syncthreads();
+        }
+        if (left <= 0) return false;
+        b = sh.first_b;
+        int64_t off = sh.first_off;
+        load_request(p);
+        const int64_t per_head = units_per_head<BM>(p, len, live);
+        h = (int)(off / per_head);
+        off -= h * per_head;
+        mb = 0;
+        item_size(p);
+        while (off >= n_units) { off -= n_units; ++mb; item_size(p); }
+        u0 = (int)off;
+        u1 = (int)min((int64_t)n_units, off + left);
+        left -= u1 - u0;
+        return true;
+    }
+    // On to the next item with units; false at the range's end.
+    __device__ __forceinline__ bool next(const AttnParams& p) {
+        if (left <= 0) return false;
+        do {
+            if (++mb >= mbs) {
+                mb = 0;
+                if (++h >= p.c.heads) {
+                    h = 0;
+                    do { ++b; load_request(p); } while (mbs == 0);
+                }
+            }
+            item_size(p);
+        } while (n_units == 0);
+        u0 = 0;
+        u1 = (int)min((int64_t)n_units, left);
+        left -= u1;
+        return true;
+    }
+    __device__ __forceinline__ bool is_tree(int u) const { return u >= ctx.total; }
+    // First key of unit u: a cached place, or a tree row.
+    __device__ __forceinline__ int first_key(int u) const {
+        if (u >= ctx.total) return (u - ctx.total) * kUnit;
+        return (u < ctx.sink_units ? u : ctx.win_first + u - ctx.sink_units) * kUnit;
+    }
+    __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == n_units; }
+};
+
+// Which of 128 keys from `key0` on row r (place len + dr) sees, as far as lengths, masks and windows say.
+__device__ __forceinline__ uint32_t bits_from(int x) { return x <= 0 ? ~0u : (x >= 32 ? 0u : ~0u << x); }       // bits x.. of a word
+__device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int key0, uint32_t (&w)[4]) {
+    if (!tree) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = key0 + 32 * i;
+            uint32_t m = ~bits_from(len - k);
+            if (p.window > 0) m &= bits_from(len + dr - p.window + 1 - k) | ~bits_from(p.n_sinks - k);
+            w[i] = m;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int k = key0 + 32 * i, word = k >> 5;
+        uint32_t m = 0;
+        if (k < live) {
+            m = p.mask_bits ? __ldg(p.mask_bits + ((int64_t)b * p.R + r) * p.mask_words + word) : ~bits_from(r + 1 - k);
+            m &= ~bits_from(live - k);
+        }
+        if (p.window > 0) {
+            for (uint32_t t = m; t; t &= t - 1) {
+                const int c = k + __ffs(t) - 1;
+                const int dc = attn_depth(p, b, c);
+                if (!(dr - dc < p.window || len + dc < p.n_sinks)) m &= ~(1u << (c - k));
+            }
+        }
+        w[i] = m;
+    }
+}
+
+// ---- what the ranges leave of an item that they share, and how it is joined ----
+template <int BM, int D> __host__ __device__ constexpr int record_floats() { return BM * (D + 2); }
+
+// What a range begins with: its first item's (b, h, mb) and flags.
+constexpr int kRangeInside = 1;      // the range begins inside that item (its sums are record 0 of the range)
+constexpr int kRangeEnds = 2;        // that item ends in the range
+constexpr int kRangeEmpty = 4;
+
+// blockIdx.x is a range: the one in which a shared item begins (its sums are record 1 there) joins it.  A thread takes eight
+// elements of one row; consecutive threads take consecutive rows, as the records lie.
+template <int BM, int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnWork w, int grid) {
+    grid_dependency_wait();
+    const AttnParams& p = w.p;
+    const int c0 = blockIdx.x;
+    const int mine = w.items[c0].w;
+    if ((mine & kRangeEmpty) || ((mine & kRangeInside) && !(mine & kRangeEnds))) return;      // no item begins here and goes on
+    int c = c0 + 1;
+    while (c < grid && (w.items[c].w & kRangeEmpty)) ++c;
+    if (c >= grid || !(w.items[c].w & kRangeInside)) return;
+    const int4 it = w.items[c];
+    const int b = it.x, h = it.y, mb = it.z, live = attn_live(p, b);
+    const int id = blockIdx.y * 256 + threadIdx.x, row = id % BM, dc = id / BM;
+    const int64_t m0 = (int64_t)mb * BM + row;
+    if (dc * 8 >= D || m0 >= (int64_t)live * p.group) return;
+    const int rec = record_floats<BM, D>();
+    const float* first = w.records + ((int64_t)c0 * 2 + 1) * rec;
+    float M = first[D * BM + row];
+    int end = c;
+    for (; end < grid; ++end) {
+        const int4 e = w.items[end];
+        if (e.w & kRangeEmpty) continue;
+        if (!((e.w & kRangeInside) && e.x == b && e.y == h && e.z == mb)) break;
+        M = fmaxf(M, w.records[(int64_t)end * 2 * rec + D * BM + row]);
+        if (e.w & kRangeEnds) { ++end; break; }
+    }
+    const float ref = M == -INFINITY ? 0.0f : M;
+    float l = 0.0f, o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = 0.0f;
+    for (int i = c0; i < end; ++i) {
+        if (i != c0 && (w.items[i].w & kRangeEmpty)) continue;
+        const float* rp = i == c0 ? first : w.records + (int64_t)i * 2 * rec;
+        const float a = exp2f(rp[D * BM + row] - ref);
+        l = fmaf(a, rp[(D + 1) * BM + row], l);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = fmaf(a, rp[(dc * 8 + j) * BM + row], o[j]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int r = (int)(m0 / p.group), hq = h * p.group + (int)(m0 - (int64_t)r * p.group);
+    uint4 out;
+    out.x = pack_bf16(o[0] * inv, o[1] * inv);
+    out.y = pack_bf16(o[2] * inv, o[3] * inv);
+    out.z = pack_bf16(o[4] * inv, o[5] * inv);
+    out.w = pack_bf16(o[6] * inv, o[7] * inv);
+    *(uint4*)(p.out + ((int64_t)b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2) = out;
+    if (p.lse && dc == 0) p.lse[((int64_t)b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (M + log2f(l)) * kLn2;
+}
+
+}  // namespace cadd

@@ -8,6 +8,8 @@
 #include "cache.cuh"
 #include "tree_attention.cuh"
 #include "cache_evict.cuh"
+#include "attn_tiles.cuh"
+#include "launch.cuh"
 
 namespace cadd {
 
@@ -63,6 +65,43 @@ static int ctas_for(int64_t groups, int64_t items, int threads) {
     int64_t need = (items + threads - 1) / threads, most = (148 * 32 + groups - 1) / groups;
     if (need < 1) need = 1;
     return (int)(need < most ? need : most);
+}
+
+static int sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
+    return n;
+}
+
+constexpr int kMaxGrid = 512;                             // ranges at most (two CTAs on each SM are fewer)
+constexpr size_t kItemsBytes = ((size_t)kMaxGrid * sizeof(int4) + 255) & ~(size_t)255;
+
+// Units that a call can have at most: what its tables and row capacity have room for.
+static int64_t most_units(const AttnParams& p, int bm) {
+    const int64_t blocks = ((int64_t)p.R * p.group + bm - 1) / bm;
+    const int64_t keys = (((int64_t)p.c.max_pages << p.c.page_shift) + kUnit - 1) / kUnit + (p.R + kUnit - 1) / kUnit;
+    return (int64_t)p.c.batch * p.c.heads * blocks * keys;
+}
+
+template <int D, bool FP4>
+static int launch_tiles(const AttnWork& w, cudaStream_t st) {
+    if (cudaFuncSetAttribute(attn_tiles_kernel<D, FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem_bytes<D>()) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    int64_t grid = 2 * (int64_t)sm_count();
+    const int64_t most = most_units(w.p, kTileBM);
+    if (grid > most) grid = most;
+    if (grid > kMaxGrid) grid = kMaxGrid;
+    attn_tiles_kernel<D, FP4><<<(unsigned)grid, kTileThreads, tile_smem_bytes<D>(), st>>>(w);
+    if (cudaGetLastError() != cudaSuccess) return CADD_ERR_LAUNCH;
+    const dim3 join((unsigned)grid, kTileBM * (D / 8) / 256);
+    if (launch_dependent(true, attn_join_kernel<kTileBM, D>, join, dim3(256), 0, st, w, (int)grid) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    return CADD_OK;
 }
 
 }  // namespace cadd
@@ -143,7 +182,9 @@ int cadd_tree_attention_workspace_bytes(const cadd_attention_args* a, size_t* ou
     int rc = check_attention_shape(a);
     if (rc != CADD_OK) return rc;
     if (!out) return CADD_ERR_NULL;
-    *out = 256;
+    // two records per range of the grid with the larger records
+    const size_t rec = (size_t)kTileBM * (a->cache.head_dim + 2) * 4;
+    *out = kItemsBytes + (size_t)kMaxGrid * 2 * rec;
     return CADD_OK;
 }
 
@@ -180,15 +221,12 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
         attn_status_kernel<<<(unsigned)p.c.batch, 128, 0, st>>>(p);
         if ((rc = launched()) != CADD_OK) return rc;
     }
-    const unsigned grid = (unsigned)(((int64_t)p.c.batch * p.R * p.heads_q + 3) / 4);
-    if (p.c.head_dim == 128) {
-        if (p.c.fp4) attn_rows_kernel<128, true><<<grid, 128, 0, st>>>(p);
-        else attn_rows_kernel<128, false><<<grid, 128, 0, st>>>(p);
-    } else {
-        if (p.c.fp4) attn_rows_kernel<64, true><<<grid, 128, 0, st>>>(p);
-        else attn_rows_kernel<64, false><<<grid, 128, 0, st>>>(p);
-    }
-    return launched();
+    AttnWork w;
+    w.p = p;
+    w.items = (int4*)a->workspace;
+    w.records = (float*)((unsigned char*)a->workspace + kItemsBytes);
+    if (p.c.head_dim == 128) return p.c.fp4 ? launch_tiles<128, true>(w, st) : launch_tiles<128, false>(w, st);
+    return p.c.fp4 ? launch_tiles<64, true>(w, st) : launch_tiles<64, false>(w, st);
 }
 
 // ---------------- accumulated weights, eviction ----------------

@@ -108,31 +108,6 @@ __device__ __noinline__ void row_attend(const AttnParams& p, int b, int h, int l
     }
 }
 
-// Simplest form: a warp per (request, row, query head) goes over all of its keys.
-template <int D, bool FP4>
-__global__ void __launch_bounds__(128) attn_rows_kernel(const AttnParams p) {
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int hq = (int)(w % p.heads_q);
-    const int64_t br = w / p.heads_q;
-    const int b = (int)(br / p.R), r = (int)(br - (int64_t)b * p.R), lane = threadIdx.x & 31;
-    if (b >= p.c.batch || r >= attn_live(p, b)) return;
-    const int len = cache_length(p.c, b), h = hq / p.group;
-    float q[D / 32];
-    load_row_bf16<D>(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2, lane, q);
-    RowSums<D> st;
-    st.m = -INFINITY;
-    st.l = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) st.o[i] = 0.0f;
-    row_attend<D, FP4, false>(p, b, h, len, r, q, 0, len, st);
-    row_attend<D, FP4, true>(p, b, h, len, r, q, 0, attn_live(p, b), st);
-    const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-    uint32_t* dst = (uint32_t*)(p.out + ((int64_t)b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head) * 2) + lane * (D / 64);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) dst[i] = pack_bf16(st.o[2 * i] * inv, st.o[2 * i + 1] * inv);
-    if (p.lse && lane == 0) p.lse[((int64_t)b * p.R + r) * p.heads_q + hq] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
-}
-
 // Status of every request (only launched where the caller asks for it).
 __global__ void __launch_bounds__(128) attn_status_kernel(const AttnParams p) {
     const int b = blockIdx.x, len = cache_length(p.c, b);
