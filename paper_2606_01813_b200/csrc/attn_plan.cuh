@@ -20,6 +20,7 @@ struct AttnWork {
     AttnParams p;
     float* records;                                      // [grid][2] partial records of BM x (D + 2) floats
     int4* items;                                         // [grid] what each range begins with
+    int* odd;                                            // [grid] not 0: the range met non-finite results
 };
 
 // The cached units of an item: `sink_units` from place 0 on, then up to the length from unit `win_first` on.
@@ -43,11 +44,10 @@ __device__ __forceinline__ CtxUnits ctx_units(const AttnParams& p, int len) {
 template <int BM>
 __device__ __forceinline__ int tree_rows(const AttnParams& p, int live, int mb) {
     if (p.mask_bits) return live;
-    const int64_t last = ((int64_t)(mb + 1) * BM - 1) / p.group;
-    return last + 1 < live ? (int)(last + 1) : live;
+    return min(live, ((mb + 1) * BM - 1) / p.group + 1);                // rows times group: at most 2^24
 }
 template <int BM>
-__device__ __forceinline__ int row_blocks(const AttnParams& p, int live) { return (int)(((int64_t)live * p.group + BM - 1) / BM); }
+__device__ __forceinline__ int row_blocks(const AttnParams& p, int live) { return (live * p.group + BM - 1) / BM; }
 template <int BM>
 __device__ __forceinline__ int64_t units_per_head(const AttnParams& p, int len, int live) {
     const int mbs = row_blocks<BM>(p, live), ctx = ctx_units(p, len).total;
@@ -59,7 +59,7 @@ __device__ __forceinline__ int64_t units_per_head(const AttnParams& p, int len, 
 
 struct PlanShared {
     int64_t part[32];
-    int64_t total, first_off;
+    int64_t first_off;
     int first_b;
 };
 
@@ -85,7 +85,7 @@ struct WorkIter {
         mbs = row_blocks<BM>(p, live);
     }
     // Whole CTA (barriers inside).  False: the range is empty.
-    __device__ __forceinline__ bool init(const AttnParams& p, PlanShared& sh, int64_t& begin, int64_t& total) {
+    __device__ __forceinline__ bool init(const AttnParams& p, PlanShared& sh, int range, int ranges) {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = (int)blockDim.x >> 5;
         int64_t mine = 0;
         for (int i = tid; i < p.c.batch; i += (int)blockDim.x) mine += p.c.heads * units_per_head<BM>(p, cache_length(p.c, i), attn_live(p, i));
@@ -93,10 +93,10 @@ struct WorkIter {
         for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(kFullMask, mine, o);
         if (lane == 0) sh.part[warp] = mine;
         __syncthreads();
-        total = 0;
+        int64_t total = 0;
         for (int i = 0; i < nw; ++i) total += sh.part[i];
-        begin = range_begin(total, blockIdx.x, gridDim.x);
-        left = range_begin(total, blockIdx.x + 1, gridDim.x) - begin;
+        const int64_t begin = range_begin(total, range, ranges);
+        left = range_begin(total, range + 1, ranges) - begin;
         __syncthreads();
         int64_t base = 0;                                            // units of the requests before this chunk of requests
         for (int i0 = 0; i0 < p.c.batch && base <= begin; i0 += (int)blockDim.x) {
@@ -202,55 +202,128 @@ constexpr int kRangeInside = 1;      // the range begins inside that item (its s
 constexpr int kRangeEnds = 2;        // that item ends in the range
 constexpr int kRangeEmpty = 4;
 
+// Does a row's part in units [u0, u1) of an item by key, as a warp.
+template <int D, bool FP4, int BM>
+__device__ __noinline__ RowSums<D> redo_row(const AttnParams& p, const WorkIter<BM>& it, int r, int hq) {
+    RowSums<D> st;
+    float q[D / 32];
+    load_row_bf16<D>(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2, threadIdx.x & 31, q);
+    st.m = -INFINITY;
+    st.l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) st.o[i] = 0.0f;
+    for (int u = 0; u < it.n_units; ++u) {
+        const int k0 = it.first_key(u);
+        if (it.is_tree(u)) row_attend<D, FP4, true>(p, it.b, it.h, it.len, r, q, k0, min(k0 + kUnit, it.live), st);
+        else row_attend<D, FP4, false>(p, it.b, it.h, it.len, r, q, k0, min(k0 + kUnit, it.len), st);
+    }
+    return st;
+}
+// Whole warp.  Each lane has looked at eight elements (chunk dc) of one row of the item in the output; where `bad`, the row is done
+// once more and those eight elements are replaced.
+template <int D, bool FP4, int BM>
+__device__ __noinline__ void redo_chunks(const AttnParams& p, const WorkIter<BM>& it, bool bad, int r, int hq, int dc) {
+    const int lane = threadIdx.x & 31;
+    for (unsigned todo = __ballot_sync(kFullMask, bad); todo; todo &= todo - 1) {
+        const int src = __ffs(todo) - 1;
+        const int rr = __shfl_sync(kFullMask, r, src), hh = __shfl_sync(kFullMask, hq, src), c = __shfl_sync(kFullMask, dc, src);
+        const RowSums<D> st = redo_row<D, FP4, BM>(p, it, rr, hh);
+        const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
+        uint32_t* dst = (uint32_t*)(p.out + ((int64_t)it.b * p.os_b + (int64_t)rr * p.os_row + (int64_t)hh * p.os_head) * 2) + lane * (D / 64);
+        if (lane * (D / 32) / 8 == c) {
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) dst[i] = pack_bf16(st.o[2 * i] * inv, st.o[2 * i + 1] * inv);
+        }
+    }
+}
+
 // blockIdx.x is a range: the one in which a shared item begins (its sums are record 1 there) joins it.  A thread takes eight
-// elements of one row; consecutive threads take consecutive rows, as the records lie.
-template <int BM, int D>
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnWork w, int grid) {
+// elements of one row; consecutive threads take consecutive rows, as the records lie.  Rows whose joined result, or whose
+// result in a whole item of a range that met non-finite numbers, is not finite are done once more.
+template <int BM, int D, bool FP4>
+__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnWork w, int grid) {
     grid_dependency_wait();
     const AttnParams& p = w.p;
     const int c0 = blockIdx.x;
     const int mine = w.items[c0].w;
-    if ((mine & kRangeEmpty) || ((mine & kRangeInside) && !(mine & kRangeEnds))) return;      // no item begins here and goes on
+    if (mine & kRangeEmpty) return;
+    const int id = blockIdx.y * 256 + threadIdx.x, row = id % BM, dc = id / BM;
+    if (w.odd[c0]) {                                                               // the range's whole items
+        __shared__ PlanShared plan;
+        WorkIter<BM> it;
+        if (it.init(p, plan, c0, grid)) {
+            do {
+                if (!it.whole()) continue;
+                const int m0 = it.mb * BM + row, r = m0 / p.group, hq = it.h * p.group + (m0 - r * p.group);
+                const bool live = dc * 8 < D && m0 < it.live * p.group;
+                bool bad = false;
+                if (live) {
+                    const uint4 x = *(const uint4*)(p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2);
+                    float f[8];
+                    Elem<CADD_DTYPE_BF16>::unpack(x, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) bad |= !(fabsf(f[i]) <= 3.4e38f);
+                }
+                redo_chunks<D, FP4, BM>(p, it, bad, r, hq, dc);
+            } while (it.next(p));
+        }
+    }
+    if ((mine & kRangeInside) && !(mine & kRangeEnds)) return;                     // no item begins here and goes on
     int c = c0 + 1;
     while (c < grid && (w.items[c].w & kRangeEmpty)) ++c;
     if (c >= grid || !(w.items[c].w & kRangeInside)) return;
-    const int4 it = w.items[c];
-    const int b = it.x, h = it.y, mb = it.z, live = attn_live(p, b);
-    const int id = blockIdx.y * 256 + threadIdx.x, row = id % BM, dc = id / BM;
-    const int64_t m0 = (int64_t)mb * BM + row;
-    if (dc * 8 >= D || m0 >= (int64_t)live * p.group) return;
+    const int4 first_of = w.items[c];
+    const int b = first_of.x, h = first_of.y, mb = first_of.z, live = attn_live(p, b);
+    const int m0 = mb * BM + row;
+    const bool there = dc * 8 < D && m0 < live * p.group;
     const int rec = record_floats<BM, D>();
     const float* first = w.records + ((int64_t)c0 * 2 + 1) * rec;
-    float M = first[D * BM + row];
-    int end = c;
+    float M = there ? first[D * BM + row] : -INFINITY;
+    int end = c, odd = w.odd[c0];
     for (; end < grid; ++end) {
         const int4 e = w.items[end];
         if (e.w & kRangeEmpty) continue;
         if (!((e.w & kRangeInside) && e.x == b && e.y == h && e.z == mb)) break;
-        M = fmaxf(M, w.records[(int64_t)end * 2 * rec + D * BM + row]);
+        odd |= w.odd[end];
+        if (there) M = fmaxf(M, w.records[(int64_t)end * 2 * rec + D * BM + row]);
         if (e.w & kRangeEnds) { ++end; break; }
     }
-    const float ref = M == -INFINITY ? 0.0f : M;
-    float l = 0.0f, o[8];
+    const int r = m0 / p.group, hq = h * p.group + (m0 - r * p.group);
+    bool bad = false;
+    if (there) {
+        const float ref = M == -INFINITY ? 0.0f : M;
+        float l = 0.0f, o[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = 0.0f;
-    for (int i = c0; i < end; ++i) {
-        if (i != c0 && (w.items[i].w & kRangeEmpty)) continue;
-        const float* rp = i == c0 ? first : w.records + (int64_t)i * 2 * rec;
-        const float a = exp2f(rp[D * BM + row] - ref);
-        l = fmaf(a, rp[(D + 1) * BM + row], l);
+        for (int j = 0; j < 8; ++j) o[j] = 0.0f;
+        for (int i = c0; i < end; ++i) {
+            if (i != c0 && (w.items[i].w & kRangeEmpty)) continue;
+            const float* rp = i == c0 ? first : w.records + (int64_t)i * 2 * rec;
+            const float a = exp2f(rp[D * BM + row] - ref);
+            l = fmaf(a, rp[(D + 1) * BM + row], l);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = fmaf(a, rp[(dc * 8 + j) * BM + row], o[j]);
+            for (int j = 0; j < 8; ++j) o[j] = fmaf(a, rp[(dc * 8 + j) * BM + row], o[j]);
+        }
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint4 out;
+        out.x = pack_bf16(o[0] * inv, o[1] * inv);
+        out.y = pack_bf16(o[2] * inv, o[3] * inv);
+        out.z = pack_bf16(o[4] * inv, o[5] * inv);
+        out.w = pack_bf16(o[6] * inv, o[7] * inv);
+        *(uint4*)(p.out + ((int64_t)b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2) = out;
+        if (p.lse && dc == 0) p.lse[((int64_t)b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (M + log2f(l)) * kLn2;
+        if (odd) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bad |= !(fabsf(o[j]) <= 3.4e38f);
+        }
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int r = (int)(m0 / p.group), hq = h * p.group + (int)(m0 - (int64_t)r * p.group);
-    uint4 out;
-    out.x = pack_bf16(o[0] * inv, o[1] * inv);
-    out.y = pack_bf16(o[2] * inv, o[3] * inv);
-    out.z = pack_bf16(o[4] * inv, o[5] * inv);
-    out.w = pack_bf16(o[6] * inv, o[7] * inv);
-    *(uint4*)(p.out + ((int64_t)b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2) = out;
-    if (p.lse && dc == 0) p.lse[((int64_t)b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (M + log2f(l)) * kLn2;
+    if (odd) {
+        __syncwarp();
+        WorkIter<BM> it;
+        it.b = b; it.h = h; it.mb = mb;
+        it.load_request(p);
+        it.item_size(p);
+        redo_chunks<D, FP4, BM>(p, it, bad, r, hq, dc);
+    }
 }
 
 }  // namespace cadd

@@ -2,10 +2,11 @@
 //
 // For each unit S = Q K^T goes to tensor memory (M 128 = rows, N 128 = keys, contraction over the head's elements), the
 // softmax warps turn it into weights P = e^{s - m} in bf16, written over S, and O += P V is accumulated in tensor memory
-// (A = P from tensor memory, B = V as it lies, [key][element], i.e. "MN-major").  m is the row's reference maximum: it
-// starts as the first unit's maximum and is raised, with O and l multiplied by e^{old - new}, only when a later maximum exceeds
-// it by more than 2^8 in units of e^s: weights up to 2^8 lose nothing in bf16, whose relative rounding does not
-// depend on the size, and most units leave O alone.  l adds the weights before they are rounded.
+// (A = P from tensor memory, B = V as it lies, [key][element], i.e. "MN-major").  m is a reference, not the exact maximum: it
+// starts as the first unit's maximum and is raised, with O and l multiplied by e^{old - new}, only when a later score exceeds
+// it by a factor of more than 2^40 in weight.  Weights above 1 lose nothing, since neither bf16's nor fp32's relative rounding
+// depends on the size, and weights, sums and products stay below 2^40 x 2^24 (the 4-bit form's factor) x keys x values; so O
+// is touched by the products alone, but for a few units.  l adds the weights before they are rounded.
 //
 // The 4-bit cache: a code's bits, moved to where bf16 keeps its low exponent bits and first fraction bit, are the number times
 // 2^-126; one packed multiplication by scale * 2^118 gives code * scale * 2^-8, exact in bf16 (<= 6 significant bits), for two
@@ -15,15 +16,17 @@
 // does not mind, the values' order is undone when O is written).
 //
 // Two CTAs share an SM and alternate on the tensor cores and the exponential units; within one, the next unit's keys are on their
-// way while the softmax runs, its values while the scores are formed.  288 threads:
-//   warps 0-3  softmax and epilogue, a row (tensor-memory lane) per thread;
+// way while the softmax runs, its values while the scores are formed.  256 threads (four warps on each quarter of an SM, which
+// leaves 128 registers a thread):
+//   warps 0-3  softmax and epilogue, a row (tensor-memory lane) per thread.  Between a unit's weights and the next unit's scores
+//              they have nothing else to do, so thread 0 also issues the products; warp 0 owns the tensor memory (256
+//              columns: S/P 128, O up to 128);
 //   warps 4-7  loaders: keys and values into the 128-byte swizzle, by asynchronous 16-byte copies (bf16), or through registers
-//              one unit ahead (4 bits);
-//   warp 8     one thread issues the products; the warp owns the tensor memory (256 columns: S/P 128, O up to 128).
+//              one unit ahead (4 bits).
 // Every wait has an iteration limit; a role that gives up sets an error word and all leave.
 //
-// A product of a weight 0 with a non-finite value that the row does not see would be NaN.  Rows with a non-finite result are
-// therefore done once more by a warp, key by key over the keys that they see (row_attend), which costs nothing otherwise.
+// A product of a weight 0 with a non-finite value that the row does not see would be NaN.  A range that meets a non-finite result
+// says so, and the join does such rows once more, key by key over the keys that they see; that costs nothing otherwise.
 #pragma once
 #include "attn_plan.cuh"
 #include "tcgen05.cuh"
@@ -31,9 +34,9 @@
 namespace cadd {
 
 constexpr int kTileBM = 128;
-constexpr int kTileThreads = 288;
+constexpr int kTileThreads = 256;
 constexpr int kTileTmemCols = 256;
-constexpr float kTileSlack = 8.0f;                       // log2 of how far weights may exceed 1 before m is raised
+constexpr float kTileSlack = 40.0f;                      // log2 of how far weights may exceed 1 before m is raised
 
 template <int D> struct alignas(1024) TileShared {
     unsigned char q[kTileBM * D * 2];                    // D/64 sub-tiles of 128 rows x 128 bytes
@@ -42,15 +45,23 @@ template <int D> struct alignas(1024) TileShared {
     int64_t key_row[2][kUnit];                           // bf16: byte offsets of the unit's rows, -1 for none
     uint64_t k_full, v_full, s_full, p_ready, pv_done, drained;
     PlanShared plan;
+    WorkIter<kTileBM> it[kTileThreads / 32];             // a walk per warp: here, not in registers, which are scarce
     uint32_t key_bits[2][4];                             // keys of the unit that exist
-    uint32_t tmem_base, error;
+    uint32_t tmem_base, error, odd;
 };
 template <int D> constexpr size_t tile_smem_bytes() { return sizeof(TileShared<D>) + 1024; }
 
+// Bounded wait without a time hint.
+__device__ __forceinline__ bool tile_try(uint64_t* bar, unsigned parity) {
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
 template <class Shared>
 __device__ __forceinline__ bool tile_wait(Shared& sh, uint64_t* bar, unsigned parity) {
-    for (int it = 0; it < (1 << 20); ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
+    for (int it = 0; it < (1 << 22); ++it) {
+        if (tile_try(bar, parity)) return true;
         if (*(volatile uint32_t*)&sh.error) return false;
     }
     sh.error = 1;
@@ -67,14 +78,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-                 "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                 "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -154,7 +167,7 @@ __device__ __forceinline__ void fp4_row_load(Fp4Row<D>& x, const unsigned char* 
     }
 }
 template <int D>
-__device__ __forceinline__ void fp4_row_store(const Fp4Row<D>& x, unsigned char* tile, int row) {
+__device__ __noinline__ void fp4_row_store(const Fp4Row<D> x, unsigned char* tile, int row) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {                   // 32 elements: a 16-byte word of codes, two scales
         uint32_t f0, f1;
@@ -166,80 +179,195 @@ __device__ __forceinline__ void fp4_row_store(const Fp4Row<D>& x, unsigned char*
     }
 }
 
-// Redoes a row by key: its keys in units [u0, u1) of the item.  The whole warp works; the sums come back in every lane's share.
-template <int D, bool FP4, int BM>
-__device__ __noinline__ void redo_row(const AttnParams& p, const WorkIter<BM>& it, int r, int hq, RowSums<D>& st) {
-    float q[D / 32];
-    load_row_bf16<D>(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2, threadIdx.x & 31, q);
-    st.m = -INFINITY;
-    st.l = 0.0f;
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// The wait names the registers that it makes valid, so that nothing that reads them can be moved in front of it.
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+__device__ __forceinline__ void mask_scores(uint32_t (&x)[16], uint32_t (&y)[16], uint32_t see) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) st.o[i] = 0.0f;
-    for (int u = it.u0; u < it.u1; ++u) {
-        const int k0 = it.first_key(u);
-        if (it.is_tree(u)) row_attend<D, FP4, true>(p, it.b, it.h, it.len, r, q, k0, min(k0 + kUnit, it.live), st);
-        else row_attend<D, FP4, false>(p, it.b, it.h, it.len, r, q, k0, min(k0 + kUnit, it.len), st);
+    for (int i = 0; i < 16; ++i) {
+        x[i] = (see >> i) & 1u ? x[i] : 0xff800000u;
+        y[i] = (see >> (16 + i)) & 1u ? y[i] : 0xff800000u;
     }
+}
+// A row's scores of a unit lie in tensor memory at `ts`; a load takes some 200 cycles.  First the largest, 64 columns at a time:
+__device__ __forceinline__ float tile_max(uint32_t ts, bool masked, const uint32_t (&see)[4]) {
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    uint32_t s[4][16];
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tmem_ld16(ts + c * 64 + j * 16, s[j]);
+        tmem_ld_wait16(s[0]); tmem_ld_wait16(s[1]); tmem_ld_wait16(s[2]); tmem_ld_wait16(s[3]);
+        if (masked) {
+            mask_scores(s[0], s[1], c ? see[2] : see[0]);
+            mask_scores(s[2], s[3], c ? see[3] : see[1]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t (&x)[16] = s[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+        }
+    }
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+// then the weights 2^(s sc + off), written over the scores (columns that have been read already) as packed bf16, and their sum:
+// 32 columns are worked on, long enough for the next 32 to arrive.
+__device__ __forceinline__ void weights_of(const uint32_t (&x)[16], uint64_t sc2, uint64_t off2, uint64_t (&sum)[2], uint32_t dst) {
+    uint32_t pk[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float e0, e1;
+        unpack2(fma2(pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc2, off2), e0, e1);
+        e0 = ex2(e0);
+        e1 = ex2(e1);
+        sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+        pk[i] = pack_bf16(e0, e1);
+    }
+    tmem_st8(dst, pk);
+}
+__device__ __forceinline__ float tile_weights(uint32_t ts, bool masked, const uint32_t (&see)[4], float sc, float off) {
+    const uint64_t sc2 = pack2(sc, sc), off2 = pack2(off, off);
+    uint64_t sum[2] = {0, 0};
+    uint32_t s[4][16];
+    tmem_ld16(ts, s[0]);
+    tmem_ld16(ts + 16, s[1]);
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+        tmem_ld_wait16(s[0]); tmem_ld_wait16(s[1]);
+        tmem_ld16(ts + c * 64 + 32, s[2]);
+        tmem_ld16(ts + c * 64 + 48, s[3]);
+        if (masked) mask_scores(s[0], s[1], c ? see[2] : see[0]);
+        weights_of(s[0], sc2, off2, sum, ts + c * 32);
+        weights_of(s[1], sc2, off2, sum, ts + c * 32 + 8);
+        tmem_ld_wait16(s[2]); tmem_ld_wait16(s[3]);
+        if (c == 0) {
+            tmem_ld16(ts + 64, s[0]);
+            tmem_ld16(ts + 80, s[1]);
+        }
+        if (masked) mask_scores(s[2], s[3], c ? see[3] : see[1]);
+        weights_of(s[2], sc2, off2, sum, ts + c * 32 + 16);
+        weights_of(s[3], sc2, off2, sum, ts + c * 32 + 24);
+    }
+    float a, b;
+    unpack2(add2(sum[0], sum[1]), a, b);
+    return a + b;
+}
+
+// A warp's walk in shared memory goes on to the next item: one lane moves it, no lane still reads the old or already reads the new.
+__device__ __forceinline__ bool tile_next(WorkIter<kTileBM>& it, const AttnParams& p) {
+    __syncwarp();
+    int more = 0;
+    if ((threadIdx.x & 31) == 0) more = it.next(p);
+    __syncwarp();
+    return __shfl_sync(kFullMask, more, 0) != 0;
+}
+
+// The end of an item, a warp's rows: O out of tensor memory (`to`), divided and written, or with m and l to the range's record.  True
+// where a row of the thread holds a non-finite number.  (A call of its own, once per item: inlined, its registers would cost the
+// units' loop theirs.)
+template <int D, bool FP4>
+__device__ __noinline__ bool tile_finish(const AttnWork& w, const WorkIter<kTileBM>& it, uint32_t to, bool live, int r, int hq, float m, float l) {
+    const AttnParams& p = w.p;
+    const int tid = threadIdx.x;
+    const bool whole = it.whole();
+    const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
+    float* rec = w.records + ((int64_t)blockIdx.x * 2 + (it.u0 > 0 ? 0 : 1)) * record_floats<kTileBM, D>() + tid;
+    unsigned char* dst = p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head) * 2;
+    bool odd = false;
+#pragma unroll 1
+    for (int c = 0; c < D / 16; ++c) {
+        uint32_t o[16];
+        tmem_ld16(to + c * 16, o);
+        tmem_ld_wait16(o);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd |= (o[i] & 0x7f800000u) == 0x7f800000u;
+        if constexpr (FP4) {                  // undo the order 0 4 1 5 2 6 3 7
+#pragma unroll
+            for (int j = 0; j < 16; j += 8) {
+                const uint32_t t[8] = {o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[j + (i >> 1) + 4 * (i & 1)] = t[i];
+            }
+        }
+        if (!live) continue;
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 8) {
+                uint4 x;
+                x.x = pack_bf16(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv);
+                x.y = pack_bf16(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv);
+                x.z = pack_bf16(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv);
+                x.w = pack_bf16(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv);
+                *(uint4*)(dst + c * 32 + j * 2) = x;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) rec[(c * 16 + i) * kTileBM] = __uint_as_float(o[i]);
+        }
+    }
+    if (live && !whole) { rec[D * kTileBM] = m; rec[(D + 1) * kTileBM] = l; }
+    if (live && whole && p.lse) p.lse[((int64_t)it.b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+    return odd && live;
 }
 
 template <int D, bool FP4>
-__global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnWork w) {
+__global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __grid_constant__ AttnWork w) {
     extern __shared__ __align__(16) unsigned char tile_smem_raw[];
     TileShared<D>& sh = *reinterpret_cast<TileShared<D>*>(tile_smem_raw + ((1024u - (smem_u32(tile_smem_raw) & 1023u)) & 1023u));
     const AttnParams& p = w.p;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    WorkIter<kTileBM> it;
-    int64_t begin, total;
-    if (tid == 0) sh.error = 0;
-    if (!it.init(p, sh.plan, begin, total)) {
-        if (tid == 0) w.items[blockIdx.x] = make_int4(0, 0, 0, kRangeEmpty);
+    if (tid == 0) sh.error = sh.odd = 0;
+    WorkIter<kTileBM> begin;
+    if (!begin.init(p, sh.plan, blockIdx.x, gridDim.x)) {
+        if (tid == 0) { w.items[blockIdx.x] = make_int4(0, 0, 0, kRangeEmpty); w.odd[blockIdx.x] = 0; }
         return;
     }
+    WorkIter<kTileBM>& it = sh.it[warp];
+    if (lane == 0) it = begin;
+    __syncwarp();
     if (tid == 0) {
         w.items[blockIdx.x] = make_int4(it.b, it.h, it.mb, (it.u0 > 0 ? kRangeInside : 0) | (it.u1 == it.n_units ? kRangeEnds : 0));
-        mbar_init(&sh.k_full, 128);
-        mbar_init(&sh.v_full, 128);
+        mbar_init(&sh.k_full, 4);
+        mbar_init(&sh.v_full, 4);
         mbar_init(&sh.s_full, 1);
-        mbar_init(&sh.p_ready, 128);
+        mbar_init(&sh.p_ready, 4);
         mbar_init(&sh.pv_done, 1);
         mbar_init(&sh.drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8) tmem_alloc(&sh.tmem_base, kTileTmemCols);
+    if (warp == 0) tmem_alloc(&sh.tmem_base, kTileTmemCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tm_s = *(volatile uint32_t*)&sh.tmem_base, tm_o = tm_s + kUnit;
     constexpr int kCh = D / 8;                            // 16-byte chunks of a bf16 row
 
-    if (warp == 8) {
-        // ---------------- products ----------------
-        if (lane == 0) {
-            unsigned n = 0;
-            bool ok = true;
-            do {
-                for (int u = it.u0; u < it.u1 && ok; ++u, ++n) {
-                    ok = tile_wait(sh, &sh.k_full, n & 1) && (n == 0 || tile_wait(sh, &sh.pv_done, (n - 1) & 1));
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tm_s, umma_desc_k_sw128(sh.q + (kk >> 2) * 16384, kk & 3), umma_desc_k_sw128(sh.k + (kk >> 2) * 16384, kk & 3),
-                                  tile_idesc(kUnit, 0), kk != 0);
-                    umma_commit(&sh.s_full);
-                    ok = tile_wait(sh, &sh.p_ready, n & 1) && tile_wait(sh, &sh.v_full, n & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int kk = 0; kk < kUnit / 16; ++kk)
-                        umma_bf16_ts(tm_o, tm_s + kk * 8, umma_desc_mn_sw128(sh.v, kk, 16384), tile_idesc(D, 1), (u > it.u0 || kk != 0) ? 1u : 0u);
-                    umma_commit(&sh.pv_done);
-                }
-            } while (ok && it.next(p));
-            umma_commit(&sh.drained);                     // no product is in flight when the tensor memory is given back
-            for (int i = 0; i < (1 << 20) && !mbar_try_wait(&sh.drained, 0); ++i) {}
-        }
-    } else if (warp >= 4) {
+    if (warp >= 4) {
         // ---------------- loaders ----------------
         const int lt = tid - 128;                         // the thread's key (and row of Q)
         unsigned n = 0;
@@ -269,8 +397,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
                 if (!__all_sync(kFullMask, ok)) { ok = false; break; }
                 if (lane == 0) sh.key_bits[n & 1][warp - 4] = there;
                 if (u == it.u0) {                         // the item's queries
-                    const int64_t m0 = (int64_t)it.mb * kTileBM + lt;
-                    const int r = (int)(m0 / p.group), g = (int)(m0 - (int64_t)r * p.group);
+                    const int m0 = it.mb * kTileBM + lt, r = m0 / p.group, g = m0 - r * p.group;
                     const uint4* src = (const uint4*)(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)(it.h * p.group + g) * p.qs_head) * 2);
                     const bool live = r < it.live;
 #pragma unroll 4
@@ -294,7 +421,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
                     }
                     if (ahead) fp4_row_load<D>(kx, p.c.k, p.c.ks, next_row);
                     fence_async_shared();
-                    mbar_arrive(&sh.k_full);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.k_full);
                     if (n > 0) ok = tile_wait(sh, &sh.pv_done, (n - 1) & 1);
                     if (!__all_sync(kFullMask, ok)) { ok = false; break; }
                     if (!tree) {
@@ -307,7 +435,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
                     if (ahead) fp4_row_load<D>(vx, p.c.v, p.c.vs, next_row);
                     held = ahead;
                     fence_async_shared();
-                    mbar_arrive(&sh.v_full);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.v_full);
                 } else {
                     const unsigned char* kb = tree ? p.k : p.c.k;
                     const unsigned char* vb = tree ? p.v : p.c.v;
@@ -329,14 +458,16 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
                     cp_async_commit();
                     cp_async_wait<1>();
                     fence_async_shared();
-                    mbar_arrive(&sh.k_full);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.k_full);
                     cp_async_wait<0>();
                     fence_async_shared();
-                    mbar_arrive(&sh.v_full);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.v_full);
                 }
                 row = next_row;
             }
-        } while (ok && it.next(p));
+        } while (ok && tile_next(it, p));
         cp_async_wait<0>();
     } else {
         // ---------------- softmax and epilogue ----------------
@@ -346,15 +477,32 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
         const float up_ctx = FP4 ? (float)(8 - p.c.v_exp) : 0.0f, down_ctx = FP4 ? exp2i(p.c.v_exp - 8) : 1.0f;
         unsigned n = 0;
         bool ok = true;
+        // thread 0: the scores of unit number i, once its keys are there
+        auto scores = [&](unsigned i) {
+            ok = tile_wait(sh, &sh.k_full, i & 1);
+            if (!ok) return;
+            tc_fence_after();
+            // rolled, as all of this kernel's loops that need not be unrolled: code that one warp runs once per unit is otherwise
+            // fetched anew from beyond the instruction caches each time
+            const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k, 0);
+#pragma unroll 1
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const int at = (kk >> 2) * 1024 + (kk & 3) * 2;
+                umma_bf16(tm_s, dq + at, dk + at, tile_idesc(kUnit, 0), kk != 0);
+            }
+            umma_commit(&sh.s_full);
+        };
+        if (tid == 0) scores(0);
+        __syncwarp();
         do {
-            const int64_t m0 = (int64_t)it.mb * kTileBM + tid, M = (int64_t)it.live * p.group;
+            const int m0 = it.mb * kTileBM + tid, M = it.live * p.group;           // at most 2^24
             const bool live = m0 < M;
-            const bool warp_live = (int64_t)it.mb * kTileBM + warp * 32 < M;
-            const int r = live ? (int)(m0 / p.group) : 0, hq = it.h * p.group + (int)(m0 - (int64_t)r * p.group);
+            const bool warp_live = it.mb * kTileBM + warp * 32 < M;
+            const int r = live ? m0 / p.group : 0, hq = it.h * p.group + (m0 - r * p.group);
             const int dr = attn_depth(p, it.b, r);
             float m = -INFINITY, l = 0.0f;
             for (int u = it.u0; u < it.u1; ++u, ++n) {
-                ok = __all_sync(kFullMask, tile_wait(sh, &sh.s_full, n & 1));
+                ok = __all_sync(kFullMask, ok && tile_wait(sh, &sh.s_full, n & 1));
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_live) {
@@ -369,136 +517,68 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const AttnW
                         all = all && see[i] == ~0u;
                     }
                     const bool masked = !__all_sync(kFullMask, all || !live);
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t s[32];
-                        tmem_ld32(ts + c * 32, s);
-                        tmem_ld_wait();
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) s[i] = (see[c] >> i) & 1u ? s[i] : 0xff800000u;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(s[i]));
-                    }
-                    mx *= sc;
+                    const float mx = tile_max(ts, masked, see) * sc;
                     if (__any_sync(kFullMask, mx > m + kTileSlack || (m == -INFINITY && mx > m))) {
                         const float mn = fmaxf(m, mx), a = m == -INFINITY ? 0.0f : ex2(m - mn);
                         m = mn;
                         l *= a;
                         if (u > it.u0) {
 #pragma unroll 1
-                            for (int c = 0; c < D / 32; ++c) {
-                                uint32_t o[32];
-                                tmem_ld32(to + c * 32, o);
-                                tmem_ld_wait();
+                            for (int c = 0; c < D / 16; ++c) {
+                                uint32_t o[16];
+                                tmem_ld16(to + c * 16, o);
+                                tmem_ld_wait16(o);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
-                                tmem_st32(to + c * 32, o);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
+                                tmem_st16(to + c * 16, o);
                             }
                         }
                     }
-                    const float off = up - (m == -INFINITY ? 0.0f : m);
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t s[32], pk[16];
-                        tmem_ld32(ts + c * 32, s);
-                        tmem_ld_wait();
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) s[i] = (see[c] >> i) & 1u ? s[i] : 0xff800000u;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float e0 = ex2(fmaf(__uint_as_float(s[2 * i]), sc, off)), e1 = ex2(fmaf(__uint_as_float(s[2 * i + 1]), sc, off));
-                            sum += e0 + e1;
-                            pk[i] = pack_bf16(e0, e1);
-                        }
-                        tmem_st16(ts + c * 16, pk);
-                    }
-                    l = fmaf(sum, down, l);
+                    l = fmaf(tile_weights(ts, masked, see, sc, up - (m == -INFINITY ? 0.0f : m)), down, l);
                     tmem_st_wait();
                 }
                 tc_fence_before();
-                mbar_arrive(&sh.p_ready);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p_ready);
+                if (tid == 0) {                           // O += P V, then the next unit's scores in P's place
+                    ok = tile_wait(sh, &sh.p_ready, n & 1) && tile_wait(sh, &sh.v_full, n & 1);
+                    if (ok) {
+                        tc_fence_after();
+                        const uint64_t dv = umma_desc_mn_sw128(sh.v, 0, 16384);
+                        const bool more = u > it.u0;
+#pragma unroll 1
+                        for (int kk = 0; kk < kUnit / 16; ++kk)
+                            umma_bf16_ts(tm_o, tm_s + kk * 8, dv + kk * 128, tile_idesc(D, 1), (more || kk != 0) ? 1u : 0u);
+                        umma_commit(&sh.pv_done);
+                        if (u + 1 < it.u1 || it.left > 0) {
+                            ok = tile_wait(sh, &sh.pv_done, n & 1);
+                            if (ok) scores(n + 1);
+                        }
+                    }
+                }
+                __syncwarp();                             // the warp's other lanes wait here: polling, they would hold lane 0 up
             }
             if (!ok) break;
             // ---- epilogue ----
-            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done, (n - 1) & 1));
+            ok = __all_sync(kFullMask, ok && tile_wait(sh, &sh.pv_done, (n - 1) & 1));
             if (!ok) break;
             tc_fence_after();
-            if (warp_live) {
-                const bool whole = it.whole();
-                const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-                float* rec = w.records + ((int64_t)blockIdx.x * 2 + (it.u0 > 0 ? 0 : 1)) * record_floats<kTileBM, D>() + tid;
-                unsigned char* dst = p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head) * 2;
-                bool odd = false;
-#pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(to + c * 32, o);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) odd |= (o[i] & 0x7f800000u) == 0x7f800000u;
-                    if constexpr (FP4) {                  // undo the order 0 4 1 5 2 6 3 7
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            const uint32_t t[8] = {o[j], o[j + 1], o[j + 2], o[j + 3], o[j + 4], o[j + 5], o[j + 6], o[j + 7]};
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[j + (i >> 1) + 4 * (i & 1)] = t[i];
-                        }
-                    }
-                    if (!live) continue;
-                    if (whole) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint4 x;
-                            x.x = pack_bf16(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv);
-                            x.y = pack_bf16(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv);
-                            x.z = pack_bf16(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv);
-                            x.w = pack_bf16(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv);
-                            *(uint4*)(dst + c * 64 + j * 2) = x;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) rec[(c * 32 + i) * kTileBM] = __uint_as_float(o[i]);
-                    }
-                }
-                if (live && !whole) { rec[D * kTileBM] = m; rec[(D + 1) * kTileBM] = l; }
-                if (live && whole && p.lse) p.lse[((int64_t)it.b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
-                // rows with a non-finite result once more, over the keys that they see and no others
-                for (uint32_t todo = __ballot_sync(kFullMask, odd && live); todo; todo &= todo - 1) {
-                    const int src = __ffs(todo) - 1;
-                    const int rr = __shfl_sync(kFullMask, r, src), hh = __shfl_sync(kFullMask, hq, src);
-                    RowSums<D> st;
-                    redo_row<D, FP4, kTileBM>(p, it, rr, hh, st);
-                    if (whole) {
-                        const float iv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-                        uint32_t* d2 = (uint32_t*)(p.out + ((int64_t)it.b * p.os_b + (int64_t)rr * p.os_row + (int64_t)hh * p.os_head) * 2) + lane * (D / 64);
-#pragma unroll
-                        for (int i = 0; i < D / 64; ++i) d2[i] = pack_bf16(st.o[2 * i] * iv, st.o[2 * i + 1] * iv);
-                        if (p.lse && lane == 0) p.lse[((int64_t)it.b * p.R + rr) * p.heads_q + hh] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
-                    } else {
-                        float* r2 = w.records + ((int64_t)blockIdx.x * 2 + (it.u0 > 0 ? 0 : 1)) * record_floats<kTileBM, D>() + warp * 32 + src;
-#pragma unroll
-                        for (int i = 0; i < D / 32; ++i) r2[(lane * (D / 32) + i) * kTileBM] = st.o[i];
-                        if (lane == 0) { r2[D * kTileBM] = st.m; r2[(D + 1) * kTileBM] = st.l; }
-                    }
-                    __syncwarp();
-                }
-            }
+            if (warp_live && tile_finish<D, FP4>(w, it, to, live, r, hq, m, l)) sh.odd = 1;
             tc_fence_before();
-        } while (it.next(p));
+        } while (tile_next(it, p));
+        if (tid == 0) {                                   // no product is in flight when the tensor memory is given back
+            umma_commit(&sh.drained);
+            for (int i = 0; i < (1 << 20) && !mbar_try_wait(&sh.drained, 0); ++i) {}
+        }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 0) {
         tc_fence_after();
         tmem_dealloc(tm_s, kTileTmemCols);
     }
+    if (tid == 0) w.odd[blockIdx.x] = (int)sh.odd;
     if (tid == 0 && sh.error && p.status)
         for (int b = 0; b < p.c.batch; ++b) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
 }

@@ -75,7 +75,7 @@ static int sm_count() {
 }
 
 constexpr int kMaxGrid = 512;                             // ranges at most (two CTAs on each SM are fewer)
-constexpr size_t kItemsBytes = ((size_t)kMaxGrid * sizeof(int4) + 255) & ~(size_t)255;
+constexpr size_t kItemsBytes = ((size_t)kMaxGrid * (sizeof(int4) + sizeof(int)) + 255) & ~(size_t)255;
 
 // Units that a call can have at most: what its tables and row capacity have room for.
 static int64_t most_units(const AttnParams& p, int bm) {
@@ -97,7 +97,7 @@ static int launch_tiles(const AttnWork& w, cudaStream_t st) {
     attn_tiles_kernel<D, FP4><<<(unsigned)grid, kTileThreads, tile_smem_bytes<D>(), st>>>(w);
     if (cudaGetLastError() != cudaSuccess) return CADD_ERR_LAUNCH;
     const dim3 join((unsigned)grid, kTileBM * (D / 8) / 256);
-    if (launch_dependent(true, attn_join_kernel<kTileBM, D>, join, dim3(256), 0, st, w, (int)grid) != cudaSuccess) {
+    if (launch_dependent(true, attn_join_kernel<kTileBM, D, FP4>, join, dim3(256), 0, st, w, (int)grid) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
@@ -224,6 +224,7 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     AttnWork w;
     w.p = p;
     w.items = (int4*)a->workspace;
+    w.odd = (int*)(w.items + kMaxGrid);
     w.records = (float*)((unsigned char*)a->workspace + kItemsBytes);
     if (p.c.head_dim == 128) return p.c.fp4 ? launch_tiles<128, true>(w, st) : launch_tiles<128, false>(w, st);
     return p.c.fp4 ? launch_tiles<64, true>(w, st) : launch_tiles<64, false>(w, st);

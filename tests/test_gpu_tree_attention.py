@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2606_01813_b200 import binding as G
-from cache_util import Problem, check_attention
+from cache_util import Problem, attention_tolerance, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -273,3 +273,28 @@ def test_places_behind_two_to_the_thirty_one_bytes():
             v[int(last[b, i])] = p.pools[1][int(p.block_table[b, i])].to(dev)
     c = G.KvCache(k=k, v=v, block_table=last.to(dev), length=torch.tensor(p.lens, dtype=torch.int32, device=dev))
     check_attention(p, p.run(G, cache=c))
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("R,group", [(1, 4), (20, 4), (150, 1)])
+def test_many_more_items_than_the_device_holds_at_once(fp4, R, group):
+    """Hundreds of requests with a few keys each: every range goes through several whole items and parts of others."""
+    batch = 160
+    g = torch.Generator().manual_seed(R)
+    lens = torch.randint(0, 300, (batch,), generator=g).tolist()
+    live = torch.randint(0, R + 1, (batch,), generator=g).tolist()
+    p = problem(fp4=fp4, batch=batch, heads=8, dim=64, group=group, lens=lens, R=R, live=live, page=64)
+    got = p.run(G)
+    status = got.status.clone()
+    for _ in range(3):
+        again = p.run(G)
+        assert torch.equal(again.out, got.out) and torch.equal(again.lse, got.lse)
+    assert int(status.abs().max()) == 0
+    pick = Problem(**{f: getattr(p, f) for f in ("batch", "heads", "group", "dim", "page", "fp4", "lens", "R", "live", "causal", "seed")})
+    for b in list(range(0, batch, 16)) + [batch - 1]:
+        want, wlse, amass, size = pick.attention(b)
+        tol, tol_lse = attention_tolerance(pick, want, wlse, amass, size, pick.lens[b] + pick.live[b])
+        n = pick.live[b]
+        assert bool(((got.out[b, :n].cpu().double() - want).abs() <= tol).all())
+        assert bool(((got.lse[b, :n].cpu().double() - wlse).abs() <= tol_lse).all())
+        assert bool((got.out[b, n:] == 0).all())
