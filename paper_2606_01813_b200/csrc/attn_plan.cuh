@@ -1,7 +1,7 @@
 // How the attention kernels share out their work.
 //
 // An item is (request, key/value head, block of BM rows), a row being one (tree row, query head of the group) pair: all
-// query heads of a group use the same keys, so they stand in one block.  An item's keys are cut into units of 128: the
+// query heads of a group use the same keys, so they stand in one block.  An item's keys are cut into units of 64: the
 // cached places that any of its rows can see (all, or with a window the sinks' units and the window's), then the tree's
 // rows.  All units of all items, one after the other, are cut into equal ranges, one per CTA, whatever the requests'
 // lengths: a CTA works through the ends and wholes of items that its range covers.  An item that lies in one range is
@@ -14,7 +14,7 @@
 
 namespace cadd {
 
-constexpr int kUnit = 128;                               // keys per unit
+constexpr int kUnit = 64;                                // keys per unit
 
 struct AttnWork {
     AttnParams p;
@@ -162,12 +162,12 @@ struct WorkIter {
     __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == n_units; }
 };
 
-// Which of 128 keys from `key0` on row r (place len + dr) sees, as far as lengths, masks and windows say.
+// Which of 64 keys from `key0` on row r (place len + dr) sees, as far as lengths, masks and windows say.
 __device__ __forceinline__ uint32_t bits_from(int x) { return x <= 0 ? ~0u : (x >= 32 ? 0u : ~0u << x); }       // bits x.. of a word
-__device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int key0, uint32_t (&w)[4]) {
+__device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int key0, uint32_t (&w)[kUnit / 32]) {
     if (!tree) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kUnit / 32; ++i) {
             const int k = key0 + 32 * i;
             uint32_t m = ~bits_from(len - k);
             if (p.window > 0) m &= bits_from(len + dr - p.window + 1 - k) | ~bits_from(p.n_sinks - k);
@@ -176,7 +176,7 @@ __device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b,
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kUnit / 32; ++i) {
         const int k = key0 + 32 * i, word = k >> 5;
         uint32_t m = 0;
         if (k < live) {

@@ -1,6 +1,6 @@
-// Tree attention on the 5th-generation tensor cores: blocks of 128 rows, units of 128 keys.
+// Tree attention on the 5th-generation tensor cores: blocks of 128 rows, units of 64 keys.
 //
-// For each unit S = Q K^T goes to tensor memory (M 128 = rows, N 128 = keys, contraction over the head's elements), the
+// For each unit S = Q K^T goes to tensor memory (M 128 = rows, N 64 = keys, contraction over the head's elements), the
 // softmax warps turn it into weights P = e^{s - m} in bf16, written over S, and O += P V is accumulated in tensor memory
 // (A = P from tensor memory, B = V as it lies, [key][element], i.e. "MN-major").  m is a reference, not the exact maximum: it
 // starts as the first unit's maximum and is raised, with O and l multiplied by e^{old - new}, only when a later score exceeds
@@ -15,14 +15,13 @@
 // values and queries stand in shared memory in the order 0 4 1 5 2 6 3 7 within each eight (the product with the keys
 // does not mind, the values' order is undone when O is written).
 //
-// Two CTAs share an SM and alternate on the tensor cores and the exponential units; within one, the next unit's keys are on their
-// way while the softmax runs, its values while the scores are formed.  256 threads (four warps on each quarter of an SM, which
-// leaves 128 registers a thread):
-//   warps 0-3  softmax and epilogue, a row (tensor-memory lane) per thread.  Between a unit's weights and the next unit's scores
-//              they have nothing else to do, so thread 0 also issues the products; warp 0 owns the tensor memory (256
-//              columns: S/P 128, O up to 128);
-//   warps 4-7  loaders: keys and values into the 128-byte swizzle, by asynchronous 16-byte copies (bf16), or through registers
-//              one unit ahead (4 bits).
+// Keys, values and scores are double-buffered: the scores of unit n + 1 are formed and the values of unit n - 1 multiplied while
+// the softmax works on unit n.  (With one buffer of 128 keys the three followed one another, and a unit of 128 keys cost 7000
+// cycles of a CTA; measured on a B200.)  Two CTAs share an SM.  288 threads:
+//   warps 0-3  softmax and epilogue, a row (tensor-memory lane) per thread;
+//   warps 4-5  keys, warps 6-7 values: into the 128-byte swizzle, 32 keys a warp, by asynchronous 16-byte copies (bf16), or
+//              a row a thread through registers, one unit ahead (4 bits); all four load the item's queries;
+//   warp 8     issues the products and owns the tensor memory (256 columns: S/P 2 x 64, O up to 128).
 // Every wait has an iteration limit; a role that gives up sets an error word and all leave.
 //
 // A product of a weight 0 with a non-finite value that the row does not see would be NaN.  A range that meets a non-finite result
@@ -34,19 +33,18 @@
 namespace cadd {
 
 constexpr int kTileBM = 128;
-constexpr int kTileThreads = 256;
+constexpr int kTileThreads = 288;
 constexpr int kTileTmemCols = 256;
 constexpr float kTileSlack = 40.0f;                      // log2 of how far weights may exceed 1 before m is raised
 
 template <int D> struct alignas(1024) TileShared {
     unsigned char q[kTileBM * D * 2];                    // D/64 sub-tiles of 128 rows x 128 bytes
-    unsigned char k[kUnit * D * 2];
-    unsigned char v[kUnit * D * 2];
-    int64_t key_row[2][kUnit];                           // bf16: byte offsets of the unit's rows, -1 for none
-    uint64_t k_full, v_full, s_full, p_ready, pv_done, drained;
+    unsigned char k[2][kUnit * D * 2];                   // D/64 sub-tiles of 64 rows x 128 bytes
+    unsigned char v[2][kUnit * D * 2];
+    uint64_t q_full, k_full[2], v_full[2], s_full[2], p_ready[2], pv_done[2], drained;
     PlanShared plan;
     WorkIter<kTileBM> it[kTileThreads / 32];             // a walk per warp: here, not in registers, which are scarce
-    uint32_t key_bits[2][4];                             // keys of the unit that exist
+    uint32_t key_bits[4][2];                             // keys of the unit that exist
     uint32_t tmem_base, error, odd;
 };
 template <int D> constexpr size_t tile_smem_bytes() { return sizeof(TileShared<D>) + 1024; }
@@ -67,10 +65,26 @@ __device__ __forceinline__ bool tile_wait(Shared& sh, uint64_t* bar, unsigned pa
     sh.error = 1;
     return false;
 }
-__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+// The products, issued by the lane with `one` set of a warp that runs them together: the operands stay in uniform registers.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void umma_ss(uint32_t one, uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %0, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%1], %2, %3, %4, p;\n\t}"
+                 ::"r"(one), "r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t one, uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %0, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%1], [%2], %3, %4, p;\n\t}"
+                 ::"r"(one), "r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit_one(uint32_t one, uint64_t* bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %0, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}"
+                 ::"r"(one), "r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {       // whole warp: 32 lanes x 16 columns
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -120,9 +134,10 @@ __host__ __device__ constexpr uint32_t tile_idesc(int n, int b_mn) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTileBM >> 4) << 24);
 }
 
-// Shared-memory offset of 16-byte chunk `ch` of row `row` in a tile of rows of D bf16 elements (sub-tiles of 64 elements).
+// Shared-memory offset of 16-byte chunk `ch` of row `row` in a tile of ROWS rows of bf16 elements (sub-tiles of 64 elements).
+template <int ROWS>
 __device__ __forceinline__ uint32_t tile_off(int row, int ch) {
-    return (uint32_t)((ch >> 3) * (128 * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+    return (uint32_t)((ch >> 3) * (ROWS * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
 }
 // Elements 0..7 of a chunk in the order 0 4 1 5 2 6 3 7.
 __device__ __forceinline__ uint4 order_pairs(uint4 w) {
@@ -167,15 +182,15 @@ __device__ __forceinline__ void fp4_row_load(Fp4Row<D>& x, const unsigned char* 
     }
 }
 template <int D>
-__device__ __noinline__ void fp4_row_store(const Fp4Row<D> x, unsigned char* tile, int row) {
+__device__ __forceinline__ void fp4_row_store(const Fp4Row<D>& x, unsigned char* tile, int row) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {                   // 32 elements: a 16-byte word of codes, two scales
         uint32_t f0, f1;
         fp4_unit_scales((x.s[i >> 1] >> ((i & 1) * 16)) & 0xffffu, f0, f1);
-        *(uint4*)(tile + tile_off(row, i * 4 + 0)) = fp4_unit_values(x.w[i].x, f0);
-        *(uint4*)(tile + tile_off(row, i * 4 + 1)) = fp4_unit_values(x.w[i].y, f0);
-        *(uint4*)(tile + tile_off(row, i * 4 + 2)) = fp4_unit_values(x.w[i].z, f1);
-        *(uint4*)(tile + tile_off(row, i * 4 + 3)) = fp4_unit_values(x.w[i].w, f1);
+        *(uint4*)(tile + tile_off<kUnit>(row, i * 4 + 0)) = fp4_unit_values(x.w[i].x, f0);
+        *(uint4*)(tile + tile_off<kUnit>(row, i * 4 + 1)) = fp4_unit_values(x.w[i].y, f0);
+        *(uint4*)(tile + tile_off<kUnit>(row, i * 4 + 2)) = fp4_unit_values(x.w[i].z, f1);
+        *(uint4*)(tile + tile_off<kUnit>(row, i * 4 + 3)) = fp4_unit_values(x.w[i].w, f1);
     }
 }
 
@@ -201,42 +216,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 // The wait names the registers that it makes valid, so that nothing that reads them can be moved in front of it.
+__device__ __forceinline__ void tmem_ld_wait8(uint32_t (&r)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]) :: "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait16(uint32_t (&r)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
-__device__ __forceinline__ void mask_scores(uint32_t (&x)[16], uint32_t (&y)[16], uint32_t see) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        x[i] = (see >> i) & 1u ? x[i] : 0xff800000u;
-        y[i] = (see >> (16 + i)) & 1u ? y[i] : 0xff800000u;
-    }
-}
-// A row's scores of a unit lie in tensor memory at `ts`; a load takes some 200 cycles.  First the largest, 64 columns at a time:
-__device__ __forceinline__ float tile_max(uint32_t ts, bool masked, const uint32_t (&see)[4]) {
-    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    uint32_t s[4][16];
-#pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) tmem_ld16(ts + c * 64 + j * 16, s[j]);
-        tmem_ld_wait16(s[0]); tmem_ld_wait16(s[1]); tmem_ld_wait16(s[2]); tmem_ld_wait16(s[3]);
-        if (masked) {
-            mask_scores(s[0], s[1], c ? see[2] : see[0]);
-            mask_scores(s[2], s[3], c ? see[3] : see[1]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t (&x)[16] = s[j];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
-        }
-    }
-    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-}
-// then the weights 2^(s sc + off), written over the scores (columns that have been read already) as packed bf16, and their sum:
-// 32 columns are worked on, long enough for the next 32 to arrive.
+// 2^(s sc + off) of 16 scores, packed and written to tensor memory.
 __device__ __forceinline__ void weights_of(const uint32_t (&x)[16], uint64_t sc2, uint64_t off2, uint64_t (&sum)[2], uint32_t dst) {
     uint32_t pk[8];
 #pragma unroll
@@ -249,33 +237,6 @@ __device__ __forceinline__ void weights_of(const uint32_t (&x)[16], uint64_t sc2
         pk[i] = pack_bf16(e0, e1);
     }
     tmem_st8(dst, pk);
-}
-__device__ __forceinline__ float tile_weights(uint32_t ts, bool masked, const uint32_t (&see)[4], float sc, float off) {
-    const uint64_t sc2 = pack2(sc, sc), off2 = pack2(off, off);
-    uint64_t sum[2] = {0, 0};
-    uint32_t s[4][16];
-    tmem_ld16(ts, s[0]);
-    tmem_ld16(ts + 16, s[1]);
-#pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
-        tmem_ld_wait16(s[0]); tmem_ld_wait16(s[1]);
-        tmem_ld16(ts + c * 64 + 32, s[2]);
-        tmem_ld16(ts + c * 64 + 48, s[3]);
-        if (masked) mask_scores(s[0], s[1], c ? see[2] : see[0]);
-        weights_of(s[0], sc2, off2, sum, ts + c * 32);
-        weights_of(s[1], sc2, off2, sum, ts + c * 32 + 8);
-        tmem_ld_wait16(s[2]); tmem_ld_wait16(s[3]);
-        if (c == 0) {
-            tmem_ld16(ts + 64, s[0]);
-            tmem_ld16(ts + 80, s[1]);
-        }
-        if (masked) mask_scores(s[2], s[3], c ? see[3] : see[1]);
-        weights_of(s[2], sc2, off2, sum, ts + c * 32 + 16);
-        weights_of(s[3], sc2, off2, sum, ts + c * 32 + 24);
-    }
-    float a, b;
-    unpack2(add2(sum[0], sum[1]), a, b);
-    return a + b;
 }
 
 // A warp's walk in shared memory goes on to the next item: one lane moves it, no lane still reads the old or already reads the new.
@@ -352,148 +313,156 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
     __syncwarp();
     if (tid == 0) {
         w.items[blockIdx.x] = make_int4(it.b, it.h, it.mb, (it.u0 > 0 ? kRangeInside : 0) | (it.u1 == it.n_units ? kRangeEnds : 0));
-        mbar_init(&sh.k_full, 4);
-        mbar_init(&sh.v_full, 4);
-        mbar_init(&sh.s_full, 1);
-        mbar_init(&sh.p_ready, 4);
-        mbar_init(&sh.pv_done, 1);
+        mbar_init(&sh.q_full, 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.k_full[i], 2);
+            mbar_init(&sh.v_full[i], 2);
+            mbar_init(&sh.s_full[i], 1);
+            mbar_init(&sh.p_ready[i], 4);
+            mbar_init(&sh.pv_done[i], 1);
+        }
         mbar_init(&sh.drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 0) tmem_alloc(&sh.tmem_base, kTileTmemCols);
+    if (warp == 8) tmem_alloc(&sh.tmem_base, kTileTmemCols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tm_s = *(volatile uint32_t*)&sh.tmem_base, tm_o = tm_s + kUnit;
+    const uint32_t tm_s = *(volatile uint32_t*)&sh.tmem_base, tm_o = tm_s + 2 * kUnit;
     constexpr int kCh = D / 8;                            // 16-byte chunks of a bf16 row
 
-    if (warp >= 4) {
+    // Units are numbered through the CTA's whole range: unit n uses buffer n & 1, in its (n >> 1)-th turn.
+    if (warp == 8) {
+        // ---------------- products ----------------
+        const uint32_t one = elect_one();
+        unsigned n = 0, items = 0;
+        bool ok = true;
+        auto output = [&](unsigned i, bool first) {       // O (+)= P V of unit i
+            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.p_ready[i & 1], (i >> 1) & 1) && tile_wait(sh, &sh.v_full[i & 1], (i >> 1) & 1)))) return;
+            tc_fence_after();
+            const uint64_t dv = umma_desc_mn_sw128(sh.v[i & 1], 0, kUnit * 128);
+            const uint32_t pm = tm_s + (i & 1) * kUnit;
+#pragma unroll
+            for (int kk = 0; kk < kUnit / 16; ++kk) umma_ts(one, tm_o, pm + kk * 8, dv + kk * 128, tile_idesc(D, 1), (!first || kk != 0) ? 1u : 0u);
+            umma_commit_one(one, &sh.pv_done[i & 1]);
+        };
+        do {
+            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.q_full, items & 1)))) break;
+            ++items;
+            for (int u = it.u0; u < it.u1; ++u, ++n) {
+                // scores of unit n, in the columns of P of unit n - 2, whose product must be done
+                ok = __all_sync(kFullMask, tile_wait(sh, &sh.k_full[n & 1], (n >> 1) & 1) && (n < 2 || tile_wait(sh, &sh.pv_done[n & 1], ((n >> 1) - 1) & 1)));
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k[n & 1], 0);
+                const uint32_t sm = tm_s + (n & 1) * kUnit;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                    umma_ss(one, sm, dq + (kk >> 2) * 1024 + (kk & 3) * 2, dk + (kk >> 2) * (kUnit * 8) + (kk & 3) * 2, tile_idesc(kUnit, 0), kk != 0);
+                umma_commit_one(one, &sh.s_full[n & 1]);
+                if (u > it.u0) output(n - 1, u == it.u0 + 1);
+                if (!ok) break;
+            }
+            if (ok) output(n - 1, it.u1 == it.u0 + 1);    // the item's last
+        } while (ok && tile_next(it, p));
+        umma_commit_one(one, &sh.drained);                // no product is in flight when the tensor memory is given back
+        for (int i = 0; i < (1 << 20) && !mbar_try_wait(&sh.drained, 0); ++i) {}
+    } else if (warp >= 4) {
         // ---------------- loaders ----------------
-        const int lt = tid - 128;                         // the thread's key (and row of Q)
+        const bool values = warp >= 6;
+        const int kt = (warp & 1) * 32 + lane;            // the thread's key of a unit
+        const unsigned char* pool = values ? p.c.v : p.c.k;
+        const unsigned char* scales = values ? p.c.vs : p.c.ks;
+        const unsigned char* own = values ? p.v : p.k;    // the tree's rows
+        uint64_t* full = values ? sh.v_full : sh.k_full;
+        uint64_t* freed = values ? sh.pv_done : sh.s_full;                         // the product that reads a buffer is done
         unsigned n = 0;
         bool ok = true;
-        Fp4Row<D> kx, vx;
+        Fp4Row<D> x;
         do {
             const int64_t kv0 = ((int64_t)it.b * p.kvs_b + (int64_t)it.h * p.kvs_head) * 2;
             auto row_of = [&](int u) -> int64_t {         // of the thread's key: cache row (4 bits), or byte offset; -1: none
-                const int key = it.first_key(u) + lt;
+                const int key = it.first_key(u) + kt;
                 if (it.is_tree(u)) return key < it.live ? kv0 + (int64_t)key * p.kvs_row * 2 : -1;
                 if (key >= it.len) return -1;
                 const int64_t row = cache_row(p.c, it.b, it.h, key);
                 return FP4 || row < 0 ? row : row * (D * 2);
             };
             int64_t row = row_of(it.u0);
-            bool held = false;                            // kx, vx hold unit u's rows
-            for (int u = it.u0; u < it.u1; ++u, ++n) {
-                const bool tree = it.is_tree(u);
-                const uint32_t there = __ballot_sync(kFullMask, row >= 0);
-                if constexpr (FP4) {
-                    if (!tree && !held) { fp4_row_load<D>(kx, p.c.k, p.c.ks, row); fp4_row_load<D>(vx, p.c.v, p.c.vs, row); }
-                } else {
-                    sh.key_row[n & 1][lt] = row;
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
-                }
-                if (n > 0) ok = tile_wait(sh, &sh.s_full, (n - 1) & 1);            // the product with the keys before is done
-                if (!__all_sync(kFullMask, ok)) { ok = false; break; }
-                if (lane == 0) sh.key_bits[n & 1][warp - 4] = there;
-                if (u == it.u0) {                         // the item's queries
-                    const int m0 = it.mb * kTileBM + lt, r = m0 / p.group, g = m0 - r * p.group;
-                    const uint4* src = (const uint4*)(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)(it.h * p.group + g) * p.qs_head) * 2);
-                    const bool live = r < it.live;
+            if constexpr (FP4) { if (!it.is_tree(it.u0)) fp4_row_load<D>(x, pool, scales, row); }
+            {   // the item's queries, once the last product with those before is done
+                const int m0 = it.mb * kTileBM + (tid - 128), r = m0 / p.group, g = m0 - r * p.group;
+                const uint4* src = (const uint4*)(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)(it.h * p.group + g) * p.qs_head) * 2);
+                const bool live = r < it.live;
+                if (n > 0) ok = tile_wait(sh, &sh.s_full[(n - 1) & 1], ((n - 1) >> 1) & 1);
+                if (!(ok = __all_sync(kFullMask, ok))) break;
 #pragma unroll 4
-                    for (int ch = 0; ch < kCh; ++ch) {
-                        uint4 x = live ? __ldg(src + ch) : make_uint4(0, 0, 0, 0);
-                        if constexpr (FP4) x = order_pairs(x);
-                        *(uint4*)(sh.q + tile_off(lt, ch)) = x;
-                    }
+                for (int ch = 0; ch < kCh; ++ch) {
+                    uint4 t = live ? __ldg(src + ch) : make_uint4(0, 0, 0, 0);
+                    if constexpr (FP4) t = order_pairs(t);
+                    *(uint4*)(sh.q + tile_off<kTileBM>(tid - 128, ch)) = t;
                 }
-                const bool more = u + 1 < it.u1;
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.q_full);
+            }
+            for (int u = it.u0; u < it.u1; ++u, ++n) {
+                const bool tree = it.is_tree(u), more = u + 1 < it.u1;
+                unsigned char* tile = values ? sh.v[n & 1] : sh.k[n & 1];
+                const uint32_t there = __ballot_sync(kFullMask, row >= 0);
+                if (n >= 2) ok = tile_wait(sh, &freed[n & 1], ((n >> 1) - 1) & 1);
+                if (!(ok = __all_sync(kFullMask, ok))) break;
+                if (!values && lane == 0) sh.key_bits[n & 3][warp & 1] = there;
                 int64_t next_row = -1;
                 if constexpr (FP4) {
-                    const bool ahead = more && !it.is_tree(u + 1);
-                    if (more) next_row = row_of(u + 1);
                     if (!tree) {
-                        fp4_row_store<D>(kx, sh.k, lt);
+                        fp4_row_store<D>(x, tile, kt);
                     } else {
 #pragma unroll 4
                         for (int ch = 0; ch < kCh; ++ch)
-                            *(uint4*)(sh.k + tile_off(lt, ch)) = row >= 0 ? order_pairs(__ldg((const uint4*)(p.k + row) + ch)) : make_uint4(0, 0, 0, 0);
+                            *(uint4*)(tile + tile_off<kUnit>(kt, ch)) = row >= 0 ? order_pairs(__ldg((const uint4*)(own + row) + ch)) : make_uint4(0, 0, 0, 0);
                     }
-                    if (ahead) fp4_row_load<D>(kx, p.c.k, p.c.ks, next_row);
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.k_full);
-                    if (n > 0) ok = tile_wait(sh, &sh.pv_done, (n - 1) & 1);
-                    if (!__all_sync(kFullMask, ok)) { ok = false; break; }
-                    if (!tree) {
-                        fp4_row_store<D>(vx, sh.v, lt);
-                    } else {
-#pragma unroll 4
-                        for (int ch = 0; ch < kCh; ++ch)
-                            *(uint4*)(sh.v + tile_off(lt, ch)) = row >= 0 ? order_pairs(__ldg((const uint4*)(p.v + row) + ch)) : make_uint4(0, 0, 0, 0);
+                    if (lane == 0) mbar_arrive(&full[n & 1]);
+                    if (more) {
+                        next_row = row_of(u + 1);
+                        if (!it.is_tree(u + 1)) fp4_row_load<D>(x, pool, scales, next_row);
                     }
-                    if (ahead) fp4_row_load<D>(vx, p.c.v, p.c.vs, next_row);
-                    held = ahead;
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.v_full);
                 } else {
-                    const unsigned char* kb = tree ? p.k : p.c.k;
-                    const unsigned char* vb = tree ? p.v : p.c.v;
-                    const int ch = lt % kCh;
+                    const unsigned char* base = tree ? own : pool;
+                    const int ch = lane % kCh;
 #pragma unroll 4
-                    for (int i = lt / kCh; i < kUnit; i += 128 / kCh) {
-                        const int64_t off = sh.key_row[n & 1][i];
-                        cp_async16(smem_u32(sh.k) + tile_off(i, ch), kb + (off < 0 ? 0 : off + ch * 16), off < 0 ? 0u : 16u);
+                    for (int i = lane / kCh; i < 32; i += 32 / kCh) {
+                        const int64_t off = __shfl_sync(kFullMask, row, i);
+                        cp_async16(smem_u32(tile) + tile_off<kUnit>((warp & 1) * 32 + i, ch), base + (off < 0 ? 0 : off + ch * 16), off < 0 ? 0u : 16u);
                     }
                     cp_async_commit();
+                    if (u > it.u0) {                      // unit n - 1 has landed
+                        cp_async_wait<1>();
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&full[(n - 1) & 1]);
+                    }
                     if (more) next_row = row_of(u + 1);
-                    if (n > 0) ok = tile_wait(sh, &sh.pv_done, (n - 1) & 1);
-                    if (!__all_sync(kFullMask, ok)) { ok = false; break; }
-#pragma unroll 4
-                    for (int i = lt / kCh; i < kUnit; i += 128 / kCh) {
-                        const int64_t off = sh.key_row[n & 1][i];
-                        cp_async16(smem_u32(sh.v) + tile_off(i, ch), vb + (off < 0 ? 0 : off + ch * 16), off < 0 ? 0u : 16u);
-                    }
-                    cp_async_commit();
-                    cp_async_wait<1>();
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.k_full);
-                    cp_async_wait<0>();
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.v_full);
                 }
                 row = next_row;
             }
+            if constexpr (!FP4) {                         // the item's last unit
+                cp_async_wait<0>();
+                fence_async_shared();
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(&full[(n - 1) & 1]);
+            }
         } while (ok && tile_next(it, p));
-        cp_async_wait<0>();
     } else {
         // ---------------- softmax and epilogue ----------------
-        const uint32_t ts = tm_s + ((uint32_t)(warp * 32) << 16), to = tm_o + ((uint32_t)(warp * 32) << 16);
+        const uint32_t to = tm_o + ((uint32_t)(warp * 32) << 16);
         // what the 4-bit form leaves to be put right: scores of cached keys times 2^(8 - k_exp), weights times 2^(8 - v_exp)
         const float sc_ctx = FP4 ? p.scale_log2 * exp2i(8 - p.c.k_exp) : p.scale_log2;
         const float up_ctx = FP4 ? (float)(8 - p.c.v_exp) : 0.0f, down_ctx = FP4 ? exp2i(p.c.v_exp - 8) : 1.0f;
         unsigned n = 0;
         bool ok = true;
-        // thread 0: the scores of unit number i, once its keys are there
-        auto scores = [&](unsigned i) {
-            ok = tile_wait(sh, &sh.k_full, i & 1);
-            if (!ok) return;
-            tc_fence_after();
-            // rolled, as all of this kernel's loops that need not be unrolled: code that one warp runs once per unit is otherwise
-            // fetched anew from beyond the instruction caches each time
-            const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k, 0);
-#pragma unroll 1
-            for (int kk = 0; kk < D / 16; ++kk) {
-                const int at = (kk >> 2) * 1024 + (kk & 3) * 2;
-                umma_bf16(tm_s, dq + at, dk + at, tile_idesc(kUnit, 0), kk != 0);
-            }
-            umma_commit(&sh.s_full);
-        };
-        if (tid == 0) scores(0);
-        __syncwarp();
         do {
             const int m0 = it.mb * kTileBM + tid, M = it.live * p.group;           // at most 2^24
             const bool live = m0 < M;
@@ -502,79 +471,77 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
             const int dr = attn_depth(p, it.b, r);
             float m = -INFINITY, l = 0.0f;
             for (int u = it.u0; u < it.u1; ++u, ++n) {
-                ok = __all_sync(kFullMask, ok && tile_wait(sh, &sh.s_full, n & 1));
+                ok = __all_sync(kFullMask, tile_wait(sh, &sh.s_full[n & 1], (n >> 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_live) {
-                    const bool tree = it.is_tree(u);
-                    const float sc = tree ? p.scale_log2 : sc_ctx, up = tree ? 0.0f : up_ctx, down = tree ? 1.0f : down_ctx;
-                    uint32_t see[4];
-                    unit_bits(p, tree, it.b, it.len, it.live, r, dr, it.first_key(u), see);
-                    bool all = true;
+                    const uint32_t ts = tm_s + (n & 1) * kUnit + ((uint32_t)(warp * 32) << 16);
+                    uint32_t s[4][16];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        see[i] &= sh.key_bits[n & 1][i];
-                        all = all && see[i] == ~0u;
+                    for (int j = 0; j < 4; ++j) tmem_ld16(ts + j * 16, s[j]);
+                    const bool tree = it.is_tree(u);
+                    uint32_t see[2];
+                    unit_bits(p, tree, it.b, it.len, it.live, r, dr, it.first_key(u), see);
+                    see[0] &= sh.key_bits[n & 3][0];
+                    see[1] &= sh.key_bits[n & 3][1];
+                    const bool masked = !__all_sync(kFullMask, (see[0] & see[1]) == ~0u || !live);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tmem_ld_wait16(s[j]);
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < kUnit; ++i) s[i >> 4][i & 15] = (see[i >> 5] >> (i & 31)) & 1u ? s[i >> 4][i & 15] : 0xff800000u;
                     }
-                    const bool masked = !__all_sync(kFullMask, all || !live);
-                    const float mx = tile_max(ts, masked, see) * sc;
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < kUnit; i += 2) mx4[(i >> 1) & 3] = max3(mx4[(i >> 1) & 3], __uint_as_float(s[i >> 4][i & 15]), __uint_as_float(s[i >> 4][(i & 15) + 1]));
+                    const float sc = tree ? p.scale_log2 : sc_ctx;
+                    const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * sc;
                     if (__any_sync(kFullMask, mx > m + kTileSlack || (m == -INFINITY && mx > m))) {
                         const float mn = fmaxf(m, mx), a = m == -INFINITY ? 0.0f : ex2(m - mn);
                         m = mn;
                         l *= a;
-                        if (u > it.u0) {
+                        if (u > it.u0) {                  // the product before must be done with O
+                            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1));
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll 1
-                            for (int c = 0; c < D / 16; ++c) {
-                                uint32_t o[16];
-                                tmem_ld16(to + c * 16, o);
-                                tmem_ld_wait16(o);
+                            for (int c = 0; c < D / 8; ++c) {
+                                uint32_t o[8];
+                                tmem_ld8(to + c * 8, o);
+                                tmem_ld_wait8(o);
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
-                                tmem_st16(to + c * 16, o);
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * a);
+                                tmem_st8(to + c * 8, o);
                             }
                         }
                     }
-                    l = fmaf(tile_weights(ts, masked, see, sc, up - (m == -INFINITY ? 0.0f : m)), down, l);
+                    const float off = (tree ? 0.0f : up_ctx) - (m == -INFINITY ? 0.0f : m);
+                    const uint64_t sc2 = pack2(sc, sc), off2 = pack2(off, off);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) weights_of(s[j], sc2, off2, sum, ts + j * 8);
+                    float sa, sb;
+                    unpack2(add2(sum[0], sum[1]), sa, sb);
+                    l = fmaf(sa + sb, tree ? 1.0f : down_ctx, l);
                     tmem_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.p_ready);
-                if (tid == 0) {                           // O += P V, then the next unit's scores in P's place
-                    ok = tile_wait(sh, &sh.p_ready, n & 1) && tile_wait(sh, &sh.v_full, n & 1);
-                    if (ok) {
-                        tc_fence_after();
-                        const uint64_t dv = umma_desc_mn_sw128(sh.v, 0, 16384);
-                        const bool more = u > it.u0;
-#pragma unroll 1
-                        for (int kk = 0; kk < kUnit / 16; ++kk)
-                            umma_bf16_ts(tm_o, tm_s + kk * 8, dv + kk * 128, tile_idesc(D, 1), (more || kk != 0) ? 1u : 0u);
-                        umma_commit(&sh.pv_done);
-                        if (u + 1 < it.u1 || it.left > 0) {
-                            ok = tile_wait(sh, &sh.pv_done, n & 1);
-                            if (ok) scores(n + 1);
-                        }
-                    }
-                }
-                __syncwarp();                             // the warp's other lanes wait here: polling, they would hold lane 0 up
+                if (lane == 0) mbar_arrive(&sh.p_ready[n & 1]);
             }
             if (!ok) break;
             // ---- epilogue ----
-            ok = __all_sync(kFullMask, ok && tile_wait(sh, &sh.pv_done, (n - 1) & 1));
+            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1));
             if (!ok) break;
             tc_fence_after();
             if (warp_live && tile_finish<D, FP4>(w, it, to, live, r, hq, m, l)) sh.odd = 1;
             tc_fence_before();
         } while (tile_next(it, p));
-        if (tid == 0) {                                   // no product is in flight when the tensor memory is given back
-            umma_commit(&sh.drained);
-            for (int i = 0; i < (1 << 20) && !mbar_try_wait(&sh.drained, 0); ++i) {}
-        }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) {
+    if (warp == 8) {
         tc_fence_after();
         tmem_dealloc(tm_s, kTileTmemCols);
     }
