@@ -3,6 +3,7 @@
 #pragma once
 #include "cache.cuh"
 #include "tree_attention.cuh"
+#include "fp4.cuh"
 
 namespace cadd {
 
@@ -19,44 +20,179 @@ struct WeightsParams {
     int32_t* status;
     int heads_q, group, window, n_sinks;
     float scale_log2;
-    int ctas_per_head;
+    int ctas_per_head, keys_per_cta;
 };
 
-// Simplest form: a warp per (request, head, place) goes over the accepted rows and the heads of the group.
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Weights of the accepted rows on the cached keys.  Few rows (the path times the group's heads, 16 to some 70) meet long
+// caches, so the keys are read once and everything else has to keep up with that: 72 bytes a key and head in 4 bits are three
+// cycles of an SM.  Warp-level products (16 rows x 8 keys x 16 elements) take a key's elements from registers as they come from
+// memory, without a detour over shared memory: which element stands in which place of the contraction is free as long as
+// rows and keys agree, so lane t of a key's four lanes holds a contiguous quarter of its row (4 bits: one 16-byte load, D 128),
+// and word m of it, eight elements, feeds contraction steps 2m and 2m + 1.  The rows stand in shared memory as 16-byte chunks in
+// the same order.  A warp takes 32 keys at a time, the next 32 being on their way; sums over rows stay in registers and are
+// joined across the lanes at the end, in a fixed order.  More than 128 rows are done in groups, the later ones adding to
+// what the earlier ones wrote.
+constexpr int kWThreads = 128;
+constexpr int kWRows = 128;                              // rows in shared memory at a time
+template <int D> struct alignas(16) WeightsShared {
+    uint4 q[kWRows][D / 8 + 1];                          // one chunk of padding: rows eight apart lie in different banks
+    float lse[kWRows];                                   // times log2(e); +Inf marks a row that adds nothing
+    int place[kWRows];
+};
+
+template <int D, bool FP4> struct WKeys;                 // eight keys' rows as a lane holds them
+template <int D> struct WKeys<D, true> { uint32_t w[D / 32]; uint32_t s; };
+template <int D> struct WKeys<D, false> { uint4 w[D / 32]; };
+
 template <int D, bool FP4>
-__global__ void __launch_bounds__(128) weights_kernel(const WeightsParams p) {
-    const int lane = threadIdx.x & 31;
-    const int64_t bh = blockIdx.x / p.ctas_per_head;
-    const int part = (int)(blockIdx.x - bh * p.ctas_per_head), b = (int)(bh / p.c.heads), h = (int)(bh - (int64_t)b * p.c.heads);
-    const int len = cache_length(p.c, b), base = min(max(p.base_length[b], 0), len);
-    int clamped;
-    const int n = min(row_count(p.rows, b, &clamped), len - base);
-    for (int pos = part * 4 + (threadIdx.x >> 5); pos < len; pos += p.ctas_per_head * 4) {
-        const int64_t row = cache_row(p.c, b, h, pos);
-        float sum = 0.0f;
+__device__ __forceinline__ void wkeys_load(WKeys<D, FP4>& x, const CacheView& c, int64_t row, int t) {
+    if constexpr (FP4) {
+        x.s = 0;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) x.w[i] = 0;
         if (row >= 0) {
-            float k[D / 32], q[D / 32];
-            load_row_cache<D, FP4>(p.c, p.c.k, p.c.ks, p.c.k_exp, row, lane, k);
-            for (int i = 0; i < n; ++i) {
-                const int r = row_at(p.rows, b, i);
-                if (r < 0 || pos > base + i || !(p.window == 0 || pos < p.n_sinks || base + i - pos < p.window)) continue;
-                for (int g = 0; g < p.group; ++g) {
-                    const int hq = h * p.group + g;
-                    load_row_bf16<D>(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2, lane, q);
-                    float s = 0.0f;
+            if constexpr (D == 128) {
+                const uint4 v = __ldg((const uint4*)(c.k + row * (D / 2)) + t);
+                x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
+                x.s = __ldg((const unsigned short*)(c.ks + row * (D / 16)) + t);
+            } else {
+                const uint2 v = __ldg((const uint2*)(c.k + row * (D / 2)) + t);
+                x.w[0] = v.x; x.w[1] = v.y;
+                x.s = __ldg(c.ks + row * (D / 16) + t);
+            }
+        }
+    } else {
 #pragma unroll
-                    for (int j = 0; j < D / 32; ++j) s = fmaf(q[j], k[j], s);
+        for (int i = 0; i < D / 32; ++i) x.w[i] = row >= 0 ? __ldg((const uint4*)(c.k + row * (D * 2)) + i * 4 + t) : make_uint4(0, 0, 0, 0);
+    }
+}
+// Word m of lane t holds chunk t * W + m (4 bits) or 4 m + t (bf16) of its key's row, W = D / 32; rows keep that chunk in slot
+// 4 m + t, so that a key's four lanes read neighbouring slots.
+template <int D, bool FP4> __device__ __forceinline__ int wkeys_slot(int chunk) { return FP4 ? (chunk % (D / 32)) * 4 + chunk / (D / 32) : chunk; }
+
+template <int D, bool FP4>
+__global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(const __grid_constant__ WeightsParams p) {
+    extern __shared__ __align__(16) unsigned char weights_smem_raw[];
+    WeightsShared<D>& sh = *reinterpret_cast<WeightsShared<D>*>(weights_smem_raw);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int bh = blockIdx.x / p.ctas_per_head, part = blockIdx.x - bh * p.ctas_per_head, b = bh / p.c.heads, h = bh - b * p.c.heads;
+    const int len = cache_length(p.c, b), begin = part * p.keys_per_cta, end = min(len, begin + p.keys_per_cta);
+    if (begin >= end) return;
+    const int base = min(max(p.base_length[b], 0), len);
+    int clamped;
+    const int rows = min(row_count(p.rows, b, &clamped), len - base) * p.group;
+    const float sc = FP4 ? p.scale_log2 * exp2i(8 - p.c.k_exp) : p.scale_log2;
+    const float* w_in = p.w_in + (int64_t)bh * p.w_stride;
+    float* w_out = p.w_out + (int64_t)bh * p.w_stride;
+    constexpr int W = D / 32;                            // words of a lane, two contraction steps each
+
+    for (int m0 = 0; m0 == 0 || m0 < rows; m0 += kWRows) {
+        const int here = min(rows - m0, kWRows), tiles = (here + 15) >> 4;
+        if (m0) __syncthreads();
+        for (int i = tid; i < tiles * 16 * (D / 8); i += kWThreads) {
+            const int m = i / (D / 8), ch = i - m * (D / 8), li = (m0 + m) / p.group, hq = h * p.group + (m0 + m - li * p.group);
+            const int r = m < here ? row_at(p.rows, b, li) : -1;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r >= 0) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
+            sh.q[m][wkeys_slot<D, FP4>(ch)] = FP4 ? order_pairs(x) : x;
+            if (ch == 0) {
+                const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
+                sh.lse[m] = fabsf(lse) == INFINITY ? INFINITY : lse * kLog2e;
+                sh.place[m] = base + li;
+            }
+        }
+        __syncthreads();
+        auto row_of = [&](int key) -> int64_t { return key < end ? cache_row(p.c, b, h, key) : -1; };
+        WKeys<D, FP4> x[4];
+        int64_t row[4];
+        int k0 = begin + warp * 32;
 #pragma unroll
-                    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFullMask, s, o);
-                    const float lse = p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq];
-                    if (fabsf(lse) != INFINITY) sum += exp2f(s * p.scale_log2 - lse * kLog2e);
+        for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row_of(k0 + j * 8 + g), t);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = row_of(k0 + kWThreads + j * 8 + g);
+        for (; k0 < end; k0 += kWThreads) {
+            uint32_t kf[4][W * 4];                       // the 32 keys as operands: [key group of 8][word][two steps x two registers]
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (FP4) {
+                    uint32_t f0, f1;
+                    fp4_unit_scales(x[j].s, f0, f1);
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const uint4 v = fp4_unit_values(x[j].w[i], (D == 128 && i >= 2) ? f1 : f0);
+                        kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) { kf[j][4 * i] = x[j].w[i].x; kf[j][4 * i + 1] = x[j].w[i].y; kf[j][4 * i + 2] = x[j].w[i].z; kf[j][4 * i + 3] = x[j].w[i].w; }
+                }
+            }
+            // the next keys' rows, and where those behind them lie
+#pragma unroll
+            for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) row[j] = row_of(k0 + 2 * kWThreads + j * 8 + g);
+            float sum[4][2] = {};
+            if (p.window == 0 || k0 < p.n_sinks || k0 + 31 > base - p.window) {
+                const bool plain = p.window == 0 && k0 + 31 <= base;               // every row sees all 32
+                for (int mt = 0; mt < tiles; ++mt) {
+                    float c[4][4] = {};
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const uint4 lo = sh.q[mt * 16 + g][i * 4 + t], hi = sh.q[mt * 16 + g + 8][i * 4 + t];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            mma_bf16(c[j], lo.x, hi.x, lo.y, hi.y, kf[j][4 * i], kf[j][4 * i + 1]);
+                            mma_bf16(c[j], lo.z, hi.z, lo.w, hi.w, kf[j][4 * i + 2], kf[j][4 * i + 3]);
+                        }
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int m = mt * 16 + half * 8 + g, place = sh.place[m];
+                        const float lse = sh.lse[m];
+                        const bool out = lse == INFINITY;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int key = k0 + j * 8 + 2 * t + e;
+                                bool see = !out;
+                                if (!plain) see = see && key <= place && (p.window == 0 || key < p.n_sinks || place - key < p.window);
+                                const float v = ex2(fmaf(c[j][half * 2 + e], sc, -lse));
+                                sum[j][e] += see ? v : 0.0f;
+                            }
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) sum[j][e] += __shfl_xor_sync(kFullMask, sum[j][e], o);
+                }
+            }
+            // lane (g, t) writes keys 2t, 2t+1 of group g (g < 4)
+            if (g < 4) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int key = k0 + g * 8 + 2 * t + e;
+                    if (key < end) {
+                        float v = g == 0 ? sum[0][e] : (g == 1 ? sum[1][e] : (g == 2 ? sum[2][e] : sum[3][e]));
+                        if (cache_row(p.c, b, h, key) < 0) v = 0.0f;               // on no page: nothing to be seen
+                        const float before = m0 ? w_out[key] : (key < base ? w_in[key] : 0.0f);
+                        w_out[key] = before + v;
+                    }
                 }
             }
         }
-        if (lane == 0) {
-            const int64_t at = bh * p.w_stride + pos;
-            p.w_out[at] = (pos < base ? p.w_in[at] : 0.0f) + sum;
-        }
+        if (rows <= kWRows) break;
     }
 }
 __global__ void __launch_bounds__(128) weights_status_kernel(const WeightsParams p) {

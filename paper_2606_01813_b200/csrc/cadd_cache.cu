@@ -104,6 +104,23 @@ static int launch_tiles(const AttnWork& w, cudaStream_t st) {
     return CADD_OK;
 }
 
+template <int D, bool FP4>
+static int launch_weights(WeightsParams& p, int64_t cap, cudaStream_t st) {
+    // Keys of a CTA: 1024, less where that would leave the device short of CTAs, 128 (32 a warp) at least.
+    const int64_t bh = (int64_t)p.c.batch * p.c.heads;
+    p.keys_per_cta = 1024;
+    while (p.keys_per_cta > 128 && bh * ((cap + p.keys_per_cta - 1) / p.keys_per_cta) < 4 * 148) p.keys_per_cta >>= 1;
+    const int64_t per_head = (cap + p.keys_per_cta - 1) / p.keys_per_cta;
+    if (bh * per_head >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
+    p.ctas_per_head = (int)per_head;
+    if (cudaFuncSetAttribute(weights_kernel<D, FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WeightsShared<D>)) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    weights_kernel<D, FP4><<<(unsigned)(bh * per_head), kWThreads, sizeof(WeightsShared<D>), st>>>(p);
+    return launched();
+}
+
 }  // namespace cadd
 
 using namespace cadd;
@@ -257,21 +274,12 @@ int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream) {
     p.base_length = a->base_length; p.w_in = a->weights; p.w_out = a->weights_out; p.w_stride = a->weights_stride; p.status = a->status;
     p.heads_q = a->heads_q; p.group = a->heads_q / a->cache.heads; p.window = a->window; p.n_sinks = a->n_sinks;
     p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
-    const int64_t bh = (int64_t)p.c.batch * p.c.heads;
-    p.ctas_per_head = ctas_for(bh, cap, 4);
     if (a->status) {
         weights_status_kernel<<<(unsigned)p.c.batch, 128, 0, st>>>(p);
         if ((rc = launched()) != CADD_OK) return rc;
     }
-    const unsigned grid = (unsigned)(bh * p.ctas_per_head);
-    if (p.c.head_dim == 128) {
-        if (p.c.fp4) weights_kernel<128, true><<<grid, 128, 0, st>>>(p);
-        else weights_kernel<128, false><<<grid, 128, 0, st>>>(p);
-    } else {
-        if (p.c.fp4) weights_kernel<64, true><<<grid, 128, 0, st>>>(p);
-        else weights_kernel<64, false><<<grid, 128, 0, st>>>(p);
-    }
-    return launched();
+    if (p.c.head_dim == 128) return p.c.fp4 ? launch_weights<128, true>(p, cap, st) : launch_weights<128, false>(p, cap, st);
+    return p.c.fp4 ? launch_weights<64, true>(p, cap, st) : launch_weights<64, false>(p, cap, st);
 }
 
 int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream) {
