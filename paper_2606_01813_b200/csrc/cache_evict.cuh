@@ -23,9 +23,14 @@ struct WeightsParams {
     int ctas_per_head, keys_per_cta;
 };
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+template <bool HALF>
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (HALF)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 // Weights of the accepted rows on the cached keys.  Few rows (the path times the group's heads, 16 to some 70) meet long
@@ -34,14 +39,15 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 // memory, without a detour over shared memory: which element stands in which place of the contraction is free as long as
 // rows and keys agree, so lane t of a key's four lanes holds a contiguous quarter of its row (4 bits: one 16-byte load, D 128),
 // and word m of it, eight elements, feeds contraction steps 2m and 2m + 1.  The rows stand in shared memory as 16-byte chunks in
-// the same order.  A warp takes 32 keys at a time, the next 32 being on their way; sums over rows stay in registers and are
-// joined across the lanes at the end, in a fixed order.  More than 128 rows are done in groups, the later ones adding to
-// what the earlier ones wrote.
+// the same order (in fp16 for a 4-bit cache: fp4.cuh).  A warp takes 32 keys at a time, the next 32 being on their way; sums
+// over rows stay in registers and are joined across the lanes at the end, in a fixed order.  More than 128 rows are done in
+// groups, the later ones adding to what the earlier ones wrote.
 constexpr int kWThreads = 128;
 constexpr int kWRows = 128;                              // rows in shared memory at a time
 template <int D> struct alignas(16) WeightsShared {
     uint4 q[kWRows][D / 8 + 1];                          // one chunk of padding: rows eight apart lie in different banks
     float lse[kWRows];                                   // times log2(e); +Inf marks a row that adds nothing
+    float scale[kWRows];                                 // of the row's scores
     int place[kWRows];
 };
 
@@ -75,6 +81,18 @@ __device__ __forceinline__ void wkeys_load(WKeys<D, FP4>& x, const CacheView& c,
 // 4 m + t, so that a key's four lanes read neighbouring slots.
 template <int D, bool FP4> __device__ __forceinline__ int wkeys_slot(int chunk) { return FP4 ? (chunk % (D / 32)) * 4 + chunk / (D / 32) : chunk; }
 
+// Rows of the lane's four keys k0 + 8 j + g; pages of 32 slots and more hold 32 aligned keys next to one another: one look-up.
+__device__ __forceinline__ void wkeys_rows(const CacheView& c, int b, int h, int k0, int g, int end, int64_t (&row)[4]) {
+    if (c.page_shift >= 5) {
+        const int64_t first = k0 < end ? cache_row(c, b, h, k0) : -1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = first >= 0 && k0 + j * 8 + g < end ? first + (int64_t)(j * 8 + g) * c.stride_slot : -1;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = k0 + j * 8 + g < end ? cache_row(c, b, h, k0 + j * 8 + g) : -1;
+    }
+}
+
 template <int D, bool FP4>
 __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(const __grid_constant__ WeightsParams p) {
     extern __shared__ __align__(16) unsigned char weights_smem_raw[];
@@ -86,7 +104,6 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
     const int base = min(max(p.base_length[b], 0), len);
     int clamped;
     const int rows = min(row_count(p.rows, b, &clamped), len - base) * p.group;
-    const float sc = FP4 ? p.scale_log2 * exp2i(8 - p.c.k_exp) : p.scale_log2;
     const float* w_in = p.w_in + (int64_t)bh * p.w_stride;
     float* w_out = p.w_out + (int64_t)bh * p.w_stride;
     constexpr int W = D / 32;                            // words of a lane, two contraction steps each
@@ -94,52 +111,63 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
     for (int m0 = 0; m0 == 0 || m0 < rows; m0 += kWRows) {
         const int here = min(rows - m0, kWRows), tiles = (here + 15) >> 4;
         if (m0) __syncthreads();
+        // a row's D / 8 chunks by as many neighbouring lanes
         for (int i = tid; i < tiles * 16 * (D / 8); i += kWThreads) {
             const int m = i / (D / 8), ch = i - m * (D / 8), li = (m0 + m) / p.group, hq = h * p.group + (m0 + m - li * p.group);
             const int r = m < here ? row_at(p.rows, b, li) : -1;
             uint4 x = make_uint4(0, 0, 0, 0);
             if (r >= 0) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
-            sh.q[m][wkeys_slot<D, FP4>(ch)] = FP4 ? order_pairs(x) : x;
+            float scale = p.scale_log2;
+            if constexpr (FP4) {
+                float amax = chunk_amax(x);
+#pragma unroll
+                for (int o = D / 16; o; o >>= 1) {       // (the loop's trip count is the same for all lanes of a row)
+                    const float y = __shfl_xor_sync(kFullMask, amax, o);
+                    amax = !(y <= amax) ? y : amax;
+                }
+                const int e = half_row_exponent(amax);
+                x = half_chunk(x, exp2i(e == 127 ? -126 : -e));
+                scale *= exp2i(-p.c.k_exp) * exp2i(e == 127 ? 126 : e);
+            }
+            sh.q[m][wkeys_slot<D, FP4>(ch)] = x;
             if (ch == 0) {
                 const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
                 sh.lse[m] = fabsf(lse) == INFINITY ? INFINITY : lse * kLog2e;
+                sh.scale[m] = scale;
                 sh.place[m] = base + li;
             }
         }
         __syncthreads();
-        auto row_of = [&](int key) -> int64_t { return key < end ? cache_row(p.c, b, h, key) : -1; };
         WKeys<D, FP4> x[4];
         int64_t row[4];
         int k0 = begin + warp * 32;
+        wkeys_rows(p.c, b, h, k0, g, end, row);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row_of(k0 + j * 8 + g), t);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) row[j] = row_of(k0 + kWThreads + j * 8 + g);
+        for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);
         for (; k0 < end; k0 += kWThreads) {
             uint32_t kf[4][W * 4];                       // the 32 keys as operands: [key group of 8][word][two steps x two registers]
+            unsigned there = 0;                          // bit j: this lane's key of group j exists
+#pragma unroll
+            for (int j = 0; j < 4; ++j) there |= row[j] >= 0 ? 1u << j : 0u;
+            wkeys_rows(p.c, b, h, k0 + kWThreads, g, end, row);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (FP4) {
-                    uint32_t f0, f1;
-                    fp4_unit_scales(x[j].s, f0, f1);
+                uint32_t f0 = 0, f1 = 0;
+                if constexpr (FP4) fp4_half_scales(x[j].s, f0, f1);
 #pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        const uint4 v = fp4_unit_values(x[j].w[i], (D == 128 && i >= 2) ? f1 : f0);
-                        kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) { kf[j][4 * i] = x[j].w[i].x; kf[j][4 * i + 1] = x[j].w[i].y; kf[j][4 * i + 2] = x[j].w[i].z; kf[j][4 * i + 3] = x[j].w[i].w; }
+                for (int i = 0; i < W; ++i) {
+                    uint4 v;
+                    if constexpr (FP4) v = fp4_half_values(x[j].w[i], (D == 128 && i >= 2) ? f1 : f0);
+                    else v = x[j].w[i];
+                    kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
                 }
             }
-            // the next keys' rows, and where those behind them lie
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) row[j] = row_of(k0 + 2 * kWThreads + j * 8 + g);
+            for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);            // the next keys
             float sum[4][2] = {};
             if (p.window == 0 || k0 < p.n_sinks || k0 + 31 > base - p.window) {
                 const bool plain = p.window == 0 && k0 + 31 <= base;               // every row sees all 32
+#pragma unroll 1
                 for (int mt = 0; mt < tiles; ++mt) {
                     float c[4][4] = {};
 #pragma unroll
@@ -147,49 +175,57 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                         const uint4 lo = sh.q[mt * 16 + g][i * 4 + t], hi = sh.q[mt * 16 + g + 8][i * 4 + t];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            mma_bf16(c[j], lo.x, hi.x, lo.y, hi.y, kf[j][4 * i], kf[j][4 * i + 1]);
-                            mma_bf16(c[j], lo.z, hi.z, lo.w, hi.w, kf[j][4 * i + 2], kf[j][4 * i + 3]);
+                            mma_16x8x16<FP4>(c[j], lo.x, hi.x, lo.y, hi.y, kf[j][4 * i], kf[j][4 * i + 1]);
+                            mma_16x8x16<FP4>(c[j], lo.z, hi.z, lo.w, hi.w, kf[j][4 * i + 2], kf[j][4 * i + 3]);
                         }
                     }
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int m = mt * 16 + half * 8 + g, place = sh.place[m];
-                        const float lse = sh.lse[m];
-                        const bool out = lse == INFINITY;
+                        const float lse = sh.lse[m], sc = sh.scale[m];
+                        if (FP4 && plain) {              // codes are finite: a row with lse = +Inf gives 2^-Inf by itself
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
+                            for (int j = 0; j < 4; ++j) {
+                                sum[j][0] += ex2(fmaf(c[j][half * 2], sc, -lse));
+                                sum[j][1] += ex2(fmaf(c[j][half * 2 + 1], sc, -lse));
+                            }
+                        } else {
+                            const bool out = lse == INFINITY;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int key = k0 + j * 8 + 2 * t + e;
-                                bool see = !out;
-                                if (!plain) see = see && key <= place && (p.window == 0 || key < p.n_sinks || place - key < p.window);
-                                const float v = ex2(fmaf(c[j][half * 2 + e], sc, -lse));
-                                sum[j][e] += see ? v : 0.0f;
+                            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    const int key = k0 + j * 8 + 2 * t + e;
+                                    const bool see = !out && key <= place && (p.window == 0 || key < p.n_sinks || place - key < p.window);
+                                    const float v = ex2(fmaf(c[j][half * 2 + e], sc, -lse));
+                                    sum[j][e] += see ? v : 0.0f;
+                                }
                             }
                         }
                     }
                 }
             }
+            // sums over the eight lanes of equal t; each round halves what a lane goes on with, and lane (g, t) ends with key
+            // (g >> 1) * 8 + 2 t + (g & 1)
+            float a[4], c2[2], v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) sum[j][e] += __shfl_xor_sync(kFullMask, sum[j][e], o);
-                }
+            for (int i = 0; i < 4; ++i) {                // g's high bit chooses between key groups 0, 1 and 2, 3
+                const float keep = g & 4 ? sum[2 + (i >> 1)][i & 1] : sum[i >> 1][i & 1], give = g & 4 ? sum[i >> 1][i & 1] : sum[2 + (i >> 1)][i & 1];
+                a[i] = keep + __shfl_xor_sync(kFullMask, give, 16);
             }
-            // lane (g, t) writes keys 2t, 2t+1 of group g (g < 4)
-            if (g < 4) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int key = k0 + g * 8 + 2 * t + e;
-                    if (key < end) {
-                        float v = g == 0 ? sum[0][e] : (g == 1 ? sum[1][e] : (g == 2 ? sum[2][e] : sum[3][e]));
-                        if (cache_row(p.c, b, h, key) < 0) v = 0.0f;               // on no page: nothing to be seen
-                        const float before = m0 ? w_out[key] : (key < base ? w_in[key] : 0.0f);
-                        w_out[key] = before + v;
-                    }
-                }
+            for (int i = 0; i < 2; ++i) {
+                const float keep = g & 2 ? a[2 + i] : a[i], give = g & 2 ? a[i] : a[2 + i];
+                c2[i] = keep + __shfl_xor_sync(kFullMask, give, 8);
+            }
+            v = (g & 1 ? c2[1] : c2[0]) + __shfl_xor_sync(kFullMask, g & 1 ? c2[0] : c2[1], 4);
+            const int mine = (g >> 1) * 8 + 2 * t + (g & 1), key = k0 + mine;
+            // whether that key exists is known to the lanes with g' = mine & 7, as bit mine >> 3
+            const unsigned known = __shfl_sync(kFullMask, there, (mine & 7) * 4);
+            if (!((known >> (mine >> 3)) & 1u)) v = 0.0f;                          // on no page: nothing to be seen
+            if (key < end) {
+                const float before = m0 ? w_out[key] : (key < base ? w_in[key] : 0.0f);
+                w_out[key] = before + v;
             }
         }
         if (rows <= kWRows) break;
