@@ -690,91 +690,94 @@ def _need_i32(t: Optional[torch.Tensor], shape, dev, name: str) -> Optional[int]
     """Pointer of an int32 input of the given shape on the call's device (None passes)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.device != dev or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {dev}")
     return t.data_ptr()
 
 
 def _need_rows(t: torch.Tensor, shape, dev, name: str):
     """Pointer and (batch, row, head) strides of a bf16 operand [batch, rows, heads, head_dim]."""
-    if t.dtype != torch.bfloat16 or t.device != dev or tuple(t.shape) != tuple(shape):
+    if t.dtype != torch.bfloat16 or t.device != dev or t.shape != shape:
         raise ValueError(f"{name} must be a bfloat16 tensor {list(shape)} on {dev}")
-    if t.stride(3) != 1:
+    sb, sr, sh, se = t.stride()
+    if se != 1:
         raise ValueError(f"{name} must have a contiguous last axis")
     # an axis of length one may carry any stride; it is never stepped along
-    return t.data_ptr(), *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3))
+    return t.data_ptr(), sb if shape[0] > 1 else 0, sr if shape[1] > 1 else 0, sh if shape[2] > 1 else 0
 
 
-def _enqueue(fn, args, dev, stream) -> torch.cuda.Stream:
-    st = _stream_of(stream, dev)
+def _enqueue(fn, args, dev, stream) -> None:
+    """The call, on the given stream or the current one of the tensors' device, with that device current."""
+    raw = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == dev.index:
-        rc = fn(C.byref(args), st.cuda_stream)
+        rc = fn(C.byref(args), raw)
     else:
         with torch.cuda.device(dev):
-            rc = fn(C.byref(args), st.cuda_stream)
+            rc = fn(C.byref(args), raw)
     if rc != OK:
         raise CaddError(rc)
-    return st
 
 
-@dataclass(frozen=True)
 class KvCache:
     """A paged key/value cache (cadd_cache): the pools and a batch's view of them.
 
     k, v: CUDA tensors [n_pages, heads, page_size, head_dim] in bf16, or in 4 bits as uint8 codes [..., head_dim / 2] with
     k_scale, v_scale uint8 (e4m3) [..., head_dim / 16].  A token's row must be contiguous; the other axes may be strided
     alike in all pools (permuted views fit).  block_table [batch, max_pages] and length [batch] are int32 on the same device.
-    In the 4-bit form k_exp and v_exp are the powers of two that rows are multiplied by before they are stored."""
-    k: torch.Tensor
-    v: torch.Tensor
-    block_table: torch.Tensor
-    length: torch.Tensor
-    k_scale: Optional[torch.Tensor] = None
-    v_scale: Optional[torch.Tensor] = None
-    k_exp: int = 0
-    v_exp: int = 0
+    In the 4-bit form k_exp and v_exp are the powers of two that rows are multiplied by before they are stored.
 
-    def __post_init__(self):
-        k, v = self.k, self.v
-        _need(k.is_cuda, "the cache must be on a CUDA device (there is no CPU path)")
-        dev, fp4 = k.device, k.dtype == torch.uint8
-        if k.dtype not in (torch.uint8, torch.bfloat16):
-            raise TypeError(f"unsupported cache dtype {k.dtype}")
-        _need(k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and v.device == dev, "k and v must be alike, [n_pages, heads, page_size, ...]")
-        pools = [k, v]
+    The object describes these tensors and is fixed; their contents may change.  For other tensors make another one."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, length: torch.Tensor,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, k_exp: int = 0, v_exp: int = 0):
+        dev, dtype, shape, strides = k.device, k.dtype, k.shape, k.stride()
+        if dev.type != "cuda":
+            raise ValueError("the cache must be on a CUDA device (there is no CPU path)")
+        fp4 = dtype == torch.uint8
+        if not fp4 and dtype != torch.bfloat16:
+            raise TypeError(f"unsupported cache dtype {dtype}")
+        if len(shape) != 4 or v.shape != shape or v.dtype != dtype or v.device != dev or v.stride() != strides:
+            raise ValueError("k and v must be alike, [n_pages, heads, page_size, ...]")
+        pages, heads, page_size, n = shape
+        rows = self._rows(shape, strides)
         if fp4:
-            ks, vs = self.k_scale, self.v_scale
-            _need(ks is not None and vs is not None, "a 4-bit cache needs k_scale and v_scale")
-            for t in (ks, vs):
-                _need(t.dtype == torch.uint8 and t.device == dev and t.shape == (*k.shape[:3], k.shape[3] // 8) and k.shape[3] % 8 == 0,
-                      "k_scale and v_scale must be uint8 with one scale for 8 bytes of codes")
-            pools += [ks, vs]
-        else:
-            _need(self.k_scale is None and self.v_scale is None, "a bf16 cache has no scales")
-        rows = None
-        for t in pools:
-            _need(t.stride(3) == 1, "a token's row must be contiguous")
-            n = t.shape[3]
-            _need(all(t.stride(i) % n == 0 for i in range(3) if t.shape[i] > 1), "the pools' strides must be whole rows")
-            mine = tuple(t.stride(i) // n if t.shape[i] > 1 else 1 for i in range(3))
-            _need(rows in (None, mine), "all pools must be laid out alike")
-            rows = mine
-        bt = self.block_table
-        _need(bt.dim() == 2 and bt.dtype == torch.int32 and bt.device == dev and bt.is_contiguous(),
-              "block_table must be a contiguous int32 tensor [batch, max_pages] on the cache's device")
-        a = CacheArgs()
-        a.struct_size = C.sizeof(CacheArgs)
-        a.format = CACHE_FP4 if fp4 else CACHE_BF16
-        a.batch, a.max_pages = bt.shape
-        a.n_pages, a.heads, a.page_size = k.shape[:3]
-        a.head_dim = k.shape[3] * (2 if fp4 else 1)
-        a.k_exp, a.v_exp = self.k_exp, self.v_exp
-        a.stride_page, a.stride_head, a.stride_slot = rows
-        a.k, a.v, a.k_scale, a.v_scale = k.data_ptr(), v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale)
-        a.block_table = bt.data_ptr()
-        a.length = _need_i32(self.length, (a.batch,), dev, "length")
-        object.__setattr__(self, "args", a)
-        object.__setattr__(self, "device", dev)
+            if k_scale is None or v_scale is None:
+                raise ValueError("a 4-bit cache needs k_scale and v_scale")
+            want = (pages, heads, page_size, n // 8)
+            for t in (k_scale, v_scale):
+                if t.dtype != torch.uint8 or t.device != dev or t.shape != want or n % 8:
+                    raise ValueError("k_scale and v_scale must be uint8 with one scale for 8 bytes of codes")
+                if self._rows(want, t.stride()) != rows:
+                    raise ValueError("all pools must be laid out alike")
+        elif k_scale is not None or v_scale is not None:
+            raise ValueError("a bf16 cache has no scales")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32 or block_table.device != dev or not block_table.is_contiguous():
+            raise ValueError("block_table must be a contiguous int32 tensor [batch, max_pages] on the cache's device")
+        batch, max_pages = block_table.shape
+        args = CacheArgs(C.sizeof(CacheArgs), CACHE_FP4 if fp4 else CACHE_BF16, batch, heads, 2 * n if fp4 else n, page_size, max_pages, k_exp, v_exp, 0,
+                         pages, *rows, k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if fp4 else None, v_scale.data_ptr() if fp4 else None,
+                         block_table.data_ptr(), _need_i32(length, (batch,), dev, "length"))
+        self.__dict__.update(k=k, v=v, block_table=block_table, length=length, k_scale=k_scale, v_scale=v_scale, k_exp=k_exp, v_exp=v_exp,
+                             args=args, device=dev, batch=batch, heads=heads, head_dim=args.head_dim, capacity=max_pages * page_size)
+
+    @staticmethod
+    def _rows(shape, strides):
+        """Strides of the first three axes in rows."""
+        n = shape[3]
+        if strides[3] != 1:
+            raise ValueError("a token's row must be contiguous")
+        out = []
+        for i in range(3):
+            if shape[i] <= 1:
+                out.append(1)                     # never stepped along
+            elif n and strides[i] % n == 0:
+                out.append(strides[i] // n)
+            else:
+                raise ValueError("the pools' strides must be whole rows")
+        return out
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a KvCache is fixed: make another one")
 
 
 @dataclass
@@ -795,18 +798,20 @@ class Evicted:
     status: Optional[torch.Tensor] = None
 
 
-def _marshal_rows(a, cache: KvCache, R: int, n_rows, path, path_len) -> None:
-    a.R = R
-    B, dev = cache.args.batch, cache.device
-    if path is not None:
-        _need(path_len is not None and n_rows is None, "path comes with path_len and without n_rows")
-        _need(path.dim() == 2, "path must be [batch, L]")
-        a.L = path.shape[1]
-        a.path = _need_i32(path, (B, a.L), dev, "path")
-        a.path_len = _need_i32(path_len, (B,), dev, "path_len")
-    else:
-        _need(path_len is None, "path_len comes with path")
-        a.n_rows = _need_i32(n_rows, (B,), dev, "n_rows")
+def _row_list(cache: KvCache, n_rows, path, path_len):
+    """L and the pointers of n_rows, path and path_len, of the calls that take a path or leading rows.  (The caller keeps its
+    own names bound to the tensors until the call is enqueued: a temporary would otherwise be freed, and its memory given out.)"""
+    B, dev = cache.batch, cache.device
+    if path is None:
+        if path_len is not None:
+            raise ValueError("path_len comes with path")
+        return 0, _need_i32(n_rows, (B,), dev, "n_rows"), None, None
+    if path_len is None or n_rows is not None:
+        raise ValueError("path comes with path_len and without n_rows")
+    if path.dim() != 2:
+        raise ValueError("path must be [batch, L]")
+    L = path.shape[1]
+    return L, None, _need_i32(path, (B, L), dev, "path"), _need_i32(path_len, (B,), dev, "path_len")
 
 
 def cadd_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, n_rows=None, path=None, path_len=None,
@@ -815,21 +820,19 @@ def cadd_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, n_row
     """Write rows of k and v (bf16 [batch, R, heads, head_dim]) behind each request's cached tokens: rows 0..n_rows[b]-1
     (all R without n_rows), or with path / path_len (a verification's accepted_nodes / accepted_len) the root and the accepted
     path.  Returns new_length (which may be given, cache.length itself included: the cache then goes on from there)."""
-    c, dev = cache.args, cache.device
-    _need(k.dim() == 4 and k.shape[0] == c.batch, "k must be [batch, R, heads, head_dim]")
-    shape = (c.batch, k.shape[1], c.heads, c.head_dim)
-    a = AppendArgs()
-    a.struct_size = C.sizeof(AppendArgs)
-    a.cache = c
-    a.k, *strides = _need_rows(k, shape, dev, "k")
-    a.v, *vs = _need_rows(v, shape, dev, "v")
+    B, dev = cache.batch, cache.device
+    _need(k.dim() == 4 and k.shape[0] == B, "k must be [batch, R, heads, head_dim]")
+    R = k.shape[1]
+    shape = (B, R, cache.heads, cache.head_dim)
+    kp, *strides = _need_rows(k, shape, dev, "k")
+    vp, *vs = _need_rows(v, shape, dev, "v")
     _need(strides == vs, "k and v must have the same strides")
-    a.stride_b, a.stride_row, a.stride_head = strides
-    _marshal_rows(a, cache, k.shape[1], n_rows, path, path_len)
+    L, *rows = _row_list(cache, n_rows, path, path_len)
     if new_length is None:
-        new_length = torch.empty(c.batch, dtype=torch.int32, device=dev)
-    a.new_length = _need_i32(new_length, (c.batch,), dev, "new_length")
-    a.status = _need_i32(status, (c.batch,), dev, "status")
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            new_length = torch.empty(B, dtype=torch.int32, device=dev)
+    a = AppendArgs(C.sizeof(AppendArgs), 0, R, L, kp, vp, *strides, *rows, _need_i32(new_length, (B,), dev, "new_length"),
+                   _need_i32(status, (B,), dev, "status"), cache.args)
     _enqueue(lib().cadd_cache_append, a, dev, stream)
     return new_length
 
@@ -838,22 +841,16 @@ def cadd_cache_read(cache: KvCache, n_max: int, *, start=None, count=None, out=N
                     stream: Optional[torch.cuda.Stream] = None):
     """Cached rows as bf16: out = (k, v), each [batch, n_max, heads, head_dim], row i being place start[b] + i (start 0 and
     count up to the length unless given).  Rows that are not read keep what `out` held (zeros if it is made here)."""
-    c, dev = cache.args, cache.device
-    shape = (c.batch, n_max, c.heads, c.head_dim)
+    B, dev = cache.batch, cache.device
+    shape = (B, n_max, cache.heads, cache.head_dim)
     if out is None:
         with torch.cuda.stream(_stream_of(stream, dev)):
             out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
-    a = ReadArgs()
-    a.struct_size = C.sizeof(ReadArgs)
-    a.cache = c
-    a.n_max = n_max
-    a.start = _need_i32(start, (c.batch,), dev, "start")
-    a.count = _need_i32(count, (c.batch,), dev, "count")
-    a.k, *strides = _need_rows(out[0], shape, dev, "out k")
-    a.v, *vs = _need_rows(out[1], shape, dev, "out v")
+    kp, *strides = _need_rows(out[0], shape, dev, "out k")
+    vp, *vs = _need_rows(out[1], shape, dev, "out v")
     _need(strides == vs, "both outputs must have the same strides")
-    a.stride_b, a.stride_row, a.stride_head = strides
-    a.status = _need_i32(status, (c.batch,), dev, "status")
+    a = ReadArgs(C.sizeof(ReadArgs), 0, n_max, 0, _need_i32(start, (B,), dev, "start"), _need_i32(count, (B,), dev, "count"), kp, vp, *strides,
+                 _need_i32(status, (B,), dev, "status"), cache.args)
     _enqueue(lib().cadd_cache_read, a, dev, stream)
     return out
 
@@ -880,50 +877,43 @@ def cadd_tree_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache
     Without mask_bits row r sees rows 0..r (a prompt chunk; one decoded token is R = 1).  window > 0: the last `window`
     places and the first n_sinks only.  scale is 1/sqrt(head_dim) unless given.  Rows above n_nodes keep what `out` held
     (zeros if it is made here, lse too)."""
-    c, dev = cache.args, cache.device
+    B, dev, D = cache.batch, cache.device, cache.head_dim
     _need(q.is_cuda, "q must be a CUDA tensor (there is no CPU path)")
     _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
     R, hq = q.shape[1], q.shape[2]
-    qshape, kvshape = (c.batch, R, hq, c.head_dim), (c.batch, R, c.heads, c.head_dim)
-    a = AttentionArgs()
-    a.struct_size = C.sizeof(AttentionArgs)
-    a.flags = flags
-    a.cache = c
-    a.R, a.heads_q, a.window, a.n_sinks = R, hq, window, n_sinks
-    a.scale = c.head_dim ** -0.5 if scale is None else scale
-    a.q, a.q_stride_b, a.q_stride_row, a.q_stride_head = _need_rows(q, qshape, dev, "q")
-    a.k, *strides = _need_rows(k, kvshape, dev, "k")
-    a.v, *vs = _need_rows(v, kvshape, dev, "v")
+    qshape, kvshape = (B, R, hq, D), (B, R, cache.heads, D)
+    qargs = _need_rows(q, qshape, dev, "q")
+    kp, *strides = _need_rows(k, kvshape, dev, "k")
+    vp, *vs = _need_rows(v, kvshape, dev, "v")
     _need(strides == vs, "k and v must have the same strides")
-    a.kv_stride_b, a.kv_stride_row, a.kv_stride_head = strides
-    a.n_nodes = _need_i32(n_nodes, (c.batch,), dev, "n_nodes")
-    a.mask_bits = _need_i32(mask_bits, (c.batch, R, (R + 31) // 32), dev, "mask_bits")
-    a.depth = _need_i32(depth, (c.batch, R), dev, "depth")
     if out is None:
         with torch.cuda.stream(_stream_of(stream, dev)):
             out = Attention(out=torch.zeros(qshape, dtype=torch.bfloat16, device=dev), lse=torch.zeros(qshape[:3], device=dev),
-                            status=torch.zeros(c.batch, dtype=torch.int32, device=dev))
-    a.out, a.out_stride_b, a.out_stride_row, a.out_stride_head = _need_rows(out.out, qshape, dev, "out")
-    if out.lse is not None:
-        _need(out.lse.dtype == torch.float32 and out.lse.device == dev and tuple(out.lse.shape) == qshape[:3] and out.lse.is_contiguous(),
+                            status=torch.zeros(B, dtype=torch.int32, device=dev))
+    lse = out.lse
+    if lse is not None:
+        _need(lse.dtype == torch.float32 and lse.device == dev and lse.shape == qshape[:3] and lse.is_contiguous(),
               "lse must be a contiguous float32 tensor [batch, R, heads_q]")
-        a.lse = out.lse.data_ptr()
-    a.status = _need_i32(out.status, (c.batch,), dev, "status")
-    made = workspace is None
-    if made:
-        workspace = torch.empty(cadd_tree_attention_workspace_bytes(c.batch, R, hq, cache), dtype=torch.uint8, device=dev)
+        lse = lse.data_ptr()
+    if workspace is None:                         # (allocated on the call's stream, so it may be given back as soon as the call is enqueued)
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            workspace = torch.empty(cadd_tree_attention_workspace_bytes(B, R, hq, cache), dtype=torch.uint8, device=dev)
     _need(workspace.device == dev and workspace.is_contiguous(), "workspace must be on the call's device")
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = _enqueue(lib().cadd_tree_attention, a, dev, stream)
-    if made:
-        workspace.record_stream(st)
+    a = AttentionArgs(C.sizeof(AttentionArgs), flags, R, hq, window, n_sinks, D ** -0.5 if scale is None else scale, 0, *qargs, kp, vp, *strides,
+                      _need_i32(n_nodes, (B,), dev, "n_nodes"), _need_i32(mask_bits, (B, R, (R + 31) // 32), dev, "mask_bits"),
+                      _need_i32(depth, (B, R), dev, "depth"), *_need_rows(out.out, qshape, dev, "out"), lse, _need_i32(out.status, (B,), dev, "status"),
+                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), cache.args)
+    _enqueue(lib().cadd_tree_attention, a, dev, stream)
     return out
 
 
 def _need_weights(w: torch.Tensor, B: int, H: int, n: int, dev, name: str):
-    _need(w.dtype == torch.float32 and w.device == dev and w.dim() == 3 and w.shape[0] == B and w.shape[1] == H and w.shape[2] >= n and w.stride(2) == 1
-          and (B == 1 or w.stride(0) == H * w.stride(1)), f"{name} must be a float32 tensor [batch, heads, >= {n}] with rows of equal stride")
-    return w.data_ptr(), w.stride(1) if B * H > 1 else w.shape[2]
+    if w.dim() != 3 or w.dtype != torch.float32 or w.device != dev:
+        raise ValueError(f"{name} must be a float32 tensor [batch, heads, >= {n}] on {dev}")
+    (wb, wh, wn), (sb, sh, sn) = w.shape, w.stride()
+    if wb != B or wh != H or wn < n or sn != 1 or (B > 1 and H > 1 and sb != H * sh):
+        raise ValueError(f"{name} must be [batch, heads, >= {n}] with rows of equal stride")
+    return w.data_ptr(), sh if H > 1 else (sb if B > 1 else wn)
 
 
 def cadd_cache_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache, base_length: torch.Tensor, weights: torch.Tensor, *,
@@ -933,26 +923,21 @@ def cadd_cache_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache, base_
     """Add the attention weight that the accepted rows (rows and lse as in cadd_tree_attention, path / path_len / n_rows as in
     cadd_cache_append, the rows being in the cache by now) spent on every cached place to weights fp32 [batch, heads, capacity].
     base_length is the length before the append.  Works in place unless `out` is given."""
-    c, dev = cache.args, cache.device
+    B, dev, D = cache.batch, cache.device, cache.head_dim
     _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
     R, hq = q.shape[1], q.shape[2]
-    a = WeightsArgs()
-    a.struct_size = C.sizeof(WeightsArgs)
-    a.cache = c
-    _marshal_rows(a, cache, R, n_rows, path, path_len)
-    a.heads_q, a.window, a.n_sinks = hq, window, n_sinks
-    a.scale = c.head_dim ** -0.5 if scale is None else scale
-    a.q, a.q_stride_b, a.q_stride_row, a.q_stride_head = _need_rows(q, (c.batch, R, hq, c.head_dim), dev, "q")
-    _need(lse.dtype == torch.float32 and lse.device == dev and tuple(lse.shape) == (c.batch, R, hq) and lse.is_contiguous(),
+    L, *rows = _row_list(cache, n_rows, path, path_len)
+    _need(lse.dtype == torch.float32 and lse.device == dev and lse.shape == (B, R, hq) and lse.is_contiguous(),
           "lse must be a contiguous float32 tensor [batch, R, heads_q]")
-    a.lse = lse.data_ptr()
-    a.base_length = _need_i32(base_length, (c.batch,), dev, "base_length")
-    out = weights if out is None else out
-    cap = c.max_pages * c.page_size
-    a.weights, a.weights_stride = _need_weights(weights, c.batch, c.heads, cap, dev, "weights")
-    a.weights_out, so = _need_weights(out, c.batch, c.heads, cap, dev, "out")
-    _need(so == a.weights_stride, "weights and out must have the same strides")
-    a.status = _need_i32(status, (c.batch,), dev, "status")
+    wp, stride = _need_weights(weights, B, cache.heads, cache.capacity, dev, "weights")
+    if out is None:
+        out, op = weights, wp
+    else:
+        op, so = _need_weights(out, B, cache.heads, cache.capacity, dev, "out")
+        _need(so == stride, "weights and out must have the same strides")
+    a = WeightsArgs(C.sizeof(WeightsArgs), 0, R, L, hq, window, n_sinks, D ** -0.5 if scale is None else scale, *_need_rows(q, (B, R, hq, D), dev, "q"),
+                    lse.data_ptr(), *rows, _need_i32(base_length, (B,), dev, "base_length"), wp, op, stride,
+                    _need_i32(status, (B,), dev, "status"), cache.args)
     _enqueue(lib().cadd_cache_weights, a, dev, stream)
     return out
 
@@ -963,25 +948,18 @@ def cadd_cache_evict(cache: KvCache, weights: torch.Tensor, new_block_table: tor
     weights (as cadd_cache_weights keeps them).  Their rows go, in order, to the pages of new_block_table [batch, pages] in the same
     pools; the old pages are not changed.  The cache goes on as KvCache(..., block_table=new_block_table,
     length=result.new_length) with result.weights."""
-    c, dev = cache.args, cache.device
-    B, H = c.batch, c.heads
-    a = EvictArgs()
-    a.struct_size = C.sizeof(EvictArgs)
-    a.cache = c
-    a.budget, a.n_sinks, a.n_recent = budget, n_sinks, n_recent
+    B, H, dev = cache.batch, cache.heads, cache.device
     _need(new_block_table.dim() == 2, "new_block_table must be [batch, pages]")
-    a.new_max_pages = new_block_table.shape[1]
-    a.new_block_table = _need_i32(new_block_table, (B, a.new_max_pages), dev, "new_block_table")
-    a.weights, a.weights_stride = _need_weights(weights, B, H, c.max_pages * c.page_size, dev, "weights")
+    pages = new_block_table.shape[1]
+    wp, stride = _need_weights(weights, B, H, cache.capacity, dev, "weights")
     if out is None:
         _need(budget >= 1, "budget must be at least 1")
         with torch.cuda.stream(_stream_of(stream, dev)):
             out = Evicted(new_length=torch.empty(B, dtype=torch.int32, device=dev), kept=torch.empty(B, H, budget, dtype=torch.int32, device=dev),
-                          weights=torch.zeros(B, H, a.new_max_pages * c.page_size, device=dev), status=torch.empty(B, dtype=torch.int32, device=dev))
-    a.new_length = _need_i32(out.new_length, (B,), dev, "new_length")
-    a.kept = _need_i32(out.kept, (B, H, budget), dev, "kept")
-    if out.weights is not None:
-        a.weights_out, a.weights_out_stride = _need_weights(out.weights, B, H, budget, dev, "out.weights")
-    a.status = _need_i32(out.status, (B,), dev, "status")
+                          weights=torch.zeros(B, H, pages * cache.args.page_size, device=dev), status=torch.empty(B, dtype=torch.int32, device=dev))
+    op, so = (None, 0) if out.weights is None else _need_weights(out.weights, B, H, budget, dev, "out.weights")
+    a = EvictArgs(C.sizeof(EvictArgs), 0, budget, n_sinks, n_recent, pages, wp, stride, _need_i32(new_block_table, (B, pages), dev, "new_block_table"),
+                  _need_i32(out.new_length, (B,), dev, "new_length"), _need_i32(out.kept, (B, H, budget), dev, "kept"), op, so,
+                  _need_i32(out.status, (B,), dev, "status"), cache.args)
     _enqueue(lib().cadd_cache_evict, a, dev, stream)
     return out

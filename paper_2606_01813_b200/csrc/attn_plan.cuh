@@ -195,6 +195,7 @@ __device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b,
 }
 
 // ---- what the ranges leave of an item that they share, and how it is joined ----
+// A record: o [BM][D], then m [BM], then l [BM].
 template <int BM, int D> __host__ __device__ constexpr int record_floats() { return BM * (D + 2); }
 
 // What a range begins with: its first item's (b, h, mb) and flags.
@@ -237,27 +238,32 @@ __device__ __noinline__ void redo_chunks(const AttnParams& p, const WorkIter<BM>
     }
 }
 
-// blockIdx.x is a range: the one in which a shared item begins (its sums are record 1 there) joins it.  A thread takes eight
-// elements of one row; consecutive threads take consecutive rows, as the records lie.  Rows whose joined result, or whose
-// result in a whole item of a range that met non-finite numbers, is not finite are done once more.
+// The join.  blockIdx.x is a range: the one in which a shared item begins (its sums are record 1 there) joins it, blockIdx.y takes
+// 16 of its rows.  Threads first find the ranges that share the item, then the rows' maxima over them, 16 ranges at a time; then
+// a thread adds up eight elements of one row, in range order.  Rows whose joined result, or whose result in a whole item of
+// a range that met non-finite numbers, is not finite are done once more.
+constexpr int kJoinRows = 16;
 template <int BM, int D, bool FP4>
-__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnWork w, int grid) {
+__global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __grid_constant__ AttnWork w, int grid) {
+    constexpr int T = kJoinRows * D / 8, kPer = T / kJoinRows;                     // threads; ranges looked at in one go
+    __shared__ int list[512];                                                      // ranges are at most 512 (kMaxGrid)
+    __shared__ int count, any_odd;
+    __shared__ float part[kPer][kJoinRows];
+    __shared__ PlanShared plan;
     grid_dependency_wait();
     const AttnParams& p = w.p;
-    const int c0 = blockIdx.x;
-    const int mine = w.items[c0].w;
-    if (mine & kRangeEmpty) return;
-    const int id = blockIdx.y * 256 + threadIdx.x, row = id % BM, dc = id / BM;
+    const int c0 = blockIdx.x, tid = threadIdx.x;
+    const int4 mine = w.items[c0];
+    if (mine.w & kRangeEmpty) return;
+    const int dc = tid % (D / 8), row = blockIdx.y * kJoinRows + tid / (D / 8);    // a row's chunks in neighbouring lanes
     if (w.odd[c0]) {                                                               // the range's whole items
-        __shared__ PlanShared plan;
         WorkIter<BM> it;
         if (it.init(p, plan, c0, grid)) {
             do {
                 if (!it.whole()) continue;
                 const int m0 = it.mb * BM + row, r = m0 / p.group, hq = it.h * p.group + (m0 - r * p.group);
-                const bool live = dc * 8 < D && m0 < it.live * p.group;
                 bool bad = false;
-                if (live) {
+                if (m0 < it.live * p.group) {
                     const uint4 x = *(const uint4*)(p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2);
                     float f[8];
                     Elem<CADD_DTYPE_BF16>::unpack(x, f);
@@ -268,40 +274,64 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
             } while (it.next(p));
         }
     }
-    if ((mine & kRangeInside) && !(mine & kRangeEnds)) return;                     // no item begins here and goes on
+    if ((mine.w & kRangeInside) && !(mine.w & kRangeEnds)) return;                 // no item begins here and goes on
     int c = c0 + 1;
     while (c < grid && (w.items[c].w & kRangeEmpty)) ++c;
-    if (c >= grid || !(w.items[c].w & kRangeInside)) return;
-    const int4 first_of = w.items[c];
-    const int b = first_of.x, h = first_of.y, mb = first_of.z, live = attn_live(p, b);
-    const int m0 = mb * BM + row;
-    const bool there = dc * 8 < D && m0 < live * p.group;
-    const int rec = record_floats<BM, D>();
-    const float* first = w.records + ((int64_t)c0 * 2 + 1) * rec;
-    float M = there ? first[D * BM + row] : -INFINITY;
-    int end = c, odd = w.odd[c0];
-    for (; end < grid; ++end) {
-        const int4 e = w.items[end];
-        if (e.w & kRangeEmpty) continue;
-        if (!((e.w & kRangeInside) && e.x == b && e.y == h && e.z == mb)) break;
-        odd |= w.odd[end];
-        if (there) M = fmaxf(M, w.records[(int64_t)end * 2 * rec + D * BM + row]);
-        if (e.w & kRangeEnds) { ++end; break; }
+    if (c >= grid) return;
+    const int4 item = w.items[c];
+    if (!(item.w & kRangeInside)) return;
+    const int b = item.x, h = item.y, mb = item.z, live = attn_live(p, b);
+    if (mb * BM + (int)blockIdx.y * kJoinRows >= live * p.group) return;
+    // the ranges that share it, in order
+    if (tid == 0) { list[0] = c0; count = 1; any_odd = w.odd[c0]; }
+    __syncthreads();
+    for (int i0 = c; i0 < grid; i0 += T) {
+        const int i = i0 + tid;
+        bool in = false;
+        if (i < grid) {
+            const int4 e = w.items[i];
+            in = (e.w & kRangeInside) && !(e.w & kRangeEmpty) && e.x == b && e.y == h && e.z == mb;
+        }
+        // they follow one another but for empty ranges, so their order is that of the warps and lanes
+        const unsigned ballot = __ballot_sync(kFullMask, in);
+        for (int k = 0; k < T / 32; ++k) {
+            if (tid >> 5 == k && in) {
+                list[count + __popc(ballot & ((1u << (tid & 31)) - 1u))] = i;
+                if (w.odd[i]) any_odd = 1;
+            }
+            __syncthreads();
+            if (tid == k * 32) count += __popc(ballot);
+            __syncthreads();
+        }
+        const bool last = i < grid && !in && !(w.items[i].w & kRangeEmpty);        // an item behind this one
+        if (__syncthreads_or(last)) break;
     }
-    const int r = m0 / p.group, hq = h * p.group + (m0 - r * p.group);
+    const int n = count, odd = any_odd, rec = record_floats<BM, D>();
+    auto record = [&](int i) -> const float* { return w.records + ((int64_t)list[i] * 2 + (i == 0 ? 1 : 0)) * rec; };
+    const int lr = tid % kJoinRows, li = tid / kJoinRows, grow = blockIdx.y * kJoinRows + lr;
+    float mx = -INFINITY;
+    for (int i = li; i < n; i += kPer) mx = fmaxf(mx, record(i)[BM * D + grow]);
+    part[li][lr] = mx;
+    __syncthreads();
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) M = fmaxf(M, part[i][tid / (D / 8)]);
+    const int m0 = mb * BM + row, r = m0 / p.group, hq = h * p.group + (m0 - r * p.group);
+    const bool there = m0 < live * p.group;
     bool bad = false;
     if (there) {
         const float ref = M == -INFINITY ? 0.0f : M;
         float l = 0.0f, o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = 0.0f;
-        for (int i = c0; i < end; ++i) {
-            if (i != c0 && (w.items[i].w & kRangeEmpty)) continue;
-            const float* rp = i == c0 ? first : w.records + (int64_t)i * 2 * rec;
-            const float a = exp2f(rp[D * BM + row] - ref);
-            l = fmaf(a, rp[(D + 1) * BM + row], l);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = fmaf(a, rp[(dc * 8 + j) * BM + row], o[j]);
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const float* rp = record(i);
+            const float a = exp2f(rp[BM * D + row] - ref);
+            const float4 x = *(const float4*)(rp + row * D + dc * 8), y = *(const float4*)(rp + row * D + dc * 8 + 4);
+            l = fmaf(a, rp[BM * (D + 1) + row], l);
+            o[0] = fmaf(a, x.x, o[0]); o[1] = fmaf(a, x.y, o[1]); o[2] = fmaf(a, x.z, o[2]); o[3] = fmaf(a, x.w, o[3]);
+            o[4] = fmaf(a, y.x, o[4]); o[5] = fmaf(a, y.y, o[5]); o[6] = fmaf(a, y.z, o[6]); o[7] = fmaf(a, y.w, o[7]);
         }
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         uint4 out;

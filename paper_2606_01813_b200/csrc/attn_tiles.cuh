@@ -225,7 +225,7 @@ __device__ __noinline__ bool tile_finish(const AttnWork& w, const WorkIter<kTile
     const int tid = threadIdx.x;
     const bool whole = it.whole();
     const float inv = whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
-    float* rec = w.records + ((int64_t)blockIdx.x * 2 + (it.u0 > 0 ? 0 : 1)) * record_floats<kTileBM, D>() + tid;
+    float* rec = w.records + ((int64_t)blockIdx.x * 2 + (it.u0 > 0 ? 0 : 1)) * record_floats<kTileBM, D>();
     unsigned char* dst = p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head) * 2;
     bool odd = false;
 #pragma unroll 1
@@ -256,10 +256,11 @@ __device__ __noinline__ bool tile_finish(const AttnWork& w, const WorkIter<kTile
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) rec[(c * 16 + i) * kTileBM] = __uint_as_float(o[i]);
+            for (int i = 0; i < 16; i += 4)
+                *(float4*)(rec + tid * D + c * 16 + i) = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]), __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
         }
     }
-    if (live && !whole) { rec[D * kTileBM] = m; rec[(D + 1) * kTileBM] = l; }
+    if (live && !whole) { rec[kTileBM * D + tid] = m; rec[kTileBM * (D + 1) + tid] = l; }
     if (live && whole && p.lse) p.lse[((int64_t)it.b * p.R + r) * p.heads_q + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
     return odd && live;
 }

@@ -96,8 +96,8 @@ static int launch_tiles(const AttnWork& w, cudaStream_t st) {
     if (grid > kMaxGrid) grid = kMaxGrid;
     attn_tiles_kernel<D, FP4><<<(unsigned)grid, kTileThreads, tile_smem_bytes<D>(), st>>>(w);
     if (cudaGetLastError() != cudaSuccess) return CADD_ERR_LAUNCH;
-    const dim3 join((unsigned)grid, kTileBM * (D / 8) / 256);
-    if (launch_dependent(true, attn_join_kernel<kTileBM, D, FP4>, join, dim3(256), 0, st, w, (int)grid) != cudaSuccess) {
+    const dim3 join((unsigned)grid, kTileBM / kJoinRows);
+    if (launch_dependent(true, attn_join_kernel<kTileBM, D, FP4>, join, dim3(kJoinRows * D / 8), 0, st, w, (int)grid) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
