@@ -6,6 +6,7 @@
 // attention kernels multiply exact numbers.
 #pragma once
 #include "common.cuh"
+#include "fp4.cuh"
 
 namespace cadd {
 
@@ -40,47 +41,6 @@ __device__ __forceinline__ int cache_bad_pages(const CacheView& c, int b, int fr
         for (int i = (from >> c.page_shift) + (int)threadIdx.x; i <= (to - 1) >> c.page_shift; i += (int)blockDim.x)
             bad |= (unsigned)c.block_table[(int64_t)b * c.max_pages + i] >= (uint64_t)c.n_pages;
     return __syncthreads_or(bad);
-}
-
-__device__ __forceinline__ float exp2i(int e) { return __int_as_float((e + 127) << 23); }          // 2^e, -126 <= e <= 127
-// An e2m1 code (four bits: sign, two of exponent, one behind the point) in fp32: the three low bits moved to where fp32 keeps
-// the low exponent bits and the first fraction bit give the number times 2^-126 (0.5 as an fp32 subnormal).
-__device__ __forceinline__ float e2m1_value(uint32_t c) {
-    return __uint_as_float(((c & 7u) << 22) | ((c & 8u) << 28)) * 0x1p126f;
-}
-// The same for an e4m3 number that is not negative: seven bits, times 2^-120.
-__device__ __forceinline__ float e4m3_value(uint32_t c) { return __uint_as_float((c & 0x7fu) << 20) * 0x1p120f; }
-
-// 16 values -> 8 code bytes and a scale byte.  amax / 6 and x / scale are correctly rounded fp32 quotients, which makes the
-// codes those of exact arithmetic: x has 8 significant bits and the scale 4, so a quotient that is not exactly half way
-// between two codes (or two scales) differs from it by more than 2^-16 of itself, far above fp32's half unit, 2^-25.
-__device__ __forceinline__ uint2 fp4_encode(const float (&x)[16], uint32_t& scale_byte) {
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(x[i]));                      // NaN is ignored
-    uint16_t s2;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s2) : "f"(0.0f), "f"(__fdiv_rn(amax, 6.0f)));
-    scale_byte = s2 & 0x7fu;
-    const float s = e4m3_value(scale_byte);
-    uint32_t w[2] = {0u, 0u};
-    if (scale_byte) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            float a = __fdiv_rn(x[i], s), b = __fdiv_rn(x[i + 1], s);
-            a = a == a ? a : 0.0f;
-            b = b == b ? b : 0.0f;
-            uint32_t byte;
-            asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(byte) : "f"(b), "f"(a));
-            w[i >> 3] |= (byte & 0xffu) << ((i & 7) * 4);
-        }
-    }
-    return make_uint2(w[0], w[1]);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
 }
 
 // Which rows a round's calls take: with a path row 0 and then path[0..], else rows 0, 1, ...
@@ -141,14 +101,8 @@ __global__ void __launch_bounds__(kCopyThreads) cache_append_kernel(const Append
                 dst[0] = w[2 * s];
                 dst[1] = w[2 * s + 1];
             } else {
-                float x[16];
-                Elem<CADD_DTYPE_BF16>::unpack(w[2 * s], x);
-                Elem<CADD_DTYPE_BF16>::unpack(w[2 * s + 1], x + 8);
-                const float e = exp2i(s ? c.v_exp : c.k_exp);                            // a power of two: exact
-#pragma unroll
-                for (int j = 0; j < 16; ++j) x[j] *= e;
                 uint32_t scale;
-                const uint2 codes = fp4_encode(x, scale);
+                const uint2 codes = fp4_encode(w[2 * s], w[2 * s + 1], exp2i(s ? c.v_exp : c.k_exp), scale);
                 *(uint2*)(pool + row * c.row_bytes + q * 8) = codes;
                 (s ? c.vs : c.ks)[row * blocks + q] = (unsigned char)scale;
             }
@@ -209,12 +163,16 @@ __global__ void __launch_bounds__(kCopyThreads) cache_read_kernel(const ReadPara
                 dst[1] = src[1];
             } else {
                 const uint2 codes = *(const uint2*)(pool + row * c.row_bytes + q * 8);
-                const float f = e4m3_value((s ? c.vs : c.ks)[row * blocks + q]) * exp2i(-(s ? c.v_exp : c.k_exp));
+                uint32_t f0, f1;
+                fp4_half_scales((s ? c.vs : c.ks)[row * blocks + q], f0, f1);
+                const float down = exp2i(-(s ? c.v_exp : c.k_exp));
+                const uint4 lo = fp4_half_values(codes.x, f0), hi = fp4_half_values(codes.y, f0);
+                const uint32_t in[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                 uint32_t w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint32_t two = ((j < 4 ? codes.x : codes.y) >> ((j & 3) * 8));
-                    w[j] = pack_bf16(e2m1_value(two & 15u) * f, e2m1_value((two >> 4) & 15u) * f);
+                    const float2 two = __half22float2(*reinterpret_cast<const __half2*>(&in[j]));
+                    w[j] = pack_bf16(two.x * down, two.y * down);
                 }
                 dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[1] = make_uint4(w[4], w[5], w[6], w[7]);

@@ -4,6 +4,7 @@
 #include "cache.cuh"
 #include "tree_attention.cuh"
 #include "fp4.cuh"
+#include "tile_ring.cuh"
 
 namespace cadd {
 
@@ -260,12 +261,14 @@ __device__ __forceinline__ uint32_t weight_key(float w) { return w == w ? ord32(
 
 // Choice: one CTA per (request, head).  Of the n - sinks - recent places between, the `left` heaviest stay.  Four passes over
 // the keys' bytes, highest first, count how often each byte value occurs among the keys that share the bytes found so far
-// and so find the left-th largest key T and how many places with exactly T stay; a last pass in place order writes
-// them down (greater than T, or among the first of the equal ones).
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
+// and so find the left-th largest key T and how many places with exactly T stay.  Then each warp takes a contiguous part of the
+// places, counts what stays there, and after one scan over the warps writes it down without further barriers.  The weights come
+// from L2 after the first pass.
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
+    constexpr int kWarps = kSelectThreads / 32;
     __shared__ unsigned hist[256];
-    __shared__ unsigned warp_keep[32], warp_tie[32];
-    __shared__ unsigned sh_prefix, sh_left, sh_keep0, sh_tie0;
+    __shared__ unsigned warp_sure[kWarps], warp_tie[kWarps];
+    __shared__ unsigned sh_prefix, sh_left;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / p.c.heads), h = (int)(bh - (int64_t)b * p.c.heads);
@@ -290,82 +293,112 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
         return;
     }
     const int lo = p.n_sinks, hi = n - p.n_recent;
-    if (tid == 0) { sh_prefix = 0; sh_left = (unsigned)(p.budget - p.n_sinks - p.n_recent); sh_keep0 = 0; sh_tie0 = 0; }
+    unsigned left = (unsigned)(p.budget - p.n_sinks - p.n_recent), prefix = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
-        const unsigned prefix = sh_prefix;
+#pragma unroll 8
         for (int i = lo + tid; i < hi; i += kSelectThreads) {
-            const unsigned key = weight_key(w[i]);
+            const unsigned key = weight_key(__ldg(w + i));
             if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
         }
         __syncthreads();
-        if (tid == 0) {
-            unsigned left = sh_left;
-            int d = 255;
-            for (; d > 0 && hist[d] < left; --d) left -= hist[d];
-            sh_left = left;                                                        // of the keys that start like this, how many stay
-            sh_prefix = prefix | ((unsigned)d << shift);
+        if (warp == 0) {                                                           // a lane has eight byte values, the highest lane the largest
+            unsigned mine[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { mine[i] = hist[lane * 8 + i]; sum += mine[i]; }
+            unsigned above = sum;                                                  // keys with a byte value of this lane's or more
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned x = __shfl_down_sync(kFullMask, above, o);
+                if (lane + o < 32) above += x;
+            }
+            above -= sum;                                                          // of higher lanes'
+            // the left-th largest is here (left = 0: nothing between stays; the largest value takes the place of T)
+            if ((left > above && left <= above + sum) || (left == 0 && lane == 31)) {
+                unsigned rest = left - above;
+                int d = 7;
+                if (left == 0) rest = 0;
+                else for (; d > 0 && mine[d] < rest; --d) rest -= mine[d];
+                sh_left = rest;
+                sh_prefix = prefix | ((unsigned)(lane * 8 + d) << shift);
+            }
         }
         __syncthreads();
+        left = sh_left;                                                            // of the keys that start like this, how many stay
+        prefix = sh_prefix;
     }
-    const unsigned T = sh_prefix, ties = sh_left;
-    for (int i0 = 0; i0 < n; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        const float x = i < n ? w[i] : 0.0f;
+    const unsigned T = prefix, ties = left;
+    const int per = (((n + kWarps - 1) / kWarps) + 31) & ~31, from = min(n, warp * per), to = min(n, from + per);
+    unsigned sure = 0, tie_n = 0;                                                  // of a lane's places: stay whatever happens, have key T
+#pragma unroll 4
+    for (int i = from + lane; i < to; i += 32) {
+        const bool inner = i >= lo && i < hi;
+        const unsigned key = weight_key(__ldg(w + i));
+        sure += !inner || key > T;
+        tie_n += inner && key == T;
+    }
+    sure = __reduce_add_sync(kFullMask, sure);
+    tie_n = __reduce_add_sync(kFullMask, tie_n);
+    if (lane == 0) { warp_sure[warp] = sure; warp_tie[warp] = tie_n; }
+    __syncthreads();
+    unsigned at = 0, tie_at = 0;                                                   // kept places and ties of the warps before
+    {
+        const unsigned s = lane < warp ? warp_sure[lane] : 0, t = lane < warp ? warp_tie[lane] : 0;
+        at = __reduce_add_sync(kFullMask, s);
+        tie_at = __reduce_add_sync(kFullMask, t);
+        at += min(tie_at, ties);
+    }
+    for (int i0 = from; i0 < to; i0 += 32) {
+        const int i = i0 + lane;
+        const float x = i < to ? __ldg(w + i) : 0.0f;
         const unsigned key = weight_key(x);
         const bool inner = i >= lo && i < hi;
-        const bool tie = inner && key == T;
-        const unsigned tb = __ballot_sync(kFullMask, tie);
-        if (lane == 0) warp_tie[warp] = __popc(tb);
-        __syncthreads();
-        unsigned tbase = sh_tie0;
-        for (int j = 0; j < warp; ++j) tbase += warp_tie[j];
-        const bool stay = i < n && (!inner || key > T || (tie && tbase + __popc(tb & ((1u << lane) - 1u)) < ties));
+        const bool tie = i < to && inner && key == T;
+        const unsigned before = (1u << lane) - 1u, tb = __ballot_sync(kFullMask, tie);
+        const bool stay = i < to && (!inner || key > T || (tie && tie_at + __popc(tb & before) < ties));
         const unsigned kb = __ballot_sync(kFullMask, stay);
-        if (lane == 0) warp_keep[warp] = __popc(kb);
-        __syncthreads();
-        unsigned kbase = sh_keep0;
-        for (int j = 0; j < warp; ++j) kbase += warp_keep[j];
-        const unsigned at = kbase + __popc(kb & ((1u << lane) - 1u));
-        if (stay && at < (unsigned)keep) {
-            kept[at] = i;
-            if (w_out) w_out[at] = x;
+        const unsigned slot = at + __popc(kb & before);
+        if (stay && slot < (unsigned)keep) {
+            kept[slot] = i;
+            if (w_out) w_out[slot] = x;
         }
-        __syncthreads();
-        if (tid == kSelectThreads - 1) { sh_tie0 = tbase + __popc(tb); sh_keep0 = kbase + __popc(kb); }
-        __syncthreads();
+        at += __popc(kb);
+        tie_at += __popc(tb);
     }
 }
 
-// Copy: 16 elements of k and v of one kept place a thread.
+// Copy: a thread moves 32 bytes of a kept place's key and value rows in bf16, 16 bytes of each and their two scales in 4 bits.
+// Bound by memory traffic.
 template <bool FP4>
-__global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const EvictParams p, int ctas_per_head) {
+__global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_constant__ EvictParams p, int ctas_per_head) {
+    grid_dependency_wait();
     const CacheView& c = p.c;
     const int64_t bh = blockIdx.x / ctas_per_head;
     const int part = (int)(blockIdx.x - bh * ctas_per_head), b = (int)(bh / c.heads), h = (int)(bh - (int64_t)b * c.heads);
     const int32_t* kept = p.kept + bh * p.budget;
-    const int blocks = c.head_dim >> 4;
+    const int per_row = FP4 ? c.head_dim >> 5 : c.head_dim >> 4;
     CacheView to = c;
     to.block_table = p.new_table;
     to.max_pages = p.new_max_pages;
-    for (int64_t it = (int64_t)part * kCopyThreads + threadIdx.x; it < (int64_t)p.budget * blocks; it += (int64_t)ctas_per_head * kCopyThreads) {
-        const int i = (int)(it / blocks), q = (int)(it - (int64_t)i * blocks);
+    const int64_t items = (int64_t)p.budget * per_row, step = (int64_t)ctas_per_head * kCopyThreads;
+    for (int64_t it = (int64_t)part * kCopyThreads + threadIdx.x; it < items; it += step) {
+        const int i = (int)(it / per_row), q = (int)(it - (int64_t)i * per_row);
         const int pos = kept[i];
         if (pos < 0) return;                                                       // all behind it are -1 too
         const int64_t src = cache_row(c, b, h, pos), dst = cache_row(to, b, h, i);
         if (src < 0 || dst < 0) continue;
         if constexpr (FP4) {
-            const uint2 k = *(const uint2*)(c.k + src * c.row_bytes + q * 8), v = *(const uint2*)(c.v + src * c.row_bytes + q * 8);
-            const unsigned char ks = c.ks[src * blocks + q], vs = c.vs[src * blocks + q];
-            *(uint2*)(c.k + dst * c.row_bytes + q * 8) = k;
-            *(uint2*)(c.v + dst * c.row_bytes + q * 8) = v;
-            c.ks[dst * blocks + q] = ks;
-            c.vs[dst * blocks + q] = vs;
+            const uint4 k = __ldcs((const uint4*)(c.k + src * c.row_bytes) + q), v = __ldcs((const uint4*)(c.v + src * c.row_bytes) + q);
+            const unsigned short ks = *((const unsigned short*)(c.ks + src * (c.head_dim >> 4)) + q), vs = *((const unsigned short*)(c.vs + src * (c.head_dim >> 4)) + q);
+            *((uint4*)(c.k + dst * c.row_bytes) + q) = k;
+            *((uint4*)(c.v + dst * c.row_bytes) + q) = v;
+            *((unsigned short*)(c.ks + dst * (c.head_dim >> 4)) + q) = ks;
+            *((unsigned short*)(c.vs + dst * (c.head_dim >> 4)) + q) = vs;
         } else {
             const uint4* k = (const uint4*)(c.k + src * c.row_bytes + q * 32);
             const uint4* v = (const uint4*)(c.v + src * c.row_bytes + q * 32);
-            const uint4 a0 = k[0], a1 = k[1], b0 = v[0], b1 = v[1];
+            const uint4 a0 = __ldcs(k), a1 = __ldcs(k + 1), b0 = __ldcs(v), b1 = __ldcs(v + 1);
             uint4* dk = (uint4*)(c.k + dst * c.row_bytes + q * 32);
             uint4* dv = (uint4*)(c.v + dst * c.row_bytes + q * 32);
             dk[0] = a0; dk[1] = a1;

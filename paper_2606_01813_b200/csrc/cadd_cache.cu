@@ -309,10 +309,13 @@ int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream) {
     const int64_t bh = (int64_t)p.c.batch * p.c.heads;
     evict_select_kernel<<<(unsigned)bh, kSelectThreads, 0, st>>>(p);
     if ((rc = launched()) != CADD_OK) return rc;
-    const int ctas = ctas_for(bh, (a->budget < cap ? a->budget : cap) * (p.c.head_dim / 16), kCopyThreads);
-    if (p.c.fp4) evict_copy_kernel<true><<<(unsigned)(bh * ctas), kCopyThreads, 0, st>>>(p, ctas);
-    else evict_copy_kernel<false><<<(unsigned)(bh * ctas), kCopyThreads, 0, st>>>(p, ctas);
-    if ((rc = launched()) != CADD_OK || !in_place) return rc;
+    const int ctas = ctas_for(bh, (a->budget < cap ? a->budget : cap) * (p.c.head_dim / (p.c.fp4 ? 32 : 16)), kCopyThreads);
+    if (launch_dependent(true, p.c.fp4 ? evict_copy_kernel<true> : evict_copy_kernel<false>, dim3((unsigned)(bh * ctas)), dim3(kCopyThreads), 0, st, p, ctas) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    rc = CADD_OK;
+    if (!in_place) return rc;
     evict_length_kernel<<<(unsigned)(p.c.batch + 127) / 128, 128, 0, st>>>(p.c, p.budget, a->new_length);
     return launched();
 }

@@ -9,9 +9,78 @@
 // of two that brings its largest element into [1, 2) (half_row_exponent), which its scores are multiplied by again: elements down
 // to 2^-14 of the largest stay exact, smaller ones are off by at most 2^-25 of the largest.
 #pragma once
-#include "cache.cuh"
+#include <cuda_fp16.h>
+#include "common.cuh"
 
 namespace cadd {
+
+__device__ __forceinline__ float exp2i(int e) { return __int_as_float((e + 127) << 23); }          // 2^e, -126 <= e <= 127
+// An e2m1 code (four bits: sign, two of exponent, one behind the point) in fp32: the three low bits moved to where fp32 keeps
+// the low exponent bits and the first fraction bit give the number times 2^-126 (0.5 as an fp32 subnormal).
+__device__ __forceinline__ float e2m1_value(uint32_t c) {
+    return __uint_as_float(((c & 7u) << 22) | ((c & 8u) << 28)) * 0x1p126f;
+}
+// The same for an e4m3 number that is not negative: seven bits, times 2^-120.
+__device__ __forceinline__ float e4m3_value(uint32_t c) { return __uint_as_float((c & 0x7fu) << 20) * 0x1p120f; }
+__device__ __forceinline__ uint32_t e2m1_byte(float lo, float hi) {
+    uint32_t byte;
+    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(byte) : "f"(hi), "f"(lo));
+    return byte & 0xffu;
+}
+__device__ __forceinline__ uint32_t e4m3_byte(float x) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(x));
+    return r & 0xffu;
+}
+
+// 16 bf16 elements times `up` (a power of two) -> 8 code bytes and a scale byte: scale = e4m3(amax / 6), code = e2m1(x / scale).
+//
+// What makes the codes those of exact arithmetic: x has 8 significant bits, the scale 4, a point half way between two codes 3.
+// So x / scale is either exactly such a point or off it by more than 2^-16 of itself, and it is enough to have the quotient to
+// 2^-20 and exactly where it is such a point.  q = x r with r = 1 / scale rounded is off by a few 2^-24; one correction with the
+// exact remainder, q + (x - q scale) r, leaves the square of that, so a half-way point comes out as itself.  (amax / 6 is one
+// division for the 16; the same argument holds for it.)  Blocks with NaN or infinities, and those whose products would leave
+// fp32's range, take true divisions: NaN becomes 0, the rest saturates.
+__device__ __noinline__ uint2 fp4_encode_slow(const uint4 w0, const uint4 w1, float up, uint32_t& scale_byte) {
+    float x[16], amax = 0.0f;
+    Elem<CADD_DTYPE_BF16>::unpack(w0, x);
+    Elem<CADD_DTYPE_BF16>::unpack(w1, x + 8);
+    for (int i = 0; i < 16; ++i) { x[i] *= up; amax = fmaxf(amax, fabsf(x[i])); }      // fmaxf ignores NaN
+    scale_byte = e4m3_byte(__fdiv_rn(amax, 6.0f)) & 0x7fu;
+    const float s = e4m3_value(scale_byte);
+    uint32_t w[2] = {0u, 0u};
+    for (int i = 0; i < 16 && scale_byte; i += 2) {
+        float a = __fdiv_rn(x[i], s), b = __fdiv_rn(x[i + 1], s);
+        a = a == a ? a : 0.0f;
+        b = b == b ? b : 0.0f;
+        w[i >> 3] |= e2m1_byte(a, b) << ((i & 7) * 4);
+    }
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint2 fp4_encode(const uint4& w0, const uint4& w1, float up, uint32_t& scale_byte) {
+    const uint32_t in[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+    uint32_t big = 0;                                    // the magnitudes' bits order like the magnitudes, NaN above infinity
+#pragma unroll
+    for (int i = 0; i < 8; ++i) big = __vmaxu2(big, in[i] & 0x7fff7fffu);
+    big = max(big & 0xffffu, big >> 16);
+    if (big >= 0x7000u) return fp4_encode_slow(w0, w1, up, scale_byte);                // 2^97 and more, infinities, NaN
+    scale_byte = e4m3_byte(__fdiv_rn(__uint_as_float(big << 16) * up, 6.0f)) & 0x7fu;
+    const float s = e4m3_value(scale_byte), r = scale_byte ? __frcp_rn(s) : 0.0f;      // a zero scale: zero codes
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float a = __uint_as_float(in[i] << 16) * up, b = __uint_as_float(in[i] & 0xffff0000u) * up;
+        const float qa = a * r, qb = b * r;
+        w[i >> 2] |= e2m1_byte(fmaf(fmaf(-qa, s, a), r, qa), fmaf(fmaf(-qb, s, b), r, qb)) << ((i & 3) * 8);
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
