@@ -318,21 +318,25 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
         do {
             if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.q_full, items & 1)))) break;
             ++items;
-            for (int u = it.u0; u < it.u1; ++u, ++n) {
-                // scores of unit n, in the columns of P of unit n - 2, whose product must be done
-                ok = __all_sync(kFullMask, tile_wait(sh, &sh.k_full[n & 1], (n >> 1) & 1) && (n < 2 || tile_wait(sh, &sh.pv_done[n & 1], ((n >> 1) - 1) & 1)));
+            // The scores of a unit take the place of the weights of the unit two before, right behind the product that reads those:
+            // products of one kind and accumulator type run in the order in which they are issued.
+            const unsigned first = n, end = n + (it.u1 - it.u0);
+            for (; n < end + 2; ++n) {
+                if (n >= first + 2) output(n - 2, n == first + 2);
                 if (!ok) break;
-                tc_fence_after();
-                const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k[n & 1], 0);
-                const uint32_t sm = tm_s + (n & 1) * kUnit;
+                if (n < end) {
+                    ok = __all_sync(kFullMask, tile_wait(sh, &sh.k_full[n & 1], (n >> 1) & 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k[n & 1], 0);
+                    const uint32_t sm = tm_s + (n & 1) * kUnit;
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                    umma_ss(one, sm, dq + (kk >> 2) * 1024 + (kk & 3) * 2, dk + (kk >> 2) * (kUnit * 8) + (kk & 3) * 2, tile_idesc(kUnit, 0), kk != 0);
-                umma_commit_one(one, &sh.s_full[n & 1]);
-                if (u > it.u0) output(n - 1, u == it.u0 + 1);
-                if (!ok) break;
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        umma_ss(one, sm, dq + (kk >> 2) * 1024 + (kk & 3) * 2, dk + (kk >> 2) * (kUnit * 8) + (kk & 3) * 2, tile_idesc(kUnit, 0), kk != 0);
+                    umma_commit_one(one, &sh.s_full[n & 1]);
+                }
             }
-            if (ok) output(n - 1, it.u1 == it.u0 + 1);    // the item's last
+            n = end;
         } while (ok && tile_next(it, p));
         umma_commit_one(one, &sh.drained);                // no product is in flight when the tensor memory is given back
         for (int i = 0; i < (1 << 20) && !mbar_try_wait(&sh.drained, 0); ++i) {}
@@ -449,11 +453,15 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
 #pragma unroll
                     for (int j = 0; j < 4; ++j) tmem_ld16(ts + j * 16, s[j]);
                     const bool tree = it.is_tree(u);
-                    uint32_t see[2];
-                    unit_bits(p, tree, it.b, it.len, it.live, r, dr, it.first_key(u), see);
-                    see[0] &= sh.key_bits[n & 3][0];
-                    see[1] &= sh.key_bits[n & 3][1];
-                    const bool masked = !__all_sync(kFullMask, (see[0] & see[1]) == ~0u || !live);
+                    uint32_t see[2] = {sh.key_bits[n & 3][0], sh.key_bits[n & 3][1]};
+                    bool masked = false;                  // a whole cached unit without a window is seen by all
+                    if (tree || p.window > 0 || (see[0] & see[1]) != ~0u) {
+                        uint32_t bits[2];
+                        unit_bits(p, tree, it.b, it.len, it.live, r, dr, it.first_key(u), bits);
+                        see[0] &= bits[0];
+                        see[1] &= bits[1];
+                        masked = !__all_sync(kFullMask, (see[0] & see[1]) == ~0u || !live);
+                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) tmem_ld_wait16(s[j]);
                     if (masked) {
