@@ -20,7 +20,7 @@ struct AttnWork {
     AttnParams p;
     float* records;                                      // [grid][2] partial records of BM x (D + 2) floats
     int4* items;                                         // [grid] what each range begins with
-    int* odd;                                            // [grid] not 0: the range met non-finite results
+    int* odd;                                            // [grid] what the range met: kRangeOdd, kRangeTimedOut
 };
 
 // The cached units of an item: `sink_units` from place 0 on, then up to the length from unit `win_first` on.
@@ -202,6 +202,8 @@ template <int BM, int D> __host__ __device__ constexpr int record_floats() { ret
 constexpr int kRangeInside = 1;      // the range begins inside that item (its sums are record 0 of the range)
 constexpr int kRangeEnds = 2;        // that item ends in the range
 constexpr int kRangeEmpty = 4;
+constexpr int kRangeOdd = 1;         // non-finite results
+constexpr int kRangeTimedOut = 2;    // a wait ran out
 
 // Does a row's part in units [u0, u1) of an item by key, as a warp.
 template <int D, bool FP4, int BM>
@@ -247,16 +249,27 @@ template <int BM, int D, bool FP4>
 __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __grid_constant__ AttnWork w, int grid) {
     constexpr int T = kJoinRows * D / 8, kPer = T / kJoinRows;                     // threads; ranges looked at in one go
     __shared__ int list[512];                                                      // ranges are at most 512 (kMaxGrid)
-    __shared__ int count, any_odd;
+    __shared__ int count, any_odd, found[T / 32];
     __shared__ float part[kPer][kJoinRows];
     __shared__ PlanShared plan;
     grid_dependency_wait();
     const AttnParams& p = w.p;
     const int c0 = blockIdx.x, tid = threadIdx.x;
+    if (p.status && blockIdx.y == 0) {                                             // the requests' status, shared out over the ranges
+        int late = 0;
+        for (int i = tid; i < grid; i += T) late |= w.odd[i] & kRangeTimedOut;
+        late = __syncthreads_or(late);
+        for (int b = c0; b < p.c.batch; b += (int)gridDim.x) {
+            const int len = cache_length(p.c, b), bad = cache_bad_pages(p.c, b, 0, len), n = p.n_nodes ? p.n_nodes[b] : p.R - 1;
+            if (tid == 0)
+                p.status[b] = (bad ? CADD_STATUS_BAD_PAGE : 0) | (p.c.length[b] != len ? CADD_STATUS_BAD_LENGTH : 0) |
+                              ((n < -1 || n > p.R - 1) ? CADD_STATUS_BAD_N_NODES : 0) | (late ? CADD_STATUS_INTERNAL_TIMEOUT : 0);
+        }
+    }
     const int4 mine = w.items[c0];
     if (mine.w & kRangeEmpty) return;
     const int dc = tid % (D / 8), row = blockIdx.y * kJoinRows + tid / (D / 8);    // a row's chunks in neighbouring lanes
-    if (w.odd[c0]) {                                                               // the range's whole items
+    if (w.odd[c0] & kRangeOdd) {                                                   // the range's whole items
         WorkIter<BM> it;
         if (it.init(p, plan, c0, grid)) {
             do {
@@ -287,24 +300,26 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
     __syncthreads();
     for (int i0 = c; i0 < grid; i0 += T) {
         const int i = i0 + tid;
-        bool in = false;
+        bool in = false, behind = false;                                           // behind: an item after this one
         if (i < grid) {
             const int4 e = w.items[i];
             in = (e.w & kRangeInside) && !(e.w & kRangeEmpty) && e.x == b && e.y == h && e.z == mb;
+            behind = !in && !(e.w & kRangeEmpty);
         }
-        // they follow one another but for empty ranges, so their order is that of the warps and lanes
         const unsigned ballot = __ballot_sync(kFullMask, in);
-        for (int k = 0; k < T / 32; ++k) {
-            if (tid >> 5 == k && in) {
-                list[count + __popc(ballot & ((1u << (tid & 31)) - 1u))] = i;
-                if (w.odd[i]) any_odd = 1;
-            }
-            __syncthreads();
-            if (tid == k * 32) count += __popc(ballot);
-            __syncthreads();
+        if ((tid & 31) == 0) found[tid >> 5] = __popc(ballot);
+        __syncthreads();
+        int at = count + __popc(ballot & ((1u << (tid & 31)) - 1u));
+        for (int k = 0; k < tid >> 5; ++k) at += found[k];
+        if (in) {
+            list[at] = i;
+            if (w.odd[i]) any_odd = 1;
         }
-        const bool last = i < grid && !in && !(w.items[i].w & kRangeEmpty);        // an item behind this one
-        if (__syncthreads_or(last)) break;
+        const bool last = __syncthreads_or(behind);
+        if (tid == 0)
+            for (int k = 0; k < T / 32; ++k) count += found[k];
+        __syncthreads();
+        if (last) break;
     }
     const int n = count, odd = any_odd, rec = record_floats<BM, D>();
     auto record = [&](int i) -> const float* { return w.records + ((int64_t)list[i] * 2 + (i == 0 ? 1 : 0)) * rec; };
@@ -324,7 +339,7 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
         float l = 0.0f, o[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < n; ++i) {
             const float* rp = record(i);
             const float a = exp2f(rp[BM * D + row] - ref);

@@ -522,9 +522,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
         tc_fence_after();
         tmem_dealloc(tm_s, kTileTmemCols);
     }
-    if (tid == 0) w.odd[blockIdx.x] = (int)sh.odd;
-    if (tid == 0 && sh.error && p.status)
-        for (int b = 0; b < p.c.batch; ++b) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
+    if (tid == 0) w.odd[blockIdx.x] = (sh.odd ? kRangeOdd : 0) | (sh.error ? kRangeTimedOut : 0);
 }
 
 }  // namespace cadd

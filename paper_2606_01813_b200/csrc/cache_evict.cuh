@@ -259,14 +259,15 @@ constexpr int kSelectThreads = 1024;
 // Order of weights as integers, NaN lowest, -0 as +0.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w == w ? ord32(__float_as_uint(w + 0.0f)) : 0u; }
 
-// Choice: one CTA per (request, head).  Of the n - sinks - recent places between, the `left` heaviest stay.  Four passes over
-// the keys' bytes, highest first, count how often each byte value occurs among the keys that share the bytes found so far
-// and so find the left-th largest key T and how many places with exactly T stay.  Then each warp takes a contiguous part of the
+// Choice: one CTA per (request, head).  Of the n - sinks - recent places between, the `left` heaviest stay.  Three passes
+// over the keys' digits of 11, 11 and 10 bits, highest first, count how often each digit occurs among the keys that share the digits
+// found so far and so find the left-th largest key T and how many places with exactly T stay.  (Weights lie close together: their
+// first eight bits take a handful of values, and counting in shared memory then waits for the same few words.)  Then each warp takes a contiguous part of the
 // places, counts what stays there, and after one scan over the warps writes it down without further barriers.  The weights come
 // from L2 after the first pass.
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ EvictParams p) {
     constexpr int kWarps = kSelectThreads / 32;
-    __shared__ unsigned hist[256];
+    __shared__ unsigned hist[2048];
     __shared__ unsigned warp_sure[kWarps], warp_tie[kWarps];
     __shared__ unsigned sh_prefix, sh_left;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -294,39 +295,45 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
     }
     const int lo = p.n_sinks, hi = n - p.n_recent;
     unsigned left = (unsigned)(p.budget - p.n_sinks - p.n_recent), prefix = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+    constexpr int kBins = 2048 / kSelectThreads;                                   // a thread has neighbouring digits, the last thread the largest
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), above_shift = pass == 0 ? 32 : (pass == 1 ? 21 : 10);
+        const unsigned mask = pass == 2 ? 1023u : 2047u;
+#pragma unroll
+        for (int i = 0; i < kBins; ++i) hist[tid * kBins + i] = 0;
         __syncthreads();
 #pragma unroll 8
         for (int i = lo + tid; i < hi; i += kSelectThreads) {
             const unsigned key = weight_key(__ldg(w + i));
-            if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+            if (pass == 0 || (key >> above_shift) == (prefix >> above_shift)) atomicAdd(&hist[(key >> shift) & mask], 1u);
         }
         __syncthreads();
-        if (warp == 0) {                                                           // a lane has eight byte values, the highest lane the largest
-            unsigned mine[8], sum = 0;
+        unsigned mine[kBins], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { mine[i] = hist[lane * 8 + i]; sum += mine[i]; }
-            unsigned above = sum;                                                  // keys with a byte value of this lane's or more
+        for (int i = 0; i < kBins; ++i) { mine[i] = hist[tid * kBins + i]; sum += mine[i]; }
+        unsigned above = sum;                                                      // keys with a digit of this thread's or more
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned x = __shfl_down_sync(kFullMask, above, o);
-                if (lane + o < 32) above += x;
-            }
-            above -= sum;                                                          // of higher lanes'
-            // the left-th largest is here (left = 0: nothing between stays; the largest value takes the place of T)
-            if ((left > above && left <= above + sum) || (left == 0 && lane == 31)) {
-                unsigned rest = left - above;
-                int d = 7;
-                if (left == 0) rest = 0;
-                else for (; d > 0 && mine[d] < rest; --d) rest -= mine[d];
-                sh_left = rest;
-                sh_prefix = prefix | ((unsigned)(lane * 8 + d) << shift);
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned x = __shfl_down_sync(kFullMask, above, o);
+            if (lane + o < 32) above += x;
+        }
+        if (lane == 0) warp_sure[warp] = above;
+        __syncthreads();
+        above -= sum;                                                              // of higher threads'
+        for (int k = warp + 1; k < kWarps; ++k) above += warp_sure[k];
+        // the left-th largest is here (left = 0: nothing between stays; the largest digit takes T's place)
+        if ((left > above && left <= above + sum) || (left == 0 && tid == kSelectThreads - 1)) {
+            unsigned rest = left - above;
+            int d = kBins - 1;
+            if (left == 0) rest = 0;
+            else for (; d > 0 && mine[d] < rest; --d) rest -= mine[d];
+            sh_left = rest;
+            sh_prefix = prefix | ((unsigned)(tid * kBins + d) << shift);
         }
         __syncthreads();
         left = sh_left;                                                            // of the keys that start like this, how many stay
         prefix = sh_prefix;
+        __syncthreads();
     }
     const unsigned T = prefix, ties = left;
     const int per = (((n + kWarps - 1) / kWarps) + 31) & ~31, from = min(n, warp * per), to = min(n, from + per);

@@ -234,10 +234,6 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     p.R = a->R; p.heads_q = a->heads_q; p.group = a->heads_q / a->cache.heads; p.window = a->window; p.n_sinks = a->n_sinks;
     p.mask_words = (a->R + 31) / 32;
     p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
-    if (a->status) {
-        attn_status_kernel<<<(unsigned)p.c.batch, 128, 0, st>>>(p);
-        if ((rc = launched()) != CADD_OK) return rc;
-    }
     AttnWork w;
     w.p = p;
     w.items = (int4*)a->workspace;

@@ -108,14 +108,4 @@ __device__ __noinline__ void row_attend(const AttnParams& p, int b, int h, int l
     }
 }
 
-// Status of every request (only launched where the caller asks for it).
-__global__ void __launch_bounds__(128) attn_status_kernel(const AttnParams p) {
-    const int b = blockIdx.x, len = cache_length(p.c, b);
-    const int bad = cache_bad_pages(p.c, b, 0, len);
-    if (threadIdx.x) return;
-    const int n = p.n_nodes ? p.n_nodes[b] : p.R - 1;
-    p.status[b] = (bad ? CADD_STATUS_BAD_PAGE : 0) | (p.c.length[b] != len ? CADD_STATUS_BAD_LENGTH : 0) |
-                  ((n < -1 || n > p.R - 1) ? CADD_STATUS_BAD_N_NODES : 0);
-}
-
 }  // namespace cadd
