@@ -392,6 +392,7 @@ typedef struct cadd_read_args {
  * rounded to bf16 for the product with the values (relative error at most 2^-8 each).
  * Rows above n_nodes[b] are left as they were in out and lse.
  */
+#define CADD_ATTENTION_TILED_PATH 1u   /* small calls too take the kernel that large ones take (results agree to rounding; for measurements and tests) */
 typedef struct cadd_attention_args {
     uint32_t struct_size;          /* = sizeof(cadd_attention_args) */
     uint32_t flags;                /* 0, or CADD_ATTENTION_TILED_PATH */

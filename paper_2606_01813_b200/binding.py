@@ -23,6 +23,7 @@ STATUS_L_EFF_CLAMPED, STATUS_COST_NONPOSITIVE, STATUS_BAD_N_NODES, STATUS_INTERN
 STATUS_BAD_TABLE_IDX = 256
 STATUS_BAD_PAGE, STATUS_BAD_LENGTH, STATUS_CACHE_FULL, STATUS_BAD_PATH = 512, 1024, 2048, 4096
 CACHE_BF16, CACHE_FP4 = 0, 1
+ATTENTION_TILED_PATH = 1                          # small calls too take the kernel that large ones take
 DTYPE_BF16, DTYPE_FP32 = 0, 1
 COST_QUADRATIC, COST_TABLE, COST_TABLE_INTERP = 0, 1, 2
 FLAG_EMIT_DENSE_MASK, FLAG_EMIT_TOPK, FLAG_FIXED_BUDGET = 1, 2, 4

@@ -4,7 +4,9 @@
 // query heads of a group use the same keys, so they stand in one block.  An item's keys are cut into units of 64: the
 // cached places that any of its rows can see (all, or with a window the sinks' units and the window's), then the tree's
 // rows.  All units of all items, one after the other, are cut into equal ranges, one per CTA, whatever the requests'
-// lengths: a CTA works through the ends and wholes of items that its range covers.  An item that lies in one range is
+// lengths (an item's beginning and end, its queries and its results, count as kItemCost units more, in front of its own: without
+// that, a request with an empty cache and a tree of 256 nodes, whose items have a few units each, kept one CTA busy for 660 us
+// where the others took 340; measured on a B200): a CTA works through the ends and wholes of items that its range covers.  An item that lies in one range is
 // finished there; of an item that does not, every range leaves sums (m, l, o) relative to its own maximum, and
 // attn_join_kernel adds them up in range order: the same inputs give the same bits.
 #pragma once
@@ -15,6 +17,8 @@
 namespace cadd {
 
 constexpr int kUnit = 64;                                // keys per unit
+
+constexpr int kItemCost = 5;                             // units' worth of time that an item takes besides its units (0 where every unit gets a CTA)
 
 struct AttnWork {
     AttnParams p;
@@ -48,11 +52,12 @@ __device__ __forceinline__ int tree_rows(const AttnParams& p, int live, int mb) 
 }
 template <int BM>
 __device__ __forceinline__ int row_blocks(const AttnParams& p, int live) { return (live * p.group + BM - 1) / BM; }
+// Units of one head of a request, the items' cost included.
 template <int BM>
 __device__ __forceinline__ int64_t units_per_head(const AttnParams& p, int len, int live) {
     const int mbs = row_blocks<BM>(p, live), ctx = ctx_units(p, len).total;
-    if (p.mask_bits) return (int64_t)mbs * (ctx + (live + kUnit - 1) / kUnit);
-    int64_t n = (int64_t)mbs * ctx;
+    if (p.mask_bits) return (int64_t)mbs * (p.item_cost + ctx + (live + kUnit - 1) / kUnit);
+    int64_t n = (int64_t)mbs * (p.item_cost + ctx);
     for (int mb = 0; mb < mbs; ++mb) n += (tree_rows<BM>(p, live, mb) + kUnit - 1) / kUnit;
     return n;
 }
@@ -129,28 +134,27 @@ struct WorkIter {
         off -= h * per_head;
         mb = 0;
         item_size(p);
-        while (off >= n_units) { off -= n_units; ++mb; item_size(p); }
-        u0 = (int)off;
-        u1 = (int)min((int64_t)n_units, off + left);
-        left -= u1 - u0;
-        return true;
+        while (off >= n_units + p.item_cost) { off -= n_units + p.item_cost; ++mb; item_size(p); }
+        const int v1 = (int)min((int64_t)n_units + p.item_cost, off + left);
+        left -= v1 - off;
+        u0 = max(0, (int)off - p.item_cost);
+        u1 = max(0, v1 - p.item_cost);
+        return u1 > u0 || next(p);                       // (of an item whose cost alone lies in the range another range does all)
     }
-    // On to the next item with units; false at the range's end.
+    // On to the next item with units in the range; false at the range's end.
     __device__ __forceinline__ bool next(const AttnParams& p) {
-        if (left <= 0) return false;
-        do {
-            if (++mb >= mbs) {
-                mb = 0;
-                if (++h >= p.c.heads) {
-                    h = 0;
-                    do { ++b; load_request(p); } while (mbs == 0);
-                }
+        if (left <= p.item_cost) return false;
+        if (++mb >= mbs) {
+            mb = 0;
+            if (++h >= p.c.heads) {
+                h = 0;
+                do { ++b; load_request(p); } while (mbs == 0);
             }
-            item_size(p);
-        } while (n_units == 0);
+        }
+        item_size(p);
         u0 = 0;
-        u1 = (int)min((int64_t)n_units, left);
-        left -= u1;
+        u1 = (int)min((int64_t)n_units, left - p.item_cost);
+        left -= u1 + p.item_cost;
         return true;
     }
     __device__ __forceinline__ bool is_tree(int u) const { return u >= ctx.total; }
@@ -164,34 +168,32 @@ struct WorkIter {
 
 // Which of 64 keys from `key0` on row r (place len + dr) sees, as far as lengths, masks and windows say.
 __device__ __forceinline__ uint32_t bits_from(int x) { return x <= 0 ? ~0u : (x >= 32 ? 0u : ~0u << x); }       // bits x.. of a word
+__device__ __forceinline__ uint32_t attn_key_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int k);
 __device__ __forceinline__ void unit_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int key0, uint32_t (&w)[kUnit / 32]) {
+#pragma unroll
+    for (int i = 0; i < kUnit / 32; ++i) w[i] = attn_key_bits(p, tree, b, len, live, r, dr, key0 + 32 * i);
+}
+
+// The same for 32 keys from `k`, a multiple of 32.
+__device__ __forceinline__ uint32_t attn_key_bits(const AttnParams& p, bool tree, int b, int len, int live, int r, int dr, int k) {
+    uint32_t m;
     if (!tree) {
-#pragma unroll
-        for (int i = 0; i < kUnit / 32; ++i) {
-            const int k = key0 + 32 * i;
-            uint32_t m = ~bits_from(len - k);
-            if (p.window > 0) m &= bits_from(len + dr - p.window + 1 - k) | ~bits_from(p.n_sinks - k);
-            w[i] = m;
-        }
-        return;
+        m = ~bits_from(len - k);
+        if (p.window > 0) m &= bits_from(len + dr - p.window + 1 - k) | ~bits_from(p.n_sinks - k);
+        return m;
     }
-#pragma unroll
-    for (int i = 0; i < kUnit / 32; ++i) {
-        const int k = key0 + 32 * i, word = k >> 5;
-        uint32_t m = 0;
-        if (k < live) {
-            m = p.mask_bits ? __ldg(p.mask_bits + ((int64_t)b * p.R + r) * p.mask_words + word) : ~bits_from(r + 1 - k);
-            m &= ~bits_from(live - k);
-        }
-        if (p.window > 0) {
-            for (uint32_t t = m; t; t &= t - 1) {
-                const int c = k + __ffs(t) - 1;
-                const int dc = attn_depth(p, b, c);
-                if (!(dr - dc < p.window || len + dc < p.n_sinks)) m &= ~(1u << (c - k));
-            }
-        }
-        w[i] = m;
+    m = 0;
+    if (k < live) {
+        m = p.mask_bits ? __ldg(p.mask_bits + ((int64_t)b * p.R + r) * p.mask_words + (k >> 5)) : ~bits_from(r + 1 - k);
+        m &= ~bits_from(live - k);
     }
+    if (p.window > 0) {
+        for (uint32_t t = m; t; t &= t - 1) {
+            const int c = k + __ffs(t) - 1, dc = attn_depth(p, b, c);
+            if (!(dr - dc < p.window || len + dc < p.n_sinks)) m &= ~(1u << (c - k));
+        }
+    }
+    return m;
 }
 
 // ---- what the ranges leave of an item that they share, and how it is joined ----

@@ -9,6 +9,7 @@
 #include "tree_attention.cuh"
 #include "cache_evict.cuh"
 #include "attn_tiles.cuh"
+#include "attn_few.cuh"
 #include "launch.cuh"
 
 namespace cadd {
@@ -84,24 +85,39 @@ static int64_t most_units(const AttnParams& p, int bm) {
     return (int64_t)p.c.batch * p.c.heads * blocks * keys;
 }
 
-template <int D, bool FP4>
-static int launch_tiles(const AttnWork& w, cudaStream_t st) {
-    if (cudaFuncSetAttribute(attn_tiles_kernel<D, FP4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem_bytes<D>()) != cudaSuccess) {
+// Attention kernel on up to `ctas` ranges, then the join.
+template <int BM, int D, bool FP4>
+static int launch_attention(void (*kernel)(AttnWork), AttnWork& w, int64_t ctas, int threads, size_t smem, cudaStream_t st) {
+    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
-    int64_t grid = 2 * (int64_t)sm_count();
-    const int64_t most = most_units(w.p, kTileBM);
-    if (grid > most) grid = most;
-    if (grid > kMaxGrid) grid = kMaxGrid;
-    attn_tiles_kernel<D, FP4><<<(unsigned)grid, kTileThreads, tile_smem_bytes<D>(), st>>>(w);
+    if (ctas > kMaxGrid) ctas = kMaxGrid;
+    // where every unit can have a CTA of its own, items need not be weighed against one another
+    w.p.item_cost = 0;
+    int64_t grid = most_units(w.p, BM);
+    if (grid > ctas) {
+        grid = ctas;
+        w.p.item_cost = kItemCost;
+    }
+    kernel<<<(unsigned)grid, threads, smem, st>>>(w);
     if (cudaGetLastError() != cudaSuccess) return CADD_ERR_LAUNCH;
-    const dim3 join((unsigned)grid, kTileBM / kJoinRows);
-    if (launch_dependent(true, attn_join_kernel<kTileBM, D, FP4>, join, dim3(kJoinRows * D / 8), 0, st, w, (int)grid) != cudaSuccess) {
+    const dim3 join((unsigned)grid, BM / kJoinRows);
+    if (launch_dependent(true, attn_join_kernel<BM, D, FP4>, join, dim3(kJoinRows * D / 8), 0, st, w, (int)grid) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
     return CADD_OK;
+}
+// Up to 16 rows of a head over a 4-bit cache go to the kernel that walks the cache with registers (measured: see there), all else
+// to the one with tensor memory.
+template <int D, bool FP4>
+static int launch_tree_attention(AttnWork& w, bool tiled, cudaStream_t st) {
+    if constexpr (FP4) {
+        if (!tiled && (int64_t)w.p.R * w.p.group <= kFewRows)
+            return launch_attention<kFewRows, D, true>(attn_few_kernel<D>, w, 3 * (int64_t)sm_count(), kFewThreads, sizeof(FewShared<D>), st);
+    }
+    return launch_attention<kTileBM, D, FP4>(attn_tiles_kernel<D, FP4>, w, 2 * (int64_t)sm_count(), kTileThreads, tile_smem_bytes<D>(), st);
 }
 
 template <int D, bool FP4>
@@ -239,8 +255,9 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     w.items = (int4*)a->workspace;
     w.odd = (int*)(w.items + kMaxGrid);
     w.records = (float*)((unsigned char*)a->workspace + kItemsBytes);
-    if (p.c.head_dim == 128) return p.c.fp4 ? launch_tiles<128, true>(w, st) : launch_tiles<128, false>(w, st);
-    return p.c.fp4 ? launch_tiles<64, true>(w, st) : launch_tiles<64, false>(w, st);
+    const bool tiled = (a->flags & CADD_ATTENTION_TILED_PATH) != 0;
+    if (p.c.head_dim == 128) return p.c.fp4 ? launch_tree_attention<128, true>(w, tiled, st) : launch_tree_attention<128, false>(w, tiled, st);
+    return p.c.fp4 ? launch_tree_attention<64, true>(w, tiled, st) : launch_tree_attention<64, false>(w, tiled, st);
 }
 
 // ---------------- accumulated weights, eviction ----------------

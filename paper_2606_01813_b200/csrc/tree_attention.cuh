@@ -18,7 +18,7 @@ struct AttnParams {
     const uint32_t* mask_bits;
     float* lse;
     int32_t* status;
-    int R, heads_q, group, window, n_sinks, mask_words;
+    int R, heads_q, group, window, n_sinks, mask_words, item_cost;
     float scale_log2;                                    // scale * log2(e): scores are kept in units of log 2
 };
 

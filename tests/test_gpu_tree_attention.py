@@ -298,3 +298,27 @@ def test_many_more_items_than_the_device_holds_at_once(fp4, R, group):
         assert bool(((got.out[b, :n].cpu().double() - want).abs() <= tol).all())
         assert bool(((got.lse[b, :n].cpu().double() - wlse).abs() <= tol_lse).all())
         assert bool((got.out[b, n:] == 0).all())
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("R,group,length", [(1, 1, 5000), (1, 16, 333), (2, 8, 1000), (16, 1, 77), (5, 3, 640), (1, 7, 0)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3)])
+def test_both_kernels_for_few_rows_over_four_bits(dim, R, group, length, window, sinks):
+    p = problem(fp4=True, dim=dim, R=R, live=[R, R], group=group, lens=[length, 130], window=window, sinks=sinks, page=16, seed=R)
+    few, tiled = p.run(G), p.run(G, flags=G.ATTENTION_TILED_PATH)
+    check_attention(p, few)
+    check_attention(p, tiled)
+
+
+def test_few_rows_see_what_they_see():
+    """Values that are not finite in the tree of a small call over a 4-bit cache: no influence on rows that do not see them."""
+    p = problem(fp4=True, R=4, live=[4, 4], group=4, lens=[90, 10])
+    p.mask[0, :, 3] = False
+    p.mask[0, 3, 3] = True
+    clean = p.run(G)
+    p.v[0, 3], p.k[0, 3] = math.nan, math.inf
+    dirty = p.run(G)
+    want, wlse, amass, size = p.attention(1)
+    assert bool(torch.isfinite(dirty.out[0, :3]).all()) and bool(torch.isnan(dirty.out[0, 3]).any())
+    assert bool(((dirty.out[0, :3].double() - clean.out[0, :3].double()).abs() <= 2.0 ** -6 * clean.out[0, :3].double().abs() + 2.0 ** -6).all())
+    assert torch.equal(dirty.out[1], clean.out[1])
