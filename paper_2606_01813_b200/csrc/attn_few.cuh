@@ -6,8 +6,8 @@
 // (warp_product.cuh).  For the values a lane (g, t) holds elements g D/8 .. (g+1) D/8 - 1 of keys 2t and 2t + 1 of each group of
 // eight: one nibble of each key side by side is what the conversion instruction turns into the operand's pair.  The four
 // warps of a CTA work on different keys of the item, each with its own maximum, sum and output, joined in shared
-// memory at the item's end; keys are shared out over the CTAs as in attn_plan.cuh.  The next 32 keys are on their way from the
-// moment the last are in their operands, the values from the step's start.  fp16 and its scalings are those of attn_tiles.cuh; the tree's rows are bf16.
+// memory at the item's end; keys are shared out over the CTAs as in attn_plan.cuh.  The next keys are on their way from the
+// moment the last are in their operands, the next values from the moment the last are multiplied.  fp16 and its scalings are those of attn_tiles.cuh; the tree's rows are bf16.
 #pragma once
 #include "attn_plan.cuh"
 #include "warp_product.cuh"
@@ -66,7 +66,7 @@ __device__ __forceinline__ void few_value_pairs(uint32_t a, uint32_t b, uint32_t
 }
 
 template <int D>
-__global__ void __launch_bounds__(kFewThreads, 3) attn_few_kernel(const __grid_constant__ AttnWork w) {
+__global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_constant__ AttnWork w) {
     extern __shared__ __align__(16) unsigned char few_smem_raw[];
     FewShared<D>& sh = *reinterpret_cast<FewShared<D>*>(few_smem_raw);
     const AttnParams& p = w.p;
@@ -167,17 +167,27 @@ __global__ void __launch_bounds__(kFewThreads, 3) attn_few_kernel(const __grid_c
             WKeys<D, true> kx[4];
             FewValues<D> vx;
             int64_t row[4];
-            auto fetch_keys = [&](int s) {
-                wkeys_rows(p.c, it.b, it.h, first_of(s), g, it.len, row);
+            // A step's keys are fetched once the last ones are in their operands, its values once the last ones are multiplied, and its
+            // rows are looked up a step before that.
+            auto look_up = [&](int s) {
+                if (s < steps) wkeys_rows(p.c, it.b, it.h, first_of(s), g, it.len, row);
+            };
+            auto exist_bits = [&]() -> unsigned {         // bit j: the lane's key (of the scores) of group j exists
+                unsigned x = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x |= row[j] >= 0 ? 1u << j : 0u;
+                return x;
+            };
+            unsigned there = 0, there_next = 0;
+            if (warp < steps) {
+                look_up(warp);
+                there = exist_bits();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) wkeys_load<D, true>(kx[j], p.c, row[j], t);
-            };
-            if (warp < steps) fetch_keys(warp);
-            for (int s = warp; s < steps; s += 4) {
-                unsigned there = 0;                       // bit j: the lane's key (of the scores) of group j exists
-#pragma unroll
-                for (int j = 0; j < 4; ++j) there |= row[j] >= 0 ? 1u << j : 0u;
-                few_values_load<D>(vx, p.c, row, g, t);   // wanted after the softmax
+                few_values_load<D>(vx, p.c, row, g, t);
+                look_up(warp + 4);
+            }
+            for (int s = warp; s < steps; s += 4, there = there_next) {
                 float c[4][4] = {};
                 {
                     uint32_t kf[4][W * 4];
@@ -191,7 +201,11 @@ __global__ void __launch_bounds__(kFewThreads, 3) attn_few_kernel(const __grid_c
                             kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
                         }
                     }
-                    if (s + 4 < steps) fetch_keys(s + 4);
+                    if (s + 4 < steps) {
+                        there_next = exist_bits();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) wkeys_load<D, true>(kx[j], p.c, row[j], t);
+                    }
 #pragma unroll
                     for (int i = 0; i < W; ++i) {
                         const uint4 lo = sh.qh[g][i * 4 + t], hi = sh.qh[g + 8][i * 4 + t];
@@ -230,6 +244,10 @@ __global__ void __launch_bounds__(kFewThreads, 3) attn_few_kernel(const __grid_c
 #pragma unroll
                         for (int n = 0; n < 8; ++n) mma_16x8x16<true>(o[i * 8 + n], a[2 * h][0], a[2 * h][1], a[2 * h + 1][0], a[2 * h + 1][1], b0[n], b1[n]);
                     }
+                }
+                if (s + 4 < steps) {
+                    few_values_load<D>(vx, p.c, row, g, t);
+                    look_up(s + 8);
                 }
             }
         }

@@ -91,15 +91,19 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
         WKeys<D, FP4> x[4];
         int64_t row[4];
         int k0 = begin + warp * 32;
+        auto exist_bits = [&]() -> unsigned {             // bit j: this lane's key of group j exists
+            unsigned e = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e |= row[j] >= 0 ? 1u << j : 0u;
+            return e;
+        };
         wkeys_rows(p.c, b, h, k0, g, end, row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);
-        for (; k0 < end; k0 += kWThreads) {
+        unsigned there = exist_bits(), there_next;
+        wkeys_rows(p.c, b, h, k0 + kWThreads, g, end, row);                        // rows are looked up a step before their keys are fetched
+        for (; k0 < end; k0 += kWThreads, there = there_next) {
             uint32_t kf[4][W * 4];                       // the 32 keys as operands: [key group of 8][word][two steps x two registers]
-            unsigned there = 0;                          // bit j: this lane's key of group j exists
-#pragma unroll
-            for (int j = 0; j < 4; ++j) there |= row[j] >= 0 ? 1u << j : 0u;
-            wkeys_rows(p.c, b, h, k0 + kWThreads, g, end, row);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t f0 = 0, f1 = 0;
@@ -114,6 +118,8 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);            // the next keys
+            there_next = exist_bits();
+            wkeys_rows(p.c, b, h, k0 + 2 * kWThreads, g, end, row);
             float sum[4][2] = {};
             if (p.window == 0 || k0 < p.n_sinks || k0 + 31 > base - p.window) {
                 const bool plain = p.window == 0 && k0 + 31 <= base;               // every row sees all 32

@@ -115,7 +115,7 @@ template <int D, bool FP4>
 static int launch_tree_attention(AttnWork& w, bool tiled, cudaStream_t st) {
     if constexpr (FP4) {
         if (!tiled && (int64_t)w.p.R * w.p.group <= kFewRows)
-            return launch_attention<kFewRows, D, true>(attn_few_kernel<D>, w, 3 * (int64_t)sm_count(), kFewThreads, sizeof(FewShared<D>), st);
+            return launch_attention<kFewRows, D, true>(attn_few_kernel<D>, w, 2 * (int64_t)sm_count(), kFewThreads, sizeof(FewShared<D>), st);
     }
     return launch_attention<kTileBM, D, FP4>(attn_tiles_kernel<D, FP4>, w, 2 * (int64_t)sm_count(), kTileThreads, tile_smem_bytes<D>(), st);
 }
