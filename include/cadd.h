@@ -427,7 +427,8 @@ typedef struct cadd_attention_args {
  * group of exp(scale * q[i] . k[p] - lse[i]) for rows i that see p (p <= base_length + i; window, n_sinks as above with
  * base_length + i as the row's place):
  *     weights_out[b, head, p] = (p < base_length[b] ? weights[b, head, p] : 0) + sum_i E_i(p).
- * Places from length[b] on are left as they were.  A row whose lse is -Inf or +Inf adds nothing.
+ * Places from length[b] on are left as they were, or copied where weights_out is another array.  A row whose lse is -Inf or
+ * +Inf adds nothing.
  */
 typedef struct cadd_weights_args {
     uint32_t struct_size;          /* = sizeof(cadd_weights_args) */
@@ -459,7 +460,7 @@ typedef struct cadd_weights_args {
 typedef struct cadd_evict_args {
     uint32_t struct_size;          /* = sizeof(cadd_evict_args) */
     uint32_t flags;                /* reserved, 0 */
-    int32_t  budget;               /* 1 .. new_max_pages * page_size, >= n_sinks + n_recent */
+    int32_t  budget;               /* >= 1; where the new pages have fewer places, those are the budget; >= n_sinks + n_recent */
     int32_t  n_sinks, n_recent;
     int32_t  new_max_pages;        /* columns of new_block_table */
     const float* weights;          /* [batch, heads, weights_stride >= max_pages * page_size] */
@@ -467,7 +468,7 @@ typedef struct cadd_evict_args {
     const int32_t* new_block_table;/* [batch, new_max_pages] */
     int32_t* new_length;           /* [batch] out; may be cache.length itself */
     int32_t* kept;                 /* [batch, heads, budget] out: the places that stay, ascending, -1 behind them */
-    float*   weights_out;          /* [batch, heads, weights_out_stride >= budget] out, may be NULL; not weights itself */
+    float*   weights_out;          /* [batch, heads, weights_out_stride >= the budget in force] out, may be NULL; not weights itself */
     int64_t  weights_out_stride;
     int32_t* status;               /* [batch], may be NULL */
     cadd_cache cache;

@@ -923,7 +923,7 @@ def cadd_cache_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache, base_
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Add the attention weight that the accepted rows (rows and lse as in cadd_tree_attention, path / path_len / n_rows as in
     cadd_cache_append, the rows being in the cache by now) spent on every cached place to weights fp32 [batch, heads, capacity].
-    base_length is the length before the append.  Works in place unless `out` is given."""
+    base_length is the length before the append.  Works in place unless `out` is given, which becomes the whole new array."""
     B, dev, D = cache.batch, cache.device, cache.head_dim
     _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
     R, hq = q.shape[1], q.shape[2]
@@ -958,7 +958,7 @@ def cadd_cache_evict(cache: KvCache, weights: torch.Tensor, new_block_table: tor
         with torch.cuda.stream(_stream_of(stream, dev)):
             out = Evicted(new_length=torch.empty(B, dtype=torch.int32, device=dev), kept=torch.empty(B, H, budget, dtype=torch.int32, device=dev),
                           weights=torch.zeros(B, H, pages * cache.args.page_size, device=dev), status=torch.empty(B, dtype=torch.int32, device=dev))
-    op, so = (None, 0) if out.weights is None else _need_weights(out.weights, B, H, budget, dev, "out.weights")
+    op, so = (None, 0) if out.weights is None else _need_weights(out.weights, B, H, min(budget, pages * cache.args.page_size), dev, "out.weights")
     a = EvictArgs(C.sizeof(EvictArgs), 0, budget, n_sinks, n_recent, pages, wp, stride, _need_i32(new_block_table, (B, pages), dev, "new_block_table"),
                   _need_i32(out.new_length, (B,), dev, "new_length"), _need_i32(out.kept, (B, H, budget), dev, "kept"), op, so,
                   _need_i32(out.status, (B,), dev, "status"), cache.args)

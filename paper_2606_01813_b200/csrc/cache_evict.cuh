@@ -49,7 +49,9 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
     WeightsShared<D>& sh = *reinterpret_cast<WeightsShared<D>*>(weights_smem_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int bh = blockIdx.x / p.ctas_per_head, part = blockIdx.x - bh * p.ctas_per_head, b = bh / p.c.heads, h = bh - b * p.c.heads;
-    const int len = cache_length(p.c, b), begin = part * p.keys_per_cta, end = min(len, begin + p.keys_per_cta);
+    const int len = cache_length(p.c, b), begin = part * p.keys_per_cta, chunk_end = min(cache_capacity(p.c), begin + p.keys_per_cta), end = min(len, chunk_end);
+    if (p.w_out != p.w_in)                               // another array: places from the length on are copied
+        for (int i = max(begin, len) + tid; i < chunk_end; i += kWThreads) p.w_out[(int64_t)bh * p.w_stride + i] = p.w_in[(int64_t)bh * p.w_stride + i];
     if (begin >= end) return;
     const int base = min(max(p.base_length[b], 0), len);
     int clamped;
@@ -207,7 +209,7 @@ struct EvictParams {
     int32_t *new_length, *kept, *status;
     float* w_out;
     int64_t w_out_stride;
-    int budget, n_sinks, n_recent, new_max_pages;
+    int budget, room, n_sinks, n_recent, new_max_pages;  // budget: columns of kept; room: places that stay at most
 };
 constexpr int kSelectThreads = 1024;
 
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t bh = blockIdx.x;
     const int b = (int)(bh / p.c.heads), h = (int)(bh - (int64_t)b * p.c.heads);
-    const int n = cache_length(p.c, b), keep = min(n, p.budget);
+    const int n = cache_length(p.c, b), keep = min(n, p.room);
     const float* w = p.weights + bh * p.w_stride;
     int32_t* kept = p.kept + bh * p.budget;
     float* w_out = p.w_out ? p.w_out + bh * p.w_out_stride : nullptr;
@@ -241,7 +243,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
         if (tid == 0) p.status[b] = (bad ? CADD_STATUS_BAD_PAGE : 0) | (p.c.length[b] != n ? CADD_STATUS_BAD_LENGTH : 0);
     }
     if (h == 0 && tid == 0 && p.new_length) p.new_length[b] = keep;
-    if (n <= p.budget) {
+    if (n <= p.room) {
         for (int i = tid; i < n; i += kSelectThreads) {
             kept[i] = i;
             if (w_out) w_out[i] = w[i];
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
         return;
     }
     const int lo = p.n_sinks, hi = n - p.n_recent;
-    unsigned left = (unsigned)(p.budget - p.n_sinks - p.n_recent), prefix = 0;
+    unsigned left = (unsigned)(p.room - p.n_sinks - p.n_recent), prefix = 0;
     constexpr int kBins = 2048 / kSelectThreads;                                   // a thread has neighbouring digits, the last thread the largest
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), above_shift = pass == 0 ? 32 : (pass == 1 ? 21 : 10);
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(kCopyThreads) evict_copy_kernel(const __grid_c
     CacheView to = c;
     to.block_table = p.new_table;
     to.max_pages = p.new_max_pages;
-    const int64_t items = (int64_t)p.budget * per_row, step = (int64_t)ctas_per_head * kCopyThreads;
+    const int64_t items = (int64_t)p.room * per_row, step = (int64_t)ctas_per_head * kCopyThreads;
     for (int64_t it = (int64_t)part * kCopyThreads + threadIdx.x; it < items; it += step) {
         const int i = (int)(it / per_row), q = (int)(it - (int64_t)i * per_row);
         const int pos = kept[i];

@@ -301,13 +301,15 @@ int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream) {
     if (a->struct_size != sizeof(cadd_evict_args)) return CADD_ERR_STRUCT_SIZE;
     int rc = check_cache(&a->cache);
     if (rc != CADD_OK) return rc;
-    if (a->n_sinks < 0 || a->n_recent < 0 || a->budget < 1 || (int64_t)a->n_sinks + a->n_recent > a->budget) return CADD_ERR_SHAPE;
-    if (a->new_max_pages < 1 || (int64_t)a->new_max_pages * a->cache.page_size >= ((int64_t)1 << 30) ||
-        (int64_t)a->new_max_pages * a->cache.page_size < a->budget)
+    if (a->n_sinks < 0 || a->n_recent < 0 || a->budget < 1 || a->budget > (1 << 30) || a->new_max_pages < 1 ||
+        (int64_t)a->new_max_pages * a->cache.page_size >= ((int64_t)1 << 30))
         return CADD_ERR_SHAPE;
+    const int64_t new_cap = (int64_t)a->new_max_pages * a->cache.page_size;
+    const int room = (int)(a->budget < new_cap ? a->budget : new_cap);
+    if ((int64_t)a->n_sinks + a->n_recent > room) return CADD_ERR_SHAPE;
     const int64_t cap = (int64_t)a->cache.max_pages * a->cache.page_size;
     if (a->weights_stride < cap || a->weights_stride >= ((int64_t)1 << 36)) return CADD_ERR_SHAPE;
-    if (a->weights_out && (a->weights_out_stride < a->budget || a->weights_out_stride >= ((int64_t)1 << 36) || a->weights_out == a->weights)) return CADD_ERR_SHAPE;
+    if (a->weights_out && (a->weights_out_stride < room || a->weights_out_stride >= ((int64_t)1 << 36) || a->weights_out == a->weights)) return CADD_ERR_SHAPE;
     if (!a->weights || !a->new_block_table || !a->new_length || !a->kept) return CADD_ERR_NULL;
     if (!aligned(a->weights, 4) || !aligned(a->new_block_table, 4) || !aligned(a->new_length, 4) || !aligned(a->kept, 4) ||
         !aligned(a->weights_out, 4) || !aligned(a->status, 4))
@@ -319,18 +321,18 @@ int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream) {
     const bool in_place = a->new_length == a->cache.length;
     p.new_length = in_place ? nullptr : a->new_length;
     p.kept = a->kept; p.status = a->status; p.w_out = a->weights_out; p.w_out_stride = a->weights_out_stride;
-    p.budget = a->budget; p.n_sinks = a->n_sinks; p.n_recent = a->n_recent; p.new_max_pages = a->new_max_pages;
+    p.budget = a->budget; p.room = room; p.n_sinks = a->n_sinks; p.n_recent = a->n_recent; p.new_max_pages = a->new_max_pages;
     const int64_t bh = (int64_t)p.c.batch * p.c.heads;
     evict_select_kernel<<<(unsigned)bh, kSelectThreads, 0, st>>>(p);
     if ((rc = launched()) != CADD_OK) return rc;
-    const int ctas = ctas_for(bh, (a->budget < cap ? a->budget : cap) * (p.c.head_dim / (p.c.fp4 ? 32 : 16)), kCopyThreads);
+    const int ctas = ctas_for(bh, (room < cap ? room : cap) * (p.c.head_dim / (p.c.fp4 ? 32 : 16)), kCopyThreads);
     if (launch_dependent(true, p.c.fp4 ? evict_copy_kernel<true> : evict_copy_kernel<false>, dim3((unsigned)(bh * ctas)), dim3(kCopyThreads), 0, st, p, ctas) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
     rc = CADD_OK;
     if (!in_place) return rc;
-    evict_length_kernel<<<(unsigned)(p.c.batch + 127) / 128, 128, 0, st>>>(p.c, p.budget, a->new_length);
+    evict_length_kernel<<<(unsigned)(p.c.batch + 127) / 128, 128, 0, st>>>(p.c, p.room, a->new_length);
     return launched();
 }
 

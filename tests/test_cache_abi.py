@@ -78,7 +78,7 @@ OWN = {
     "weights": [(dict(R=0), G.ERR_SHAPE), (dict(L=0), G.ERR_SHAPE), (dict(heads_q=7), G.ERR_SHAPE), (dict(scale=0.0), G.ERR_SHAPE), (dict(window=-2), G.ERR_SHAPE),
                 (dict(weights_stride=159), G.ERR_SHAPE), (dict(q=None), G.ERR_NULL), (dict(lse=None), G.ERR_NULL), (dict(base_length=None), G.ERR_NULL),
                 (dict(weights=None), G.ERR_NULL), (dict(weights_out=None), G.ERR_NULL), (dict(path_len=None), G.ERR_NULL), (dict(lse=PTR + 2), G.ERR_ALIGN)],
-    "evict": [(dict(budget=0), G.ERR_SHAPE), (dict(budget=65), G.ERR_SHAPE), (dict(budget=11), G.ERR_SHAPE), (dict(n_sinks=-1), G.ERR_SHAPE), (dict(n_recent=-1), G.ERR_SHAPE),
+    "evict": [(dict(budget=0), G.ERR_SHAPE), (dict(budget=11), G.ERR_SHAPE), (dict(new_max_pages=1, n_recent=13), G.ERR_SHAPE), (dict(n_sinks=-1), G.ERR_SHAPE), (dict(n_recent=-1), G.ERR_SHAPE),
               (dict(new_max_pages=0), G.ERR_SHAPE), (dict(weights_stride=100), G.ERR_SHAPE), (dict(weights_out_stride=63), G.ERR_SHAPE),
               (dict(weights_out=PTR), G.ERR_SHAPE), (dict(weights=None), G.ERR_NULL), (dict(new_block_table=None), G.ERR_NULL), (dict(new_length=None), G.ERR_NULL),
               (dict(kept=None), G.ERR_NULL), (dict(kept=PTR + 2), G.ERR_ALIGN)],

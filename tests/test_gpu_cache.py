@@ -215,7 +215,7 @@ def check_weights(case, in_place=False):
         err = (got[b, :, :n] - want[b]).abs()
         assert bool((err <= tol[b]).all()), (b, float((err / tol[b]).max()))
         rest = got[b, :, n:]
-        assert torch.equal(rest, w[b, :, n:].double() if in_place else torch.full_like(rest, -1.0))
+        assert torch.equal(rest, w[b, :, n:].double())
     return out
 
 
@@ -343,6 +343,20 @@ def test_eviction_with_ties_and_odd_weights(kind, page):
          "close": lambda: 1.0 + torch.randint(0, 300, shape, generator=p.g) * 2.0 ** -23,
          "special": lambda: torch.tensor([math.nan, math.inf, -math.inf, -1.0, 3e38, 1e-45, 0.0])[torch.randint(0, 7, shape, generator=p.g)]}[kind]()
     check_evict(p, w, 700, 3, 40)
+
+
+def test_a_budget_above_what_the_new_pages_hold_means_what_they_hold():
+    p = problem(batch=2, lens=[90, 20], live=[1] * 2, extra_places=0)
+    c = p.cache(G)
+    new = torch.stack([p.spare[:2], torch.tensor([int(p.spare[2]), int(p.block_table[1, 5])])]).int()
+    w = torch.rand(2, 2, p.max_pages * 16, generator=p.g)
+    got = G.cadd_cache_evict(c, w.to(DEV), new.to(DEV), 1000, n_sinks=3, n_recent=5)
+    assert got.new_length.tolist() == [32, 20] and got.status.tolist() == [0, 0]
+    k, v = read_all(at_length(G.KvCache(k=c.k, v=c.v, block_table=new.to(DEV), length=c.length), got.new_length), 32)
+    for b in range(2):
+        for h, places in enumerate(evict_wanted(p, b, w, 32, 3, 5)):
+            assert got.kept[b, h].tolist() == places + [-1] * (1000 - len(places))
+            assert torch.equal(k[b, :len(places), h], p.K[b][places, h]) and torch.equal(v[b, :len(places), h], p.V[b][places, h])
 
 
 @pytest.mark.parametrize("n", [49000, 57000, 140000])
