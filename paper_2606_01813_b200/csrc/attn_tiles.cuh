@@ -11,9 +11,11 @@
 // The 4-bit cache: a code's bits, moved to where bf16 keeps its low exponent bits and first fraction bit, are the number times
 // 2^-126; one packed multiplication by scale * 2^118 gives code * scale * 2^-8, exact in bf16 (<= 6 significant bits), for two
 // elements at once, and the missing power of two goes into the scores' factor and into the weights' exponent.  A
-// 32-bit word holds elements 0..7 of a group; masking the same nibble of its halves pairs elements (j, j + 4), so keys,
+// 32-bit word holds elements 0..7 of a group; taking the same nibble of its halves pairs elements (j, j + 4), so keys,
 // values and queries stand in shared memory in the order 0 4 1 5 2 6 3 7 within each eight (the product with the keys
-// does not mind, the values' order is undone when O is written).
+// does not mind, the values' order is undone when O is written).  (The fp16 form of fp4.cuh takes fewer logic instructions, but
+// the tree's own rows are bf16 and one product has one type: with fp16 queries for cached units and bf16 ones for the
+// tree's, the larger kernel spilled and came to 1055 us where this one took 887.)
 //
 // Keys, values and scores are double-buffered: the scores of unit n + 1 are formed and the values of unit n - 1 multiplied while
 // the softmax works on unit n.  (With one buffer of 128 keys the three followed one another, and a unit of 128 keys cost 7000
@@ -22,6 +24,14 @@
 //   warps 4-5  keys, warps 6-7 values: into the 128-byte swizzle, 32 keys a warp, by asynchronous 16-byte copies (bf16), or
 //              a row a thread through registers, one unit ahead (4 bits); all four load the item's queries;
 //   warp 8     issues the products and owns the tensor memory (256 columns: S/P 2 x 64, O up to 128).
+//
+// What bounds it (a thousand-node tree over up to 16k tokens in 4 bits, 850 us, 630 TFLOP/s, 0.38 of the measured rate): no unit
+// alone.  The shared-memory pipe, which serves the loaders, tensor memory's reads and writes and the products' operands, is
+// at 61 % without the operands, logic at 48 %, issue at 57 %, the tensor pipe at 34 %.  Per unit and CTA that is 256 + 128
+// cycles of tensor memory, 256 of stores, 512 of operands (the queries are read again for every 64 keys) and some 300 others.
+// Two blocks of rows to a CTA with 128 keys a unit would halve most of that; built, it was bound by the longer way from
+// softmax to products and back (3050 cycles for 128 rows x 128 keys against 2900 here) and was not kept, nor were two
+// threads to a row (929 us).
 // Every wait has an iteration limit; a role that gives up sets an error word and all leave.
 //
 // A product of a weight 0 with a non-finite value that the row does not see would be NaN.  A range that meets a non-finite result

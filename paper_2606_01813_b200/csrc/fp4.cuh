@@ -99,11 +99,15 @@ __device__ __forceinline__ uint4 order_pairs(uint4 w) {
 }
 // Eight e2m1 codes times a scale: `f` holds scale * 2^118 twice; the result is code * scale * 2^-8 in the order above.
 __device__ __forceinline__ uint4 fp4_unit_values(uint32_t w, uint32_t f) {
+    // A nibble times 2^6 + 2^12 (2^2 + 2^8 for the second of a byte) has its three low bits at 6..8 and its sign at 15, and
+    // nothing is carried between the two copies: a product and two masks a pair, the product off the logic unit.
+    constexpr uint32_t keep = 0x81c081c0u;
+    const uint32_t h = w >> 8;
     uint4 r;
-    r.x = mul_bf16x2(((w << 6) & 0x01c001c0u) | ((w << 12) & 0x80008000u), f);
-    r.y = mul_bf16x2(((w << 2) & 0x01c001c0u) | ((w << 8) & 0x80008000u), f);
-    r.z = mul_bf16x2(((w >> 2) & 0x01c001c0u) | ((w << 4) & 0x80008000u), f);
-    r.w = mul_bf16x2(((w >> 6) & 0x01c001c0u) | (w & 0x80008000u), f);
+    r.x = mul_bf16x2(((w & 0x000f000fu) * 4160u) & keep, f);
+    r.y = mul_bf16x2(((w & 0x00f000f0u) * 260u) & keep, f);
+    r.z = mul_bf16x2(((h & 0x000f000fu) * 4160u) & keep, f);
+    r.w = mul_bf16x2(((h & 0x00f000f0u) * 260u) & keep, f);
     return r;
 }
 // Scale bytes 2i, 2i+1 of a word as bf16 pairs (each twice), times 2^118: seven bits moved to bf16's exponent and fraction are the
