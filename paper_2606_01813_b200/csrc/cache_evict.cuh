@@ -34,8 +34,9 @@ struct WeightsParams {
 // the same order (in fp16 for a 4-bit cache: fp4.cuh).  A warp takes 32 keys at a time, the next 32 being on their way; sums
 // over rows stay in registers and are joined across the lanes at the end, in a fixed order.  More than 128 rows are done in
 // groups, the later ones adding to what the earlier ones wrote.
-// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 236 us, 1.6 TB/s, 0.24 of the measured copy rate;
-// bound by instruction issue and the warp-level products (a quarter of the tensor rate that tensor memory's would have).
+// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 245 us, a quarter of the
+// measured copy rate.  By count, what bounds it is issue: some 190 instructions to dequantise a warp's 32 keys, and per
+// 16 rows 32 products, 16 exponentials a thread and their sums.
 constexpr int kWThreads = 128;
 constexpr int kWRows = 128;                              // rows in shared memory at a time
 template <int D> struct alignas(16) WeightsShared {
@@ -52,8 +53,18 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int bh = blockIdx.x / p.ctas_per_head, part = blockIdx.x - bh * p.ctas_per_head, b = bh / p.c.heads, h = bh - b * p.c.heads;
     const int len = cache_length(p.c, b), begin = part * p.keys_per_cta, chunk_end = min(cache_capacity(p.c), begin + p.keys_per_cta), end = min(len, chunk_end);
-    if (p.w_out != p.w_in)                               // another array: places from the length on are copied
-        for (int i = max(begin, len) + tid; i < chunk_end; i += kWThreads) p.w_out[(int64_t)bh * p.w_stride + i] = p.w_in[(int64_t)bh * p.w_stride + i];
+    if (p.w_out != p.w_in) {                             // another array: places from the length on are copied
+        const float* src = p.w_in + (int64_t)bh * p.w_stride;
+        float* dst = p.w_out + (int64_t)bh * p.w_stride;
+        for (int i0 = max(begin, len) + tid; i0 < chunk_end; i0 += 8 * kWThreads) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = i0 + j * kWThreads < chunk_end ? __ldg(src + i0 + j * kWThreads) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i0 + j * kWThreads < chunk_end) dst[i0 + j * kWThreads] = x[j];
+        }
+    }
     if (begin >= end) return;
     const int base = min(max(p.base_length[b], 0), len);
     int clamped;
