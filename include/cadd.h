@@ -62,7 +62,7 @@ extern "C" {
 #define CADD_STATUS_BAD_PAGE           512   /* cache: an entry of block_table in use was outside [0, n_pages); its tokens are neither read nor written */
 #define CADD_STATUS_BAD_LENGTH        1024   /* cache: length / base_length / start / count / n_rows / path_len was out of range and was clamped */
 #define CADD_STATUS_CACHE_FULL        2048   /* cache append: the request's pages could not hold every row; those beyond were dropped */
-#define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out */
+#define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out (in append its place counts and keeps what it held) */
 #define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax */
 
 #define CADD_DTYPE_BF16 0
@@ -390,7 +390,7 @@ typedef struct cadd_read_args {
  * One decoded token is R = 1.  A row that sees nothing (or only scores of -Inf) gets 0 and lse -Inf.  What a row does not
  * see has no influence on it, whatever it holds.  Products are bf16 with fp32 sums, the softmax is fp32, its weights are
  * rounded to bf16 for the product with the values (relative error at most 2^-8 each).
- * Rows above n_nodes[b] are left as they were in out and lse.
+ * Rows above n_nodes[b] are left as they were in out and lse.  out and lse overlap no input.  R * heads_q / heads is at most 2^24.
  */
 #define CADD_ATTENTION_TILED_PATH 1u   /* small calls too take the kernel that large ones take (results agree to rounding; for measurements and tests) */
 typedef struct cadd_attention_args {
@@ -428,7 +428,7 @@ typedef struct cadd_attention_args {
  * base_length + i as the row's place):
  *     weights_out[b, head, p] = (p < base_length[b] ? weights[b, head, p] : 0) + sum_i E_i(p).
  * Places from length[b] on are left as they were, or copied where weights_out is another array.  A row whose lse is -Inf or
- * +Inf adds nothing.
+ * +Inf adds nothing.  Rows times heads_q / heads (path: L + 1 rows) are at most 2^24.
  */
 typedef struct cadd_weights_args {
     uint32_t struct_size;          /* = sizeof(cadd_weights_args) */
@@ -540,11 +540,11 @@ int cadd_tree_attention_workspace_bytes(const cadd_attention_args* a, size_t* ou
 int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream);
 
 /* Attention weight of the accepted rows, added up per cached place (see cadd_weights_args).  Asynchronous on
- * `cuda_stream`: one kernel.  The same inputs give the same bits. */
+ * `cuda_stream`: one kernel (a second, small one before it where status is given).  The same inputs give the same bits. */
 int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream);
 
 /* Eviction by accumulated weight into new pages (see cadd_evict_args).  Asynchronous on `cuda_stream`: two kernels
- * (choice, copy). */
+ * (choice, copy; a third, tiny one where new_length is cache.length). */
 int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream);
 
 /*

@@ -270,6 +270,7 @@ int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream) {
     if (rc != CADD_OK) return rc;
     if (a->R < 1 || a->R > 65536 || (a->path && (a->L < 1 || a->L > 65536)) || a->heads_q < 1 || a->heads_q > 65536 || a->heads_q % a->cache.heads)
         return CADD_ERR_SHAPE;
+    if (((int64_t)(a->path ? a->L + 1 : a->R) * (a->heads_q / a->cache.heads)) > ((int64_t)1 << 24)) return CADD_ERR_SHAPE;
     if (a->window < 0 || a->n_sinks < 0 || a->n_sinks > (1 << 30) || !(a->scale > 0.0f) || !isfinite(a->scale)) return CADD_ERR_SHAPE;
     const int64_t cap = (int64_t)a->cache.max_pages * a->cache.page_size;
     if (a->weights_stride < cap || a->weights_stride >= ((int64_t)1 << 36)) return CADD_ERR_SHAPE;

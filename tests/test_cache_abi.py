@@ -112,6 +112,14 @@ def test_calls_refuse_bad_arguments(lib, name):
         assert fn(C.byref(a), None) == code, change
 
 
+def test_more_rows_than_weights_count_are_refused(lib):
+    a = weights()
+    a.cache.heads, a.heads_q, a.L = 1, 65536, 256                          # 257 rows of 2^16 heads: above 2^24
+    assert lib.cadd_cache_weights(C.byref(a), None) == G.ERR_SHAPE
+    a.R, a.path, a.path_len = 65536, None, None                            # 2^32
+    assert lib.cadd_cache_weights(C.byref(a), None) == G.ERR_SHAPE
+
+
 def test_workspace_query_is_host_arithmetic(lib):
     a = attention()
     for f in ("q", "k", "v", "out", "workspace"):
