@@ -80,8 +80,10 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
         for (int i = tid; i < tiles * 16 * (D / 8); i += kWThreads) {
             const int m = i / (D / 8), ch = i - m * (D / 8), li = (m0 + m) / p.group, hq = h * p.group + (m0 + m - li * p.group);
             const int r = m < here ? row_at(p.rows, b, li) : -1;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (r >= 0) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
+            const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
+            const bool out = fabsf(lse) == INFINITY;
+            uint4 x = make_uint4(0, 0, 0, 0);            // a row that adds nothing: zeros, whatever it holds
+            if (!out) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
             float scale = p.scale_log2;
             if constexpr (FP4) {
                 float amax = chunk_amax(x);
@@ -96,8 +98,7 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
             }
             sh.q[m][wkeys_slot<D, FP4>(ch)] = x;
             if (ch == 0) {
-                const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
-                sh.lse[m] = fabsf(lse) == INFINITY ? INFINITY : lse * kLog2e;
+                sh.lse[m] = out ? INFINITY : lse * kLog2e;
                 sh.scale[m] = scale;
                 sh.place[m] = base + li;
             }

@@ -251,6 +251,15 @@ def test_many_rows_of_a_prompt_and_rows_without_a_sum():
         assert bool(((out[b, :, :p.lens[b]].cpu().double() - want[b]).abs() <= tol[b]).all())
 
 
+@pytest.mark.parametrize("fp4", [False, True])
+def test_rows_without_a_sum_add_nothing_whatever_they_hold(fp4):
+    p, path, path_lens, base, rows, lse, w, *_ = weights_case(fp4=fp4, group=2, R=9, base=[70, 200], path_lens=[5, 3])
+    for b, r, h, x, e in ((0, 0, 0, math.inf, math.inf), (0, rows[0][2], 3, math.nan, -math.inf), (1, rows[1][3], 1, -math.inf, math.inf)):
+        p.q[b, r, h] = x
+        lse[b, r, h] = e
+    check_weights((p, path, path_lens, base, rows, lse, w, 0, 0))
+
+
 def test_weights_flag_bad_paths_pages_and_lengths():
     p, path, path_lens, base, rows, lse, w, *_ = weights_case(fp4=False, R=9, base=[70, 20, 33], path_lens=[3, 2, 1])
     path[1, 1] = 9
