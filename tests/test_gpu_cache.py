@@ -495,3 +495,91 @@ def test_rounds_of_building_attending_verifying_committing_and_evicting(fp4):
         got_k, _ = read_all(cache, budget)
         for b in range(B):
             assert torch.equal(got_k[b, :keys[b].shape[0]], keys[b])
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_a_captured_round_follows_its_inputs(fp4):
+    """Attention, commit in place, weights and eviction captured into one graph: replayed with other lengths, paths and rows it gives
+    what the calls give one by one, bit for bit."""
+    B, H, GR, D, P, R, L, budget = 3, 2, 4, 64, 16, 12, 4, 48
+    g = torch.Generator().manual_seed(11)
+    per, new_per = 8, 3
+    n_pages = B * (per + new_per)
+    table = torch.arange(B * per, dtype=torch.int32, device=DEV).reshape(B, per)
+    new_table = torch.arange(B * per, n_pages, dtype=torch.int32, device=DEV).reshape(B, new_per)
+
+    def buffers():
+        if fp4:
+            pools = [torch.zeros(n_pages, H, P, n, dtype=torch.uint8, device=DEV) for n in (D // 2, D // 2, D // 16, D // 16)]
+        else:
+            pools = [torch.zeros(n_pages, H, P, D, dtype=torch.bfloat16, device=DEV) for _ in range(2)] + [None, None]
+        d = dict(pools=pools, length=i32([0] * B), base=i32([0] * B), path=torch.zeros(B, L, dtype=torch.int32, device=DEV), path_len=i32([0] * B),
+                 q=torch.zeros(B, R, H * GR, D, dtype=torch.bfloat16, device=DEV), k=torch.zeros(B, R, H, D, dtype=torch.bfloat16, device=DEV),
+                 v=torch.zeros(B, R, H, D, dtype=torch.bfloat16, device=DEV), w=torch.zeros(B, H, per * P, device=DEV),
+                 att=G.Attention(out=torch.zeros(B, R, H * GR, D, dtype=torch.bfloat16, device=DEV), lse=torch.zeros(B, R, H * GR, device=DEV), status=i32([0] * B)),
+                 ev=G.Evicted(new_length=i32([0] * B), kept=torch.zeros(B, H, budget, dtype=torch.int32, device=DEV),
+                              weights=torch.zeros(B, H, new_per * P, device=DEV), status=i32([0] * B)))
+        d["cache"] = G.KvCache(k=pools[0], v=pools[1], k_scale=pools[2], v_scale=pools[3], block_table=table, length=d["length"])
+        d["ws"] = torch.zeros(G.cadd_tree_attention_workspace_bytes(B, R, H * GR, d["cache"]), dtype=torch.uint8, device=DEV)
+        return d
+
+    def step(d):
+        G.cadd_tree_attention(d["q"], d["k"], d["v"], d["cache"], out=d["att"], workspace=d["ws"])
+        d["base"].copy_(d["length"])
+        G.cadd_cache_append(d["cache"], d["k"], d["v"], path=d["path"], path_len=d["path_len"], new_length=d["length"])
+        G.cadd_cache_weights(d["q"], d["att"].lse, d["cache"], d["base"], d["w"], path=d["path"], path_len=d["path_len"])
+        G.cadd_cache_evict(d["cache"], d["w"], new_table, budget, n_sinks=2, n_recent=5, out=d["ev"])
+
+    def put(d, x):
+        for name in ("length", "path", "path_len", "q", "k", "v", "w"):
+            d[name].copy_(x[name])
+        G.cadd_cache_append(d["cache"], x["prompt"][0], x["prompt"][1], n_rows=x["n"], new_length=d["length"])
+
+    a, b = buffers(), buffers()
+    step(a)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a)
+    for lens, path_lens in (([100, 1, 47], [4, 0, 2]), ([0, 60, 124], [1, 3, 3]), ([33, 32, 31], [0, 4, 1])):
+        x = dict(length=i32([0] * B), path=torch.randint(1, R, (B, L), generator=g).int().to(DEV), path_len=i32(path_lens), n=i32(lens),
+                 q=torch.randn(B, R, H * GR, D, generator=g).bfloat16().to(DEV), k=torch.randn(B, R, H, D, generator=g).bfloat16().to(DEV),
+                 v=torch.randn(B, R, H, D, generator=g).bfloat16().to(DEV), w=torch.rand(B, H, per * P, generator=g).to(DEV),
+                 prompt=torch.randn(2, B, max(lens), H, D, generator=g).bfloat16().to(DEV))
+        put(a, x)
+        put(b, x)
+        graph.replay()
+        step(b)
+        torch.cuda.synchronize()
+        assert a["length"].tolist() == [n + m + 1 for n, m in zip(lens, path_lens)]
+        for i in range(4 if fp4 else 2):
+            assert torch.equal(a["pools"][i], b["pools"][i])
+        for t, u in ((a["att"].out, b["att"].out), (a["att"].lse, b["att"].lse), (a["w"], b["w"]), (a["length"], b["length"]), (a["base"], b["base"]),
+                     (a["ev"].new_length, b["ev"].new_length), (a["ev"].kept, b["ev"].kept), (a["ev"].weights, b["ev"].weights), (a["ev"].status, b["ev"].status)):
+            assert torch.equal(t, u)
+
+
+def test_rows_of_a_pool_of_more_than_four_gigabytes():
+    """Four-bit pools whose last pages are used: every call's row offsets need 64 bits.  Small pools with the same contents say what is right."""
+    H, P, D, B, R = 8, 64, 128, 2, 3
+    n_pages = (1 << 32) // (H * P * D // 2) + 40
+    sizes = (D // 2, D // 2, D // 16, D // 16)
+    prompt = torch.randn(2, B, 150, H, D, generator=torch.Generator().manual_seed(3)).bfloat16().to(DEV)
+    q = torch.randn(B, R, 2 * H, D, device=DEV).bfloat16()
+    got = []
+    for pages in (12, n_pages):
+        pools = [torch.empty(pages, H, P, n, dtype=torch.uint8, device=DEV) for n in sizes]
+        table = torch.arange(pages - 6, pages, dtype=torch.int32, device=DEV).reshape(B, 3)
+        new = torch.arange(pages - 10, pages - 6, dtype=torch.int32, device=DEV).reshape(B, 2)
+        c = G.KvCache(k=pools[0], v=pools[1], k_scale=pools[2], v_scale=pools[3], block_table=table, length=i32([0, 0]))
+        G.cadd_cache_append(c, prompt[0], prompt[1], n_rows=i32([150, 97]), new_length=c.length)
+        own = prompt[:, :, :R].contiguous()
+        outs = [G.cadd_tree_attention(q, own[0], own[1], c, flags=f) for f in (0, G.ATTENTION_TILED_PATH)]
+        w = torch.zeros(B, H, 3 * P, device=DEV)
+        G.cadd_cache_weights(q, outs[0].lse, c, i32([147, 94]), w, n_rows=i32([3, 3]))
+        ev = G.cadd_cache_evict(c, w, new, 100, n_sinks=1)
+        after = G.KvCache(k=pools[0], v=pools[1], k_scale=pools[2], v_scale=pools[3], block_table=new, length=ev.new_length)
+        got.append([*G.cadd_cache_read(c, 160), *G.cadd_cache_read(after, 100), outs[0].out, outs[0].lse, outs[1].out, outs[1].lse, w, ev.kept])
+        assert ev.status.tolist() == [0, 0]
+    for t, u in zip(*got):
+        assert torch.equal(t, u)
+    assert torch.equal(got[1][0][0, :150].cpu(), stored(prompt[0, 0].cpu(), True).bfloat16())
