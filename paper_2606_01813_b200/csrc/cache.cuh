@@ -62,6 +62,15 @@ __device__ __forceinline__ int row_at(const RowList& r, int b, int i) {
     return (unsigned)j < (unsigned)r.R ? j : -1;
 }
 
+// Item `it` of [rows][heads][head_dim / 16], head_dim / 16 being 4 or 8; a 64-bit division is only taken where it is needed.
+__device__ __forceinline__ void cache_item(int64_t it, int64_t items, const CacheView& c, int& i, int& h, int& q) {
+    const int shift = c.head_dim == 128 ? 3 : 2;
+    q = (int)it & ((1 << shift) - 1);
+    const int64_t rest = it >> shift;
+    i = items <= 0xffffffffll ? (int)((unsigned)rest / (unsigned)c.heads) : (int)(rest / c.heads);
+    h = (int)(rest - (int64_t)i * c.heads);
+}
+
 struct AppendParams {
     CacheView c;
     const unsigned char *k, *v;
@@ -74,7 +83,8 @@ struct AppendParams {
 constexpr int kCopyThreads = 256;
 
 // Rows into the cache: one thread moves 16 elements of one row of one head, of k and of v.  Bound by memory traffic (and by
-// the launch for a round's few rows): prompts of 37k rows in all, 8 heads of 128, to 4 bits in 48 us (4.0 TB/s), read back in 44 us.  The first CTA of a request also writes its new length and status.
+// the launch for a round's few rows): prompts of 37k rows in all, 8 heads of 128, to 4 bits and read back in 92 us together, 4.0 TB/s.
+// The first CTA of a request also writes its new length and status.
 template <bool FP4>
 __global__ void __launch_bounds__(kCopyThreads) cache_append_kernel(const AppendParams p) {
     const int b = blockIdx.x / p.ctas_per_request, part = blockIdx.x - b * p.ctas_per_request;
@@ -85,7 +95,8 @@ __global__ void __launch_bounds__(kCopyThreads) cache_append_kernel(const Append
     const int blocks = c.head_dim >> 4, per_row = c.heads * blocks;
     const int64_t items = (int64_t)n * per_row;
     for (int64_t it = (int64_t)part * kCopyThreads + threadIdx.x; it < items; it += (int64_t)p.ctas_per_request * kCopyThreads) {
-        const int i = (int)(it / per_row), rem = (int)(it - (int64_t)i * per_row), h = rem / blocks, q = rem - h * blocks;
+        int i, h, q;
+        cache_item(it, items, c, i, h, q);
         const int src = row_at(p.rows, b, i);
         const int64_t row = cache_row(c, b, h, base + i);
         if (src < 0 || row < 0) continue;
@@ -149,7 +160,8 @@ __global__ void __launch_bounds__(kCopyThreads) cache_read_kernel(const ReadPara
     const int blocks = c.head_dim >> 4, per_row = c.heads * blocks;
     const int64_t items = (int64_t)n * per_row;
     for (int64_t it = (int64_t)part * kCopyThreads + threadIdx.x; it < items; it += (int64_t)p.ctas_per_request * kCopyThreads) {
-        const int i = (int)(it / per_row), rem = (int)(it - (int64_t)i * per_row), h = rem / blocks, q = rem - h * blocks;
+        int i, h, q;
+        cache_item(it, items, c, i, h, q);
         const int64_t row = cache_row(c, b, h, from + i);
         if (row < 0) continue;
         const int64_t at = ((int64_t)b * p.stride_b + (int64_t)i * p.stride_row + (int64_t)h * p.stride_head + q * 16) * 2;
