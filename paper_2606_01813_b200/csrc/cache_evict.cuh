@@ -34,8 +34,9 @@ struct WeightsParams {
 // the same order (in fp16 for a 4-bit cache: fp4.cuh).  A warp takes 32 keys at a time, the next 32 being on their way; sums
 // over rows stay in registers and are joined across the lanes at the end, in a fixed order.  More than 128 rows are done in
 // groups, the later ones adding to what the earlier ones wrote.
-// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 245 us, a quarter of the
-// measured copy rate.  By count, what bounds it is issue: some 190 instructions to dequantise a warp's 32 keys, and per
+// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 201 us, 0.29 of the
+// measured copy rate.  Twelve warps an SM hide little (issue was active 40 % of the time at 245 us), so table entries and totals are
+// fetched a step before their use (245 -> 201 us; four CTAs an SM, with spills, came to 270).  By count: 190 instructions to dequantise a warp's 32 keys, and per
 // 16 rows 32 products, 16 exponentials a thread and their sums.
 constexpr int kWThreads = 128;
 constexpr int kWRows = 128;                              // rows in shared memory at a time
@@ -113,12 +114,21 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
             for (int j = 0; j < 4; ++j) e |= row[j] >= 0 ? 1u << j : 0u;
             return e;
         };
-        wkeys_rows(p.c, b, h, k0, g, end, row);
+        int page[4];
+        wkeys_pages(p.c, b, k0, g, end, page);
+        wkeys_rows(p.c, h, k0, g, end, page, row);
 #pragma unroll
         for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);
         unsigned there = exist_bits(), there_next;
-        wkeys_rows(p.c, b, h, k0 + kWThreads, g, end, row);                        // rows are looked up a step before their keys are fetched
-        for (; k0 < end; k0 += kWThreads, there = there_next) {
+        wkeys_pages(p.c, b, k0 + kWThreads, g, end, page);                         // looked up a step before the keys are fetched
+        const int mine = (g >> 1) * 8 + 2 * t + (g & 1);    // the key of each 32 whose sum this lane ends with
+        const float* totals = m0 ? w_out : w_in;
+        const int counted = m0 ? end : min(base, end);      // places that have a total
+        auto total_of = [&](int key) { return key < counted ? totals[key] : 0.0f; };
+        float before = total_of(k0 + mine), before_next;    // (and so are the totals: what a step waits for has been under way for a step)
+        for (; k0 < end; k0 += kWThreads, there = there_next, before = before_next) {
+            const int key = k0 + mine;
+            before_next = total_of(key + kWThreads);
             uint32_t kf[4][W * 4];                       // the 32 keys as operands: [key group of 8][word][two steps x two registers]
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -132,10 +142,11 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                     kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
                 }
             }
+            wkeys_rows(p.c, h, k0 + kWThreads, g, end, page, row);
 #pragma unroll
             for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);            // the next keys
             there_next = exist_bits();
-            wkeys_rows(p.c, b, h, k0 + 2 * kWThreads, g, end, row);
+            wkeys_pages(p.c, b, k0 + 2 * kWThreads, g, end, page);
             float sum[4][2] = {};
             if (p.window == 0 || k0 < p.n_sinks || k0 + 31 > base - p.window) {
                 const bool plain = p.window == 0 && k0 + 31 <= base;               // every row sees all 32
@@ -167,8 +178,8 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                             for (int j = 0; j < 4; ++j) {
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    const int key = k0 + j * 8 + 2 * t + e;
-                                    const bool see = !out && key <= place && (p.window == 0 || key < p.n_sinks || place - key < p.window);
+                                    const int at = k0 + j * 8 + 2 * t + e;
+                                    const bool see = !out && at <= place && (p.window == 0 || at < p.n_sinks || place - at < p.window);
                                     const float v = ex2(fmaf(c[j][half * 2 + e], sc, -lse));
                                     sum[j][e] += see ? v : 0.0f;
                                 }
@@ -177,8 +188,7 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                     }
                 }
             }
-            // sums over the eight lanes of equal t; each round halves what a lane goes on with, and lane (g, t) ends with key
-            // (g >> 1) * 8 + 2 t + (g & 1)
+            // sums over the eight lanes of equal t; each round halves what a lane goes on with
             float a[4], c2[2], v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                // g's high bit chooses between key groups 0, 1 and 2, 3
@@ -191,14 +201,10 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                 c2[i] = keep + __shfl_xor_sync(kFullMask, give, 8);
             }
             v = (g & 1 ? c2[1] : c2[0]) + __shfl_xor_sync(kFullMask, g & 1 ? c2[0] : c2[1], 4);
-            const int mine = (g >> 1) * 8 + 2 * t + (g & 1), key = k0 + mine;
             // whether that key exists is known to the lanes with g' = mine & 7, as bit mine >> 3
             const unsigned known = __shfl_sync(kFullMask, there, (mine & 7) * 4);
             if (!((known >> (mine >> 3)) & 1u)) v = 0.0f;                          // on no page: nothing to be seen
-            if (key < end) {
-                const float before = m0 ? w_out[key] : (key < base ? w_in[key] : 0.0f);
-                w_out[key] = before + v;
-            }
+            if (key < end) w_out[key] = before + v;
         }
         if (rows <= kWRows) break;
     }

@@ -122,7 +122,7 @@ static int launch_tree_attention(AttnWork& w, bool tiled, cudaStream_t st) {
 
 template <int D, bool FP4>
 static int launch_weights(WeightsParams& p, int64_t cap, cudaStream_t st) {
-    // Keys of a CTA: 2048 (32 requests of up to 32k tokens: 236 us; 1024: 255, 4096: 248, 8192: 325), less where that would leave the
+    // Keys of a CTA: 2048 (32 requests of up to 32k tokens, before totals were fetched ahead: 236 us; 1024: 255, 4096: 248, 8192: 325), less where that would leave the
     // device short of CTAs, 128 (32 a warp) at least.
     const int64_t bh = (int64_t)p.c.batch * p.c.heads;
     p.keys_per_cta = 2048;

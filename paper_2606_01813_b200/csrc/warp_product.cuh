@@ -56,4 +56,31 @@ __device__ __forceinline__ void wkeys_rows(const CacheView& c, int b, int h, int
     }
 }
 
+// The same in two steps: table entries, and, a step later when those have come, rows.  (The weights kernel gains by it, 245 -> 234 us;
+// the few-rows kernel, short of registers, loses: 170 -> 203 us for 16 tokens over up to 32k.)
+__device__ __forceinline__ void wkeys_pages(const CacheView& c, int b, int k0, int g, int end, int (&page)[4]) {
+    const int32_t* table = c.block_table + (int64_t)b * c.max_pages;
+    if (c.page_shift >= 5) {
+        page[0] = k0 < end ? table[k0 >> c.page_shift] : -1;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) page[j] = k0 + j * 8 + g < end ? table[(k0 + j * 8 + g) >> c.page_shift] : -1;
+    }
+}
+__device__ __forceinline__ void wkeys_rows(const CacheView& c, int h, int k0, int g, int end, const int (&page)[4], int64_t (&row)[4]) {
+    const int slots = (1 << c.page_shift) - 1;
+    if (c.page_shift >= 5) {
+        int64_t first = -1;
+        if ((unsigned)page[0] < (uint64_t)c.n_pages)
+            first = (int64_t)page[0] * c.stride_page + (int64_t)h * c.stride_head + (int64_t)(k0 & slots) * c.stride_slot;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) row[j] = first >= 0 && k0 + j * 8 + g < end ? first + (int64_t)(j * 8 + g) * c.stride_slot : -1;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            row[j] = (unsigned)page[j] < (uint64_t)c.n_pages
+                         ? (int64_t)page[j] * c.stride_page + (int64_t)h * c.stride_head + (int64_t)((k0 + j * 8 + g) & slots) * c.stride_slot : -1;
+    }
+}
+
 }  // namespace cadd
