@@ -1,0 +1,92 @@
+"""Tree attention where numbers and shapes leave the ordinary: weights far below the largest, queries whose elements differ by
+many powers of two, ranges of many units (buffers reused, the running maximum raised, steps of a warp one after the other), and
+what rows with non-finite numbers cost."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_01813_b200 import binding as G
+from cache_util import Problem, check_attention, decode, encode
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def problem(**kw):
+    d = dict(batch=2, heads=2, group=2, dim=128, page=16, fp4=False, lens=[70, 33], R=5, live=[5, 3], causal=False, seed=1)
+    d.update(kw)
+    return Problem(**d)
+
+
+def store(p, which, b, x):
+    """Rows x [n, heads, dim] in place of request b's keys (0) or values (1)."""
+    if p.fp4:
+        exp = (p.k_exp, p.v_exp)[which]
+        codes, scales = encode(x, exp)
+        p.put(which, b, 0, codes)
+        p.put(which + 2, b, 0, scales)
+        x = decode(codes, scales, exp)
+    else:
+        x = x.bfloat16().double()
+        p.put(which, b, 0, x.bfloat16())
+    (p.V if which else p.K)[b] = x
+
+
+FLAGS = [0, G.ATTENTION_TILED_PATH]
+
+
+LONG = [(False, 0, 16), (False, 0, 64), (True, 0, 16), (True, 0, 64), (True, G.ATTENTION_TILED_PATH, 64)]
+
+
+@pytest.mark.parametrize("fp4,flags,page", LONG)
+@pytest.mark.parametrize("growing", [False, True])
+def test_ranges_of_many_units(fp4, flags, page, growing):
+    """Eight heads over 20000 places: 2500 units and more for some 300 ranges, so a CTA goes through eight and more of one item, and a warp
+    of the few-rows kernel through several steps.  Growing: keys whose scores rise by far more than 40 powers of two along a range."""
+    p = problem(batch=1, heads=8, group=2, page=page, fp4=fp4, lens=[20011], R=2, live=[2], seed=2, scale=8.0 if growing else None)
+    if growing:
+        store(p, 0, 0, p.K[0] * torch.linspace(0.05, 3.0, 20011, dtype=torch.float64)[:, None, None])
+    got = p.run(G, flags=flags)
+    check_attention(p, got)
+    again = p.run(G, flags=flags)
+    assert torch.equal(again.out, got.out) and torch.equal(again.lse, got.lse)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_blocks_of_rows_over_many_units(fp4):
+    """Two blocks of rows to an item, the second one partly empty, over ranges of many units; a window whose units lie apart from the sinks'."""
+    p = problem(batch=1, heads=4, group=8, page=32, fp4=fp4, lens=[20011], R=20, live=[20], seed=3)
+    check_attention(p, p.run(G))
+    p.window, p.sinks = 15000, 70
+    check_attention(p, p.run(G))
+
+
+def time_of(call):
+    call()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    call()
+    b.record()
+    torch.cuda.synchronize()
+    return a.elapsed_time(b)
+
+
+@pytest.mark.parametrize("fp4,R", [(False, 4), (True, 4), (False, 50), (True, 50)])
+def test_single_elements_that_are_not_finite(fp4, R):
+    """In a long cache: one element of a tree row's value is Inf and another NaN; everything else is what it was without them."""
+    p = problem(fp4=fp4, batch=1, heads=2, group=2, lens=[3001], R=R, live=[R], page=32)
+    last = R - 1
+    p.v[0, 0, 0, 17], p.v[0, last, 1, 90], p.v[0, last, 0, 0] = math.inf, math.nan, -math.inf
+    got = p.run(G).out.cpu().double()
+    p.v[0, 0, 0, 17] = p.v[0, last, 1, 90] = p.v[0, last, 0, 0] = 0.0
+    want, _, amass, _ = p.attention(0)
+    sees = p.mask[0, :, last]
+    odd = torch.zeros(R, 4, 128, dtype=torch.bool)
+    odd[:, :2, 17] = True
+    odd[sees, 2:, 90] = True
+    odd[sees, :2, 0] = True
+    assert bool((got[0, :, :2, 17] == math.inf).all()) and bool(torch.isnan(got[0, sees][:, 2:, 90]).all()) and bool((got[0, sees][:, :2, 0] == -math.inf).all())
+    err = (got[0] - want).abs()[~odd]
+    assert bool((err <= 2.0 ** -6 * amass[~odd] + 1e-6).all())

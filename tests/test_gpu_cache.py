@@ -583,3 +583,15 @@ def test_rows_of_a_pool_of_more_than_four_gigabytes():
     for t, u in zip(*got):
         assert torch.equal(t, u)
     assert torch.equal(got[1][0][0, :150].cpu(), stored(prompt[0, 0].cpu(), True).bfloat16())
+
+
+# ---- what is stored, byte by byte; queries and shapes out of the ordinary ----
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("page,window", [(16, 0), (64, 0), (64, 5000)])
+def test_weights_of_warps_that_go_through_many_steps(fp4, page, window):
+    """32 heads' caches of up to 16000 places: a CTA has 512 keys and more, a warp four steps and more, totals and pages fetched ahead."""
+    case = weights_case(fp4=fp4, heads=8, group=2, page=page, R=9, base=[16000, 9000, 12345, 100], path_lens=[3, 8, 0, 5], window=window, sinks=40 if window else 0)
+    check_weights(case)
+    check_weights(case, in_place=True)
