@@ -7,7 +7,8 @@
 // eight: one nibble of each key side by side is what the conversion instruction turns into the operand's pair.  The four
 // warps of a CTA work on different keys of the item, each with its own maximum, sum and output, joined in shared
 // memory at the item's end; keys are shared out over the CTAs as in attn_plan.cuh.  The next keys are on their way from the
-// moment the last are in their operands, the next values from the moment the last are multiplied.  fp16 and its scalings are those of attn_tiles.cuh; the tree's rows are bf16.
+// moment the last are in their operands, the next values from the moment the last are multiplied.  Cached keys and values are
+// products in fp16 (fp4.cuh), the tree's rows in bf16.
 #pragma once
 #include "attn_plan.cuh"
 #include "warp_product.cuh"
@@ -16,8 +17,14 @@ namespace cadd {
 
 constexpr int kFewRows = 16;
 constexpr int kFewThreads = 128;
+// Weights are formed as 2^(s - m + kFewUp): up to 2^15 where a score exceeds the reference m by the slack, so that fp16 holds them to
+// 2^-8 of themselves or better from 2^-25 of the reference's weight on (2^-17, an fp16 subnormal with seven bits).  A step of 32
+// keys with a smaller one takes its products in bf16, which has fp32's range; the values, code * scale, are the same in both.
+// (16 tokens over up to 32k places on a B200: 170 us without the look at the smallest score, 179 with it, 196 where nearly every
+// step has one.)
 constexpr float kFewSlack = 7.0f;                        // as kTileSlack for fp16 weights
 constexpr int kFewUp = 8;
+constexpr float kFewHalfRange = 25.0f;
 
 template <int D> struct alignas(16) FewShared {
     uint4 qh[kFewRows][D / 8 + 1], qb[kFewRows][D / 8 + 1];                        // fp16 scaled, bf16; one chunk of padding
@@ -28,6 +35,12 @@ template <int D> struct alignas(16) FewShared {
     PlanShared plan;
     int odd;
 };
+
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 template <int D> struct FewValues {                      // a lane's share of 32 keys' values: [group of eight][key 2t, 2t + 1]
     uint32_t w[4][2][D / 64];
@@ -110,8 +123,16 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_c
         const float scale[2] = {sh.scale[g], sh.scale[g + 8]};
         const int2 at[2] = {sh.row_at[g], sh.row_at[g + 8]};
 
-        // scores -> weights as product operands, m, l and o following; `see` of a row: bits of the 32 keys
-        auto softmax = [&](float (&c)[4][4], const float (&sc)[2], bool masked, const uint32_t (&see)[2], int up, bool half, uint32_t (&a)[4][2]) {
+        // scores -> weights times 2^up in their place, m, l and o following; `see` of a row: bits of the 32 keys.  True: a weight (or what
+        // a score that is masked would weigh) lies below what fp16 holds.
+        auto softmax = [&](float (&c)[4][4], const float (&sc)[2], bool masked, const uint32_t (&see)[2], int up) -> bool {
+            float low[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                low[h] = fminf(c[0][2 * h], c[0][2 * h + 1]);
+#pragma unroll
+                for (int j = 1; j < 4; ++j) low[h] = min3(low[h], c[j][2 * h], c[j][2 * h + 1]);
+            }
             if (masked) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -151,12 +172,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_c
                 float sum = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float e0 = ex2(fmaf(c[j][2 * h], sc[h], off)), e1 = ex2(fmaf(c[j][2 * h + 1], sc[h], off));
-                    sum += e0 + e1;
-                    a[j][h] = half ? pack_half(e0, e1) : pack_bf16(e0, e1);
+                    c[j][2 * h] = ex2(fmaf(c[j][2 * h], sc[h], off));
+                    c[j][2 * h + 1] = ex2(fmaf(c[j][2 * h + 1], sc[h], off));
+                    sum += c[j][2 * h] + c[j][2 * h + 1];
                 }
                 l[h] = fmaf(sum, down, l[h]);
             }
+            return __any_sync(kFullMask, low[0] * sc[0] < m[0] - kFewHalfRange || low[1] * sc[1] < m[1] - kFewHalfRange);
         };
 
         const int ctx_end = min(it.u1, it.ctx.total);
@@ -231,18 +253,28 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_c
 #pragma unroll
                     for (int h = 0; h < 2; ++h) see[h] = exist & attn_key_bits(p, false, it.b, it.len, it.live, at[h].x, at[h].y, k0);
                 }
-                uint32_t a[4][2];
-                softmax(c, scale, !whole, see, kFewUp, true, a);
+                const bool wide = softmax(c, scale, !whole, see, kFewUp);
                 // O += P V, two steps of 16 keys
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    uint32_t a[4];                        // rows g, g + 8 of keys 0..7, then of keys 8..15
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = c[2 * h + (e >> 1)][2 * (e & 1)], y = c[2 * h + (e >> 1)][2 * (e & 1) + 1];
+                        a[e] = wide ? pack_bf16(x, y) : pack_half(x, y);
+                    }
 #pragma unroll
                     for (int i = 0; i < D / 64; ++i) {
                         uint32_t b0[8], b1[8];
                         few_value_pairs(vx.w[2 * h][0][i], vx.w[2 * h][1][i], vx.s[2 * h], b0);
                         few_value_pairs(vx.w[2 * h + 1][0][i], vx.w[2 * h + 1][1][i], vx.s[2 * h + 1], b1);
+                        if (!wide) {
 #pragma unroll
-                        for (int n = 0; n < 8; ++n) mma_16x8x16<true>(o[i * 8 + n], a[2 * h][0], a[2 * h][1], a[2 * h + 1][0], a[2 * h + 1][1], b0[n], b1[n]);
+                            for (int n = 0; n < 8; ++n) mma_16x8x16<true>(o[i * 8 + n], a[0], a[1], a[2], a[3], b0[n], b1[n]);
+                        } else {
+#pragma unroll
+                            for (int n = 0; n < 8; ++n) mma_16x8x16<false>(o[i * 8 + n], a[0], a[1], a[2], a[3], bf16_of_half(b0[n]), bf16_of_half(b1[n]));
+                        }
                     }
                 }
                 if (s + 4 < steps) {
@@ -272,7 +304,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_c
 #pragma unroll
             for (int h = 0; h < 2; ++h) see[h] = attn_key_bits(p, true, it.b, it.len, it.live, at[h].x, at[h].y, k0);
             const float sc[2] = {p.scale_log2, p.scale_log2};
-            softmax(c, sc, true, see, kFewUp + p.c.v_exp, false, a);
+            softmax(c, sc, true, see, kFewUp + p.c.v_exp);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { a[j][0] = pack_bf16(c[j][0], c[j][1]); a[j][1] = pack_bf16(c[j][2], c[j][3]); }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll

@@ -81,6 +81,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// A pair of fp16 numbers code * scale as bf16: exact, both hold six significant bits.
+__device__ __forceinline__ uint32_t bf16_of_half(uint32_t x) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x));
+    return pack_bf16(f.x, f.y);
+}
 
 __device__ __forceinline__ float ex2(float x) {
     float r;

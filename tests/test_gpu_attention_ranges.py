@@ -36,6 +36,25 @@ def store(p, which, b, x):
 FLAGS = [0, G.ATTENTION_TILED_PATH]
 
 
+@pytest.mark.parametrize("fp4,flags", [(False, 0), (True, 0), (True, G.ATTENTION_TILED_PATH)])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("gap", [8.0, 17.0, 20.0, 23.0, 40.0, 80.0])
+@pytest.mark.parametrize("at", [0, 150, 299])
+def test_one_key_far_above_the_rest_whose_value_is_zero(fp4, flags, dim, gap, at):
+    """What a row gets is then a sum over weights of e^-gap and less, each of which is to be good to its rounding: the outputs'
+    tolerance goes by the sum of their products with the values."""
+    p = problem(fp4=fp4, dim=dim, lens=[300, 300], R=2, live=[2, 1], group=4, seed=int(gap))
+    p.q[:] = 1.0
+    p.k[:] = 0.0
+    for b in range(2):
+        k, v = p.K[b] * 0.125, p.V[b].clone()
+        k[at], v[at] = 1.0, 0.0
+        store(p, 0, b, k)
+        store(p, 1, b, v)
+    p.scale = gap / float(p.K[0][at, 0].sum())
+    check_attention(p, p.run(G, flags=flags))
+
+
 LONG = [(False, 0, 16), (False, 0, 64), (True, 0, 16), (True, 0, 64), (True, G.ATTENTION_TILED_PATH, 64)]
 
 
