@@ -390,7 +390,8 @@ typedef struct cadd_read_args {
  * One decoded token is R = 1.  A row that sees nothing (or only scores of -Inf) gets 0 and lse -Inf.  What a row does not
  * see has no influence on it, whatever it holds.  Products are bf16 with fp32 sums, the softmax is fp32, its weights are
  * rounded for the product with the values to bf16, or in small calls over a 4-bit cache to fp16 where that holds them (relative
- * error at most 2^-8 each either way; below 2^-126 of the row's largest weight they may count as zero).
+ * error at most 2^-8 each either way; below 2^-126 of the row's largest weight they may count as zero).  Rows that come out
+ * non-finite are computed once more, key by key, which is exact about what a row sees but takes some tens of times as long.
  * Rows above n_nodes[b] are left as they were in out and lse.  out and lse overlap no input.  R * heads_q / heads is at most 2^24.
  */
 #define CADD_ATTENTION_TILED_PATH 1u   /* small calls too take the kernel that large ones take (results agree to rounding; for measurements and tests) */

@@ -29,18 +29,6 @@ __device__ __forceinline__ int attn_live(const AttnParams& p, int b) {
 __device__ __forceinline__ int attn_depth(const AttnParams& p, int b, int r) {
     return p.depth ? min(max(p.depth[(int64_t)b * p.R + r], 0), 1 << 20) : r;
 }
-// Does a row at place len + depth see cached place pos?
-__device__ __forceinline__ bool attn_sees_place(const AttnParams& p, int place, int pos) {
-    return p.window == 0 || pos < p.n_sinks || place - pos < p.window;
-}
-// Does tree row r see tree row c?
-__device__ __forceinline__ bool attn_sees_row(const AttnParams& p, int b, int len, int r, int dr, int c) {
-    const bool link = p.mask_bits ? (p.mask_bits[((int64_t)b * p.R + r) * p.mask_words + (c >> 5)] >> (c & 31)) & 1u : c <= r;
-    if (!link || p.window == 0) return link;
-    const int dc = attn_depth(p, b, c);
-    return dr - dc < p.window || len + dc < p.n_sinks;
-}
-
 // ---- one row at a time: a warp holds the row's query and sums, four (two) of the head's elements a lane ----
 template <int D> struct RowSums {
     float m, l, o[D / 32];
@@ -71,13 +59,7 @@ __device__ __forceinline__ void load_row_cache(const CacheView& c, const unsigne
     }
 }
 template <int D>
-__device__ __forceinline__ void row_add(RowSums<D>& st, const float (&q)[D / 32], const float (&k)[D / 32], const float (&v)[D / 32], float scale_log2) {
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) s = fmaf(q[i], k[i], s);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFullMask, s, o);
-    s *= scale_log2;
+__device__ __forceinline__ void row_add(RowSums<D>& st, float s, const float (&v)[D / 32]) {
     if (s == -INFINITY) return;
     const float m = fmaxf(st.m, s);                      // a NaN score leaves m and makes the sums NaN
     const float a = st.m == -INFINITY ? 0.0f : exp2f(st.m - m), e = exp2f(s - m);
@@ -86,25 +68,45 @@ __device__ __forceinline__ void row_add(RowSums<D>& st, const float (&q)[D / 32]
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) st.o[i] = fmaf(e, v[i], st.o[i] * a);
 }
-// Adds the keys [from, to) that row r sees: cached places, or (TREE) rows of the tree.
-template <int D, bool FP4, bool TREE>
-__device__ __noinline__ void row_attend(const AttnParams& p, int b, int h, int len, int r, const float (&q)[D / 32], int from, int to, RowSums<D>& st) {
-    const int lane = threadIdx.x & 31, dr = attn_depth(p, b, r);
-    float k[D / 32], v[D / 32];
-    for (int i = from; i < to; ++i) {
-        if constexpr (TREE) {
-            if (!attn_sees_row(p, b, len, r, dr, i)) continue;
-            const int64_t at = ((int64_t)b * p.kvs_b + (int64_t)i * p.kvs_row + (int64_t)h * p.kvs_head) * 2;
-            load_row_bf16<D>(p.k + at, lane, k);
-            load_row_bf16<D>(p.v + at, lane, v);
-        } else {
-            if (!attn_sees_place(p, len + dr, i)) continue;
-            const int64_t row = cache_row(p.c, b, h, i);
-            if (row < 0) continue;
-            load_row_cache<D, FP4>(p.c, p.c.k, p.c.ks, p.c.k_exp, row, lane, k);
-            load_row_cache<D, FP4>(p.c, p.c.v, p.c.vs, p.c.v_exp, row, lane, v);
+// Adds the keys of `see` (bits of the 32 from k0: cached places, or rows of the tree), as a warp: a lane looks up one key's row, and
+// four rows at a time are fetched and multiplied side by side.
+template <int D, bool FP4>
+__device__ __forceinline__ void row_attend(const AttnParams& p, bool tree, int b, int h, uint32_t see, const float (&q)[D / 32], int k0, RowSums<D>& st) {
+    constexpr int kAtOnce = 4;
+    const int lane = threadIdx.x & 31;
+    int64_t row = -1;                                    // cache row, or row of the tree
+    if ((see >> lane) & 1u) row = tree ? k0 + lane : cache_row(p.c, b, h, k0 + lane);
+    const int64_t kv0 = (int64_t)b * p.kvs_b + (int64_t)h * p.kvs_head;
+    for (unsigned todo = __ballot_sync(kFullMask, row >= 0); todo;) {
+        const int n = min(__popc(todo), kAtOnce);
+        float k[kAtOnce][D / 32], v[kAtOnce][D / 32], s[kAtOnce];
+        int src = 0;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (todo) src = __ffs(todo) - 1;             // past the end: the last key once more, not added
+            todo &= todo - 1;
+            const int64_t r = __shfl_sync(kFullMask, row, src);
+            if (tree) {
+                load_row_bf16<D>(p.k + (kv0 + r * p.kvs_row) * 2, lane, k[j]);
+                load_row_bf16<D>(p.v + (kv0 + r * p.kvs_row) * 2, lane, v[j]);
+            } else {
+                load_row_cache<D, FP4>(p.c, p.c.k, p.c.ks, p.c.k_exp, r, lane, k[j]);
+                load_row_cache<D, FP4>(p.c, p.c.v, p.c.vs, p.c.v_exp, r, lane, v[j]);
+            }
         }
-        row_add<D>(st, q, k, v, p.scale_log2);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            s[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) s[j] = fmaf(q[i], k[j][i], s[j]);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) s[j] += __shfl_xor_sync(kFullMask, s[j], o);
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (j < n) row_add<D>(st, s[j] * p.scale_log2, v[j]);
     }
 }
 

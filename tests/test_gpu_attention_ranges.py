@@ -92,6 +92,26 @@ def time_of(call):
     return a.elapsed_time(b)
 
 
+@pytest.mark.parametrize("fp4,R", [(False, 4), (True, 4), (True, 40)])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_rows_with_results_that_are_not_finite_are_walked_once(fp4, R, value):
+    """A value row of Inf or NaN that all rows see.  Bound: the 16 rows of a block go once through 8192 places, shared out over 8 warps,
+    at no more than 1 us a key and warp (a look-up, a row and five exchanges one after the other): 16 * 8232 / 8 us."""
+    p = problem(fp4=fp4, batch=1, heads=1, group=4, lens=[8192], R=R, live=[R], page=64)
+    p.v[0, 0] = value
+    c = p.cache(G)
+    q, k, v, mask, depth = (x.to(DEV) for x in (p.q, p.k, p.v, p.mask_bits(), p.depth))
+    out = G.Attention(out=torch.zeros(1, R, 4, 128, dtype=torch.bfloat16, device=DEV), lse=torch.zeros(1, R, 4, device=DEV))
+    ws = torch.zeros(G.cadd_tree_attention_workspace_bytes(1, R, 4, c), dtype=torch.uint8, device=DEV)
+    ms = time_of(lambda: G.cadd_tree_attention(q, k, v, c, mask_bits=mask, depth=depth, out=out, workspace=ws))
+    if value == math.inf:
+        assert bool((out.out == math.inf).all())
+    else:
+        assert bool(torch.isnan(out.out).all())
+    assert bool(torch.isfinite(out.lse).all())
+    assert ms <= 16 * 8232 / 8 * 1e-3, ms
+
+
 @pytest.mark.parametrize("fp4,R", [(False, 4), (True, 4), (False, 50), (True, 50)])
 def test_single_elements_that_are_not_finite(fp4, R):
     """In a long cache: one element of a tree row's value is Inf and another NaN; everything else is what it was without them."""
