@@ -388,7 +388,8 @@ typedef struct cadd_read_args {
  *     tree row c:     bit c of mask_bits row r (mask_bits NULL: c <= r, the rows of a prompt chunk), and
  *                     window = 0, or depth[r] - depth[c] < window, or length + depth[c] < n_sinks.
  * One decoded token is R = 1.  A row that sees nothing (or only scores of -Inf) gets 0 and lse -Inf.  What a row does not
- * see has no influence on it, whatever it holds.  Products are bf16 with fp32 sums, the softmax is fp32, its weights are
+ * see has no influence on it, whatever it holds.  Products are of bf16 numbers with fp32 sums (of fp16 in small calls over a
+ * 4-bit cache, where that moves no score by more than 2^-20), the softmax is fp32, its weights are
  * rounded for the product with the values to bf16, or in small calls over a 4-bit cache to fp16 where that holds them (relative
  * error at most 2^-8 each either way; below 2^-126 of the row's largest weight they may count as zero).  Rows that come out
  * non-finite are computed once more, key by key, which is exact about what a row sees but takes some tens of times as long.

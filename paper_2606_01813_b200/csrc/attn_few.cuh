@@ -105,11 +105,16 @@ __global__ void __launch_bounds__(kFewThreads, 2) attn_few_kernel(const __grid_c
                 const float y = __shfl_xor_sync(kFullMask, amax, o);
                 amax = !(y <= amax) ? y : amax;
             }
-            const int e = min(half_row_exponent(amax), 126);
+            int e;
+            unsigned met = 0;
             sh.qb[m][ch] = x;
-            sh.qh[m][wkeys_slot<D, true>(ch)] = half_chunk(x, exp2i(-e));
+            sh.qh[m][wkeys_slot<D, true>(ch)] = half_row_chunk(x, amax, e, met);
+            const unsigned mine = ((1u << NB) - 1) << (lane & ~(NB - 1));          // the row's lanes
+            const unsigned rounded = __ballot_sync(kFullMask, met & kHalfRounded) & mine, unfit = __ballot_sync(kFullMask, met & kHalfUnfit) & mine;
             if (ch == 0) {
-                sh.scale[m] = p.scale_log2 * exp2i(-p.c.k_exp) * exp2i(e);
+                // a row lost to fp16: NaN, which sends it to the join's rows that are done key by key
+                const float scale = p.scale_log2 * exp2i(e - p.c.k_exp);
+                sh.scale[m] = half_row_lost(rounded, unfit, scale) ? __int_as_float(0x7fc00000) : scale;
                 sh.row_at[m] = make_int2(m < M ? r : 0, attn_depth(p, it.b, m < M ? r : 0));
             }
         }

@@ -210,11 +210,11 @@ constexpr int kRangeTimedOut = 2;    // a wait ran out
 // ---- rows done once more, key by key ----
 constexpr int kJoinRows = 16;                            // rows of an item that a CTA of the join takes
 // What a product of a weight 0 with a non-finite value that the row does not see has made NaN, and what the sums of large weights
-// have made infinite, is right when it is computed from the row's own keys alone.  A row goes once through its keys, 32 at a time
-// shared out over the warps of the CTA, whose sums are joined in warp order; elements that came out finite stay.  A row stops as
-// soon as every element asked for is NaN.  Measured on a B200: 16 rows over 8192 places, one row of Inf that all see, 5 ms (7 over
-// 4 bits); 65 rows and 32 heads of one request over 32k places 33 ms, where the call takes 0.76 ms without.  (A walk for each eight
-// elements of a row by one warp took 175 ms for the 16 rows.)
+// have made infinite, is right when it is computed from the row's own keys alone; so are rows that a kernel gave up (all NaN, lse
+// too).  A row goes once through its keys, 32 at a time shared out over the warps of the CTA, whose sums are joined in warp
+// order; elements that came out finite stay.  A row stops as soon as all that is asked for is NaN.  Measured on a B200: 16 rows
+// over 8192 places, one row of Inf that all see, 5 ms (7 over 4 bits); 65 rows and 32 heads of one request over 32k places 33 ms,
+// where the call takes 0.76 ms without.  (A walk for each eight elements of a row by one warp took 175 ms for the 16 rows.)
 template <int D, int T> struct RedoShared {
     uint32_t want[kJoinRows][D / 32];                    // elements asked for, as bits
     float o[T / 32][D];
@@ -237,6 +237,8 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, const WorkIter<BM>& 
         const int m0 = it.mb * BM + (int)blockIdx.y * kJoinRows + row, r = m0 / p.group, hq = it.h * p.group + (m0 - r * p.group);
         const int dr = attn_depth(p, it.b, r), d0 = lane * (D / 32);
         const uint32_t mine = sh.want[row][d0 >> 5] >> (d0 & 31);                  // of the lane's D / 32 elements
+        float* lse = p.lse ? p.lse + ((int64_t)it.b * p.R + r) * p.heads_q + hq : nullptr;
+        const bool want_lse = lse && *lse != *lse;
         if (tid == 0) sh.stop = 0;
         __syncthreads();
         float q[D / 32];
@@ -252,7 +254,7 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, const WorkIter<BM>& 
             const uint32_t see = attn_key_bits(p, tree, it.b, it.len, it.live, r, dr, k0);
             if (!see) continue;
             row_attend<D, FP4>(p, tree, it.b, it.h, see, q, k0, st);
-            bool number = false;                         // an element asked for that is not NaN so far
+            bool number = want_lse && st.l == st.l;      // something asked for is not NaN so far
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) number |= ((mine >> i) & 1u) && st.o[i] == st.o[i];
             if (!__any_sync(kFullMask, number) && lane == 0) *(volatile int*)&sh.stop = 1;
@@ -268,6 +270,7 @@ __device__ __noinline__ void redo_rows(const AttnParams& p, const WorkIter<BM>& 
         const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (int k = 0; k < T / 32; ++k) l = fmaf(exp2f(sh.ml[k].x - ref), sh.ml[k].y, l);
+        if (want_lse && tid == 0) *lse = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
         for (int d = tid; d < D; d += T) {
             if (!((sh.want[row][d >> 5] >> (d & 31)) & 1u)) continue;
             float o = 0.0f;

@@ -77,42 +77,54 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
     for (int m0 = 0; m0 == 0 || m0 < rows; m0 += kWRows) {
         const int here = min(rows - m0, kWRows), tiles = (here + 15) >> 4;
         if (m0) __syncthreads();
-        // a row's D / 8 chunks by as many neighbouring lanes
-        for (int i = tid; i < tiles * 16 * (D / 8); i += kWThreads) {
-            const int m = i / (D / 8), ch = i - m * (D / 8), li = (m0 + m) / p.group, hq = h * p.group + (m0 + m - li * p.group);
-            const int r = m < here ? row_at(p.rows, b, li) : -1;
-            const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
-            const bool out = fabsf(lse) == INFINITY;
-            uint4 x = make_uint4(0, 0, 0, 0);            // a row that adds nothing: zeros, whatever it holds
-            if (!out) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
-            float scale = p.scale_log2;
-            if constexpr (FP4) {
-                float amax = chunk_amax(x);
+        // a row's D / 8 chunks by as many neighbouring lanes; true: a row is lost to fp16 (then once more, all of them as bf16)
+        auto stage = [&](bool wide) -> bool {
+            bool lost = false;
+            for (int i = tid; i < tiles * 16 * (D / 8); i += kWThreads) {
+                const int m = i / (D / 8), ch = i - m * (D / 8), li = (m0 + m) / p.group, hq = h * p.group + (m0 + m - li * p.group);
+                const int r = m < here ? row_at(p.rows, b, li) : -1;
+                const float lse = r >= 0 ? p.lse[((int64_t)b * p.rows.R + r) * p.heads_q + hq] : INFINITY;
+                const bool out = fabsf(lse) == INFINITY;
+                uint4 x = make_uint4(0, 0, 0, 0);        // a row that adds nothing: zeros, whatever it holds
+                if (!out) x = __ldg((const uint4*)(p.q + ((int64_t)b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)hq * p.qs_head) * 2) + ch);
+                float scale = p.scale_log2;
+                if constexpr (FP4) {
+                    float amax = chunk_amax(x);
 #pragma unroll
-                for (int o = D / 16; o; o >>= 1) {       // (the loop's trip count is the same for all lanes of a row)
-                    const float y = __shfl_xor_sync(kFullMask, amax, o);
-                    amax = !(y <= amax) ? y : amax;
+                    for (int o = D / 16; o; o >>= 1) {   // (the loop's trip count is the same for all lanes of a row)
+                        const float y = __shfl_xor_sync(kFullMask, amax, o);
+                        amax = !(y <= amax) ? y : amax;
+                    }
+                    int e = 0;
+                    unsigned met = 0;
+                    if (!wide) x = half_row_chunk(x, amax, e, met);
+                    scale *= exp2i(e - p.c.k_exp);
+                    const unsigned mine = ((1u << (D / 8)) - 1) << (lane & ~(D / 8 - 1));      // the row's lanes
+                    const unsigned rounded = __ballot_sync(kFullMask, met & kHalfRounded) & mine, unfit = __ballot_sync(kFullMask, met & kHalfUnfit) & mine;
+                    lost |= half_row_lost(rounded, unfit, scale);
                 }
-                const int e = half_row_exponent(amax);
-                x = half_chunk(x, exp2i(e == 127 ? -126 : -e));
-                scale *= exp2i(-p.c.k_exp) * exp2i(e == 127 ? 126 : e);
+                sh.q[m][wkeys_slot<D, FP4>(ch)] = x;
+                if (ch == 0) {
+                    sh.lse[m] = out ? INFINITY : lse * kLog2e;
+                    sh.scale[m] = scale;
+                    sh.place[m] = base + li;
+                }
             }
-            sh.q[m][wkeys_slot<D, FP4>(ch)] = x;
-            if (ch == 0) {
-                sh.lse[m] = out ? INFINITY : lse * kLog2e;
-                sh.scale[m] = scale;
-                sh.place[m] = base + li;
-            }
-        }
-        __syncthreads();
-        WKeys<D, FP4> x[4];
-        int64_t row[4];
-        int k0 = begin + warp * 32;
-        auto exist_bits = [&]() -> unsigned {             // bit j: this lane's key of group j exists
-            unsigned e = 0;
+            return __syncthreads_or(lost);
+        };
+        const bool wide = stage(false);
+        if (FP4 && wide) stage(true);
+        // (a loop for rows in fp16 and one for rows in bf16: a choice inside the loop, 232 us where this takes 201)
+        auto cached = [&](auto wide_tag) {
+            constexpr bool kHalf = FP4 && !decltype(wide_tag)::value;
+            WKeys<D, FP4> x[4];
+            int64_t row[4];
+            int k0 = begin + warp * 32;
+            auto exist_bits = [&]() -> unsigned {             // bit j: this lane's key of group j exists
+                unsigned e = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e |= row[j] >= 0 ? 1u << j : 0u;
-            return e;
+                for (int j = 0; j < 4; ++j) e |= row[j] >= 0 ? 1u << j : 0u;
+                return e;
         };
         int page[4];
         wkeys_pages(p.c, b, k0, g, end, page);
@@ -142,6 +154,12 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                     kf[j][4 * i] = v.x; kf[j][4 * i + 1] = v.y; kf[j][4 * i + 2] = v.z; kf[j][4 * i + 3] = v.w;
                 }
             }
+            if constexpr (FP4 && !kHalf) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < W * 4; ++i) kf[j][i] = bf16_of_half(kf[j][i]);
+            }
             wkeys_rows(p.c, h, k0 + kWThreads, g, end, page, row);
 #pragma unroll
             for (int j = 0; j < 4; ++j) wkeys_load<D, FP4>(x[j], p.c, row[j], t);            // the next keys
@@ -158,8 +176,8 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
                         const uint4 lo = sh.q[mt * 16 + g][i * 4 + t], hi = sh.q[mt * 16 + g + 8][i * 4 + t];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            mma_16x8x16<FP4>(c[j], lo.x, hi.x, lo.y, hi.y, kf[j][4 * i], kf[j][4 * i + 1]);
-                            mma_16x8x16<FP4>(c[j], lo.z, hi.z, lo.w, hi.w, kf[j][4 * i + 2], kf[j][4 * i + 3]);
+                            mma_16x8x16<kHalf>(c[j], lo.x, hi.x, lo.y, hi.y, kf[j][4 * i], kf[j][4 * i + 1]);
+                            mma_16x8x16<kHalf>(c[j], lo.z, hi.z, lo.w, hi.w, kf[j][4 * i + 2], kf[j][4 * i + 3]);
                         }
                     }
 #pragma unroll
@@ -205,6 +223,13 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
             const unsigned known = __shfl_sync(kFullMask, there, (mine & 7) * 4);
             if (!((known >> (mine >> 3)) & 1u)) v = 0.0f;                          // on no page: nothing to be seen
             if (key < end) w_out[key] = before + v;
+        }
+        };
+        if constexpr (FP4) {
+            if (!wide) cached(Flag<false>{});
+            else cached(Flag<true>{});
+        } else {
+            cached(Flag<false>{});
         }
         if (rows <= kWRows) break;
     }

@@ -5,9 +5,11 @@
 // bf16's fields (logic instructions issue every second cycle; measured on a B200).  code * scale has at most six significant
 // bits and lies in [2^-10, 2688]: exact in fp16.
 //
-// The other factor, queries, comes as bf16, whose range fp16 does not have.  A row of queries is therefore divided by the power
-// of two that brings its largest element into [1, 2) (half_row_exponent), which its scores are multiplied by again: elements down
-// to 2^-14 of the largest stay exact, smaller ones are off by at most 2^-25 of the largest.
+// The other factor, queries, comes as bf16, whose range fp16 does not have.  A row of queries is therefore multiplied by the power
+// of two that brings its largest element into [2^14, 2^15) (half_row_exponent), and its scores by the inverse: bf16's eight bits
+// then fit fp16 exactly down to 2^-31 of the largest element.  Smaller ones are rounded, by at most 2^-25; where that could move a
+// score by more than 2^-20 of a power of two, or the largest element is beyond 2^54, the row is lost to fp16 (half_row_lost) and
+// goes another way: slower, and not rounded.
 #pragma once
 #include <cuda_fp16.h>
 #include "common.cuh"
@@ -143,21 +145,45 @@ __device__ __forceinline__ void fp4_half_scales(uint32_t two_bytes, uint32_t& f0
     f0 = __byte_perm(t, 0, 0x1010);
     f1 = __byte_perm(t, 0, 0x3232);
 }
-// Exponent of the largest magnitude of a row; 0 for a row of zeros or one with non-finite elements (which stay what they are).
+// The power of two that a row with this largest magnitude is divided by for fp16; 0 for a row of zeros or one with non-finite elements
+// (which stay what they are).
 __device__ __forceinline__ int half_row_exponent(float amax) {
     const int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
-    return e < -126 || e > 127 ? 0 : e;
+    return e < -126 || e > 127 ? 0 : e - 14;
 }
+constexpr int kHalfMaxExponent = 40;                     // scale * 2^(e - k_exp) stays a normal fp32 number
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// Eight bf16 elements times 2^-e as fp16.
-__device__ __forceinline__ uint4 half_chunk(const uint4& x, float down) {
+// What a chunk meets on its way to fp16.
+constexpr unsigned kHalfRounded = 1;                     // an element rounded, by at most 2^-25
+constexpr unsigned kHalfUnfit = 2;                       // one that does not fit, or NaN
+// Eight elements of a row with largest magnitude `amax`, times 2^-e as fp16; e is chosen here.
+__device__ __forceinline__ uint4 half_row_chunk(const uint4& x, float amax, int& e, unsigned& met) {
+    const int want = half_row_exponent(amax);
+    e = min(max(want, -kHalfMaxExponent), kHalfMaxExponent);
+    if (want > e) met |= kHalfUnfit;
+    const float down = exp2i(-e);
     float f[8];
     Elem<CADD_DTYPE_BF16>::unpack(x, f);
-    return make_uint4(pack_half(f[0] * down, f[1] * down), pack_half(f[2] * down, f[3] * down), pack_half(f[4] * down, f[5] * down), pack_half(f[6] * down, f[7] * down));
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[i] = pack_half(f[2 * i] * down, f[2 * i + 1] * down);
+        const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float was = f[2 * i + j] * down, is = j ? back.y : back.x;
+            if (was != is) met |= fabsf(was - is) <= 0x1p-25f ? kHalfRounded : kHalfUnfit;
+        }
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+// Is a row lost to fp16?  `rounded`, `unfit`: its chunks that met either; `scale`: of its scores.  Values of keys are at most 2688.
+__device__ __forceinline__ bool half_row_lost(unsigned rounded, unsigned unfit, float scale) {
+    return unfit || (float)(__popc(rounded) * 8) * (2688.0f * 0x1p-25f) * scale > 0x1p-20f;
 }
 __device__ __forceinline__ float chunk_amax(const uint4& x) {
     float f[8], m = 0.0f;

@@ -14,6 +14,9 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// A truth value as a type, for loops that exist once for either value.
+template <bool B> struct Flag { static constexpr bool value = B; };
+
 template <int D, bool FP4> struct WKeys;                 // eight keys' rows as a lane holds them
 template <int D> struct WKeys<D, true> { uint32_t w[D / 32]; uint32_t s; };
 template <int D> struct WKeys<D, false> { uint4 w[D / 32]; };

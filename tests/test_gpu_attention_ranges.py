@@ -55,6 +55,36 @@ def test_one_key_far_above_the_rest_whose_value_is_zero(fp4, flags, dim, gap, at
     check_attention(p, p.run(G, flags=flags))
 
 
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("power", [12, 16, 20, 30, 33, 60, 100, -100])
+@pytest.mark.parametrize("every", [True, False])
+def test_queries_with_an_element_far_above_the_others(flags, dim, power, every):
+    """Keys are zero at that element, so the scores are the other elements', which have to keep their bits."""
+    p = problem(fp4=True, dim=dim, lens=[400, 90], R=3, live=[3, 3], group=4, seed=5)
+    for b in range(2):
+        k = p.K[b].clone()
+        k[:, :, 5] = 0.0
+        store(p, 0, b, k)
+    p.k[..., 5] = 0.0
+    rows = slice(None) if every else slice(1, 2)
+    p.q[:, rows, :, 5] = 1.5 * 2.0 ** power
+    if power < 0:
+        p.q[:, rows] = p.q[:, rows, :, 5:6] * (1 + torch.arange(dim) % 3)
+    check_attention(p, p.run(G, flags=flags))
+
+
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** 40])
+def test_small_and_large_scales(flags, scale):
+    """Queries make up for the scale; a row of the smallest normal numbers has scores of nearly zero."""
+    p = problem(fp4=True, lens=[75, 40], R=3, live=[3, 3], group=4, seed=9, scale=scale, k_exp=16, v_exp=0)
+    p.q = (p.q.double() / scale * 128 ** -0.5 * 2.0 ** 16).bfloat16()
+    p.q[0, 1] = 2.0 ** -126
+    p.k = (p.k.double() * 2.0 ** -16).bfloat16()
+    check_attention(p, p.run(G, flags=flags))
+
+
 LONG = [(False, 0, 16), (False, 0, 64), (True, 0, 16), (True, 0, 64), (True, G.ATTENTION_TILED_PATH, 64)]
 
 
@@ -129,3 +159,20 @@ def test_single_elements_that_are_not_finite(fp4, R):
     assert bool((got[0, :, :2, 17] == math.inf).all()) and bool(torch.isnan(got[0, sees][:, 2:, 90]).all()) and bool((got[0, sees][:, :2, 0] == -math.inf).all())
     err = (got[0] - want).abs()[~odd]
     assert bool((err <= 2.0 ** -6 * amass[~odd] + 1e-6).all())
+
+
+def test_rows_lost_to_fp16_whose_results_are_not_finite():
+    """Queries that the few-rows kernel cannot hold in fp16, over values of NaN that all or some of a row's elements get: lse, and the
+    other elements, are still the row's."""
+    p = problem(fp4=True, lens=[300, 70], R=2, live=[2, 2], group=2, heads=1)
+    p.q[..., 9] = 2.0 ** -70
+    wants = [p.attention(b) for b in range(2)]
+    root = p.v[:, 0].clone()
+    p.v[0, 0], p.v[1, 0, 0, 3] = math.nan, math.nan
+    got = p.run(G)
+    assert bool(torch.isnan(got.out[0]).all()) and bool(torch.isnan(got.out[1, :, :, 3]).all())
+    p.v[:, 0] = root
+    out = got.out.cpu()
+    for b, at in ((0, slice(None)), (1, slice(3, 4))):
+        out[b, ..., at] = wants[b][0][..., at].bfloat16()
+    check_attention(p, G.Attention(out=out, lse=got.lse))

@@ -588,6 +588,27 @@ def test_rows_of_a_pool_of_more_than_four_gigabytes():
 # ---- what is stored, byte by byte; queries and shapes out of the ordinary ----
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("power", [12, 20, 30, 33, 60, 100, -100])
+@pytest.mark.parametrize("path_lens", [[4, 0], [60, 3]])
+def test_weights_of_queries_with_an_element_far_above_the_others(dim, power, path_lens):
+    """Keys are zero at that element: the scores are the other elements', which have to keep their bits."""
+    base = [300, 70]
+    p, path, path_lens, base, rows, lse, w, *_ = weights_case(fp4=True, dim=dim, group=4, R=70, base=base, path_lens=path_lens)
+    for b in range(2):
+        k = p.K[b].clone()
+        k[:, :, 5] = 0.0
+        codes, scales = encode(k)
+        p.put(0, b, 0, codes)
+        p.put(2, b, 0, scales)
+        p.K[b] = decode(codes, scales)
+        p.q[b, rows[b][::2], :, 5] = 1.5 * 2.0 ** power
+        for i, r in enumerate(rows[b]):
+            for h in range(p.heads * p.group):
+                lse[b, r, h] = torch.logsumexp(p.K[b][:base[b] + i + 1, h // p.group] @ p.q[b, r, h].double() * p.scale, 0)
+    check_weights((p, path, path_lens, base, rows, lse, w, 0, 0))
+
+
 @pytest.mark.parametrize("fp4", [False, True])
 @pytest.mark.parametrize("page,window", [(16, 0), (64, 0), (64, 5000)])
 def test_weights_of_warps_that_go_through_many_steps(fp4, page, window):
