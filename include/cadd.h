@@ -309,11 +309,12 @@ typedef struct cadd_fit_args {
  * pages that are only read.
  *   CADD_CACHE_BF16  k, v: bf16, head_dim elements a row.
  *   CADD_CACHE_FP4   k, v: e2m1 codes, two to a byte (the even element in the low four bits), head_dim / 2 bytes a row;
- *                    k_scale, v_scale: one e4m3 scale (never negative) for 16 elements along the row, head_dim / 16 bytes.
+ *                    k_scale, v_scale: one e4m3 scale (bytes 0 to 0x7e: neither negative nor NaN) for 16 elements along the
+ *                    row, head_dim / 16 bytes.
  *                    An element stands for  code * scale * 2^-k_exp  (2^-v_exp for values).  Stored is, of x * 2^k_exp:
  *                    scale = e4m3(max|x| / 6) over the 16, code = e2m1(x / scale), both to nearest even and saturating;
- *                    a zero scale has zero codes; NaN is stored as zero.  The exponents, -16..16, move a model's values
- *                    into e4m3's range (blocks whose largest value is below 2^-9 lose precision otherwise).
+ *                    zero is code 0, never -0, and a zero scale has zero codes; NaN is stored as zero.  The exponents, -16..16,
+ *                    move a model's values into e4m3's range (blocks whose largest value is below 2^-9 lose precision otherwise).
  * Unused slots and pages are never read.
  */
 #define CADD_CACHE_BF16 0

@@ -35,6 +35,10 @@ __device__ __forceinline__ uint32_t e4m3_byte(float x) {
     return r & 0xffu;
 }
 
+// Zero has one code: where the conversion keeps the sign of a small negative number, 8, the sign is taken off.  (Seven added to a
+// nibble's three low bits carries into its high bit where they are not zero, and never beyond.)
+__device__ __forceinline__ uint32_t e2m1_one_zero(uint32_t w) { return w & (((w & 0x77777777u) + 0x77777777u) | 0x77777777u); }
+
 // 16 bf16 elements times `up` (a power of two) -> 8 code bytes and a scale byte: scale = e4m3(amax / 6), code = e2m1(x / scale).
 //
 // What makes the codes those of exact arithmetic: x has 8 significant bits, the scale 4, a point half way between two codes 3.
@@ -57,7 +61,7 @@ __device__ __noinline__ uint2 fp4_encode_slow(const uint4 w0, const uint4 w1, fl
         b = b == b ? b : 0.0f;
         w[i >> 3] |= e2m1_byte(a, b) << ((i & 7) * 4);
     }
-    return make_uint2(w[0], w[1]);
+    return make_uint2(e2m1_one_zero(w[0]), e2m1_one_zero(w[1]));
 }
 __device__ __forceinline__ uint2 fp4_encode(const uint4& w0, const uint4& w1, float up, uint32_t& scale_byte) {
     const uint32_t in[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
@@ -75,7 +79,7 @@ __device__ __forceinline__ uint2 fp4_encode(const uint4& w0, const uint4& w1, fl
         const float qa = a * r, qb = b * r;
         w[i >> 2] |= e2m1_byte(fmaf(fmaf(-qa, s, a), r, qa), fmaf(fmaf(-qb, s, b), r, qb)) << ((i & 3) * 8);
     }
-    return make_uint2(w[0], w[1]);
+    return make_uint2(e2m1_one_zero(w[0]), e2m1_one_zero(w[1]));
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

@@ -587,6 +587,28 @@ def test_rows_of_a_pool_of_more_than_four_gigabytes():
 
 # ---- what is stored, byte by byte; queries and shapes out of the ordinary ----
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("exps", [(0, 0), (4, -3), (-16, 16)])
+def test_append_stores_the_bytes_of_the_definition(dim, exps):
+    """Zero has one code, 0, under a zero scale and under any other."""
+    p = problem(fp4=True, dim=dim, lens=[0, 0], R=48, live=[48, 48], k_exp=exps[0], v_exp=exps[1], page=8)
+    for b in range(2):
+        for x in (p.k, p.v):
+            x[b, :10] = awkward_rows(10, 2, dim, p.g)
+            x[b, 10] = -x[b, 10].abs() * 2.0 ** -40                        # blocks of tiny negative numbers
+            x[b, 11] = -0.0
+            x[b, 12] = torch.where(torch.arange(dim) % 16 == 3, 1.0, -2.0 ** -9).bfloat16()
+            x[b, 13] = -x[b, 13].abs()
+    c = p.cache(G)
+    G.cadd_cache_append(c, p.k.to(DEV), p.v.to(DEV))
+    for src, pool, scale, exp in ((p.k, c.k, c.k_scale, exps[0]), (p.v, c.v, c.v_scale, exps[1])):
+        codes, scales = encode(src.double(), exp)
+        for b in range(2):
+            for i in range(48):
+                page, slot = int(p.block_table[b, i // 8]), i % 8
+                assert torch.equal(scale[page, :, slot].cpu(), scales[b, i]), (b, i)
+                assert torch.equal(pool[page, :, slot].cpu(), codes[b, i]), (b, i)
+
 
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("power", [12, 20, 30, 33, 60, 100, -100])
