@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kWThreads, D == 128 ? 3 : 4) weights_kernel(co
             uint32_t kf[4][W * 4];                       // the 32 keys as operands: [key group of 8][word][two steps x two registers]
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t f0 = 0, f1 = 0;
+                [[maybe_unused]] uint32_t f0 = 0, f1 = 0;
                 if constexpr (FP4) fp4_half_scales(x[j].s, f0, f1);
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
