@@ -63,7 +63,8 @@ extern "C" {
 #define CADD_STATUS_BAD_LENGTH        1024   /* cache: length / base_length / start / count / n_rows / path_len was out of range and was clamped */
 #define CADD_STATUS_CACHE_FULL        2048   /* cache append: the request's pages could not hold every row; those beyond were dropped */
 #define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out (in append its place counts and keeps what it held) */
-#define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax */
+#define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax,
+                                                attention leaves NaN in out and lse of the rows concerned and sets the bit for every request of the call */
 
 #define CADD_DTYPE_BF16 0
 #define CADD_DTYPE_FP32 1
@@ -99,7 +100,9 @@ extern "C" {
    kernel never issues the asynchronous copy of the second tile (16 KB) of each row it reads (the first, if the row has
    only one), and its wait for that one tile gives up after a few tries.  Nothing hangs and nothing faults: the call
    exercises the library's bounded-wait exit (copies already in flight are waited for, then the CTA leaves) and every
-   request reports CADD_STATUS_INTERNAL_TIMEOUT with the empty tree (build) or accepted_len 0 (verify).  For tests only. */
+   request reports CADD_STATUS_INTERNAL_TIMEOUT with the empty tree (build) or accepted_len 0 (verify).  For tests only.
+   cadd_tree_attention takes it too: in its tiled kernel the keys of each CTA's second unit (its first, if its first item has
+   only one there) are never announced, and every wait gives up after some 16 ms. */
 #define CADD_FLAG_TEST_DROP_TILE  0x80000000u
 
 #define CADD_ROWS_LIVE  0        /* verify reads target rows 0..n_nodes[b] only */
@@ -399,7 +402,7 @@ typedef struct cadd_read_args {
 #define CADD_ATTENTION_TILED_PATH 1u   /* small calls too take the kernel that large ones take (results agree to rounding; for measurements and tests) */
 typedef struct cadd_attention_args {
     uint32_t struct_size;          /* = sizeof(cadd_attention_args) */
-    uint32_t flags;                /* 0, or CADD_ATTENTION_TILED_PATH */
+    uint32_t flags;                /* 0, CADD_ATTENTION_TILED_PATH, CADD_FLAG_TEST_DROP_TILE */
     int32_t  R;                    /* row capacity, 1..65536 */
     int32_t  heads_q;              /* a multiple of cache.heads */
     int32_t  window;               /* 0: none */

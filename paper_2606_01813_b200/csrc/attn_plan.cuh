@@ -289,10 +289,17 @@ __device__ __forceinline__ unsigned not_finite(const float (&x)[8]) {
     return bad;
 }
 
+// Eight elements of a row whose range gave up on a wait: NaN, and its lse.
+__device__ __forceinline__ void give_up_row(const AttnParams& p, int b, int r, int hq, int dc) {
+    *(uint4*)(p.out + ((int64_t)b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2) =
+        make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+    if (p.lse && dc == 0) p.lse[((int64_t)b * p.R + r) * p.heads_q + hq] = __int_as_float(0x7fffffff);
+}
+
 // The join.  blockIdx.x is a range: the one in which a shared item begins (its sums are record 1 there) joins it, blockIdx.y takes
 // 16 of its rows.  Threads first find the ranges that share the item, then the rows' maxima over them, 16 ranges at a time; then
 // a thread adds up eight elements of one row, in range order.  Rows whose joined result, or whose result in a whole item of
-// a range that met non-finite numbers, is not finite are done once more.
+// a range that met non-finite numbers, is not finite are done once more.  Rows of items in which a range gave up on a wait get NaN.
 template <int BM, int D, bool FP4>
 __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __grid_constant__ AttnWork w, int grid) {
     constexpr int T = kJoinRows * D / 8, kPer = T / kJoinRows;                     // threads; ranges looked at in one go
@@ -318,13 +325,17 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
     const int4 mine = w.items[c0];
     if (mine.w & kRangeEmpty) return;
     const int dc = tid % (D / 8), row = blockIdx.y * kJoinRows + tid / (D / 8);    // a row's chunks in neighbouring lanes
-    if (w.odd[c0] & kRangeOdd) {                                                   // the range's whole items
+    if (w.odd[c0]) {                                                               // the range's whole items
         WorkIter<BM> it;
         if (it.init(p, plan, c0, grid)) {
             do {
                 if (!it.whole()) continue;
                 const int m0 = it.mb * BM + row, r = m0 / p.group, hq = it.h * p.group + (m0 - r * p.group);
                 unsigned bad = 0;
+                if (w.odd[c0] & kRangeTimedOut) {
+                    if (m0 < it.live * p.group) give_up_row(p, it.b, r, hq, dc);
+                    continue;
+                }
                 if (m0 < it.live * p.group) {
                     const uint4 x = *(const uint4*)(p.out + ((int64_t)it.b * p.os_b + (int64_t)r * p.os_row + (int64_t)hq * p.os_head + dc * 8) * 2);
                     float f[8];
@@ -361,7 +372,7 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
         for (int k = 0; k < tid >> 5; ++k) at += found[k];
         if (in) {
             list[at] = i;
-            if (w.odd[i]) any_odd = 1;
+            if (w.odd[i]) atomicOr(&any_odd, w.odd[i]);
         }
         const bool last = __syncthreads_or(behind);
         if (tid == 0)
@@ -369,7 +380,7 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
         __syncthreads();
         if (last) break;
     }
-    const int n = count, odd = any_odd, rec = record_floats<BM, D>();
+    const int n = count, odd = any_odd & kRangeOdd, rec = record_floats<BM, D>();
     auto record = [&](int i) -> const float* { return w.records + ((int64_t)list[i] * 2 + (i == 0 ? 1 : 0)) * rec; };
     const int lr = tid % kJoinRows, li = tid / kJoinRows, grow = blockIdx.y * kJoinRows + lr;
     float mx = -INFINITY;
@@ -381,6 +392,10 @@ __global__ void __launch_bounds__(kJoinRows * D / 8) attn_join_kernel(const __gr
     for (int i = 0; i < kPer; ++i) M = fmaxf(M, part[i][tid / (D / 8)]);
     const int m0 = mb * BM + row, r = m0 / p.group, hq = h * p.group + (m0 - r * p.group);
     const bool there = m0 < live * p.group;
+    if (any_odd & kRangeTimedOut) {
+        if (there) give_up_row(p, b, r, hq, dc);
+        return;
+    }
     unsigned bad = 0;
     if (there) {
         const float ref = M == -INFINITY ? 0.0f : M;

@@ -46,6 +46,7 @@ namespace cadd {
 constexpr int kTileBM = 128;
 constexpr int kTileThreads = 288;
 constexpr int kTileTmemCols = 256;
+constexpr int kTileWaitLimit = 1 << 19, kTileTestWaitLimit = 1 << 12;     // tries of a wait, 3.9 us each (measured): 2 s, 16 ms
 constexpr float kTileSlack = 40.0f;                      // log2 of how far weights may exceed 1 before m is raised
 
 template <int D> struct alignas(1024) TileShared {
@@ -68,8 +69,8 @@ __device__ __forceinline__ bool tile_try(uint64_t* bar, unsigned parity) {
     return ok != 0;
 }
 template <class Shared>
-__device__ __forceinline__ bool tile_wait(Shared& sh, uint64_t* bar, unsigned parity) {
-    for (int it = 0; it < (1 << 22); ++it) {
+__device__ __forceinline__ bool tile_wait(Shared& sh, uint64_t* bar, unsigned parity, int limit) {
+    for (int it = 0; it < limit; ++it) {
         if (tile_try(bar, parity)) return true;
         if (*(volatile uint32_t*)&sh.error) return false;
     }
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
         w.items[blockIdx.x] = make_int4(it.b, it.h, it.mb, (it.u0 > 0 ? kRangeInside : 0) | (it.u1 == it.n_units ? kRangeEnds : 0));
         mbar_init(&sh.q_full, 4);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.k_full[i], 2);
+            mbar_init(&sh.k_full[i], p.test_drop && i == min(it.u1 - it.u0 - 1, 1) ? 3 : 2);       // test hook: an arrival that never comes
             mbar_init(&sh.v_full[i], 2);
             mbar_init(&sh.s_full[i], 1);
             mbar_init(&sh.p_ready[i], 4);
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
         unsigned n = 0, items = 0;
         bool ok = true;
         auto output = [&](unsigned i, bool first) {       // O (+)= P V of unit i
-            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.p_ready[i & 1], (i >> 1) & 1) && tile_wait(sh, &sh.v_full[i & 1], (i >> 1) & 1)))) return;
+            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.p_ready[i & 1], (i >> 1) & 1, p.wait_limit) && tile_wait(sh, &sh.v_full[i & 1], (i >> 1) & 1, p.wait_limit)))) return;
             tc_fence_after();
             const uint64_t dv = umma_desc_mn_sw128(sh.v[i & 1], 0, kUnit * 128);
             const uint32_t pm = tm_s + (i & 1) * kUnit;
@@ -326,7 +327,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
             umma_commit_one(one, &sh.pv_done[i & 1]);
         };
         do {
-            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.q_full, items & 1)))) break;
+            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.q_full, items & 1, p.wait_limit)))) break;
             ++items;
             // The scores of a unit take the place of the weights of the unit two before, right behind the product that reads those:
             // products of one kind and accumulator type run in the order in which they are issued.
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
                 if (n >= first + 2) output(n - 2, n == first + 2);
                 if (!ok) break;
                 if (n < end) {
-                    ok = __all_sync(kFullMask, tile_wait(sh, &sh.k_full[n & 1], (n >> 1) & 1));
+                    ok = __all_sync(kFullMask, tile_wait(sh, &sh.k_full[n & 1], (n >> 1) & 1, p.wait_limit));
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t dq = umma_desc_k_sw128(sh.q, 0), dk = umma_desc_k_sw128(sh.k[n & 1], 0);
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
                 const int m0 = it.mb * kTileBM + (tid - 128), r = m0 / p.group, g = m0 - r * p.group;
                 const uint4* src = (const uint4*)(p.q + ((int64_t)it.b * p.qs_b + (int64_t)r * p.qs_row + (int64_t)(it.h * p.group + g) * p.qs_head) * 2);
                 const bool live = r < it.live;
-                if (n > 0) ok = tile_wait(sh, &sh.s_full[(n - 1) & 1], ((n - 1) >> 1) & 1);
+                if (n > 0) ok = tile_wait(sh, &sh.s_full[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_limit);
                 if (!(ok = __all_sync(kFullMask, ok))) break;
 #pragma unroll 4
                 for (int ch = 0; ch < kCh; ++ch) {
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
                 const bool tree = it.is_tree(u), more = u + 1 < it.u1;
                 unsigned char* tile = values ? sh.v[n & 1] : sh.k[n & 1];
                 const uint32_t there = __ballot_sync(kFullMask, row >= 0);
-                if (n >= 2) ok = tile_wait(sh, &freed[n & 1], ((n >> 1) - 1) & 1);
+                if (n >= 2) ok = tile_wait(sh, &freed[n & 1], ((n >> 1) - 1) & 1, p.wait_limit);
                 if (!(ok = __all_sync(kFullMask, ok))) break;
                 if (!values && lane == 0) sh.key_bits[n & 3][warp & 1] = there;
                 int64_t next_row = -1;
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
             const int dr = attn_depth(p, it.b, r);
             float m = -INFINITY, l = 0.0f;
             for (int u = it.u0; u < it.u1; ++u, ++n) {
-                ok = __all_sync(kFullMask, tile_wait(sh, &sh.s_full[n & 1], (n >> 1) & 1));
+                ok = __all_sync(kFullMask, tile_wait(sh, &sh.s_full[n & 1], (n >> 1) & 1, p.wait_limit));
                 if (!ok) break;
                 tc_fence_after();
                 if (warp_live) {
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
                         m = mn;
                         l *= a;
                         if (u > it.u0) {                  // the product before must be done with O
-                            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1));
+                            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_limit));
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll 1
@@ -518,7 +519,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
             }
             if (!ok) break;
             // ---- epilogue ----
-            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1));
+            ok = __all_sync(kFullMask, tile_wait(sh, &sh.pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_limit));
             if (!ok) break;
             tc_fence_after();
             if (warp_live && tile_finish<D, FP4>(w, it, to, live, r, hq, m, l)) sh.odd = 1;

@@ -251,12 +251,14 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     p.R = a->R; p.heads_q = a->heads_q; p.group = a->heads_q / a->cache.heads; p.window = a->window; p.n_sinks = a->n_sinks;
     p.mask_words = (a->R + 31) / 32;
     p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    p.test_drop = (a->flags & CADD_FLAG_TEST_DROP_TILE) ? 1 : 0;
+    p.wait_limit = p.test_drop ? kTileTestWaitLimit : kTileWaitLimit;
     AttnWork w;
     w.p = p;
     w.items = (int4*)a->workspace;
     w.odd = (int*)(w.items + kMaxGrid);
     w.records = (float*)((unsigned char*)a->workspace + kItemsBytes);
-    const bool tiled = (a->flags & CADD_ATTENTION_TILED_PATH) != 0;
+    const bool tiled = (a->flags & (CADD_ATTENTION_TILED_PATH | CADD_FLAG_TEST_DROP_TILE)) != 0;
     if (p.c.head_dim == 128) return p.c.fp4 ? launch_tree_attention<128, true>(w, tiled, st) : launch_tree_attention<128, false>(w, tiled, st);
     return p.c.fp4 ? launch_tree_attention<64, true>(w, tiled, st) : launch_tree_attention<64, false>(w, tiled, st);
 }

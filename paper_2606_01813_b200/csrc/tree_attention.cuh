@@ -19,6 +19,7 @@ struct AttnParams {
     float* lse;
     int32_t* status;
     int R, heads_q, group, window, n_sinks, mask_words, item_cost;
+    int test_drop, wait_limit;                           // of attn_tiles.cuh: a unit never comes; tries of a wait
     float scale_log2;                                    // scale * log2(e): scores are kept in units of log 2
 };
 

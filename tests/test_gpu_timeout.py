@@ -9,6 +9,7 @@ import torch
 from oracle import cadd_oracle as O
 from paper_2606_01813_b200 import binding as G
 from paper_2606_01813_b200 import synth
+from cache_util import Problem, check_attention
 from parity_util import compare_build, compare_verify, to_cpu
 
 pytestmark = pytest.mark.gpu
@@ -79,3 +80,25 @@ def test_row_sample_wait_runs_out(rows_mode):
     torch.cuda.synchronize()
     assert int(to_cpu(good.status).max()) == 0 and int(to_cpu(good.node_argmax).max()) >= 0
     assert torch.equal(good.node_argmax, again.node_argmax) and torch.equal(good.accepted_len, again.accepted_len)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens,heads,R", [([70, 33], 2, 5), ([70, 33], 2, 90), ([0, 0], 1, 3), ([9000, 5000], 8, 40)])
+def test_tree_attention_wait_runs_out(fp4, dim, lens, heads, R):
+    """One unit to a range, some, and many: the call returns, says so, and leaves NaN in the live rows; the next one is right."""
+    p = Problem(batch=2, heads=heads, group=2, dim=dim, page=64, fp4=fp4, lens=lens, R=R, live=[R, R - 1], causal=False, seed=4)
+    out = G.Attention(out=torch.full((2, R, heads * 2, dim), 3.0, dtype=torch.bfloat16, device="cuda"), lse=torch.full((2, R, heads * 2), 3.0, device="cuda"),
+                      status=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    bad = p.run(G, flags=G.FLAG_TEST_DROP_TILE, out=out)
+    torch.cuda.synchronize()
+    assert bad.status.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2
+    for b in range(2):
+        n = p.live[b]
+        assert bool(torch.isnan(bad.out[b, :n]).all()) and bool(torch.isnan(bad.lse[b, :n]).all())
+        assert bool((bad.out[b, n:] == 3.0).all()) and bool((bad.lse[b, n:] == 3.0).all())
+    if max(lens) < 1000:
+        check_attention(p, p.run(G, flags=G.ATTENTION_TILED_PATH))
+    good, again = p.run(G), p.run(G)
+    assert good.status.tolist() == [0, 0] and torch.equal(good.out, again.out) and torch.equal(good.lse, again.lse)
+    assert bool(torch.isfinite(good.out).all())
