@@ -318,7 +318,8 @@ typedef struct cadd_fit_args {
  *                    scale = e4m3(max|x| / 6) over the 16, code = e2m1(x / scale), both to nearest even and saturating;
  *                    zero is code 0, never -0, and a zero scale has zero codes; NaN is stored as zero.  The exponents, -16..16,
  *                    move a model's values into e4m3's range (blocks whose largest value is below 2^-9 lose precision otherwise).
- * Unused slots and pages are never read.
+ * Unused slots and pages are never read (but for row 0 of the pools, whose contents then do not matter, where a table entry
+ * in use is outside the pool).
  */
 #define CADD_CACHE_BF16 0
 #define CADD_CACHE_FP4  1
