@@ -408,7 +408,7 @@ typedef struct cadd_attention_args {
     int32_t  heads_q;              /* a multiple of cache.heads */
     int32_t  window;               /* 0: none */
     int32_t  n_sinks;              /* 0..2^30 */
-    float    scale;                /* > 0 */
+    float    scale;                /* 2^-64 .. 2^64 */
     int32_t  reserved0;
     const void* q;                 /* bf16 [batch, R, heads_q, head_dim]; strides in elements, multiples of 8; 16-byte aligned */
     int64_t  q_stride_b, q_stride_row, q_stride_head;
@@ -443,7 +443,7 @@ typedef struct cadd_weights_args {
     uint32_t flags;                /* reserved, 0 */
     int32_t  R, L, heads_q;
     int32_t  window, n_sinks;
-    float    scale;                /* > 0 */
+    float    scale;                /* 2^-64 .. 2^64 */
     const void* q;                 /* as in cadd_attention_args */
     int64_t  q_stride_b, q_stride_row, q_stride_head;
     const float* lse;              /* [batch, R, heads_q] */

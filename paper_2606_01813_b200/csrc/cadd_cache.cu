@@ -1,7 +1,6 @@
 // Host side of the cache and tree-attention calls of the C ABI (cadd.h): argument checks, grids, launches.  No allocation,
 // no synchronisation, no state kept between calls.
 #include <cuda_runtime.h>
-#include <math.h>
 #include <stdint.h>
 
 #include "cadd.h"
@@ -58,6 +57,8 @@ static int check_strides(int64_t b, int64_t row, int64_t head) {
     if (b < 0 || row < 0 || head < 0 || b >= ((int64_t)1 << 50) || row >= ((int64_t)1 << 40) || head >= ((int64_t)1 << 40)) return CADD_ERR_SHAPE;
     return (b % 8 || row % 8 || head % 8) ? CADD_ERR_ALIGN : CADD_OK;
 }
+// Beyond these the scores' factors, scale * 2^(what the 4-bit form leaves), leave fp32's range, and a masked score times 0 is NaN.
+static bool scale_in_range(float scale) { return scale >= 0x1p-64f && scale <= 0x1p64f; }
 static int launched() {
     return cudaGetLastError() == cudaSuccess ? CADD_OK : CADD_ERR_LAUNCH;
 }
@@ -227,7 +228,7 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     if (rc != CADD_OK) return rc;
     rc = check_cache(&a->cache);
     if (rc != CADD_OK) return rc;
-    if (a->window < 0 || a->n_sinks < 0 || a->n_sinks > (1 << 30) || !(a->scale > 0.0f) || !isfinite(a->scale)) return CADD_ERR_SHAPE;
+    if (a->window < 0 || a->n_sinks < 0 || a->n_sinks > (1 << 30) || !scale_in_range(a->scale)) return CADD_ERR_SHAPE;
     if (!a->q || !a->k || !a->v || !a->out) return CADD_ERR_NULL;
     if (a->mask_bits && a->window && !a->depth) return CADD_ERR_NULL;
     if ((rc = check_strides(a->q_stride_b, a->q_stride_row, a->q_stride_head)) != CADD_OK ||
@@ -273,7 +274,7 @@ int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream) {
     if (a->R < 1 || a->R > 65536 || (a->path && (a->L < 1 || a->L > 65536)) || a->heads_q < 1 || a->heads_q > 65536 || a->heads_q % a->cache.heads)
         return CADD_ERR_SHAPE;
     if (((int64_t)(a->path ? a->L + 1 : a->R) * (a->heads_q / a->cache.heads)) > ((int64_t)1 << 24)) return CADD_ERR_SHAPE;
-    if (a->window < 0 || a->n_sinks < 0 || a->n_sinks > (1 << 30) || !(a->scale > 0.0f) || !isfinite(a->scale)) return CADD_ERR_SHAPE;
+    if (a->window < 0 || a->n_sinks < 0 || a->n_sinks > (1 << 30) || !scale_in_range(a->scale)) return CADD_ERR_SHAPE;
     const int64_t cap = (int64_t)a->cache.max_pages * a->cache.page_size;
     if (a->weights_stride < cap || a->weights_stride >= ((int64_t)1 << 36)) return CADD_ERR_SHAPE;
     if (!a->q || !a->lse || !a->base_length || !a->weights || !a->weights_out || (a->path && !a->path_len)) return CADD_ERR_NULL;

@@ -154,3 +154,11 @@ def test_the_plain_four_bit_form():
     codes, scales = encode(y)
     s = E4M3[scales.long()].repeat_interleave(16, -1)
     assert bool(((decode(codes, scales) - y).abs() <= s * (1 + 6 * 2.0 ** -4)).all())
+
+
+@pytest.mark.parametrize("name", ["attention", "weights"])
+@pytest.mark.parametrize("scale", [1e-45, 2.0 ** -65, 2.0 ** 65, 3e38])
+def test_scales_out_of_range_are_refused(lib, name, scale):
+    a = CALLS[name]()
+    a.scale = scale
+    assert getattr(lib, NAMES[name])(C.byref(a), None) == G.ERR_SHAPE
