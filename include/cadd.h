@@ -378,7 +378,7 @@ typedef struct cadd_read_args {
     const int32_t* count;          /* [batch], NULL => up to length; at most n_max and length - start are read */
     void*    k;                    /* out: bf16 [batch, n_max, heads, head_dim], last axis contiguous, 16-byte aligned */
     void*    v;
-    int64_t  stride_b, stride_row, stride_head;      /* of k and of v, in elements, multiples of 8 */
+    int64_t  stride_b, stride_row, stride_head;      /* of k and of v, in elements, multiples of 8; at least head_dim along an axis longer than one */
     int32_t* status;               /* [batch], may be NULL */
     cadd_cache cache;
 } cadd_read_args;
@@ -420,7 +420,7 @@ typedef struct cadd_attention_args {
     const uint32_t* mask_bits;     /* [batch, R, ceil(R/32)] as from cadd_build_tree, or NULL */
     const int32_t* depth;          /* [batch, R]; NULL => the row's number (allowed where mask_bits is NULL or window is 0) */
     void*    out;                  /* bf16 [batch, R, heads_q, head_dim] */
-    int64_t  out_stride_b, out_stride_row, out_stride_head;
+    int64_t  out_stride_b, out_stride_row, out_stride_head;   /* at least head_dim along an axis longer than one */
     float*   lse;                  /* [batch, R, heads_q], natural logarithm; may be NULL */
     int32_t* status;               /* [batch], may be NULL */
     void*    workspace;            /* >= cadd_tree_attention_workspace_bytes, 256-byte aligned */

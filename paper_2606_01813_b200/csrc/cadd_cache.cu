@@ -57,6 +57,12 @@ static int check_strides(int64_t b, int64_t row, int64_t head) {
     if (b < 0 || row < 0 || head < 0 || b >= ((int64_t)1 << 50) || row >= ((int64_t)1 << 40) || head >= ((int64_t)1 << 40)) return CADD_ERR_SHAPE;
     return (b % 8 || row % 8 || head % 8) ? CADD_ERR_ALIGN : CADD_OK;
 }
+// The same of an output: along an axis longer than one, rows must not lie in one another.
+static int check_out_strides(int64_t b, int64_t row, int64_t head, const cadd_cache* c, int64_t rows, int64_t heads) {
+    const int rc = check_strides(b, row, head);
+    if (rc != CADD_OK) return rc;
+    return (c->batch > 1 && b < c->head_dim) || (rows > 1 && row < c->head_dim) || (heads > 1 && head < c->head_dim) ? CADD_ERR_SHAPE : CADD_OK;
+}
 // Beyond these the scores' factors, scale * 2^(what the 4-bit form leaves), leave fp32's range, and a masked score times 0 is NaN.
 static bool scale_in_range(float scale) { return scale >= 0x1p-64f && scale <= 0x1p64f; }
 static int launched() {
@@ -183,7 +189,7 @@ int cadd_cache_read(const cadd_read_args* a, void* cuda_stream) {
     if (rc != CADD_OK) return rc;
     if (a->n_max < 1 || a->n_max > (1 << 30)) return CADD_ERR_SHAPE;
     if (!a->k || !a->v) return CADD_ERR_NULL;
-    rc = check_strides(a->stride_b, a->stride_row, a->stride_head);
+    rc = check_out_strides(a->stride_b, a->stride_row, a->stride_head, &a->cache, a->n_max, a->cache.heads);
     if (rc != CADD_OK) return rc;
     if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->start, 4) || !aligned(a->count, 4) || !aligned(a->status, 4)) return CADD_ERR_ALIGN;
     cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -233,7 +239,7 @@ int cadd_tree_attention(const cadd_attention_args* a, void* cuda_stream) {
     if (a->mask_bits && a->window && !a->depth) return CADD_ERR_NULL;
     if ((rc = check_strides(a->q_stride_b, a->q_stride_row, a->q_stride_head)) != CADD_OK ||
         (rc = check_strides(a->kv_stride_b, a->kv_stride_row, a->kv_stride_head)) != CADD_OK ||
-        (rc = check_strides(a->out_stride_b, a->out_stride_row, a->out_stride_head)) != CADD_OK)
+        (rc = check_out_strides(a->out_stride_b, a->out_stride_row, a->out_stride_head, &a->cache, a->R, a->heads_q)) != CADD_OK)
         return rc;
     if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->out, 16) || !aligned(a->n_nodes, 4) ||
         !aligned(a->mask_bits, 4) || !aligned(a->depth, 4) || !aligned(a->lse, 4) || !aligned(a->status, 4))

@@ -162,3 +162,12 @@ def test_scales_out_of_range_are_refused(lib, name, scale):
     a = CALLS[name]()
     a.scale = scale
     assert getattr(lib, NAMES[name])(C.byref(a), None) == G.ERR_SHAPE
+
+
+@pytest.mark.parametrize("name,fields", [("read", ("stride_b", "stride_row", "stride_head")), ("attention", ("out_stride_b", "out_stride_row", "out_stride_head"))])
+@pytest.mark.parametrize("axis", [0, 1, 2])
+@pytest.mark.parametrize("stride", [0, 64])
+def test_outputs_whose_rows_lie_in_one_another_are_refused(lib, name, fields, axis, stride):
+    a = CALLS[name]()
+    setattr(a, fields[axis], stride)
+    assert getattr(lib, NAMES[name])(C.byref(a), None) == G.ERR_SHAPE
