@@ -359,7 +359,7 @@ typedef struct cadd_append_args {
     const int32_t* n_rows;         /* [batch], NULL => R; ignored with path */
     const int32_t* path;           /* [batch, L] or NULL */
     const int32_t* path_len;       /* [batch], required with path */
-    int32_t* new_length;           /* [batch] out: length + rows written; may be cache.length itself */
+    int32_t* new_length;           /* [batch] out: length + rows written; may be cache.length itself, and no other input */
     int32_t* status;               /* [batch] CADD_STATUS_* bits, may be NULL */
     cadd_cache cache;
 } cadd_append_args;
@@ -367,7 +367,7 @@ typedef struct cadd_append_args {
 /*
  * Arguments of cadd_cache_read: places start[b] .. start[b]+count[b]-1 of the cache as bf16 rows (of a 4-bit cache: what
  * the codes stand for, which bf16 holds exactly).  Row i of the output is place start[b] + i; output rows from the number
- * of rows read on are left as they were.
+ * of rows read on are left as they were.  (A count above n_max is no error: n_max rows are read.)
  */
 typedef struct cadd_read_args {
     uint32_t struct_size;          /* = sizeof(cadd_read_args) */
@@ -418,7 +418,8 @@ typedef struct cadd_attention_args {
     const int32_t* n_nodes;        /* [batch] as from cadd_build_tree: rows 0..n_nodes[b] are live; NULL => R-1; -1: none.
                                       Outside [-1, R-1]: clamped, CADD_STATUS_BAD_N_NODES */
     const uint32_t* mask_bits;     /* [batch, R, ceil(R/32)] as from cadd_build_tree, or NULL */
-    const int32_t* depth;          /* [batch, R]; NULL => the row's number (allowed where mask_bits is NULL or window is 0) */
+    const int32_t* depth;          /* [batch, R], taken as 0 below 0 and as 2^20 above that; NULL => the row's number (allowed where
+                                      mask_bits is NULL or window is 0) */
     void*    out;                  /* bf16 [batch, R, heads_q, head_dim] */
     int64_t  out_stride_b, out_stride_row, out_stride_head;   /* at least head_dim along an axis longer than one */
     float*   lse;                  /* [batch, R, heads_q], natural logarithm; may be NULL */
@@ -464,6 +465,9 @@ typedef struct cadd_weights_args {
  * lowest).  The rows that stay are copied, in order, to the places 0, 1, ... of new pages (new_block_table), their weights
  * with them; the old pages stay as they are, for requests that share them.  A request with at most `budget` tokens keeps
  * all.  New pages must not be among the pages in use.
+ * After an eviction the places are no longer positions in the sequence: `window` and n_sinks of cadd_tree_attention and
+ * cadd_cache_weights then count places that stayed, head by head (the first n_sinks and the last window of them).  Keys keep what
+ * was stored, rotary positions among it.
  */
 typedef struct cadd_evict_args {
     uint32_t struct_size;          /* = sizeof(cadd_evict_args) */
@@ -540,7 +544,8 @@ int cadd_fit_cost_tables(const cadd_fit_args* a, void* cuda_stream);
 int cadd_cache_append(const cadd_append_args* a, void* cuda_stream);
 int cadd_cache_read(const cadd_read_args* a, void* cuda_stream);
 
-/* Scratch size of cadd_tree_attention: pure host arithmetic on R, heads_q and the cache's shape. */
+/* Scratch size of cadd_tree_attention: pure host arithmetic on the arguments, the same for every size of problem (some 34 MB at
+ * head dimension 64, 68 MB at 128), so a caller keeps one and gives it to every call on a stream. */
 int cadd_tree_attention_workspace_bytes(const cadd_attention_args* a, size_t* out);
 
 /* Attention of tree rows over the paged cache and the tree (see cadd_attention_args).  Asynchronous on `cuda_stream`:

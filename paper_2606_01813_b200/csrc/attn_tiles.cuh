@@ -98,12 +98,6 @@ __device__ __forceinline__ void umma_commit_one(uint32_t one, uint64_t* bar) {
                  "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%1];\n\t}"
                  ::"r"(one), "r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {       // whole warp: 32 lanes x 16 columns
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                 "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -318,7 +312,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) attn_tiles_kernel(const __gri
         unsigned n = 0, items = 0;
         bool ok = true;
         auto output = [&](unsigned i, bool first) {       // O (+)= P V of unit i
-            if (!(ok = __all_sync(kFullMask, tile_wait(sh, &sh.p_ready[i & 1], (i >> 1) & 1, p.wait_limit) && tile_wait(sh, &sh.v_full[i & 1], (i >> 1) & 1, p.wait_limit)))) return;
+            ok = tile_wait(sh, &sh.p_ready[i & 1], (i >> 1) & 1, p.wait_limit) && tile_wait(sh, &sh.v_full[i & 1], (i >> 1) & 1, p.wait_limit);
+            if (!(ok = __all_sync(kFullMask, ok))) return;
             tc_fence_after();
             const uint64_t dv = umma_desc_mn_sw128(sh.v[i & 1], 0, kUnit * 128);
             const uint32_t pm = tm_s + (i & 1) * kUnit;

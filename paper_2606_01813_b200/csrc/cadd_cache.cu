@@ -68,18 +68,17 @@ static bool scale_in_range(float scale) { return scale >= 0x1p-64f && scale <= 0
 static int launched() {
     return cudaGetLastError() == cudaSuccess ? CADD_OK : CADD_ERR_LAUNCH;
 }
-// CTAs for one of `groups` equal pieces of work of up to `items` thread items each: enough to fill the device a few times over.
-static int ctas_for(int64_t groups, int64_t items, int threads) {
-    int64_t need = (items + threads - 1) / threads, most = (148 * 32 + groups - 1) / groups;
-    if (need < 1) need = 1;
-    return (int)(need < most ? need : most);
-}
-
 static int sm_count() {
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 148;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
     return n;
+}
+// CTAs for one of `groups` equal pieces of work of up to `items` thread items each: enough to fill the device a few times over.
+static int ctas_for(int64_t groups, int64_t items, int threads) {
+    int64_t need = (items + threads - 1) / threads, most = ((int64_t)sm_count() * 32 + groups - 1) / groups;
+    if (need < 1) need = 1;
+    return (int)(need < most ? need : most);
 }
 
 constexpr int kMaxGrid = 512;                             // ranges at most (two CTAs on each SM are fewer)
@@ -116,8 +115,10 @@ static int launch_attention(void (*kernel)(AttnWork), AttnWork& w, int64_t ctas,
     }
     return CADD_OK;
 }
-// Up to 16 rows of a head over a 4-bit cache go to the kernel that walks the cache with registers (measured: see there), all else
-// to the one with tensor memory.
+// Up to 16 rows of a head (as many as the call has room for: live rows are not known here) over a 4-bit cache go to the kernel that
+// walks the cache with registers, all else to the one with tensor memory.  Measured on a B200, 4 query heads to each of 8 key
+// heads, this kernel / that one: 64 tokens over up to 8191 places 211 / 227 us, 16 over up to 32k 180 / 215, one over 32k 37 / 42,
+// 8 trees of 4 rows over up to 16k 68 / 80; scores so far apart that every step is in bf16, 16 over up to 32k, 197 / 216.
 template <int D, bool FP4>
 static int launch_tree_attention(AttnWork& w, bool tiled, cudaStream_t st) {
     if constexpr (FP4) {
@@ -129,11 +130,11 @@ static int launch_tree_attention(AttnWork& w, bool tiled, cudaStream_t st) {
 
 template <int D, bool FP4>
 static int launch_weights(WeightsParams& p, int64_t cap, cudaStream_t st) {
-    // Keys of a CTA: 2048 (32 requests of up to 32k tokens, before totals were fetched ahead: 236 us; 1024: 255, 4096: 248, 8192: 325), less where that would leave the
-    // device short of CTAs, 128 (32 a warp) at least.
-    const int64_t bh = (int64_t)p.c.batch * p.c.heads;
+    // Keys of a CTA: 2048 (32 requests of up to 32k tokens, measured while totals were not yet fetched ahead: 236 us; 1024: 255,
+    // 4096: 248, 8192: 325), less where that would leave the device short of CTAs, 128 (32 a warp) at least.
+    const int64_t bh = (int64_t)p.c.batch * p.c.heads, enough = 6 * (int64_t)sm_count();
     p.keys_per_cta = 2048;
-    while (p.keys_per_cta > 128 && bh * ((cap + p.keys_per_cta - 1) / p.keys_per_cta) < 6 * 148) p.keys_per_cta >>= 1;
+    while (p.keys_per_cta > 128 && bh * ((cap + p.keys_per_cta - 1) / p.keys_per_cta) < enough) p.keys_per_cta >>= 1;
     const int64_t per_head = (cap + p.keys_per_cta - 1) / p.keys_per_cta;
     if (bh * per_head >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
     p.ctas_per_head = (int)per_head;
