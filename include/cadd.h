@@ -396,7 +396,7 @@ typedef struct cadd_read_args {
  * see has no influence on it, whatever it holds.  Products are of bf16 numbers with fp32 sums (of fp16 in small calls over a
  * 4-bit cache, where that moves no score by more than 2^-20), the softmax is fp32, its weights are
  * rounded for the product with the values to bf16, or in small calls over a 4-bit cache to fp16 where that holds them (relative
- * error at most 2^-8 each either way; below 2^-126 of the row's largest weight they may count as zero).  Rows that come out
+ * error at most 2^-8 each either way; below 2^-80 of the row's largest weight they may count as zero).  Rows that come out
  * non-finite are computed once more, key by key, which is exact about what a row sees but takes some tens of times as long.
  * Rows above n_nodes[b] are left as they were in out and lse.  out and lse overlap no input.  R * heads_q / heads is at most 2^24.
  */
@@ -462,7 +462,7 @@ typedef struct cadd_weights_args {
 /*
  * Arguments of cadd_cache_evict: every (request, head) keeps at most `budget` of its places: the first n_sinks, the last
  * n_recent and, of the places between, those with the largest weights (equal weights: the lower place; NaN counts as the
- * lowest).  The rows that stay are copied, in order, to the places 0, 1, ... of new pages (new_block_table), their weights
+ * lowest, below -Inf).  The rows that stay are copied, in order, to the places 0, 1, ... of new pages (new_block_table), their weights
  * with them; the old pages stay as they are, for requests that share them.  A request with at most `budget` tokens keeps
  * all.  New pages must not be among the pages in use.
  * After an eviction the places are no longer positions in the sequence: `window` and n_sinks of cadd_tree_attention and

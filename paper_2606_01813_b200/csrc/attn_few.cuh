@@ -8,7 +8,12 @@
 // warps of a CTA work on different keys of the item, each with its own maximum, sum and output, joined in shared
 // memory at the item's end; keys are shared out over the CTAs as in attn_plan.cuh.  The next keys are on their way from the
 // moment the last are in their operands, the next values from the moment the last are multiplied.  Cached keys and values are
-// products in fp16 (fp4.cuh), the tree's rows in bf16.
+// multiplied in fp16 (fp4.cuh), the tree's rows in bf16.
+//
+// Measured on a B200, 8x4 heads of 128: 16 tokens over up to 32k places 180 us, 0.30 of the copy rate; 64 over up to 8191 places
+// 211 us, one over 32k 37.  Latency and issue bound it: 255 registers leave eight warps an SM with one step of 32 keys each on its
+// way; issue is active 43 % of the time, logic 36 %, tensor pipe 22 %, DRAM 25 %, and a warp waits 1.5 issue slots for its own last
+// instructions and 1.0 for memory for each one it issues.
 #pragma once
 #include "attn_plan.cuh"
 #include "warp_product.cuh"

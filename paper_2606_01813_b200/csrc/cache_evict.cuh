@@ -34,10 +34,11 @@ struct WeightsParams {
 // the same order (in fp16 for a 4-bit cache: fp4.cuh).  A warp takes 32 keys at a time, the next 32 being on their way; sums
 // over rows stay in registers and are joined across the lanes at the end, in a fixed order.  More than 128 rows are done in
 // groups, the later ones adding to what the earlier ones wrote.
-// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 201 us, 0.29 of the
-// measured copy rate.  Twelve warps an SM hide little (issue was active 40 % of the time at 245 us), so table entries and totals are
-// fetched a step before their use (245 -> 201 us; four CTAs an SM, with spills, came to 270).  By count: 190 instructions to dequantise a warp's 32 keys, and per
-// 16 rows 32 products, 16 exponentials a thread and their sums.
+// Measured on a B200 (32 requests of up to 32k places, 4 to 52 rows a head, 4 bits): 202 us, 0.29 of the measured copy rate (236
+// where every row is in bf16; bf16 cache: 360 us, 0.53, with 176 bytes of spills a thread, 4 bits 12).  Twelve warps an SM hide
+// little: table entries and totals are fetched a step before their use (245 -> 201 us; four CTAs an SM, with spills, came to
+// 270); issue is then active 50 % of the time, logic 33 %, tensor pipe 28 %, DRAM 20 %.  By count: 190 instructions to dequantise a
+// warp's 32 keys, and per 16 rows 32 products, 16 exponentials a thread and their sums.
 constexpr int kWThreads = 128;
 constexpr int kWRows = 128;                              // rows in shared memory at a time
 template <int D> struct alignas(16) WeightsShared {
