@@ -68,15 +68,17 @@ static bool scale_in_range(float scale) { return scale >= 0x1p-64f && scale <= 0
 static int launched() {
     return cudaGetLastError() == cudaSuccess ? CADD_OK : CADD_ERR_LAUNCH;
 }
+// Grids that only have to be large enough go by a B200's SMs without asking the device, which small calls would feel.
+constexpr int kSms = 148;
 static int sm_count() {
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return 148;
+    if (cudaGetDevice(&dev) != cudaSuccess) return kSms;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) return kSms;
     return n;
 }
 // CTAs for one of `groups` equal pieces of work of up to `items` thread items each: enough to fill the device a few times over.
 static int ctas_for(int64_t groups, int64_t items, int threads) {
-    int64_t need = (items + threads - 1) / threads, most = ((int64_t)sm_count() * 32 + groups - 1) / groups;
+    int64_t need = (items + threads - 1) / threads, most = (kSms * 32 + groups - 1) / groups;
     if (need < 1) need = 1;
     return (int)(need < most ? need : most);
 }
@@ -132,7 +134,7 @@ template <int D, bool FP4>
 static int launch_weights(WeightsParams& p, int64_t cap, cudaStream_t st) {
     // Keys of a CTA: 2048 (32 requests of up to 32k tokens, measured while totals were not yet fetched ahead: 236 us; 1024: 255,
     // 4096: 248, 8192: 325), less where that would leave the device short of CTAs, 128 (32 a warp) at least.
-    const int64_t bh = (int64_t)p.c.batch * p.c.heads, enough = 6 * (int64_t)sm_count();
+    const int64_t bh = (int64_t)p.c.batch * p.c.heads, enough = 6 * kSms;
     p.keys_per_cta = 2048;
     while (p.keys_per_cta > 128 && bh * ((cap + p.keys_per_cta - 1) / p.keys_per_cta) < enough) p.keys_per_cta >>= 1;
     const int64_t per_head = (cap + p.keys_per_cta - 1) / p.keys_per_cta;
