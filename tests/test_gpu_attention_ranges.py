@@ -176,3 +176,28 @@ def test_rows_lost_to_fp16_whose_results_are_not_finite():
     for b, at in ((0, slice(None)), (1, slice(3, 4))):
         out[b, ..., at] = wants[b][0][..., at].bfloat16()
     check_attention(p, G.Attention(out=out, lse=got.lse))
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("R,group", [(1, 4), (20, 4), (40, 7)])
+def test_non_finite_rows_in_ranges_of_many_items(fp4, dim, R, group):
+    """Hundreds of items of a few units each: a range goes through several whole ones and parts of others, some with elements that are not
+    finite, different ones in each."""
+    batch = 150
+    g = torch.Generator().manual_seed(R)
+    lens, live = torch.randint(0, 200, (batch,), generator=g).tolist(), torch.randint(1, R + 1, (batch,), generator=g).tolist()
+    p = problem(fp4=fp4, batch=batch, heads=4, dim=dim, group=group, lens=lens, R=R, live=live, page=64)
+    clean = p.run(G)
+    put = {}
+    for b in range(0, batch, 3):
+        h, d = int(torch.randint(0, 4, (), generator=g)), int(torch.randint(0, dim, (), generator=g))
+        value = (math.nan, math.inf, -math.inf)[b // 3 % 3]
+        put[b] = (h, d, value)
+        p.v[b, 0, h, d] = value
+    got = p.run(G)
+    assert torch.equal(got.lse, clean.lse)
+    want = clean.out.clone()
+    for b, (h, d, value) in put.items():
+        want[b, :live[b], h * group:(h + 1) * group, d] = value           # the root: every row sees it
+    assert torch.equal(torch.isnan(got.out), torch.isnan(want)) and torch.equal(torch.nan_to_num(got.out, nan=0.0), torch.nan_to_num(want, nan=0.0))
