@@ -60,11 +60,18 @@ extern "C" {
 #define CADD_STATUS_BAD_N_NODES         64   /* verify: n_nodes[b] was outside [0, R-1] and was clamped */
 #define CADD_STATUS_BAD_TABLE_IDX      256   /* build, CADD_COST_TABLE: table_idx[b] was outside [0, n_tables); the request returns the empty tree */
 #define CADD_STATUS_BAD_PAGE           512   /* cache: an entry of block_table in use was outside [0, n_pages); its tokens are neither read nor written */
-#define CADD_STATUS_BAD_LENGTH        1024   /* cache: length / base_length / start / count / n_rows / path_len was out of range and was clamped */
+#define CADD_STATUS_BAD_LENGTH        1024   /* cache, distill: length / base_length / start / count / n_rows / path_len was out of range and was clamped;
+                                                adjust: history_len / prompt_len */
 #define CADD_STATUS_CACHE_FULL        2048   /* cache append: the request's pages could not hold every row; those beyond were dropped */
-#define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out (in append its place counts and keeps what it held) */
+#define CADD_STATUS_BAD_PATH          4096   /* cache append / weights: path held a row outside [0, R); that row was left out (in append its place counts and keeps what it held);
+                                                distill: the same of a row outside [0, R); adjust: a live row's path had more than 64 nodes below its first, or a parent
+                                                that is the row itself or a later one: what lies above was left out */
+#define CADD_STATUS_BAD_MASK          8192   /* adjust: allowed_row held a number outside [-1, n_allowed); that row was not masked */
+#define CADD_STATUS_NOTHING_ALLOWED  16384   /* adjust: a row's mask allows no token; all its logits became -Inf */
+#define CADD_STATUS_BAD_TOKEN        32768   /* distill: teacher_token held a number outside [-1, V); that entry was left out */
 #define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax,
-                                                attention leaves NaN in out and lse of the rows concerned and sets the bit for every request of the call */
+                                                attention leaves NaN in out and lse of the rows concerned and sets the bit for every request of the call,
+                                                distill leaves NaN in loss, stats and grad of the rows concerned */
 
 #define CADD_DTYPE_BF16 0
 #define CADD_DTYPE_FP32 1
@@ -101,6 +108,7 @@ extern "C" {
    only one), and its wait for that one tile gives up after a few tries.  Nothing hangs and nothing faults: the call
    exercises the library's bounded-wait exit (copies already in flight are waited for, then the CTA leaves) and every
    request reports CADD_STATUS_INTERNAL_TIMEOUT with the empty tree (build) or accepted_len 0 (verify).  For tests only.
+   cadd_distill_loss and cadd_distill_grad take it too (each CTA's second tile of a row, or its first; NaN).
    cadd_tree_attention takes it too: in its tiled kernel the keys of each CTA's second unit (its first, if its first item has
    only one there) are never announced, and every wait gives up after some 16 ms. */
 #define CADD_FLAG_TEST_DROP_TILE  0x80000000u
@@ -486,6 +494,105 @@ typedef struct cadd_evict_args {
     cadd_cache cache;
 } cadd_evict_args;
 
+/*
+ * Arguments of cadd_adjust_logits: what a server does to the logits of a round before it verifies (or builds) on them.  The
+ * logits at row j of a request predict the token behind the request's history and row j's own path, so each row has its own
+ * context.  With n_out(v) = how often v stands in history[prompt_len .. history_len-1] and on the path of row j (the tokens of
+ * rows 0 .. j along parent_idx, row 0 and j included; negative ones are skipped), and n_all(v) = n_out(v) + how often it stands
+ * in the prompt, history[0 .. prompt_len-1], every live row gets
+ *     x = logits[v]
+ *     if n_all(v) > 0:   x = x > 0 ? x / repetition : x * repetition
+ *     if n_out(v) > 0:   x = x - frequency * n_out(v) - presence
+ *     x = x + every bias listed for v
+ *     x = -Inf           where the row's mask has bit v clear, whatever x is
+ * computed in 64 bits for tokens that penalties or biases concern and rounded once; all others keep their bits.  Tokens outside
+ * [0, V) in the history, on a path or in bias_token have no effect.  Rows above n_nodes[b] are left as they were in out.
+ * A row whose mask allows nothing becomes -Inf throughout (CADD_STATUS_NOTHING_ALLOWED); verification then takes token 0 there.
+ * Greedy and sampled verification and tree construction take the result as it is.
+ */
+typedef struct cadd_adjust_args {
+    uint32_t struct_size;          /* = sizeof(cadd_adjust_args) */
+    uint32_t flags;                /* reserved, 0 */
+    int32_t  batch, R;             /* requests, rows of each (nodes of a tree; 1: one decoded token; draft positions) */
+    int32_t  logits_dtype;         /* CADD_DTYPE_*, of out too */
+    int32_t  n_bias;               /* columns of bias_token and bias, 0..65536 */
+    int64_t  V;
+    const void* logits;            /* [batch, R, V]; element (b,j,v) at b*stride_b + j*stride_row + v */
+    int64_t  stride_b, stride_row; /* in elements, >= 0 */
+    void*    out;                  /* the same shape; may be logits with the same strides (in place: only what changes is written),
+                                      otherwise overlaps no input.  No two of its rows may overlap.  Fastest where the rows of logits and out
+                                      start equally far behind a 16-byte boundary */
+    int64_t  out_stride_b, out_stride_row;
+    const int32_t* n_nodes;        /* [batch]: rows 0..n_nodes[b] are live; NULL => R-1; -1: none.  Outside [-1, R-1]: clamped, CADD_STATUS_BAD_N_NODES */
+    const int32_t* token_ids;      /* [batch,R] from cadd_build_tree, NULL: no paths */
+    const int32_t* parent_idx;     /* [batch,R] from cadd_build_tree, required with token_ids */
+    const int32_t* history;        /* [batch, history_cols], rows history_stride apart; NULL: none.  What came before row 0's token */
+    int64_t  history_stride;       /* in elements, >= 0 */
+    int32_t  history_cols;         /* >= 1 with history */
+    int32_t  n_allowed;            /* rows of allowed, >= 1 with it */
+    const int32_t* history_len;    /* [batch], NULL => history_cols; clamped to [0, history_cols] */
+    const int32_t* prompt_len;     /* [batch], NULL => 0; clamped to [0, history_len] */
+    const float* repetition;       /* [batch], above 0; NULL => 1.  Where all three are NULL, history and paths are not read */
+    const float* presence;         /* [batch]; NULL => 0 */
+    const float* frequency;        /* [batch]; NULL => 0 */
+    const int32_t* bias_token;     /* [batch, n_bias], in any order, a token more than once gets the sum; negative: unused entry */
+    const float* bias;             /* [batch, n_bias] */
+    const uint32_t* allowed;       /* [n_allowed, ceil(V/32)] bit v % 32 of word v / 32: token v may follow; NULL: no masks */
+    const int32_t* allowed_row;    /* [batch,R] row of allowed for each row of the request, -1: no mask; rows may share one.  Required with allowed */
+    int32_t* status;               /* [batch] CADD_STATUS_* bits, may be NULL */
+} cadd_adjust_args;
+
+/*
+ * Arguments of cadd_distill_loss and cadd_distill_grad: the drafter learns from the target.  For position i of a request, with s
+ * the drafter's logits there, T the temperature, q = softmax(s / T), and the target's row r for that position (r = i; or, with
+ * path, r = 0 for i = 0 and r = path[b, i-1] above: a verification's accepted_nodes, whose logits the positions stand for):
+ *     p_k = softmax over the listed entries of teacher_logit[b,r,k] / T
+ *     loss[b,i] = weight[b,i] * sum_k p_k (log p_k - log q(teacher_token[b,r,k]))
+ * With CADD_DISTILL_REST the listed probabilities are the target's own and all other tokens together are one more class:
+ *     p_k = exp(teacher_logit[b,r,k] / T - teacher_lse[b,r]),  p_rest = max(0, 1 - sum_k p_k),  q_rest = sum of q over tokens not listed
+ *     loss[b,i] = weight[b,i] * (sum_k p_k (log p_k - log q_k) + p_rest (log p_rest - log q_rest))
+ * (teacher_lse = log sum_v exp(y_v / T) over the target's whole row y; NULL means 0: entries that are log-probabilities, T = 1.)
+ * Entries may be cadd_build_tree's lists (CADD_FLAG_EMIT_TOPK) as they are: token -1 is no entry; a token listed twice counts
+ * twice in p.  0 log 0 = 0.  Where q_rest is 0, a p_rest of at most 2^-20 counts as rounding of the list; a larger one gives +Inf.
+ * The gradient with respect to the logits, times the gradient g = grad_loss[b,i] of the loss (1 without grad_loss), is, with
+ * S = sum_k p_k (+ p_rest):
+ *     grad[b,i,v] = g * weight / T * (S q_v - sum of p_k over the entries of v),  for tokens not listed  g * weight / T * q_v (S - p_rest / q_rest)
+ * Left out are positions from path_len[b] + 1 (path) or n_rows[b] on, those with weight 0, and those whose entries have no
+ * token (without CADD_DISTILL_REST: no mass): loss 0, stats 0, gradient 0, whatever the logits hold.
+ * stats[b,i] = (m, Z, m', Z'): m the largest logit of the row, Z = sum_v exp((s_v - m) / T); m' and Z' the same over the tokens that
+ * are not listed (-Inf and 0 where there are none).  cadd_distill_grad reads them instead of passing over the logits twice.
+ * Logits of -Inf (and below -1e30) have probability 0; a row without any other gives NaN, as do NaN and +Inf in the logits or entries.
+ * Exponentials of the logits are fp32, their sums fp64, list and loss are fp64; the gradient is rounded once.
+ */
+#define CADD_DISTILL_REST 1u
+#define CADD_DISTILL_MAX_K 256
+typedef struct cadd_distill_args {
+    uint32_t struct_size;          /* = sizeof(cadd_distill_args) */
+    uint32_t flags;                /* 0, CADD_DISTILL_REST, CADD_FLAG_TEST_DROP_TILE */
+    int32_t  batch, L, R, K;       /* requests, drafter's positions, target's rows, entries of a list (1..CADD_DISTILL_MAX_K) */
+    int32_t  logits_dtype;         /* CADD_DTYPE_*, of grad too */
+    int32_t  path_cols;            /* columns of path */
+    int64_t  V;                    /* at most 800,000 (bf16) / 400,000 (fp32) */
+    double   temperature;          /* 2^-20 .. 2^20 */
+    const void* logits;            /* [batch, L, V]; element (b,i,v) at b*stride_b + i*stride_l + v */
+    int64_t  stride_b, stride_l;   /* in elements, >= 0 */
+    const int32_t* teacher_token;  /* [batch, R, K] */
+    const double*  teacher_logit;  /* [batch, R, K] logits or log-probabilities */
+    const double*  teacher_lse;    /* [batch, R], CADD_DISTILL_REST only; may be NULL */
+    const int32_t* path;           /* [batch, path_cols] or NULL (then R >= L) */
+    const int32_t* path_len;       /* [batch], required with path; clamped to [0, min(L-1, path_cols)] */
+    const int32_t* n_rows;         /* [batch] without path; NULL => L; clamped to [0, L] */
+    const float* weight;           /* [batch, L], NULL => 1 */
+    const float* grad_loss;        /* [batch, L], NULL => 1 */
+    float*   loss;                 /* [batch, L] out of cadd_distill_loss, may be NULL there; cadd_distill_grad ignores it */
+    float*   stats;                /* [batch, L, 4], 16-byte aligned: out of cadd_distill_loss, may be NULL there; required in cadd_distill_grad */
+    void*    grad;                 /* [batch, L, V] out; may be logits with the same strides, otherwise overlaps no input.  No two of its rows
+                                      may overlap.  cadd_distill_loss: NULL for the loss alone.  Fastest where its rows start as far behind a
+                                      16-byte boundary as those of logits */
+    int64_t  grad_stride_b, grad_stride_l;
+    int32_t* status;               /* [batch] CADD_STATUS_* bits, may be NULL */
+} cadd_distill_args;
+
 /* ABI version of the loaded library (CADD_ABI_VERSION it was built with). */
 int cadd_version(void);
 
@@ -559,6 +666,18 @@ int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream);
 /* Eviction by accumulated weight into new pages (see cadd_evict_args).  Asynchronous on `cuda_stream`: two kernels
  * (choice, copy; a third, tiny one where new_length is cache.length). */
 int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream);
+
+/* Penalties, biases and grammar masks on the logits of a tree's rows (see cadd_adjust_args).  Asynchronous on `cuda_stream`:
+ * one kernel (a second, small one where status is given).  The same inputs give the same bits. */
+int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream);
+
+/* Divergence of the drafter's distribution from the target's top tokens and, where `grad` is given, its gradient in the same pass
+ * (see cadd_distill_args).  Asynchronous on `cuda_stream`: one kernel (a second, small one before it where status is given).
+ * CADD_ERR_NULL if none of loss, stats and grad is given. */
+int cadd_distill_loss(const cadd_distill_args* a, void* cuda_stream);
+
+/* The gradient alone, from the stats of an earlier cadd_distill_loss on the same inputs.  Asynchronous on `cuda_stream`: as above. */
+int cadd_distill_grad(const cadd_distill_args* a, void* cuda_stream);
 
 /*
  * cadd_build_tree for callers that cannot provide scratch memory.  (The paper has no counterpart to

@@ -22,6 +22,8 @@ STATUS_NONFINITE_INPUT, STATUS_FEWER_THAN_K_FINITE, STATUS_CAP_HIT, STATUS_FRONT
 STATUS_L_EFF_CLAMPED, STATUS_COST_NONPOSITIVE, STATUS_BAD_N_NODES, STATUS_INTERNAL_TIMEOUT = 16, 32, 64, 128
 STATUS_BAD_TABLE_IDX = 256
 STATUS_BAD_PAGE, STATUS_BAD_LENGTH, STATUS_CACHE_FULL, STATUS_BAD_PATH = 512, 1024, 2048, 4096
+STATUS_BAD_MASK, STATUS_NOTHING_ALLOWED, STATUS_BAD_TOKEN = 8192, 16384, 32768
+DISTILL_REST, DISTILL_MAX_K = 1, 256
 CACHE_BF16, CACHE_FP4 = 0, 1
 ATTENTION_TILED_PATH = 1                          # small calls too take the kernel that large ones take
 DTYPE_BF16, DTYPE_FP32 = 0, 1
@@ -40,7 +42,7 @@ EXPORTS = ("cadd_version", "cadd_status_string", "cadd_build_workspace_bytes", "
            "cadd_head_workspace_bytes", "cadd_verify_tree_fused_head", "cadd_fit_cost_tables",
            "cadd_build_head_workspace_bytes", "cadd_build_tree_fused_head", "cadd_verify_tree_sampled",
            "cadd_cache_append", "cadd_cache_read", "cadd_tree_attention_workspace_bytes", "cadd_tree_attention",
-           "cadd_cache_weights", "cadd_cache_evict")
+           "cadd_cache_weights", "cadd_cache_evict", "cadd_adjust_logits", "cadd_distill_loss", "cadd_distill_grad")
 ERR_STATIC_SCRATCH = -8
 STATIC_SCRATCH_BYTES = 8 << 20
 
@@ -181,6 +183,32 @@ class EvictArgs(C.Structure):
     ]
 
 
+class AdjustArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("batch", C.c_int32), ("R", C.c_int32),
+        ("logits_dtype", C.c_int32), ("n_bias", C.c_int32), ("V", C.c_int64),
+        ("logits", C.c_void_p), ("stride_b", C.c_int64), ("stride_row", C.c_int64),
+        ("out", C.c_void_p), ("out_stride_b", C.c_int64), ("out_stride_row", C.c_int64),
+        ("n_nodes", C.c_void_p), ("token_ids", C.c_void_p), ("parent_idx", C.c_void_p),
+        ("history", C.c_void_p), ("history_stride", C.c_int64), ("history_cols", C.c_int32), ("n_allowed", C.c_int32),
+        ("history_len", C.c_void_p), ("prompt_len", C.c_void_p),
+        ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+        ("bias_token", C.c_void_p), ("bias", C.c_void_p), ("allowed", C.c_void_p), ("allowed_row", C.c_void_p), ("status", C.c_void_p),
+    ]
+
+
+class DistillArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("flags", C.c_uint32), ("batch", C.c_int32), ("L", C.c_int32), ("R", C.c_int32), ("K", C.c_int32),
+        ("logits_dtype", C.c_int32), ("path_cols", C.c_int32), ("V", C.c_int64), ("temperature", C.c_double),
+        ("logits", C.c_void_p), ("stride_b", C.c_int64), ("stride_l", C.c_int64),
+        ("teacher_token", C.c_void_p), ("teacher_logit", C.c_void_p), ("teacher_lse", C.c_void_p),
+        ("path", C.c_void_p), ("path_len", C.c_void_p), ("n_rows", C.c_void_p), ("weight", C.c_void_p), ("grad_loss", C.c_void_p),
+        ("loss", C.c_void_p), ("stats", C.c_void_p), ("grad", C.c_void_p), ("grad_stride_b", C.c_int64), ("grad_stride_l", C.c_int64),
+        ("status", C.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -214,6 +242,9 @@ def lib() -> C.CDLL:
         l.cadd_tree_attention.argtypes = [C.POINTER(AttentionArgs), C.c_void_p]
         l.cadd_cache_weights.argtypes = [C.POINTER(WeightsArgs), C.c_void_p]
         l.cadd_cache_evict.argtypes = [C.POINTER(EvictArgs), C.c_void_p]
+        l.cadd_adjust_logits.argtypes = [C.POINTER(AdjustArgs), C.c_void_p]
+        l.cadd_distill_loss.argtypes = [C.POINTER(DistillArgs), C.c_void_p]
+        l.cadd_distill_grad.argtypes = [C.POINTER(DistillArgs), C.c_void_p]
         _lib = l
     return _lib
 
@@ -964,3 +995,152 @@ def cadd_cache_evict(cache: KvCache, weights: torch.Tensor, new_block_table: tor
                   _need_i32(out.status, (B,), dev, "status"), cache.args)
     _enqueue(lib().cadd_cache_evict, a, dev, stream)
     return out
+
+
+# ---- the logits of a round: penalties, biases, masks; distillation ----
+
+def _need_logits(t: torch.Tensor, shape, dtype, dev, name: str):
+    """Pointer and (batch, row) strides of logits [batch, rows, V]."""
+    if t.dim() != 3 or t.dtype != dtype or t.device != dev or t.shape != shape or t.stride(2) != 1:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {dev} with a contiguous vocabulary axis")
+    # an axis of length one may carry any stride; it is never stepped along
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else 0
+
+
+def _need_like(t: Optional[torch.Tensor], dtype, shape, dev, name: str) -> Optional[int]:
+    """Pointer of a contiguous input or output of the given dtype and shape on the call's device (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _logits_of(t: torch.Tensor, name: str):
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a CUDA tensor (there is no CPU path)")
+    if t.dim() != 3 or t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must be [batch, rows, V] with a contiguous vocabulary axis")
+    return t.device, _dtype_code(t)
+
+
+def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, parent_idx=None, history=None, history_len=None,
+                       prompt_len=None, repetition=None, presence=None, frequency=None, bias_token=None, bias=None, allowed=None,
+                       allowed_row=None, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Penalties, biases and grammar masks on logits [batch, R, V] (bf16 or fp32), before cadd_verify_tree,
+    cadd_verify_tree_sampled or cadd_build_tree: each row by its own context, the history and, with token_ids / parent_idx
+    (and n_nodes) of cadd_build_tree, the row's path.  Works in place unless `out` is given; rows above n_nodes keep what `out` held.
+
+    history int32 [batch, n] (rows may be strided) with history_len and prompt_len int32 [batch]: what stands before row 0's token;
+    the first prompt_len tokens count for repetition alone.  repetition, presence, frequency fp32 [batch].  bias_token int32,
+    bias fp32 [batch, n_bias].  allowed int32 [n_masks, ceil(V / 32)] (bit v % 32 of word v / 32), allowed_row int32 [batch, R],
+    -1 for rows without a mask.  status int32 [batch]."""
+    dev, code = _logits_of(logits, "logits")
+    B, R, V = shape = logits.shape
+    lp, sb, sr = _need_logits(logits, shape, logits.dtype, dev, "logits")
+    if out is None or out is logits:
+        out, op, ob, orow = logits, lp, sb, sr
+    else:
+        op, ob, orow = _need_logits(out, shape, logits.dtype, dev, "out")
+    hp, hs, hc = None, 0, 0
+    if history is not None:
+        _need(history.dim() == 2 and history.shape[0] == B and history.dtype == torch.int32 and history.device == dev
+              and (history.shape[1] <= 1 or history.stride(1) == 1), "history must be an int32 tensor [batch, n] on the call's device with contiguous rows")
+        hc = history.shape[1]
+        hp, hs = (history.data_ptr(), history.stride(0) if B > 1 else 0) if hc else (None, 0)
+    else:
+        _need(history_len is None and prompt_len is None, "history_len and prompt_len come with history")
+    _need((bias_token is None) == (bias is None), "bias comes with bias_token")
+    _need((allowed is None) == (allowed_row is None), "allowed comes with allowed_row")
+    _need((token_ids is None) == (parent_idx is None), "token_ids comes with parent_idx")
+    n_bias, n_allowed, f32, i32 = 0, 0, torch.float32, torch.int32
+    if bias is not None:
+        _need(bias.dim() == 2, "bias must be [batch, n_bias]")
+        n_bias = bias.shape[1]
+    if allowed is not None:
+        _need(allowed.dim() == 2, "allowed must be [n_masks, ceil(V / 32)]")
+        n_allowed = allowed.shape[0]
+    a = AdjustArgs(C.sizeof(AdjustArgs), 0, B, R, code, n_bias, V, lp, sb, sr, op, ob, orow,
+                   _need_like(n_nodes, i32, (B,), dev, "n_nodes"), _need_like(token_ids, i32, (B, R), dev, "token_ids"),
+                   _need_like(parent_idx, i32, (B, R), dev, "parent_idx"), hp, hs, hc, n_allowed,
+                   _need_like(history_len, i32, (B,), dev, "history_len"), _need_like(prompt_len, i32, (B,), dev, "prompt_len"),
+                   _need_like(repetition, f32, (B,), dev, "repetition"), _need_like(presence, f32, (B,), dev, "presence"),
+                   _need_like(frequency, f32, (B,), dev, "frequency"), _need_like(bias_token, i32, (B, n_bias), dev, "bias_token"),
+                   _need_like(bias, f32, (B, n_bias), dev, "bias"), _need_like(allowed, i32, (n_allowed, (V + 31) // 32), dev, "allowed"),
+                   _need_like(allowed_row, i32, (B, R), dev, "allowed_row"), _need_like(status, i32, (B,), dev, "status"))
+    _enqueue(lib().cadd_adjust_logits, a, dev, stream)
+    return out
+
+
+@dataclass
+class Distilled:
+    """Outputs of cadd_distill_loss (device tensors): loss fp32 [batch, L], stats fp32 [batch, L, 4], grad like the logits and
+    status int32 [batch]; those that are None are not written."""
+    loss: Optional[torch.Tensor] = None
+    stats: Optional[torch.Tensor] = None
+    grad: Optional[torch.Tensor] = None
+    status: Optional[torch.Tensor] = None
+
+
+def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags):
+    dev, code = _logits_of(x, "draft_logits")
+    B, L, V = shape = x.shape
+    _need(teacher_token.dim() == 3 and teacher_token.shape[0] == B, "teacher_token must be [batch, R, K]")
+    R, K = teacher_token.shape[1:]
+    _need(teacher_lse is None or rest, "teacher_lse goes with rest")
+    f32, f64, i32, P = torch.float32, torch.float64, torch.int32, 0
+    if path is not None:
+        _need(path_len is not None and n_rows is None, "path comes with path_len and without n_rows")
+        _need(path.dim() == 2, "path must be [batch, columns]")
+        P = path.shape[1]
+    else:
+        _need(path_len is None, "path_len comes with path")
+    gp, gb, gl = (None, 0, 0) if out.grad is None else _need_logits(out.grad, shape, x.dtype, dev, "grad")
+    return dev, DistillArgs(
+        C.sizeof(DistillArgs), flags | (DISTILL_REST if rest else 0), B, L, R, K, code, P, V, float(temperature), *_need_logits(x, shape, x.dtype, dev, "draft_logits"),
+        _need_like(teacher_token, i32, (B, R, K), dev, "teacher_token"), _need_like(teacher_logit, f64, (B, R, K), dev, "teacher_logit"),
+        _need_like(teacher_lse, f64, (B, R), dev, "teacher_lse"), _need_like(path, i32, (B, P), dev, "path"), _need_like(path_len, i32, (B,), dev, "path_len"),
+        _need_like(n_rows, i32, (B,), dev, "n_rows"), _need_like(weight, f32, (B, L), dev, "weight"), _need_like(grad_loss, f32, (B, L), dev, "grad_loss"),
+        _need_like(out.loss, f32, (B, L), dev, "loss"), _need_like(out.stats, f32, (B, L, 4), dev, "stats"), gp, gb, gl, _need_like(out.status, i32, (B,), dev, "status"))
+
+
+def cadd_distill_loss(draft_logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, *, teacher_lse=None,
+                      rest: bool = False, temperature: float = 1.0, path=None, path_len=None, n_rows=None, weight=None, grad_loss=None,
+                      grad: bool = False, out: Optional[Distilled] = None, flags: int = 0,
+                      stream: Optional[torch.cuda.Stream] = None) -> Distilled:
+    """Distillation: the divergence of the drafter's distribution at each position of draft_logits [batch, L, V] from the
+    target's top tokens, teacher_token int32 and teacher_logit fp64 [batch, R, K] (cadd_build_tree's topk_token and topk_logprob fit),
+    and with `grad` (or out.grad, which may be draft_logits itself) the gradient of its sum in the same pass: go on with
+    draft_logits.backward(result.grad).  Position i learns from row i of the lists, with path / path_len (a verification's
+    accepted_nodes / accepted_len) from row 0, then from the accepted nodes, as far as they go.  `rest`: all tokens that are not
+    listed are one more class (teacher_logit are then log-probabilities, or logits with teacher_lse fp64 [batch, R]).
+    weight and grad_loss fp32 [batch, L]; n_rows int32 [batch]."""
+    dev = draft_logits.device
+    if out is None:
+        _need(dev.type == "cuda" and draft_logits.dim() == 3, "draft_logits must be a CUDA tensor [batch, L, V] (there is no CPU path)")
+        B, L = draft_logits.shape[:2]
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            out = Distilled(loss=torch.empty(B, L, device=dev), stats=torch.empty(B, L, 4, device=dev),
+                            grad=torch.empty(draft_logits.shape, dtype=draft_logits.dtype, device=dev) if grad else None,
+                            status=torch.empty(B, dtype=torch.int32, device=dev))
+    dev, a = _distill_args(draft_logits, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags)
+    _enqueue(lib().cadd_distill_loss, a, dev, stream)
+    return out
+
+
+def cadd_distill_grad(draft_logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, stats: torch.Tensor, *,
+                      teacher_lse=None, rest: bool = False, temperature: float = 1.0, path=None, path_len=None, n_rows=None, weight=None,
+                      grad_loss=None, grad: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, flags: int = 0,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The gradient of cadd_distill_loss with respect to draft_logits, given the gradient grad_loss fp32 [batch, L] of its losses (1
+    without) and the stats it left; the other arguments as there.  Returns grad (made here unless given; may be draft_logits)."""
+    dev = draft_logits.device
+    if grad is None:
+        _need(dev.type == "cuda" and draft_logits.dim() == 3, "draft_logits must be a CUDA tensor [batch, L, V] (there is no CPU path)")
+        with torch.cuda.stream(_stream_of(stream, dev)):
+            grad = torch.empty(draft_logits.shape, dtype=draft_logits.dtype, device=dev)
+    dev, a = _distill_args(draft_logits, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss,
+                           Distilled(stats=stats, grad=grad, status=status), flags)
+    _enqueue(lib().cadd_distill_grad, a, dev, stream)
+    return grad

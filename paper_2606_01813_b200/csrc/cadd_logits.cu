@@ -1,0 +1,164 @@
+// Host side of the calls on a round's logits (cadd.h): penalties, biases and masks; distillation.  Argument checks, grids,
+// launches.  No allocation, no synchronisation, no state kept between calls.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cadd.h"
+#include "adjust_logits.cuh"
+#include "distill.cuh"
+
+namespace cadd {
+
+static inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+static int launched() { return cudaGetLastError() == cudaSuccess ? CADD_OK : CADD_ERR_LAUNCH; }
+// Grids that only have to be large enough go by a B200's SMs without asking the device, which small calls would feel.
+constexpr int kSms = 148;
+
+static int check_logits(int batch, int rows, int64_t V, int dtype, const void* x, int64_t stride_b, int64_t stride_row) {
+    if (batch < 1 || batch > (1 << 20) || rows < 1 || rows > 65536 || V < 1 || V >= ((int64_t)1 << 31) || (int64_t)batch * rows >= ((int64_t)1 << 28))
+        return CADD_ERR_SHAPE;
+    if (dtype != CADD_DTYPE_BF16 && dtype != CADD_DTYPE_FP32) return CADD_ERR_DTYPE;
+    if (stride_b < 0 || stride_row < 0 || stride_b >= ((int64_t)1 << 50) || stride_row >= ((int64_t)1 << 40)) return CADD_ERR_SHAPE;
+    if (!x) return CADD_ERR_NULL;
+    return aligned(x, dtype == CADD_DTYPE_BF16 ? 2 : 4) ? CADD_OK : CADD_ERR_ALIGN;
+}
+// The same of an output: rows must not lie in one another, whichever axis is the outer one.
+static int check_output(int batch, int rows, int64_t V, int dtype, const void* x, int64_t stride_b, int64_t stride_row) {
+    const int rc = check_logits(batch, rows, V, dtype, x, stride_b, stride_row);
+    if (rc != CADD_OK) return rc;
+    const int64_t by_rows = (int64_t)(rows - 1) * stride_row + V, by_batch = (int64_t)(batch - 1) * stride_b + V;
+    const bool rows_in = (rows == 1 || stride_row >= V) && (batch == 1 || stride_b >= by_rows);
+    const bool batch_in = (batch == 1 || stride_b >= V) && (rows == 1 || stride_row >= by_batch);
+    return rows_in || batch_in ? CADD_OK : CADD_ERR_SHAPE;
+}
+
+// ---------------- penalties, biases, masks ----------------
+
+template <int DT>
+static int launch_adjust(const AdjustParams& p, cudaStream_t st) {
+    const size_t smem = adjust_smem_bytes(p.n_bias);
+    if (cudaFuncSetAttribute((const void*)adjust_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    adjust_kernel<DT><<<(unsigned)((int64_t)p.batch * p.groups * p.tiles), kAdjustThreads, smem, st>>>(p);
+    return launched();
+}
+
+// ---------------- distillation ----------------
+
+// Chunks of a row at most: its whole 16-byte chunks where it starts on a boundary.
+static int64_t row_chunks(int dtype, int64_t V) { return V / (dtype == CADD_DTYPE_BF16 ? 8 : 4); }
+
+template <int DT, bool kLoss, bool kGrad>
+static int launch_distill(const DistillParams& p, int64_t rows, cudaStream_t st) {
+    const size_t smem = distill_smem_bytes(p.chunks_max);
+    if (cudaFuncSetAttribute((const void*)distill_kernel<DT, kLoss, kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * p.C)); cfg.blockDim = dim3(kDistillThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, distill_kernel<DT, kLoss, kGrad>, p) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    return CADD_OK;
+}
+
+static int distill(const cadd_distill_args* a, bool loss, cudaStream_t st) {
+    if (!a) return CADD_ERR_NULL;
+    if (a->struct_size != sizeof(cadd_distill_args)) return CADD_ERR_STRUCT_SIZE;
+    int rc = check_logits(a->batch, a->L, a->V, a->logits_dtype, a->logits, a->stride_b, a->stride_l);
+    if (rc != CADD_OK) return rc;
+    if (a->K < 1 || a->K > CADD_DISTILL_MAX_K || a->R < 1 || a->R > 65536 || a->V > (a->logits_dtype == CADD_DTYPE_BF16 ? 800000 : 400000)) return CADD_ERR_SHAPE;
+    if (a->path ? a->path_cols < (a->L > 1 ? 1 : 0) || a->path_cols > 65536 : a->R < a->L) return CADD_ERR_SHAPE;
+    if (!(a->temperature >= 0x1p-20 && a->temperature <= 0x1p20)) return CADD_ERR_SHAPE;
+    if (!a->teacher_token || !a->teacher_logit || (a->path && !a->path_len)) return CADD_ERR_NULL;
+    if (loss ? !a->loss && !a->stats && !a->grad : !a->stats || !a->grad) return CADD_ERR_NULL;
+    if (a->grad) {
+        if ((rc = check_output(a->batch, a->L, a->V, a->logits_dtype, a->grad, a->grad_stride_b, a->grad_stride_l)) != CADD_OK) return rc;
+        if (a->grad == a->logits && ((a->batch > 1 && a->grad_stride_b != a->stride_b) || (a->L > 1 && a->grad_stride_l != a->stride_l))) return CADD_ERR_SHAPE;
+    }
+    if (!aligned(a->teacher_token, 4) || !aligned(a->teacher_logit, 8) || !aligned(a->teacher_lse, 8) || !aligned(a->path, 4) || !aligned(a->path_len, 4) ||
+        !aligned(a->n_rows, 4) || !aligned(a->weight, 4) || !aligned(a->grad_loss, 4) || !aligned(a->loss, 4) || !aligned(a->stats, 16) || !aligned(a->status, 4))
+        return CADD_ERR_ALIGN;
+    DistillParams p;
+    p.logits = (const char*)a->logits; p.grad = (char*)a->grad;
+    p.V = a->V; p.in_b = a->stride_b; p.in_row = a->stride_l; p.out_b = a->grad_stride_b; p.out_row = a->grad_stride_l;
+    p.L = a->L; p.R = a->R; p.K = a->K; p.path_cols = a->path_cols; p.rest = (a->flags & CADD_DISTILL_REST) ? 1 : 0;
+    p.c = (float)(1.4426950408889634 / a->temperature);
+    p.inv_t = 1.0 / a->temperature;
+    p.token = a->teacher_token; p.path = a->path; p.path_len = a->path_len; p.n_rows = a->n_rows;
+    p.value = a->teacher_logit; p.lse = a->teacher_lse; p.weight = a->weight; p.grad_loss = a->grad_loss;
+    p.loss = a->loss; p.stats = a->stats; p.status = a->status;
+    p.drop = (a->flags & CADD_FLAG_TEST_DROP_TILE) ? 1 : -1;
+    const int64_t rows = (int64_t)a->batch * a->L, chunks = row_chunks(a->logits_dtype, a->V);
+    int C = 1;
+    while (C < kDistillMaxC && ((chunks + C - 1) / C > 4 * kDistillTile || (rows * C < kSms && (chunks + C - 1) / C > kDistillThreads))) ++C;
+    p.C = C;
+    p.chunks_max = (int)((chunks + C - 1) / C);
+    if (a->status) {
+        distill_status_kernel<<<(unsigned)a->batch, kDistillThreads, 0, st>>>(p);
+        if ((rc = launched()) != CADD_OK) return rc;
+    }
+    const bool bf16 = a->logits_dtype == CADD_DTYPE_BF16;
+    if (!loss) return bf16 ? launch_distill<CADD_DTYPE_BF16, false, true>(p, rows, st) : launch_distill<CADD_DTYPE_FP32, false, true>(p, rows, st);
+    if (a->grad) return bf16 ? launch_distill<CADD_DTYPE_BF16, true, true>(p, rows, st) : launch_distill<CADD_DTYPE_FP32, true, true>(p, rows, st);
+    return bf16 ? launch_distill<CADD_DTYPE_BF16, true, false>(p, rows, st) : launch_distill<CADD_DTYPE_FP32, true, false>(p, rows, st);
+}
+
+}  // namespace cadd
+
+using namespace cadd;
+
+extern "C" {
+
+int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream) {
+    if (!a) return CADD_ERR_NULL;
+    if (a->struct_size != sizeof(cadd_adjust_args)) return CADD_ERR_STRUCT_SIZE;
+    int rc = check_logits(a->batch, a->R, a->V, a->logits_dtype, a->logits, a->stride_b, a->stride_row);
+    if (rc == CADD_OK) rc = check_output(a->batch, a->R, a->V, a->logits_dtype, a->out, a->out_stride_b, a->out_stride_row);
+    if (rc != CADD_OK) return rc;
+    const bool in_place = a->out == a->logits;
+    if (in_place && ((a->batch > 1 && a->out_stride_b != a->stride_b) || (a->R > 1 && a->out_stride_row != a->stride_row))) return CADD_ERR_SHAPE;
+    if (a->n_bias < 0 || a->n_bias > 65536) return CADD_ERR_SHAPE;
+    if (a->history && (a->history_cols < 1 || a->history_stride < 0 || a->history_stride >= ((int64_t)1 << 50))) return CADD_ERR_SHAPE;
+    if (a->allowed && a->n_allowed < 1) return CADD_ERR_SHAPE;
+    if ((a->n_bias > 0 && (!a->bias_token || !a->bias)) || (a->token_ids && !a->parent_idx) || (a->allowed && !a->allowed_row)) return CADD_ERR_NULL;
+    if (!aligned(a->n_nodes, 4) || !aligned(a->token_ids, 4) || !aligned(a->parent_idx, 4) || !aligned(a->history, 4) || !aligned(a->history_len, 4) ||
+        !aligned(a->prompt_len, 4) || !aligned(a->repetition, 4) || !aligned(a->presence, 4) || !aligned(a->frequency, 4) || !aligned(a->bias_token, 4) ||
+        !aligned(a->bias, 4) || !aligned(a->allowed, 4) || !aligned(a->allowed_row, 4) || !aligned(a->status, 4))
+        return CADD_ERR_ALIGN;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    AdjustParams p;
+    p.in = (const char*)a->logits; p.out = (char*)a->out;
+    p.V = a->V; p.in_b = a->stride_b; p.in_row = a->stride_row; p.out_b = a->out_stride_b; p.out_row = a->out_stride_row;
+    p.batch = a->batch; p.R = a->R;
+    p.n_bias = a->n_bias; p.history_cols = a->history_cols; p.n_allowed = a->n_allowed; p.words = (int)((a->V + 31) / 32);
+    p.in_place = in_place;
+    p.penalised = a->repetition || a->presence || a->frequency;
+    p.n_nodes = a->n_nodes; p.token_ids = a->token_ids; p.parent_idx = a->parent_idx;
+    p.history = a->history; p.history_len = a->history_len; p.prompt_len = a->prompt_len; p.history_stride = a->history_stride;
+    p.bias_token = a->bias_token; p.bias = a->bias; p.allowed = a->allowed; p.allowed_row = a->allowed_row;
+    p.repetition = a->repetition; p.presence = a->presence; p.frequency = a->frequency;
+    p.status = a->status;
+    p.tiles = (int)((a->V + kAdjustTile - 1) / kAdjustTile);
+    p.groups = (a->R + kAdjustRows - 1) / kAdjustRows;
+    p.rows_per_cta = (a->R + p.groups - 1) / p.groups;
+    if ((int64_t)p.batch * p.groups * p.tiles >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
+    if (a->status) {
+        adjust_status_kernel<<<(unsigned)p.batch, kAdjustThreads, 0, st>>>(p);
+        if ((rc = launched()) != CADD_OK) return rc;
+    }
+    return a->logits_dtype == CADD_DTYPE_BF16 ? launch_adjust<CADD_DTYPE_BF16>(p, st) : launch_adjust<CADD_DTYPE_FP32>(p, st);
+}
+
+int cadd_distill_loss(const cadd_distill_args* a, void* cuda_stream) { return distill(a, true, (cudaStream_t)cuda_stream); }
+int cadd_distill_grad(const cadd_distill_args* a, void* cuda_stream) { return distill(a, false, (cudaStream_t)cuda_stream); }
+
+}  // extern "C"

@@ -36,6 +36,7 @@
 #pragma once
 #include "common.cuh"
 #include "tile_ring.cuh"
+#include "packed.cuh"
 
 namespace cadd {
 
@@ -88,12 +89,6 @@ struct TopkParams {
 
 constexpr float kLog2eHi = 1.44269502162933349609375f;     // float(log2 e)
 constexpr float kLog2eLo = 1.92596299112661746e-8f;        // log2 e - kLog2eHi
-
-__device__ __forceinline__ float ex2_approx(float t) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
-    return r;
-}
 
 // Per-thread running sum: acc = sum of 2^(x*log2e - c) over the elements this thread has folded in.
 struct ThreadSum {
@@ -155,26 +150,6 @@ struct TopkShared {
 };
 static_assert(sizeof(EndArea) <= sizeof(uint4) * kStages * kTkTileChunks, "the end-of-segment area must fit in the ring");
 
-
-// ---- packed fp32x2 arithmetic (one instruction for two lanes of a register pair) ----
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 
 // Examine one element on the careful path (ragged row ends, retries, poisoned segments).  Returns
 // true when the element had to be dropped because the candidate buffer was full (the caller retries
@@ -316,11 +291,6 @@ __device__ __noinline__ ThreadSum refresh_candidates(TopkShared& sh, ThreadSum s
     __syncthreads();
     return s;
 }
-
-// ex2.approx on sm_100 returns the exponential truncated toward zero: measured mean relative error
-// -5.05e-8 (arguments -32..-1, spread +-0.1e-8 over unit intervals).  The fast sums are scaled by this
-// factor; the remaining per-term error is zero-mean.
-constexpr double kEx2BiasFix = 1.0 + 5.05e-8;
 
 // Dynamic shared memory of the kernel.
 inline size_t topk_smem_bytes() { return sizeof(TopkShared) + 128; }
