@@ -52,7 +52,7 @@ static int64_t row_chunks(int dtype, int64_t V) { return V / (dtype == CADD_DTYP
 
 template <int DT, bool kLoss, bool kGrad>
 static int launch_distill(const DistillParams& p, int64_t rows, cudaStream_t st) {
-    const size_t smem = distill_smem_bytes(p.chunks_max);
+    const size_t smem = distill_smem_bytes(p.chunks_max, kLoss && kGrad ? p.chunks_max : (p.chunks_max < kDistillRing * kDistillTile ? p.chunks_max : kDistillRing * kDistillTile));
     if (cudaFuncSetAttribute((const void*)distill_kernel<DT, kLoss, kGrad>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
@@ -99,7 +99,8 @@ static int distill(const cadd_distill_args* a, bool loss, cudaStream_t st) {
     p.drop = (a->flags & CADD_FLAG_TEST_DROP_TILE) ? 1 : -1;
     const int64_t rows = (int64_t)a->batch * a->L, chunks = row_chunks(a->logits_dtype, a->V);
     int C = 1;
-    while (C < kDistillMaxC && ((chunks + C - 1) / C > 4 * kDistillTile || (rows * C < kSms && (chunks + C - 1) / C > kDistillThreads))) ++C;
+    const bool stays = loss && a->grad;
+    while (C < kDistillMaxC && ((stays && (chunks + C - 1) / C > 4 * kDistillTile) || (rows * C < 4 * kSms && (chunks + C - 1) / C > kDistillThreads))) ++C;
     p.C = C;
     p.chunks_max = (int)((chunks + C - 1) / C);
     if (a->status) {

@@ -1,14 +1,13 @@
 // Distillation of the drafter from the target's top tokens: losses and gradients (cadd_distill_args has the definition).
 //
-// A cluster of CTAs takes one row of drafter's logits, a CTA one contiguous segment of it, which it brings to shared memory whole
-// (bulk copies of 16 KB, each with a barrier of its own, all issued at the start).  As the tiles land, every thread adds up the
-// exponentials of its elements that are not listed, relative to a power of two at or above its own largest; listed tokens are
-// left out of that sum (their elements count as -Inf) and go into the row's statistics one by one, in fp64: the rest's probability
-// is therefore right even where the listed tokens have all but nothing to spare.  The segments' (largest, sum) pairs cross the
-// cluster through distributed shared memory.  With the statistics known the gradient is formed from the segment as it
-// lies in shared memory: a row is read from memory once and written once, whether or not its loss is asked for.
-//
-// The gradient alone (statistics given) takes the same kernel without the exchange.
+// A cluster of CTAs takes one row of drafter's logits, a CTA one contiguous segment of it, which comes to shared memory in tiles of
+// 16 KB (bulk copies, each with a barrier).  As the tiles land, every thread adds up the exponentials of its elements that are
+// not listed, relative to a power of two at or above its own largest; listed tokens are left out of that sum (their elements
+// count as -Inf) and go into the row's statistics one by one, in fp64: the rest's probability is therefore right even where the
+// listed tokens leave all but nothing.  The segments' (largest, sum) pairs cross the cluster through distributed shared memory.
+// Where the gradient is wanted too, all tiles of the segment have room and stay, and with the statistics known it is formed from them:
+// a row is read from memory once and written once.  The loss alone, and the gradient alone (statistics given, no exchange), need a
+// tile once, so these walk through a ring of a few tiles and give a CTA more of the row.
 #pragma once
 #include "common.cuh"
 #include "tile_ring.cuh"
@@ -19,8 +18,8 @@ namespace cadd {
 constexpr int kDistillThreads = 256;
 constexpr int kDistillMaxC = 8;                                     // CTAs a row at most
 constexpr int kDistillTile = 4 * kDistillThreads;                   // 16-byte chunks of one copy: four a thread
-constexpr int kDistillMaxTiles = 13;
-constexpr int kDistillMaxChunks = kDistillMaxTiles * kDistillTile;  // of a segment: 208 KB
+constexpr int kDistillMaxTiles = 13;                                // that stay in shared memory: 208 KB
+constexpr int kDistillRing = 3;                                     // tiles of the ring, where they do not stay
 constexpr int kDistillK = CADD_DISTILL_MAX_K;
 static_assert(kDistillK <= kDistillThreads, "one thread an entry");
 constexpr float kDistillLowest = -1.0e30f;                          // logits below count as -Inf; also the reference of an empty sum
@@ -31,7 +30,7 @@ struct DistillParams {
     char* grad;
     int64_t V, in_b, in_row, out_b, out_row;
     int L, R, K, path_cols, rest;
-    int C, chunks_max;                            // CTAs a row; chunks of a segment at most, what shared memory has room for
+    int C, chunks_max;                            // CTAs a row; chunks of a segment at most
     float c;                                      // log2(e) / T
     double inv_t;
     const int32_t *token, *path, *path_len, *n_rows;
@@ -46,18 +45,20 @@ struct DistillParams {
 // two groups are the row's scalar head and tail), then the segment.
 struct DistillShared {
     alignas(8) uint64_t full[kDistillMaxTiles];
+    int sent[kDistillMaxTiles];                   // last tile sent for into each stage, -1: none
+    unsigned released[kDistillRing];              // ring: warps done with the stage's current tile
     double value[kDistillK];                      // entries of the list: target's logit
     double prob[kDistillK];                       // entries: p
     double peer_sum[kDistillMaxC];
     double warp_sum[kDistillThreads / 32];
     double factor;                                // of the exponentials in the gradient of tokens that are not listed
-    float peer_max[kDistillMaxC];
-    float warp_max[kDistillThreads / 32];
+    float peer_max[kDistillMaxC], peer_ref[kDistillMaxC];
+    float warp_max[kDistillThreads / 32], warp_ref[kDistillThreads / 32];
     float logit[kDistillK];                       // entries: drafter's logit
     float g[kDistillK];                           // entries: gradient of their token
     int token[kDistillK];                         // entries: token, -1 where there is none
+    int chunk[kDistillK];                         // entries: chunk of the segment
     int16_t next[kDistillK];                      // next entry of the same group, -1: none
-    int16_t chunk[kDistillK];                     // chunk of the segment
     uint8_t elem[kDistillK], once[kDistillK];     // element of the chunk; 1: the token's first entry
     float ref;                                    // reference exponent of the gradient's exponentials
     int twice;                                    // some token is listed more than once
@@ -66,7 +67,7 @@ struct DistillShared {
 };
 __host__ __device__ inline size_t distill_first_bytes(int chunks) { return (((size_t)(chunks + 31) / 32 + 2) * 4 + 127) & ~(size_t)127; }
 __host__ __device__ inline size_t distill_shared_bytes() { return (sizeof(DistillShared) + 127) & ~(size_t)127; }
-inline size_t distill_smem_bytes(int chunks) { return distill_shared_bytes() + distill_first_bytes(chunks) + (size_t)chunks * 16; }
+inline size_t distill_smem_bytes(int chunks, int room) { return distill_shared_bytes() + distill_first_bytes(chunks) + (size_t)room * 16; }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -137,19 +138,23 @@ __device__ __forceinline__ void distill_raise(DistillSum& s, float m, float c) {
         s.ref = ref;
     }
 }
-// (m, ref, acc) of two sums together.
-__device__ __forceinline__ void distill_join(DistillSum& s, float m, double acc, float c) {
-    const float ref = fmaxf(ceilf(m * c), kDistillLowest);
-    if (ref > s.ref) {
-        s.acc = s.acc * pow2_down(s.ref - ref) + acc;
-        s.ref = ref;
-    } else {
-        s.acc += acc * pow2_down(ref - s.ref);
-    }
-    s.m = fmaxf(s.m, m);
+__device__ __forceinline__ float warp_max(float x) {                // NaN ignored
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
 }
+// The warp's sums together, in every lane.
+__device__ __forceinline__ void distill_join(DistillSum& s) {
+    const float m = warp_max(s.m), ref = warp_max(s.ref);
+    s.acc *= pow2_down(s.ref - ref);
+    s.m = m;
+    s.ref = ref;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s.acc += __shfl_xor_sync(kFullMask, s.acc, o);
+}
+// Packed sums of the exponentials of a chunk's even and odd elements.
 template <int DT>
-__device__ __forceinline__ double chunk_terms(const uint4& w, uint64_t c2, uint64_t nref2) {
+__device__ __forceinline__ uint64_t chunk_terms(const uint4& w, uint64_t c2, uint64_t nref2) {
     using E = Elem<DT>;
     float f[E::EPC];
     E::unpack(w, f);
@@ -162,9 +167,7 @@ __device__ __forceinline__ double chunk_terms(const uint4& w, uint64_t c2, uint6
     }
     uint64_t r = add2(pr[0], pr[1]);
     if constexpr (E::EPC == 8) r = add2(r, add2(pr[2], pr[3]));
-    float a, b;
-    unpack2(r, a, b);
-    return (double)(a + b);
+    return r;
 }
 
 // kLoss: statistics and loss are computed here; otherwise they are given.  kGrad: the gradient is written.
@@ -176,9 +179,9 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
     int* first_of = reinterpret_cast<int*>(distill_smem_raw + distill_shared_bytes());
     const uint4* seg = reinterpret_cast<const uint4*>(distill_smem_raw + distill_shared_bytes() + distill_first_bytes(p.chunks_max));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned C = (unsigned)p.C, rank = blockIdx.x % C;
-    const int64_t row = blockIdx.x / C;
-    const int b = (int)(row / p.L), i = (int)(row - (int64_t)b * p.L);
+    constexpr bool kRing = !(kLoss && kGrad);
+    const unsigned C = (unsigned)p.C, row = blockIdx.x / C, rank = blockIdx.x - row * C;
+    const int b = (int)(row / (unsigned)p.L), i = (int)(row - (unsigned)b * (unsigned)p.L);
 
     // ---- the row, and the target's row for it ----
     const char* in = p.logits + ((int64_t)b * p.in_b + (int64_t)i * p.in_row) * E::ES;
@@ -217,23 +220,47 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
         write_zeros();
         return;
     }
-    if (kLoss) cluster_arrive();                                     // waited for before the first access to another CTA's memory
+    if (kLoss && C > 1) cluster_arrive();                                     // waited for before the first access to another CTA's memory
 
     // ---- copies under way, then the list ----
     const int n_tiles = (nc + kDistillTile - 1) / kDistillTile;
     const int drop = p.drop < 0 ? -1 : min(p.drop, n_tiles - 1);
+    constexpr int stages = kRing ? kDistillRing : kDistillMaxTiles;
+    auto stage = [](int t) { return kRing ? t % kDistillRing : t; };
+    auto parity = [](int t) { return kRing ? (unsigned)(t / kDistillRing) & 1u : 0u; };
+    auto issue = [&](int t) {
+        if (t == drop) return;                                       // test hook: this copy is never made
+        const int c0 = t * kDistillTile, s = stage(t);
+        const unsigned bytes = (unsigned)min(kDistillTile, nc - c0) * 16u;
+        *(volatile int*)&sh.sent[s] = t;
+        mbar_arrive_expect_tx(&sh.full[s], bytes);
+        bulk_load((void*)(seg + s * kDistillTile), in + e0 * E::ES + (int64_t)c0 * 16, bytes, &sh.full[s]);
+    };
+    // a warp is done with tile t: the last one sends for the tile that takes its place
+    auto release = [&](int t) {
+        if constexpr (kRing) {
+            __syncwarp();
+            const int s = t % kDistillRing;
+            if (lane == 0 && atomicAdd(&sh.released[s], 1u) == kDistillThreads / 32 - 1) {
+                atomicExch(&sh.released[s], 0u);
+                if (t + kDistillRing < n_tiles) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    issue(t + kDistillRing);
+                }
+            }
+        }
+    };
+    auto landed = [&](int t) {
+        return __all_sync(kFullMask, mbar_wait_limited(&sh.full[stage(t)], parity(t), tile_wait_limit(t, drop))) != 0;
+    };
     if (tid == 0) {
-        for (int t = 0; t < n_tiles; ++t) mbar_init(&sh.full[t], 1);
+        for (int s = 0; s < stages; ++s) mbar_init(&sh.full[s], 1);
+        for (int s = 0; s < stages; ++s) sh.sent[s] = -1;
+        for (int s = 0; s < kDistillRing; ++s) sh.released[s] = 0;
         sh.timeout = 0;
         sh.twice = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int t = 0; t < n_tiles; ++t) {
-            if (t == drop) continue;
-            const int c0 = t * kDistillTile;
-            const unsigned bytes = (unsigned)min(kDistillTile, nc - c0) * 16u;
-            mbar_arrive_expect_tx(&sh.full[t], bytes);
-            bulk_load((void*)(seg + c0), in + e0 * E::ES + (int64_t)c0 * 16, bytes, &sh.full[t]);
-        }
+        for (int t = 0; t < stages && t < n_tiles; ++t) issue(t);
     }
     const int groups = (nc + 31) / 32;
     for (int k = tid; k < groups + 2; k += kDistillThreads) first_of[k] = -1;
@@ -260,7 +287,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
             group = c / 32;
         } else if (rank == 0 && tok < sp.head) { c = tok; group = groups; }
         else if (rank == C - 1 && tok >= p.V - sp.tail) { c = (int)(tok - (p.V - sp.tail)) + (rank == 0 ? sp.head : 0); group = groups + 1; }
-        sh.chunk[tid] = (int16_t)c;
+        sh.chunk[tid] = c;
         sh.elem[tid] = (uint8_t)e;
         if (group >= 0) {
             if (!kLoss) sh.logit[tid] = E::load(in, tok);
@@ -338,53 +365,60 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
             if (!(x == x)) s.m = -INFINITY;
         }
         for (int t = 0; t < n_tiles; ++t) {
-            if (!__all_sync(kFullMask, mbar_wait_limited(&sh.full[t], 0u, tile_wait_limit(t, drop)))) { timeout = true; break; }
-            const uint32_t ninf = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
+            if (!landed(t)) { timeout = true; break; }
+            const uint4* tile = seg + stage(t) * kDistillTile;
+            const int c0 = t * kDistillTile + tid;
+            constexpr uint32_t ninf = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
             uint4 w[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int c = t * kDistillTile + u * kDistillThreads + tid;
-                w[u] = c < nc ? seg[c] : make_uint4(ninf, ninf, ninf, ninf);
+                const int c = c0 + u * kDistillThreads;
+                w[u] = make_uint4(ninf, ninf, ninf, ninf);
                 if (c < nc) {
+                    w[u] = tile[u * kDistillThreads + tid];
                     const int first = first_of[c / 32];
                     if (first >= 0) blank<DT>(w[u], listed(first, c));
                 }
             }
+            release(t);
             const float m = E::max4(w[0], w[1], w[2], w[3]);
             if (m > s.m) distill_raise(s, m, p.c);
             const uint64_t nref2 = pack2(-s.ref, -s.ref);
-            double part = 0.0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) part += chunk_terms<DT>(w[u], c2, nref2);
-            s.acc += part;
+            const uint64_t sum2 = add2(add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2)),
+                                       add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
+            float a0, a1;
+            unpack2(sum2, a0, a1);
+            s.acc += (double)(a0 + a1);
         }
         // ---- threads, warps, CTAs ----
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float m = __shfl_xor_sync(kFullMask, s.m, o);
-            const double a = __shfl_xor_sync(kFullMask, s.acc, o);
-            distill_join(s, m, a, p.c);
-        }
-        if (lane == 0) { sh.warp_max[warp] = s.m; sh.warp_sum[warp] = s.acc; }
+        distill_join(s);
+        if (lane == 0) { sh.warp_max[warp] = s.m; sh.warp_ref[warp] = s.ref; sh.warp_sum[warp] = s.acc; }
         if (timeout) sh.timeout = 1;
         __syncthreads();
         timeout = sh.timeout != 0;
         if (warp == 0) {
-            s = DistillSum{-INFINITY, kDistillLowest, 0.0};
-            for (int k = 0; k < kDistillThreads / 32; ++k) distill_join(s, sh.warp_max[k], sh.warp_sum[k], p.c);
+            const bool in_use = lane < kDistillThreads / 32;
+            s = DistillSum{in_use ? sh.warp_max[lane] : -INFINITY, in_use ? sh.warp_ref[lane] : kDistillLowest, in_use ? sh.warp_sum[lane] : 0.0};
+            distill_join(s);
             if (timeout) s.acc = __longlong_as_double(0x7ff8000000000000ll);
         }
-        cluster_wait();
-        if (warp == 0 && lane < (int)C) {
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&sh.peer_max[rank], lane)), "f"(s.m) : "memory");
-            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&sh.peer_sum[rank], lane)), "d"(s.acc) : "memory");
+        if (C > 1) {
+            cluster_wait();
+            if (warp == 0 && lane < (int)C) {
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&sh.peer_max[rank], lane)), "f"(s.m) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&sh.peer_ref[rank], lane)), "f"(s.ref) : "memory");
+                asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&sh.peer_sum[rank], lane)), "d"(s.acc) : "memory");
+            }
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+            if (warp == 0) {
+                const bool in_use = lane < (int)C;
+                s = DistillSum{in_use ? sh.peer_max[lane] : -INFINITY, in_use ? sh.peer_ref[lane] : kDistillLowest, in_use ? sh.peer_sum[lane] : 0.0};
+                distill_join(s);
+            }
         }
-        __syncwarp();
-        cluster_arrive();
-        cluster_wait();
         if (warp == 0) {
-            s = DistillSum{-INFINITY, kDistillLowest, 0.0};
-            for (unsigned k = 0; k < C; ++k) distill_join(s, sh.peer_max[k], sh.peer_sum[k], p.c);
             m_rest = s.m >= kDistillLowest ? s.m : -INFINITY;
             z_rest = m_rest > -INFINITY ? s.acc * kEx2BiasFix * exp2((double)s.ref - (double)m_rest * (double)p.c) : (s.acc == s.acc ? 0.0 : s.acc);
             m_all = m_rest;
@@ -469,14 +503,15 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
             const uint64_t c2 = pack2(p.c, p.c), nref2 = pack2(nref, nref);
             uint4* o4 = reinterpret_cast<uint4*>(out + e0 * E::ES);
             for (int t = 0; t < n_tiles; ++t) {
-                if (!kLoss && !timeout && !__all_sync(kFullMask, mbar_wait_limited(&sh.full[t], 0u, tile_wait_limit(t, drop)))) timeout = true;
+                if (!kLoss && !timeout && !landed(t)) timeout = true;
                 if (!kLoss && timeout) factor = __int_as_float(0x7fc00000);
+                const uint4* tile = seg + stage(t) * kDistillTile;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const int c = t * kDistillTile + u * kDistillThreads + tid;
                     if (c >= nc) break;
                     float f[E::EPC];
-                    E::unpack(seg[c], f);
+                    E::unpack(tile[u * kDistillThreads + tid], f);
 #pragma unroll
                     for (int q = 0; q < E::EPC; q += 2) {
                         float t0, t1;
@@ -498,18 +533,20 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams 
                         for (int q = 0; q < E::EPC; ++q) store_element<DT>(out, e0 + (int64_t)c * E::EPC + q, f[q]);
                     }
                 }
+                if (!timeout) release(t);
             }
         }
     }
-    // no CTA leaves with a copy of its own in flight
-    if (!kLoss && sh.left_out) {
-        for (int t = 0; t < n_tiles; ++t)
-            if (t != drop) mbar_wait_bounded(&sh.full[t], 0u);
+    // No CTA leaves with a copy of its own in flight.  All tiles have been waited for, but where a wait ran out or the list left the
+    // row out before its first tile: then the last tile sent for in each stage is, once no warp can send for another.
+    if constexpr (!kLoss) {
+        if (timeout) sh.timeout = 1;
+        __syncthreads();
     }
-    if (timeout && lane == 0) {
-        for (int t = 0; t < n_tiles; ++t)
-            if (t != drop) mbar_wait_bounded(&sh.full[t], 0u);
-        if (p.status) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
+    if (tid == 0 && (sh.timeout || (!kLoss && sh.left_out))) {
+        for (int s = 0; s < stages; ++s)
+            if (sh.sent[s] >= 0) mbar_wait_bounded(&sh.full[s], parity(sh.sent[s]));
+        if (sh.timeout && p.status) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
     }
 }
 
