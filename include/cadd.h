@@ -71,7 +71,7 @@ extern "C" {
 #define CADD_STATUS_BAD_TOKEN        32768   /* distill: teacher_token held a number outside [-1, V); that entry was left out */
 #define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax,
                                                 attention leaves NaN in out and lse of the rows concerned and sets the bit for every request of the call,
-                                                distill leaves NaN in loss, stats and grad of the rows concerned */
+                                                distill leaves NaN in loss, stats and grad, adjust in out of the rows concerned */
 
 #define CADD_DTYPE_BF16 0
 #define CADD_DTYPE_FP32 1
@@ -108,7 +108,8 @@ extern "C" {
    only one), and its wait for that one tile gives up after a few tries.  Nothing hangs and nothing faults: the call
    exercises the library's bounded-wait exit (copies already in flight are waited for, then the CTA leaves) and every
    request reports CADD_STATUS_INTERNAL_TIMEOUT with the empty tree (build) or accepted_len 0 (verify).  For tests only.
-   cadd_distill_loss and cadd_distill_grad take it too (each CTA's second tile of a row, or its first; NaN).
+   cadd_distill_loss and cadd_distill_grad take it too (each CTA's second tile of a row, or its first; NaN), and cadd_adjust_logits
+   into another array (the first piece of every warp; NaN).
    cadd_tree_attention takes it too: in its tiled kernel the keys of each CTA's second unit (its first, if its first item has
    only one there) are never announced, and every wait gives up after some 16 ms. */
 #define CADD_FLAG_TEST_DROP_TILE  0x80000000u
@@ -512,7 +513,7 @@ typedef struct cadd_evict_args {
  */
 typedef struct cadd_adjust_args {
     uint32_t struct_size;          /* = sizeof(cadd_adjust_args) */
-    uint32_t flags;                /* reserved, 0 */
+    uint32_t flags;                /* 0, CADD_FLAG_TEST_DROP_TILE */
     int32_t  batch, R;             /* requests, rows of each (nodes of a tree; 1: one decoded token; draft positions) */
     int32_t  logits_dtype;         /* CADD_DTYPE_*, of out too */
     int32_t  n_bias;               /* columns of bias_token and bias, 0..65536 */
@@ -528,7 +529,7 @@ typedef struct cadd_adjust_args {
     const int32_t* parent_idx;     /* [batch,R] from cadd_build_tree, required with token_ids */
     const int32_t* history;        /* [batch, history_cols], rows history_stride apart; NULL: none.  What came before row 0's token */
     int64_t  history_stride;       /* in elements, >= 0 */
-    int32_t  history_cols;         /* >= 1 with history */
+    int32_t  history_cols;         /* >= 1 with history, < 2^30 */
     int32_t  n_allowed;            /* rows of allowed, >= 1 with it */
     const int32_t* history_len;    /* [batch], NULL => history_cols; clamped to [0, history_cols] */
     const int32_t* prompt_len;     /* [batch], NULL => 0; clamped to [0, history_len] */

@@ -1026,7 +1026,7 @@ def _logits_of(t: torch.Tensor, name: str):
 
 def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, parent_idx=None, history=None, history_len=None,
                        prompt_len=None, repetition=None, presence=None, frequency=None, bias_token=None, bias=None, allowed=None,
-                       allowed_row=None, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                       allowed_row=None, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, flags: int = 0,
                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Penalties, biases and grammar masks on logits [batch, R, V] (bf16 or fp32), before cadd_verify_tree,
     cadd_verify_tree_sampled or cadd_build_tree: each row by its own context, the history and, with token_ids / parent_idx
@@ -1061,7 +1061,7 @@ def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, pa
     if allowed is not None:
         _need(allowed.dim() == 2, "allowed must be [n_masks, ceil(V / 32)]")
         n_allowed = allowed.shape[0]
-    a = AdjustArgs(C.sizeof(AdjustArgs), 0, B, R, code, n_bias, V, lp, sb, sr, op, ob, orow,
+    a = AdjustArgs(C.sizeof(AdjustArgs), flags, B, R, code, n_bias, V, lp, sb, sr, op, ob, orow,
                    _need_like(n_nodes, i32, (B,), dev, "n_nodes"), _need_like(token_ids, i32, (B, R), dev, "token_ids"),
                    _need_like(parent_idx, i32, (B, R), dev, "parent_idx"), hp, hs, hc, n_allowed,
                    _need_like(history_len, i32, (B,), dev, "history_len"), _need_like(prompt_len, i32, (B,), dev, "prompt_len"),

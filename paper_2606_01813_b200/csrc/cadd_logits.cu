@@ -14,6 +14,21 @@ static int launched() { return cudaGetLastError() == cudaSuccess ? CADD_OK : CAD
 // Grids that only have to be large enough go by a B200's SMs without asking the device, which small calls would feel.
 constexpr int kSms = 148;
 
+template <typename P>
+static int launch_cluster(void (*kernel)(P), unsigned grid, unsigned threads, unsigned cluster, size_t smem, cudaStream_t st, const P& p) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
+        cudaGetLastError();
+        return CADD_ERR_LAUNCH;
+    }
+    return CADD_OK;
+}
+
 static int check_logits(int batch, int rows, int64_t V, int dtype, const void* x, int64_t stride_b, int64_t stride_row) {
     if (batch < 1 || batch > (1 << 20) || rows < 1 || rows > 65536 || V < 1 || V >= ((int64_t)1 << 31) || (int64_t)batch * rows >= ((int64_t)1 << 28))
         return CADD_ERR_SHAPE;
@@ -34,15 +49,39 @@ static int check_output(int batch, int rows, int64_t V, int dtype, const void* x
 
 // ---------------- penalties, biases, masks ----------------
 
-template <int DT>
-static int launch_adjust(const AdjustParams& p, cudaStream_t st) {
-    const size_t smem = adjust_smem_bytes(p.n_bias);
-    if (cudaFuncSetAttribute((const void*)adjust_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
+template <int DT, bool kInPlace>
+static int launch_adjust(AdjustParams& p, cudaStream_t st) {
+    constexpr int tile = kAdjustTile<DT>;
+    p.tiles = (int)((p.V + tile - 1) / tile);
+    // A short history is read by every CTA, a long one shared out over a cluster of them.
+    p.C = 1;
+    if (p.penalised && p.history && p.history_cols > 1024)
+        while (p.C < kAdjustMaxC && p.C < p.tiles) p.C *= 2;
+    const int64_t padded = (int64_t)(p.tiles + p.C - 1) / p.C * p.C;
+    // Rows a CTA: what they have in common is gathered once for all of them, but the device wants CTAs enough.
+    p.groups = (p.R + kAdjustRows - 1) / kAdjustRows;
+    while (p.batch * padded * p.groups < 4 * kSms && (p.R + p.groups - 1) / p.groups > kAdjustWarps) p.groups *= 2;
+    p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
+    p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
+    p.part_shift = 0;
+    while (p.part_shift < 3 && (p.rows_per_cta << p.part_shift) < kAdjustWarps) ++p.part_shift;
+    const int64_t grid = p.batch * padded * p.groups;
+    if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
+    if (p.status) {
+        adjust_status_kernel<<<(unsigned)p.batch, kAdjustThreads, 0, st>>>(p);
+        const int rc = launched();
+        if (rc != CADD_OK) return rc;
+    }
+    const size_t smem = (size_t)adjust_layout(tile, kInPlace, p.penalised || p.n_bias > 0, p.n_bias > 0).bytes;
+    if (cudaFuncSetAttribute((const void*)adjust_kernel<DT, kInPlace>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
-    adjust_kernel<DT><<<(unsigned)((int64_t)p.batch * p.groups * p.tiles), kAdjustThreads, smem, st>>>(p);
-    return launched();
+    if (p.C == 1) {
+        adjust_kernel<DT, kInPlace><<<(unsigned)grid, kAdjustThreads, smem, st>>>(p);
+        return launched();
+    }
+    return launch_cluster(adjust_kernel<DT, kInPlace>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p);
 }
 
 // ---------------- distillation ----------------
@@ -57,17 +96,7 @@ static int launch_distill(const DistillParams& p, int64_t rows, cudaStream_t st)
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * p.C)); cfg.blockDim = dim3(kDistillThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, distill_kernel<DT, kLoss, kGrad>, p) != cudaSuccess) {
-        cudaGetLastError();
-        return CADD_ERR_LAUNCH;
-    }
-    return CADD_OK;
+    return launch_cluster(distill_kernel<DT, kLoss, kGrad>, (unsigned)(rows * p.C), kDistillThreads, (unsigned)p.C, smem, st, p);
 }
 
 static int distill(const cadd_distill_args* a, bool loss, cudaStream_t st) {
@@ -128,7 +157,7 @@ int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream) {
     const bool in_place = a->out == a->logits;
     if (in_place && ((a->batch > 1 && a->out_stride_b != a->stride_b) || (a->R > 1 && a->out_stride_row != a->stride_row))) return CADD_ERR_SHAPE;
     if (a->n_bias < 0 || a->n_bias > 65536) return CADD_ERR_SHAPE;
-    if (a->history && (a->history_cols < 1 || a->history_stride < 0 || a->history_stride >= ((int64_t)1 << 50))) return CADD_ERR_SHAPE;
+    if (a->history && (a->history_cols < 1 || a->history_cols >= (1 << 30) || a->history_stride < 0 || a->history_stride >= ((int64_t)1 << 50))) return CADD_ERR_SHAPE;
     if (a->allowed && a->n_allowed < 1) return CADD_ERR_SHAPE;
     if ((a->n_bias > 0 && (!a->bias_token || !a->bias)) || (a->token_ids && !a->parent_idx) || (a->allowed && !a->allowed_row)) return CADD_ERR_NULL;
     if (!aligned(a->n_nodes, 4) || !aligned(a->token_ids, 4) || !aligned(a->parent_idx, 4) || !aligned(a->history, 4) || !aligned(a->history_len, 4) ||
@@ -148,15 +177,9 @@ int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream) {
     p.bias_token = a->bias_token; p.bias = a->bias; p.allowed = a->allowed; p.allowed_row = a->allowed_row;
     p.repetition = a->repetition; p.presence = a->presence; p.frequency = a->frequency;
     p.status = a->status;
-    p.tiles = (int)((a->V + kAdjustTile - 1) / kAdjustTile);
-    p.groups = (a->R + kAdjustRows - 1) / kAdjustRows;
-    p.rows_per_cta = (a->R + p.groups - 1) / p.groups;
-    if ((int64_t)p.batch * p.groups * p.tiles >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
-    if (a->status) {
-        adjust_status_kernel<<<(unsigned)p.batch, kAdjustThreads, 0, st>>>(p);
-        if ((rc = launched()) != CADD_OK) return rc;
-    }
-    return a->logits_dtype == CADD_DTYPE_BF16 ? launch_adjust<CADD_DTYPE_BF16>(p, st) : launch_adjust<CADD_DTYPE_FP32>(p, st);
+    p.drop = (a->flags & CADD_FLAG_TEST_DROP_TILE) ? 1 : 0;
+    if (a->logits_dtype == CADD_DTYPE_BF16) return in_place ? launch_adjust<CADD_DTYPE_BF16, true>(p, st) : launch_adjust<CADD_DTYPE_BF16, false>(p, st);
+    return in_place ? launch_adjust<CADD_DTYPE_FP32, true>(p, st) : launch_adjust<CADD_DTYPE_FP32, false>(p, st);
 }
 
 int cadd_distill_loss(const cadd_distill_args* a, void* cuda_stream) { return distill(a, true, (cudaStream_t)cuda_stream); }

@@ -255,3 +255,19 @@ def test_refusals_of_the_binding():
         G.cadd_adjust_logits(x[:, :, ::2])
     with pytest.raises(TypeError):
         G.cadd_adjust_logits(x.half())
+
+
+def test_wait_that_runs_out():
+    """Copies that are never made: NaN and the status bit, and the next call is right (nothing hangs or faults)."""
+    a = random_adjust(2, 9, 9000, torch.bfloat16, seed=5, dead=False)
+    x, st = a.logits.cuda(), torch.zeros(2, dtype=torch.int32, device="cuda")
+    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE, **a.args("cuda"))
+    torch.cuda.synchronize()
+    assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(out).all())
+    both(a)
+
+
+@pytest.mark.parametrize("V,history", [(4097, 1025), (40000, 3000), (2048 * 9, 5000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_histories_that_several_ctas_share(V, history, dtype):
+    both(random_adjust(2, 3, V, dtype, seed=V, history=history, spread=V, n_bias=20))

@@ -50,7 +50,7 @@ DISTILL = [
 OWN = {
     "adjust": [
         (dict(batch=0), G.ERR_SHAPE), (dict(R=0), G.ERR_SHAPE), (dict(R=65537), G.ERR_SHAPE), (dict(V=0), G.ERR_SHAPE), (dict(V=1 << 31), G.ERR_SHAPE),
-        (dict(logits_dtype=2), G.ERR_DTYPE), (dict(logits_dtype=-1), G.ERR_DTYPE), (dict(n_bias=-1), G.ERR_SHAPE), (dict(n_bias=65537), G.ERR_SHAPE), (dict(history_cols=0), G.ERR_SHAPE),
+        (dict(logits_dtype=2), G.ERR_DTYPE), (dict(logits_dtype=-1), G.ERR_DTYPE), (dict(n_bias=-1), G.ERR_SHAPE), (dict(n_bias=65537), G.ERR_SHAPE), (dict(history_cols=0), G.ERR_SHAPE), (dict(history_cols=1 << 30), G.ERR_SHAPE),
         (dict(history_stride=-9), G.ERR_SHAPE), (dict(n_allowed=0), G.ERR_SHAPE), (dict(logits=None), G.ERR_NULL), (dict(out=None), G.ERR_NULL),
         (dict(parent_idx=None), G.ERR_NULL), (dict(bias=None), G.ERR_NULL), (dict(bias_token=None), G.ERR_NULL), (dict(allowed_row=None), G.ERR_NULL),
         (dict(logits=PTR + 1), G.ERR_ALIGN), (dict(out=2 * PTR + 1), G.ERR_ALIGN), (dict(logits_dtype=1, out=2 * PTR + 2), G.ERR_ALIGN), (dict(history=PTR + 2), G.ERR_ALIGN),
