@@ -1,14 +1,18 @@
 // Penalties, biases and grammar masks on the logits of a tree's rows (cadd_adjust_args has the definition).
 //
-// A CTA takes a tile of consecutive tokens (8 KB of logits) of some rows of one request.  It first gathers what its tokens have
-// in common over the rows: how often each stands in the history (a table in shared memory), the sum of its biases, and a list of
-// the tokens with either, in order.  A history is as long as many tiles, so the CTAs of a cluster, consecutive tiles of the
-// same rows, share it: each reads a part and counts into the tables of all (distributed shared memory).  Then a warp takes a row's
-// piece of the tile at a time:
-//   into another array: the piece comes to shared memory by a bulk copy, the tokens that penalties or biases concern are replaced there,
-//     what the mask hides is set, and a bulk copy takes it to its place; the copy of the warp's first piece is under way meanwhile;
-//   in place: the same on memory itself, where only what changes is written (and read).
-// Tokens of a row's own path are computed before the list's and written after them, from the input's value and their own count.
+// adjust_rows_kernel, into another array.  A CTA takes a tile of consecutive tokens (8 KB of logits) of some rows of one request.  It
+// first gathers what its tokens have in common over the rows: how often each stands in the history (a table in shared memory), the
+// sum of its biases, and a list of the tokens with either, in order.  A history is as long as many tiles, so the CTAs of a cluster,
+// consecutive tiles of the same rows, share it: each reads a part and counts into the tables of all (distributed shared memory).
+// Then a warp takes a row's piece of the tile at a time: it comes to shared memory by a bulk copy, the tokens that penalties or
+// biases concern are replaced there, what the mask hides is set, and a bulk copy takes it to its place; the copy of the warp's
+// first piece is under way from the start.  Tokens of a row's own path are computed before the list's and written after
+// them, from the input's value and their own count.
+//
+// With few rows the table is not worth its while for every tile: then that kernel only copies and masks, and
+// adjust_tokens_kernel replaces single tokens in memory afterwards.  In place it is the same with adjust_mask_kernel, which
+// writes (and reads) only what masks change.  adjust_tokens_kernel deals the vocabulary out to its CTAs like cards (token t to CTA t % S), since the
+// tokens that come up are the frequent ones, whose numbers lie together; its tables fill while the kernel before it still runs.
 #pragma once
 #include "common.cuh"
 #include "tile_ring.cuh"
@@ -17,9 +21,11 @@ namespace cadd {
 
 constexpr int kAdjustThreads = 256;
 constexpr int kAdjustWarps = kAdjustThreads / 32;
-constexpr int kAdjustTileBytes = 8192;         // of a row: what a warp's buffer holds
+constexpr int kAdjustTileBytes = 8192;         // of a row: the tokens whose tables a CTA of adjust_rows_kernel has; a piece of adjust_stream_kernel
+constexpr int kAdjustPieceBytes = 4096;        // of a row: a piece of adjust_rows_kernel
 constexpr int kAdjustRows = 32;                // rows a CTA takes at most
 constexpr int kAdjustMaxC = 8;                 // CTAs that share a history
+constexpr int kAdjustBatch = 4;                // tokens of the history that a thread has under way
 constexpr int kMaxPath = 65;                   // nodes of a path: the deepest tree there is, and its root
 constexpr uint32_t kInPrompt = 1u, kHasBias = 2u, kOnce = 4u;      // a token's word in the table: two flags, then n_out of the history
 
@@ -28,8 +34,10 @@ struct AdjustParams {
     char* out;
     int64_t V, in_b, in_row, out_b, out_row;
     int batch, R, tiles, groups, rows_per_cta, part_shift, C;      // pieces of a row's tile: 1 << part_shift
+    int S;                                                          // adjust_tokens_kernel: CTAs that share a request's vocabulary, a multiple of C
     int n_bias, history_cols, n_allowed, words;
-    bool in_place, penalised;
+    bool penalised;
+    bool followed;                                                  // adjust_tokens_kernel comes next
     int drop;                                                       // test hook: 1: no warp's first copy is ever made
     const int32_t *n_nodes, *token_ids, *parent_idx, *history, *history_len, *prompt_len, *bias_token, *allowed_row;
     int64_t history_stride;
@@ -40,24 +48,30 @@ struct AdjustParams {
 
 template <int DT> constexpr int kAdjustTile = kAdjustTileBytes / Elem<DT>::ES;   // tokens
 
-// Behind this, as far as the call needs them (see adjust_layout): the warps' buffers, the table, the list, the sums of biases.
+// Tokens of a tile that the history or biases concern, in order; what list_from and the like index.  An entry without a bias is one
+// word: place | kListPrompt | n_out << kListShift; one with a bias has the same word and the sum of its biases.
+constexpr uint32_t kListPlace = 4095u, kListPrompt = 4096u;
+constexpr int kListShift = 13;
+constexpr int kListMost = (1 << (32 - kListShift)) - 1;             // uses that a word has room for
+// Behind this (see adjust_layout): the table and the sums of biases by place, and then, in their stead, the warps' buffers; the two lists.
 struct AdjustShared {
     alignas(8) uint64_t full[kAdjustWarps];    // a warp's piece has landed
-    int32_t mask_row[kAdjustRows];             // row of `allowed` of each of the CTA's rows, -1: none
     int path_n[kAdjustRows];
     uint16_t path[kAdjustRows][kMaxPath];      // tokens of each row's path that lie in the tile
-    int list_from[kAdjustWarps + 1];           // the list's entries of each eighth of the tile
+    int from[2][kAdjustWarps + 1];             // the entries, without and with a bias, of each eighth of the tile
     int twice;                                 // some token has two biases
 };
-constexpr int kAdjustBuffer = kAdjustTileBytes + 16;                // of one warp: the piece keeps its distance from a 16-byte boundary
-struct AdjustLayout { int buffers, table, list, bias, bytes; };
-__host__ __device__ inline AdjustLayout adjust_layout(int tile, bool in_place, bool sparse, bool biased) {
+template <int kBytes> constexpr int kAdjustBuffer = kBytes + 16;    // of one warp: the piece keeps its distance from a 16-byte boundary
+struct AdjustLayout { int table, bias, buffers, plain, biased, sums, bytes; };
+__host__ __device__ inline AdjustLayout adjust_layout(int tile, int n_bias) {
     AdjustLayout l;
-    l.buffers = (int)((sizeof(AdjustShared) + 127) & ~(size_t)127);
-    l.table = l.buffers + (in_place ? 0 : kAdjustWarps * kAdjustBuffer);
-    l.list = l.table + (sparse ? tile * 4 : 0);
-    l.bias = l.list + (sparse ? tile * 2 : 0);
-    l.bytes = l.bias + (biased ? tile * 4 : 0);
+    const int most = n_bias < tile ? n_bias : tile, tables = tile * (n_bias > 0 ? 8 : 4), buffers = kAdjustWarps * (kAdjustPieceBytes + 16);
+    l.table = l.buffers = (int)((sizeof(AdjustShared) + 127) & ~(size_t)127);
+    l.bias = l.table + tile * 4;
+    l.plain = l.table + (tables > buffers ? tables : buffers);
+    l.biased = l.plain + tile * 4;
+    l.sums = l.biased + most * 4;
+    l.bytes = l.sums + most * 4;
     return l;
 }
 
@@ -85,9 +99,14 @@ __device__ __forceinline__ void hide(uint4& w, uint32_t bits) {
     uint32_t* x = &w.x;
     if constexpr (DT == CADD_DTYPE_BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t keep = ((bits >> (2 * i)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
-            x[i] = (x[i] & keep) | (0xff80ff80u & ~keep);
+        for (int i = 0; i < 4; i += 2) {
+            // four bits to the top bits of four bytes (the shifted copies share no position), and each byte's top bit over a half word
+            const uint32_t tops = ((bits >> (2 * i)) & 15u) * 0x10204080u;
+            uint32_t lo, hi;
+            asm("prmt.b32 %0, %1, 0, 0x9988;" : "=r"(lo) : "r"(tops));
+            asm("prmt.b32 %0, %1, 0, 0xbbaa;" : "=r"(hi) : "r"(tops));
+            x[i] = (x[i] & lo) | (0xff80ff80u & ~lo);
+            x[i + 1] = (x[i + 1] & hi) | (0xff80ff80u & ~hi);
         }
     } else {
 #pragma unroll
@@ -116,12 +135,14 @@ __device__ __forceinline__ double penalised(const Penalty& q, double x, uint32_t
     return x;
 }
 
+// Words of a mask that a lane holds for a piece of so many bytes: 4, 2 or 1.
+template <int DT, int kBytes> constexpr int kMaskRegs = kBytes / Elem<DT>::ES / 1024;
 // What a mask hides of n elements at x, whose first is token v (a multiple of 32): x lies in shared memory, or is memory itself.  A warp.
-template <int DT, bool kShared>
-__device__ __forceinline__ void mask_piece(char* x, int n, const uint32_t* mask, int words, int64_t v, const uint32_t (&first)[kAdjustTileBytes / Elem<DT>::ES / 1024]) {
+template <int DT, int kBytes>
+__device__ __forceinline__ void mask_piece(char* x, int n, const uint32_t* mask, int words, int64_t v, const uint32_t (&first)[kMaskRegs<DT, kBytes>]) {
     using E = Elem<DT>;
     using T = typename Raw<DT>::T;
-    constexpr int kRegs = kAdjustTileBytes / E::ES / 1024;          // words of the mask a lane holds: 4 or 2
+    constexpr int kRegs = kMaskRegs<DT, kBytes>;
     constexpr int kPer = 32 / E::EPC;                               // chunks a word covers: 4 or 8
     const int lane = threadIdx.x & 31;
     const int mis = (int)(((uintptr_t)x & 15u) / E::ES);
@@ -150,7 +171,7 @@ __device__ __forceinline__ void mask_piece(char* x, int n, const uint32_t* mask,
     constexpr uint32_t ninf2 = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
     constexpr int kStep = 4;                                        // chunks of a lane under way
 #pragma unroll
-    for (int i0 = 0; i0 < kAdjustTileBytes / 512; i0 += kStep) {
+    for (int i0 = 0; i0 < kBytes / 512; i0 += kStep) {
         if (32 * i0 >= nc) break;
         uint4 w[kStep];
         uint32_t bits[kStep];
@@ -175,293 +196,528 @@ __device__ __forceinline__ void mask_piece(char* x, int n, const uint32_t* mask,
     }
 }
 
+// One use of a token more in the table of CTA `rank` of the cluster, or in this CTA's own (shared false).
+__device__ __forceinline__ void count_use(uint32_t* word, uint32_t rank, bool shared, bool in_prompt) {
+    if (!shared) {
+        if (in_prompt) atomicOr(word, kInPrompt);
+        else atomicAdd(word, kOnce);
+    } else {
+        uint32_t a;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(word)), "r"(rank));
+        if (in_prompt) asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(a), "r"(kInPrompt) : "memory");
+        else asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(a), "r"(kOnce) : "memory");
+    }
+}
+// Sums of the biases of the tokens that have a place here (place(token) >= 0), marked in the table.
+template <typename Place>
+__device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint32_t* table, float* bias_of, int* twice, Place place) {
+    const int32_t* at = p.bias_token + (int64_t)b * p.n_bias;
+    const float* val = p.bias + (int64_t)b * p.n_bias;
+    for (int i = threadIdx.x; i < p.n_bias; i += kAdjustThreads) {
+        const int t = place(at[i]);
+        if (t < 0) continue;
+        if (atomicOr(&table[t], kHasBias) & kHasBias) *twice = 1;
+        bias_of[t] = val[i];
+    }
+    __syncthreads();
+    if (!*twice) return;
+    for (int i = threadIdx.x; i < p.n_bias; i += kAdjustThreads) {  // a token's first entry adds up all of them, in their order
+        const int t = place(at[i]);
+        if (t < 0) continue;
+        bool once = true;
+        for (int k = 0; k < i && once; ++k) once = at[k] != at[i];
+        if (!once) continue;
+        double s = 0.0;
+        for (int k = i; k < p.n_bias; ++k)
+            if (at[k] == at[i]) s += (double)val[k];
+        bias_of[t] = (float)s;
+    }
+}
+// Places of the tokens on row j's path, the row's own first; returns how many.  One thread.
+template <typename Place>
+__device__ __forceinline__ int gather_path(const AdjustParams& p, int b, int j, uint16_t* path, Place place) {
+    const int32_t* tok = p.token_ids + (int64_t)b * p.R;
+    const int32_t* par = p.parent_idx + (int64_t)b * p.R;
+    int k = 0;
+    for (int step = 0; step < kMaxPath; ++step) {
+        const int t = place(tok[j]), up = par[j];
+        if (t >= 0) path[k++] = (uint16_t)t;
+        if (up < 0 || up >= j) break;
+        j = up;
+    }
+    return k;
+}
+// Number of set bits, over the lanes before this one, of a four-bit mask that each lane has.
+__device__ __forceinline__ int before_lane(uint32_t m) {
+    const uint32_t lower = (1u << (threadIdx.x & 31)) - 1u;
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n += __popc(__ballot_sync(kFullMask, (m >> j) & 1u) & lower);
+    return n;
+}
+__device__ __forceinline__ uint32_t four(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
+// The lists from the table (whole CTA; warp w has the w-th eighth of the places).  With kWords the entries are words as described at
+// kListPlace, those with a bias in a list of their own; otherwise all are places in one list.
+template <int kPlaces, bool kWords>
+__device__ __forceinline__ void gather_lists(const uint32_t* table, const float* bias_of, void* plain, uint32_t* biased, float* sums, int (*from)[kAdjustWarps + 1]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kEighth = kPlaces / kAdjustWarps, kSteps = kEighth / 128;
+    uint4 w[kSteps];
+    int n = 0, n2 = 0;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        w[k] = reinterpret_cast<const uint4*>(table)[(warp * kEighth) / 4 + k * 32 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = four(w[k], j);
+            const bool two = kWords && (x & kHasBias);
+            n += x != 0u && !two;
+            n2 += two;
+        }
+    }
+    n = __reduce_add_sync(kFullMask, n);
+    if (kWords) n2 = __reduce_add_sync(kFullMask, n2);
+    if (lane == 0) { from[0][warp + 1] = n; if (kWords) from[1][warp + 1] = n2; }
+    __syncthreads();
+    int at = 0, at2 = 0, all = 0, all2 = 0;
+#pragma unroll
+    for (int k = 0; k < kAdjustWarps; ++k) {
+        if (k == warp) { at = all; at2 = all2; }
+        all += from[0][k + 1];
+        if (kWords) all2 += from[1][k + 1];
+    }
+    __syncthreads();                                                // (everybody has read the counts, and, of the table, what becomes the lists)
+    if (lane == 0) {
+        from[0][warp + 1] = at + n;
+        if (kWords) from[1][warp + 1] = at2 + n2;
+        if (warp == 0) { from[0][0] = 0; if (kWords) from[1][0] = 0; }
+    }
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+        uint32_t m = 0, m2 = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = four(w[k], j);
+            const bool two = kWords && (x & kHasBias);
+            m |= (x != 0u && !two ? 1u : 0u) << j;
+            m2 |= (two ? 1u : 0u) << j;
+        }
+        int to = at + before_lane(m), to2 = at2;
+        if (kWords) to2 += before_lane(m2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = four(w[k], j);
+            const int place = warp * kEighth + k * 128 + lane * 4 + j;
+            const uint32_t word = (uint32_t)place | (x & kInPrompt ? kListPrompt : 0u) | (x / kOnce) << kListShift;
+            if ((m >> j) & 1u) {
+                if constexpr (kWords) ((uint32_t*)plain)[to++] = word;
+                else ((uint16_t*)plain)[to++] = (uint16_t)place;
+            }
+            if (kWords && ((m2 >> j) & 1u)) {
+                biased[to2] = word;
+                sums[to2++] = bias_of[place];
+            }
+        }
+        at += __popc(__ballot_sync(kFullMask, m & 1u)) + __popc(__ballot_sync(kFullMask, m & 2u)) + __popc(__ballot_sync(kFullMask, m & 4u)) + __popc(__ballot_sync(kFullMask, m & 8u));
+        if (kWords) at2 += __popc(__ballot_sync(kFullMask, m2 & 1u)) + __popc(__ballot_sync(kFullMask, m2 & 2u)) + __popc(__ballot_sync(kFullMask, m2 & 4u)) + __popc(__ballot_sync(kFullMask, m2 & 8u));
+    }
+}
+// Where an ordered list of words has a place between from and to, or -1.
+__device__ __forceinline__ int find_place(const uint32_t* list, int from, int to, int place) {
+    while (from < to) {
+        const int mid = (from + to) / 2, here = (int)(list[mid] & kListPlace);
+        if (here == place) return mid;
+        if (here < place) from = mid + 1;
+        else to = mid;
+    }
+    return -1;
+}
+// What a CTA asks memory for first, all at once: each of these would cost a round trip where it is needed.
+struct AdjustFirst {
+    float rep, pres, freq;
+    int live, len, prompt;
+    int tok[kAdjustBatch];                     // the thread's first tokens of the history, from `at` on, `step` apart (-1 behind its room)
+    __device__ __forceinline__ AdjustFirst(const AdjustParams& p, int b, int at, int step) {
+        const int32_t* h = p.history + (int64_t)b * p.history_stride;
+        const bool history = p.penalised && p.history;
+        rep = p.repetition ? p.repetition[b] : 1.0f;
+        pres = p.presence ? p.presence[b] : 0.0f;
+        freq = p.frequency ? p.frequency[b] : 0.0f;
+        len = prompt = 0;
+        if (history) len = adjust_history(p, b, &prompt);
+#pragma unroll
+        for (int u = 0; u < kAdjustBatch; ++u) tok[u] = history && at + u * step < p.history_cols ? h[at + u * step] : -1;
+        live = adjust_live(p, b);
+    }
+    __device__ __forceinline__ Penalty penalty() const { return Penalty{(double)rep, 1.0 / (double)rep, (double)pres, (double)freq}; }
+    // count(i, token) for all of the thread's part of the history; more is asked for while a batch is counted
+    template <typename Count>
+    __device__ __forceinline__ void for_history(const AdjustParams& p, int b, int at, int step, Count count) {
+        const int32_t* h = p.history + (int64_t)b * p.history_stride;
+        while (at < len) {
+            int now[kAdjustBatch];
+#pragma unroll
+            for (int u = 0; u < kAdjustBatch; ++u) {
+                const int next = at + (kAdjustBatch + u) * step;
+                now[u] = tok[u];
+                tok[u] = next < len ? h[next] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < kAdjustBatch; ++u)
+                if (at + u * step < len) count(at + u * step, now[u]);
+            at += kAdjustBatch * step;
+        }
+    }
+};
+
+// A piece of a row that a warp takes at a time: n elements from token v on (a multiple of 32).
+struct AdjustPiece {
+    char *src, *dst;
+    int64_t v;
+    int n;
+};
+// Its way into the warp's buffer: whole 16-byte chunks by one copy, the elements before and behind them by the lanes.  The piece keeps its
+// distance from a 16-byte boundary there.  False: no copy is under way.
+template <int DT>
+__device__ __forceinline__ bool fetch_piece(const AdjustPiece& u, unsigned char* buffer, uint64_t* full, bool dropped) {
+    using E = Elem<DT>;
+    using T = typename Raw<DT>::T;
+    const int lane = threadIdx.x & 31, mis = (int)((uintptr_t)u.src & 15u);
+    const int head = min(u.n, mis ? E::EPC - mis / E::ES : 0), nc = (u.n - head) / E::EPC, tail = u.n - head - nc * E::EPC;
+    if (lane == 0 && nc > 0 && !dropped) {
+        mbar_arrive_expect_tx(full, (unsigned)nc * 16u);
+        bulk_load(buffer + (mis ? 16 : 0), u.src + head * E::ES, (unsigned)nc * 16u, full);
+    }
+    if (lane < head + tail) {
+        const int i = lane < head ? lane : u.n - tail + (lane - head);
+        ((T*)(buffer + mis))[i] = ((const T*)u.src)[i];
+    }
+    return nc > 0;
+}
+// And out again; the buffer is free when it returns.
+template <int DT>
+__device__ __forceinline__ void deliver_piece(const AdjustPiece& u, unsigned char* buffer) {
+    using E = Elem<DT>;
+    using T = typename Raw<DT>::T;
+    const int lane = threadIdx.x & 31, mis = (int)((uintptr_t)u.src & 15u);
+    const T* x = (const T*)(buffer + mis);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (mis == (int)((uintptr_t)u.dst & 15u)) {
+        const int head = min(u.n, mis ? E::EPC - mis / E::ES : 0), nc = (u.n - head) / E::EPC, tail = u.n - head - nc * E::EPC;
+        if (lane == 0 && nc > 0) {
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                         ::"l"(u.dst + head * E::ES), "r"(smem_u32(buffer + (mis ? 16 : 0))), "r"((unsigned)nc * 16u) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        if (lane < head + tail) {
+            const int i = lane < head ? lane : u.n - tail + (lane - head);
+            ((T*)u.dst)[i] = x[i];
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    } else {                                                        // rows that start differently: element by element
+        for (int i = lane; i < u.n; i += 32) ((T*)u.dst)[i] = x[i];
+    }
+    __syncwarp();
+}
+// A copy that does not come: NaN in the piece, and the request is flagged.
+template <int DT>
+__device__ __forceinline__ void lose_piece(const AdjustParams& p, const AdjustPiece& u, int b) {
+    using T = typename Raw<DT>::T;
+    const int lane = threadIdx.x & 31;
+    for (int i = lane; i < u.n; i += 32) ((T*)u.dst)[i] = Raw<DT>::nan;
+    if (lane == 0 && p.status) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
+}
+// The words of a mask that a lane needs of a piece.
+template <int N>
+__device__ __forceinline__ void mask_words(const uint32_t* mask, const AdjustPiece& u, uint32_t (&word)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int at = 32 * i + (int)(threadIdx.x & 31);
+        word[i] = 32 * at < u.n ? mask[(u.v >> 5) + at] : 0u;
+    }
+}
+
+// Logits without penalties and biases, or before them: copied (kCopy) and masked.  A warp takes pieces of 8 KB, all of them dealt out to the CTAs
+// first, then to their warps, so that few pieces have SMs to themselves.
+template <int DT, bool kCopy>
+__global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 4) adjust_stream_kernel(AdjustParams p) {
+    using E = Elem<DT>;
+    constexpr int kTile = kAdjustTile<DT>;
+    extern __shared__ __align__(128) unsigned char adjust_smem_raw[];
+    __shared__ alignas(8) uint64_t full[kAdjustWarps];
+    if (p.followed) grid_launch_dependents();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned char* buffer = adjust_smem_raw + warp * kAdjustBuffer<kAdjustTileBytes>;
+    unsigned phase = 0;
+    if constexpr (kCopy) {
+        if (lane == 0) {
+            mbar_init(&full[warp], 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    }
+    const int64_t units = (int64_t)p.batch * p.R * p.tiles;
+    for (int64_t k = blockIdx.x + (int64_t)warp * gridDim.x; k < units; k += (int64_t)gridDim.x * kAdjustWarps) {
+        const int64_t row = k / p.tiles;
+        const int b = (int)(row / p.R), j = (int)(row - (int64_t)b * p.R);
+        if (j >= adjust_live(p, b)) continue;
+        AdjustPiece u;
+        u.v = (k - row * p.tiles) * kTile;
+        u.n = (int)min((int64_t)kTile, p.V - u.v);
+        u.src = const_cast<char*>(p.in) + ((int64_t)b * p.in_b + (int64_t)j * p.in_row + u.v) * E::ES;
+        u.dst = p.out + ((int64_t)b * p.out_b + (int64_t)j * p.out_row + u.v) * E::ES;
+        bool coming = false;
+        if constexpr (kCopy) coming = fetch_piece<DT>(u, buffer, &full[warp], p.drop != 0);
+        const uint32_t* mask = adjust_mask(p, b, j);
+        uint32_t word[kMaskRegs<DT, kAdjustTileBytes>];
+        if (mask) mask_words(mask, u, word);
+        if constexpr (kCopy) {
+            if (coming && !__all_sync(kFullMask, mbar_wait_limited(&full[warp], phase, p.drop ? kTestSpinLimit : kSpinLimit))) {
+                lose_piece<DT>(p, u, b);
+                if (p.drop) continue;
+                if (lane == 0) mbar_wait_bounded(&full[warp], phase);      // not to leave with a copy in flight
+                return;
+            }
+            if (coming) phase ^= 1u;
+            __syncwarp();
+            if (mask) mask_piece<DT, kAdjustTileBytes>((char*)buffer + ((uintptr_t)u.src & 15u), u.n, mask, p.words, u.v, word);
+            deliver_piece<DT>(u, buffer);
+        } else if (mask) mask_piece<DT, kAdjustTileBytes>(u.dst, u.n, mask, p.words, u.v, word);
+    }
+}
+
 __device__ __forceinline__ void adjust_cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <int DT, bool kInPlace>
-__global__ void __launch_bounds__(kAdjustThreads, kInPlace ? 4 : 2) adjust_kernel(AdjustParams p) {
+template <int DT>
+__global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustParams p) {
     using E = Elem<DT>;
     using T = typename Raw<DT>::T;
     constexpr int kTile = kAdjustTile<DT>;
     extern __shared__ __align__(128) unsigned char adjust_smem_raw[];
     AdjustShared& sh = *reinterpret_cast<AdjustShared*>(adjust_smem_raw);
-    const bool sparse = p.penalised || p.n_bias > 0;
-    const AdjustLayout lay = adjust_layout(kTile, kInPlace, sparse, p.n_bias > 0);
+    const AdjustLayout lay = adjust_layout(kTile, p.n_bias);
     uint32_t* table = reinterpret_cast<uint32_t*>(adjust_smem_raw + lay.table);
-    uint16_t* list = reinterpret_cast<uint16_t*>(adjust_smem_raw + lay.list);
     float* bias_of = reinterpret_cast<float*>(adjust_smem_raw + lay.bias);
+    uint32_t* plain = reinterpret_cast<uint32_t*>(adjust_smem_raw + lay.plain);
+    uint32_t* biased = reinterpret_cast<uint32_t*>(adjust_smem_raw + lay.biased);
+    float* sums = reinterpret_cast<float*>(adjust_smem_raw + lay.sums);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned padded = (unsigned)((p.tiles + p.C - 1) / p.C * p.C);
     const unsigned bg = blockIdx.x / padded;
     const int tile = (int)(blockIdx.x - bg * padded);
     const int b = (int)(bg / (unsigned)p.groups), g = (int)(bg - (unsigned)b * (unsigned)p.groups);
-    const int live = adjust_live(p, b);
-    const int j0 = g * p.rows_per_cta, j1 = min(live, j0 + p.rows_per_cta);
+    const int rank = (int)((unsigned)tile % (unsigned)p.C), step = p.C * kAdjustThreads;
+    AdjustFirst first(p, b, rank * kAdjustThreads + tid, step);
+    const int j0 = g * p.rows_per_cta, j1 = min(first.live, j0 + p.rows_per_cta);
     if (j0 >= j1) return;                                           // the same for every CTA of a cluster
     const int64_t v0 = (int64_t)tile * kTile;
     const int n = (int)max((int64_t)0, min((int64_t)kTile, p.V - v0));     // 0: a CTA that only helps with the history
     const int parts = 1 << p.part_shift, piece = kTile >> p.part_shift;
     const int units = (j1 - j0) << p.part_shift;                   // a row's pieces one after the other
 
-    struct Unit { char *src, *dst; int row, e0, n; };
-    auto unit_at = [&](int k) {
-        Unit u;
-        u.row = k >> p.part_shift;
-        u.e0 = (k & (parts - 1)) * piece;
-        u.n = min(piece, n - u.e0);
-        const int64_t j = j0 + u.row;
-        u.src = const_cast<char*>(p.in) + ((int64_t)b * p.in_b + j * p.in_row + v0 + u.e0) * E::ES;
-        u.dst = p.out + ((int64_t)b * p.out_b + j * p.out_row + v0 + u.e0) * E::ES;
+    auto piece_at = [&](int k) {
+        const int e0 = (k & (parts - 1)) * piece;
+        const int64_t j = j0 + (k >> p.part_shift);
+        AdjustPiece u;
+        u.v = v0 + e0;
+        u.n = min(piece, n - e0);
+        u.src = const_cast<char*>(p.in) + ((int64_t)b * p.in_b + j * p.in_row + u.v) * E::ES;
+        u.dst = p.out + ((int64_t)b * p.out_b + j * p.out_row + u.v) * E::ES;
         return u;
     };
-    unsigned char* buffer = adjust_smem_raw + lay.buffers + warp * kAdjustBuffer;
-    // a piece's way into the warp's buffer: whole 16-byte chunks by one copy, the elements before and behind them by the lanes
-    bool dropped = p.drop != 0;
-    auto fetch = [&](const Unit& u) {
-        const int mis = (int)((uintptr_t)u.src & 15u);
-        const int head = min(u.n, mis ? E::EPC - mis / E::ES : 0), nc = (u.n - head) / E::EPC, tail = u.n - head - nc * E::EPC;
-        if (lane == 0 && nc > 0 && !dropped) {
-            mbar_arrive_expect_tx(&sh.full[warp], (unsigned)nc * 16u);
-            bulk_load(buffer + (mis ? 16 : 0), u.src + head * E::ES, (unsigned)nc * 16u, &sh.full[warp]);
-        }
-        if (lane < head + tail) {
-            const int i = lane < head ? lane : u.n - tail + (lane - head);
-            ((T*)(buffer + mis))[i] = ((const T*)u.src)[i];
-        }
-        return nc > 0;
-    };
+    unsigned char* buffer = adjust_smem_raw + lay.buffers + warp * kAdjustBuffer<kAdjustPieceBytes>;
     bool coming = false;
     unsigned phase = 0;
-    if constexpr (!kInPlace) {
-        if (lane == 0) {
-            mbar_init(&sh.full[warp], 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        }
-        __syncwarp();
-        if (warp < units) {
-            const Unit u = unit_at(warp);
-            if (u.n > 0) coming = fetch(u);
-        }
+    if (lane == 0) {
+        mbar_init(&sh.full[warp], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncwarp();
+    const uint32_t* mask = nullptr;                                 // of the piece under way, and its words
+    uint32_t word[kMaskRegs<DT, kAdjustPieceBytes>];
+    auto fetch = [&](int k) {
+        const AdjustPiece u = piece_at(k);
+        if (u.n <= 0) return;
+        coming = fetch_piece<DT>(u, buffer, &sh.full[warp], p.drop != 0);
+        mask = adjust_mask(p, b, j0 + (k >> p.part_shift));
+        if (mask) mask_words(mask, u, word);
+    };
 
     // ---- what the rows have in common ----
     if (tid == 0) sh.twice = 0;
-    if (tid < j1 - j0) {
-        sh.path_n[tid] = 0;
-        int m = -1;
-        if (p.allowed) m = p.allowed_row[(int64_t)b * p.R + j0 + tid];
-        sh.mask_row[tid] = m < p.n_allowed ? m : -1;
-    }
-    if (sparse) {
-        uint4* t4 = reinterpret_cast<uint4*>(table);
-        for (int i = tid; i < kTile / 4; i += kAdjustThreads) t4[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (p.C > 1) adjust_cluster_sync();
-        else __syncthreads();
-        if (p.n_bias > 0) {
-            const int32_t* at = p.bias_token + (int64_t)b * p.n_bias;
-            const float* val = p.bias + (int64_t)b * p.n_bias;
-            for (int i = tid; i < p.n_bias; i += kAdjustThreads) {
-                const int64_t t = (int64_t)at[i] - v0;
-                if (t < 0 || t >= n) continue;
-                if (atomicOr(&table[t], kHasBias) & kHasBias) sh.twice = 1;
-                bias_of[t] = val[i];
-            }
-            __syncthreads();
-            if (sh.twice)                                           // a token's first entry adds up all of them, in their order
-                for (int i = tid; i < p.n_bias; i += kAdjustThreads) {
-                    const int64_t t = (int64_t)at[i] - v0;
-                    if (t < 0 || t >= n) continue;
-                    bool once = true;
-                    for (int k = 0; k < i && once; ++k) once = at[k] != at[i];
-                    if (!once) continue;
-                    double s = 0.0;
-                    for (int k = i; k < p.n_bias; ++k)
-                        if (at[k] == at[i]) s += (double)val[k];
-                    bias_of[t] = (float)s;
-                }
-        }
-        if (p.penalised && p.history) {
-            int prompt;
-            const int len = adjust_history(p, b, &prompt);
-            const int32_t* h = p.history + (int64_t)b * p.history_stride;
-            const unsigned rank = (unsigned)tile % (unsigned)p.C;
-            const int64_t base = v0 - (int64_t)rank * kTile;        // first token of the cluster's tiles
-            const int step = p.C * kAdjustThreads;
-            auto count = [&](int i, int tok) {
-                const int64_t t64 = (int64_t)tok - base;
-                if (t64 < 0 || t64 >= (int64_t)p.C * kTile || tok >= p.V) return;
-                const uint32_t t = (uint32_t)t64;
-                if (p.C == 1) {
-                    if (i < prompt) atomicOr(&table[t], kInPrompt);
-                    else atomicAdd(&table[t], kOnce);
-                } else {
-                    uint32_t a;
-                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(&table[t % kTile])), "r"(t / kTile));
-                    if (i < prompt) asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(a), "r"(kInPrompt) : "memory");
-                    else asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(a), "r"(kOnce) : "memory");
-                }
-            };
-            for (int i0 = (int)rank * kAdjustThreads + tid; i0 < len; i0 += 4 * step) {
-                int tok[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) tok[u] = (int64_t)i0 + (int64_t)u * step < len ? h[i0 + (int64_t)u * step] : -1;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) count(i0 + u * step, tok[u]);
-            }
-        }
-        if (p.penalised && p.token_ids && tid < j1 - j0) {          // one thread a row: up the path
-            const int32_t* tok = p.token_ids + (int64_t)b * p.R;
-            const int32_t* par = p.parent_idx + (int64_t)b * p.R;
-            int at = j0 + tid, k = 0;
-            for (int step = 0; step < kMaxPath; ++step) {
-                const int64_t t = (int64_t)tok[at] - v0;
-                if (t >= 0 && t < n) sh.path[tid][k++] = (uint16_t)t;
-                const int up = par[at];
-                if (up < 0 || up >= at) break;
-                at = up;
-            }
-            sh.path_n[tid] = k;
-        }
-        if (p.C > 1) adjust_cluster_sync();                         // no CTA counts into another's table from here on
-        else __syncthreads();
-        // the list: every thread has kTile / kAdjustThreads consecutive tokens, a warp an eighth of the tile
-        constexpr int kEach = kTile / kAdjustThreads;               // 16 or 8
-        uint32_t have = 0;
-#pragma unroll
-        for (int k = 0; k < kEach; k += 4) {
-            const uint4 w = t4[(tid * kEach + k) / 4];
-            have |= (w.x ? 1u : 0u) << k | (w.y ? 2u : 0u) << k | (w.z ? 4u : 0u) << k | (w.w ? 8u : 0u) << k;
-        }
-        int at = __popc(have), sum = at;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(kFullMask, sum, o);
-            if (lane >= o) sum += up;
-        }
-        if (lane == 31) sh.list_from[warp + 1] = sum;
-        __syncthreads();
-        int before = 0;
-        for (int k = 0; k < warp; ++k) before += sh.list_from[k + 1];
-        __syncthreads();
-        if (lane == 31) sh.list_from[warp + 1] = before + sum;
-        if (tid == 0) sh.list_from[0] = 0;
-        at = before + sum - at;
-        while (have) {
-            list[at++] = (uint16_t)(tid * kEach + __ffs(have) - 1);
-            have &= have - 1;
-        }
-    }
+    if (tid < j1 - j0) sh.path_n[tid] = 0;
+    uint4* t4 = reinterpret_cast<uint4*>(table);
+    for (int i = tid; i < kTile / 4; i += kAdjustThreads) t4[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (p.C > 1) adjust_cluster_sync();
+    else __syncthreads();
+    // (a token's place in the tile, or -1)
+    auto place = [&](int tok) { return tok >= v0 && tok < v0 + n ? (int)(tok - v0) : -1; };
+    if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
+    const int64_t base = v0 - (int64_t)rank * kTile;                // first token of the cluster's tiles
+    first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
+        const int64_t t64 = (int64_t)tok - base;
+        if (t64 < 0 || t64 >= (int64_t)p.C * kTile || tok >= p.V) return;
+        const uint32_t t = (uint32_t)t64;
+        count_use(&table[t % kTile], t / kTile, p.C > 1, i < first.prompt);
+    });
+    if (p.penalised && p.token_ids && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, sh.path[tid], place);
+    if (p.C > 1) adjust_cluster_sync();                         // no CTA counts into another's table from here on
+    else __syncthreads();
+    gather_lists<kTile, true>(table, bias_of, plain, biased, sums, sh.from);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the tables' place becomes the buffers
     __syncthreads();
     // ---- the rows ----
-    Penalty q;
-    q.rep = p.repetition ? (double)p.repetition[b] : 1.0;
-    q.inv = 1.0 / q.rep;
-    q.pres = p.presence ? (double)p.presence[b] : 0.0;
-    q.freq = p.frequency ? (double)p.frequency[b] : 0.0;
+    if (warp < units) fetch(warp);
+    const Penalty q = first.penalty();
     for (int k = warp; k < units; k += kAdjustWarps) {
-        const Unit u = unit_at(k);
-        if (u.n <= 0) continue;
-        constexpr int kRegs = kTile / 1024;
-        const int m = sh.mask_row[u.row];
-        const uint32_t* mask = m < 0 ? nullptr : p.allowed + (int64_t)m * p.words;
-        const int64_t v = v0 + u.e0;
-        uint32_t word[kRegs];
-        if (mask) {
+        const AdjustPiece u = piece_at(k);
+        if (u.n <= 0) break;                                        // (a warp's pieces are all the same part of the tile)
+        const int row = k >> p.part_shift, e0 = (int)(u.v - v0);
+        char* x = (char*)buffer + ((uintptr_t)u.src & 15u);
+        if (coming && !__all_sync(kFullMask, mbar_wait_limited(&sh.full[warp], phase, p.drop ? kTestSpinLimit : kSpinLimit))) {
+            for (int o = k; o < units; o += kAdjustWarps) lose_piece<DT>(p, piece_at(o), b);
+            if (lane == 0 && !p.drop) mbar_wait_bounded(&sh.full[warp], phase);      // not to leave with a copy in flight
+            break;
+        }
+        if (coming) phase ^= 1u;
+        __syncwarp();
+        const int np = sh.path_n[row];
+        const uint16_t* path = sh.path[row];
+        constexpr int kOwn = (kMaxPath + 31) / 32;
+        T own[kOwn];
 #pragma unroll
-            for (int i = 0; i < kRegs; ++i) {
-                const int at = 32 * i + lane;
-                word[i] = 32 * at < u.n ? mask[(v >> 5) + at] : 0u;
+        for (int s = 0; s < kOwn; ++s) {
+            const int i = s * 32 + lane;
+            if (i < np && path[i] >= e0 && path[i] < e0 + u.n) {
+                const int t = path[i], eighth = t / (kTile / kAdjustWarps);
+                const int a = find_place(plain, sh.from[0][eighth], sh.from[0][eighth + 1], t), c = find_place(biased, sh.from[1][eighth], sh.from[1][eighth + 1], t);
+                uint32_t times = a >= 0 ? plain[a] >> kListShift : (c >= 0 ? biased[c] >> kListShift : 0u);
+                for (int o = 0; o < np; ++o) times += path[o] == t;
+                own[s] = Raw<DT>::round(penalised(q, (double)E::load(x, t - e0), times, true) + (c >= 0 ? (double)sums[c] : 0.0));
             }
         }
-        char* x = u.src;
-        if constexpr (!kInPlace) {
-            x = (char*)buffer + ((uintptr_t)u.src & 15u);
-            if (coming) {
-                if (!__all_sync(kFullMask, mbar_wait_limited(&sh.full[warp], phase, dropped ? kTestSpinLimit : kSpinLimit))) {
-                    // a copy that does not come: NaN in the warp's pieces from here on, and the copy is waited for once more before leaving
-                    for (int o = k; o < units; o += kAdjustWarps) {
-                        const Unit lost = unit_at(o);
-                        for (int i = lane; i < lost.n; i += 32) ((T*)lost.dst)[i] = Raw<DT>::nan;
-                    }
-                    if (lane == 0) {
-                        if (!dropped) mbar_wait_bounded(&sh.full[warp], phase);
-                        if (p.status) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
-                    }
-                    break;
-                }
-                phase ^= 1u;
-            }
-            __syncwarp();
-        }
-        if (sparse) {
-            const int np = sh.path_n[u.row];
-            const uint16_t* path = sh.path[u.row];
-            T own[3];
-            constexpr int kOwn = (kMaxPath + 31) / 32;
+        __syncwarp();
+        // the lists' entries in [e0, e0 + piece): pieces are whole eighths
+        const int part0 = e0 / (kTile / kAdjustWarps), part1 = part0 + (kAdjustWarps >> p.part_shift);
+        for (int i = sh.from[0][part0] + lane, to = sh.from[0][part1]; i < to; i += 64) {      // two at a time
+            uint32_t e[2];
+            float y[2];
 #pragma unroll
-            for (int s = 0; s < kOwn; ++s) {
-                const int i = s * 32 + lane;
-                if (i < np) {
-                    const int t = path[i], at = t - u.e0;
-                    if (at >= 0 && at < u.n) {
-                        const uint32_t word = table[t];
-                        uint32_t times = word / kOnce;
-                        for (int o = 0; o < np; ++o) times += path[o] == t;
-                        own[s] = Raw<DT>::round(penalised(q, (double)E::load(x, at), times, true) + (word & kHasBias ? (double)bias_of[t] : 0.0));
-                    }
-                }
+            for (int o = 0; o < 2; ++o) {
+                e[o] = plain[min(i + 32 * o, to - 1)];
+                y[o] = E::load(x, (int)(e[o] & kListPlace) - e0);
             }
-            __syncwarp();
-            // entries of the list in [e0, e0 + piece): pieces are whole eighths
-            const int from = sh.list_from[(u.e0 * kAdjustWarps) / kTile], to = sh.list_from[((u.e0 + piece) * kAdjustWarps) / kTile];
-            for (int i = from + lane; i < to; i += 32) {
-                const int t = list[i], at = t - u.e0;
-                const uint32_t word = table[t], times = word / kOnce;
-                double y = penalised(q, (double)E::load(x, at), times, times > 0u || (word & kInPrompt));
-                if (word & kHasBias) y += (double)bias_of[t];
-                ((T*)x)[at] = Raw<DT>::round(y);
-            }
-            __syncwarp();
 #pragma unroll
-            for (int s = 0; s < kOwn; ++s) {
-                const int i = s * 32 + lane;
-                if (i < np) {
-                    const int at = path[i] - u.e0;
-                    if (at >= 0 && at < u.n) ((T*)x)[at] = own[s];
-                }
-            }
-            __syncwarp();
+            for (int o = 0; o < 2; ++o)
+                if (i + 32 * o < to) ((T*)x)[(int)(e[o] & kListPlace) - e0] = Raw<DT>::round(penalised(q, (double)y[o], e[o] >> kListShift, true));
         }
-        if (mask) mask_piece<DT, !kInPlace>(x, u.n, mask, p.words, v, word);
-        if constexpr (!kInPlace) {
-            const int mis = (int)((uintptr_t)u.src & 15u);
-            if (mis == (int)((uintptr_t)u.dst & 15u)) {
-                const int head = min(u.n, mis ? E::EPC - mis / E::ES : 0), nc = (u.n - head) / E::EPC, tail = u.n - head - nc * E::EPC;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0 && nc > 0) {
-                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                                 ::"l"(u.dst + head * E::ES), "r"(smem_u32(buffer + (mis ? 16 : 0))), "r"((unsigned)nc * 16u) : "memory");
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                }
-                if (lane < head + tail) {
-                    const int i = lane < head ? lane : u.n - tail + (lane - head);
-                    ((T*)u.dst)[i] = ((const T*)x)[i];
-                }
-            } else {                                                // rows that start differently: element by element
-                __syncwarp();
-                for (int i = lane; i < u.n; i += 32) ((T*)u.dst)[i] = ((const T*)x)[i];
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            __syncwarp();
-            coming = false;
-            if (k + kAdjustWarps < units) {
-                const Unit next = unit_at(k + kAdjustWarps);
-                if (next.n > 0) coming = fetch(next);
-            }
+        for (int i = sh.from[1][part0] + lane, to = sh.from[1][part1]; i < to; i += 32) {
+            const uint32_t e = biased[i], times = e >> kListShift;
+            const int at = (int)(e & kListPlace) - e0;
+            ((T*)x)[at] = Raw<DT>::round(penalised(q, (double)E::load(x, at), times, times > 0u || (e & kListPrompt)) + (double)sums[i]);
         }
+        __syncwarp();
+#pragma unroll
+        for (int s = 0; s < kOwn; ++s) {
+            const int i = s * 32 + lane;
+            if (i < np && path[i] >= e0 && path[i] < e0 + u.n) ((T*)x)[path[i] - e0] = own[s];
+        }
+        __syncwarp();
+        if (mask) mask_piece<DT, kAdjustPieceBytes>(x, u.n, mask, p.words, u.v, word);
+        deliver_piece<DT>(u, buffer);
+        coming = false;
+        if (k + kAdjustWarps < units) fetch(k + kAdjustWarps);
+    }
+}
+
+// Behind this: the table, the list, the sums of biases, all for kCards places.
+struct AdjustTokensShared {
+    int path_n[kAdjustRows];
+    uint16_t path[kAdjustRows][kMaxPath];      // places of each row's path
+    int from[1][kAdjustWarps + 1];
+    int twice;
+};
+constexpr int kTokensTable = (sizeof(AdjustTokensShared) + 15) & ~15;
+template <int kCards> inline size_t adjust_tokens_smem(bool biased) { return kTokensTable + (size_t)kCards * (biased ? 10 : 6); }
+
+// Single tokens of rows that have been copied and masked: CTA s of the S that share a request and its rows has the tokens t = place * S + s.  CTAs
+// of a cluster, neighbours among the S, share the history.
+template <int DT, int kCards>
+__global__ void __launch_bounds__(kAdjustThreads, 4) adjust_tokens_kernel(AdjustParams p) {
+    using E = Elem<DT>;
+    extern __shared__ __align__(128) unsigned char adjust_smem_raw[];
+    AdjustTokensShared& sh = *reinterpret_cast<AdjustTokensShared*>(adjust_smem_raw);
+    uint32_t* table = reinterpret_cast<uint32_t*>(adjust_smem_raw + kTokensTable);
+    uint16_t* list = reinterpret_cast<uint16_t*>(table + kCards);
+    float* bias_of = reinterpret_cast<float*>(list + kCards);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned S = (unsigned)p.S, bg = blockIdx.x / S, s = blockIdx.x - bg * S;
+    const int b = (int)(bg / (unsigned)p.groups), g = (int)(bg - (unsigned)b * (unsigned)p.groups);
+    const int rank = (int)(s % (unsigned)p.C), step = p.C * kAdjustThreads;
+    AdjustFirst first(p, b, rank * kAdjustThreads + tid, step);
+    const int j0 = g * p.rows_per_cta, j1 = min(first.live, j0 + p.rows_per_cta);
+    if (j0 >= j1) return;                                           // the same for every CTA of a cluster
+    if (tid == 0) sh.twice = 0;
+    if (tid < j1 - j0) sh.path_n[tid] = 0;
+    for (int i = tid; i < kCards / 4; i += kAdjustThreads) reinterpret_cast<uint4*>(table)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (p.C > 1) adjust_cluster_sync();
+    else __syncthreads();
+    auto place = [&](int tok) {
+        if (tok < 0 || tok >= p.V) return -1;
+        const unsigned c = (unsigned)tok / S;
+        return (unsigned)tok - c * S == s ? (int)c : -1;
+    };
+    if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
+    first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
+        if (tok < 0 || tok >= p.V) return;
+        const unsigned c = (unsigned)tok / S, owner = (unsigned)tok - c * S - (s - (unsigned)rank);     // CTA of the cluster, if one of it
+        if (owner < (unsigned)p.C) count_use(&table[c], owner, p.C > 1, i < first.prompt);
+    });
+    if (p.penalised && p.token_ids && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, sh.path[tid], place);
+    if (p.C > 1) adjust_cluster_sync();                             // no CTA counts into another's table from here on
+    else __syncthreads();
+    gather_lists<kCards, false>(table, nullptr, list, nullptr, nullptr, sh.from);
+    __syncthreads();
+    const Penalty q = first.penalty();
+    const int parts = 1 << p.part_shift, n_list = sh.from[0][kAdjustWarps];
+    grid_dependency_wait();                                         // the rows have been copied and masked
+    for (int k = warp; k < (j1 - j0) << p.part_shift; k += kAdjustWarps) {
+        const int row = k >> p.part_shift, part = k & (parts - 1);
+        const int64_t j = j0 + row;
+        const char* x = p.in + ((int64_t)b * p.in_b + j * p.in_row) * E::ES;
+        char* y = p.out + ((int64_t)b * p.out_b + j * p.out_row) * E::ES;
+        const uint32_t* mask = adjust_mask(p, b, (int)j);
+        const uint16_t* path = sh.path[row];
+        const int np = sh.path_n[row];
+        auto replace = [&](int t, uint32_t times, uint32_t uses) {
+            const int64_t v = (int64_t)t * S + s;
+            if (mask && !((mask[v >> 5] >> (v & 31)) & 1u)) return;
+            double z = penalised(q, (double)E::load(x, v), times, times > 0u || (uses & kInPrompt));
+            if (uses & kHasBias) z += (double)bias_of[t];
+            ((typename Raw<DT>::T*)y)[v] = Raw<DT>::round(z);
+        };
+        // one warp a token, in place too: the list's without those of the path, which the row's first warp takes, each once
+        const int to = (int)((int64_t)n_list * (part + 1) >> p.part_shift);
+        for (int i = (int)((int64_t)n_list * part >> p.part_shift) + lane; i < to; i += 32) {
+            const int t = list[i];
+            bool on_path = false;
+            for (int o = 0; o < np; ++o) on_path = on_path || path[o] == t;
+            if (!on_path) replace(t, table[t] / kOnce, table[t]);
+        }
+        if (part == 0)
+            for (int i = lane; i < np; i += 32) {
+                const int t = path[i];
+                uint32_t times = table[t] / kOnce;
+                bool once = true;
+                for (int o = 0; o < np; ++o) {
+                    times += path[o] == t;
+                    once = once && (o >= i || path[o] != t);
+                }
+                if (once) replace(t, times, table[t]);
+            }
     }
 }
 

@@ -14,14 +14,21 @@ static int launched() { return cudaGetLastError() == cudaSuccess ? CADD_OK : CAD
 // Grids that only have to be large enough go by a B200's SMs without asking the device, which small calls would feel.
 constexpr int kSms = 148;
 
+// A launch in clusters, or a plain one; with `overlap`, one that may be set up while the kernel before it still runs (see launch_dependent).
 template <typename P>
-static int launch_cluster(void (*kernel)(P), unsigned grid, unsigned threads, unsigned cluster, size_t smem, cudaStream_t st, const P& p) {
+static int launch_cluster(void (*kernel)(P), unsigned grid, unsigned threads, unsigned cluster, size_t smem, cudaStream_t st, const P& p, bool overlap = false) {
+    if (cluster == 1 && !overlap) {
+        kernel<<<grid, threads, smem, st>>>(p);
+        return launched();
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = overlap ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
         cudaGetLastError();
         return CADD_ERR_LAUNCH;
@@ -49,39 +56,85 @@ static int check_output(int batch, int rows, int64_t V, int dtype, const void* x
 
 // ---------------- penalties, biases, masks ----------------
 
-template <int DT, bool kInPlace>
-static int launch_adjust(AdjustParams& p, cudaStream_t st) {
-    constexpr int tile = kAdjustTile<DT>;
-    p.tiles = (int)((p.V + tile - 1) / tile);
-    // A short history is read by every CTA, a long one shared out over a cluster of them.
-    p.C = 1;
-    if (p.penalised && p.history && p.history_cols > 1024)
-        while (p.C < kAdjustMaxC && p.C < p.tiles) p.C *= 2;
-    const int64_t padded = (int64_t)(p.tiles + p.C - 1) / p.C * p.C;
-    // Rows a CTA: what they have in common is gathered once for all of them, but the device wants CTAs enough.
+template <typename K>
+static int room(K kernel, size_t smem) {
+    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess) return CADD_OK;
+    cudaGetLastError();
+    return CADD_ERR_LAUNCH;
+}
+// Rows a CTA: what they have in common is gathered once for all of them, but the device wants CTAs enough.
+static void group_rows(AdjustParams& p, int64_t ctas_a_group, int part_shift) {
     p.groups = (p.R + kAdjustRows - 1) / kAdjustRows;
-    while (p.batch * padded * p.groups < 4 * kSms && (p.R + p.groups - 1) / p.groups > kAdjustWarps) p.groups *= 2;
+    while (p.batch * ctas_a_group * p.groups < 4 * kSms && (p.R + p.groups - 1) / p.groups > kAdjustWarps) p.groups *= 2;
     p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
     p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
-    p.part_shift = 0;
+    p.part_shift = part_shift;
     while (p.part_shift < 3 && (p.rows_per_cta << p.part_shift) < kAdjustWarps) ++p.part_shift;
-    const int64_t grid = p.batch * padded * p.groups;
+}
+
+// A short history is read by every CTA, a long one shared out over a cluster of them.
+static void share_history(AdjustParams& p, int ctas) {
+    p.C = 1;
+    if (p.penalised && p.history && p.history_cols > 1024)
+        while (p.C < kAdjustMaxC && p.C < ctas) p.C *= 2;
+}
+
+template <int DT, int kCards>
+static int launch_tokens(AdjustParams& p, cudaStream_t st) {
+    p.S = (int)((p.V + kCards - 1) / kCards);
+    share_history(p, p.S);
+    p.S = (p.S + p.C - 1) / p.C * p.C;
+    group_rows(p, p.S, 0);
+    const int64_t grid = (int64_t)p.batch * p.S * p.groups;
     if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
+    const size_t smem = adjust_tokens_smem<kCards>(p.n_bias > 0);
+    const int rc = room(adjust_tokens_kernel<DT, kCards>, smem);
+    if (rc != CADD_OK) return rc;
+    return launch_cluster(adjust_tokens_kernel<DT, kCards>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p, p.followed);
+}
+
+// Rows of a request from which on the tables of adjust_rows_kernel are worth their while; where all its CTAs run at once they
+// always are, since one launch is less than two (one token over 151936: 5.8 us on the device and 15 on the host, against 6.2 and 25).
+constexpr int kFewRows = 8;
+
+template <int DT>
+static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
+    constexpr int tile = kAdjustTile<DT>;
+    p.tiles = (int)((p.V + tile - 1) / tile);
     if (p.status) {
         adjust_status_kernel<<<(unsigned)p.batch, kAdjustThreads, 0, st>>>(p);
         const int rc = launched();
         if (rc != CADD_OK) return rc;
     }
-    const size_t smem = (size_t)adjust_layout(tile, kInPlace, p.penalised || p.n_bias > 0, p.n_bias > 0).bytes;
-    if (cudaFuncSetAttribute((const void*)adjust_kernel<DT, kInPlace>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) {
-        cudaGetLastError();
-        return CADD_ERR_LAUNCH;
+    const bool sparse = p.penalised || p.n_bias > 0;
+    if (sparse && !in_place && (!p.penalised || !p.history || p.history_cols <= kListMost) && (p.R >= kFewRows || (int64_t)p.batch * p.tiles <= 2 * kSms)) {
+        share_history(p, p.tiles);
+        const int64_t padded = (int64_t)(p.tiles + p.C - 1) / p.C * p.C;
+        group_rows(p, padded, kAdjustTileBytes / kAdjustPieceBytes == 2 ? 1 : 0);
+        const int64_t grid = p.batch * padded * p.groups;
+        if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
+        const size_t smem = (size_t)adjust_layout(tile, p.n_bias).bytes;
+        const int rc = room(adjust_rows_kernel<DT>, smem);
+        if (rc != CADD_OK) return rc;
+        return launch_cluster(adjust_rows_kernel<DT>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p);
     }
-    if (p.C == 1) {
-        adjust_kernel<DT, kInPlace><<<(unsigned)grid, kAdjustThreads, smem, st>>>(p);
-        return launched();
+    if (!in_place || p.allowed) {
+        p.followed = sparse;
+        const int64_t units = (int64_t)p.batch * p.R * p.tiles;
+        int rc = CADD_OK;
+        if (in_place) {
+            const int64_t most = kSms * 4;
+            adjust_stream_kernel<DT, false><<<(unsigned)(units < most ? units : most), kAdjustThreads, 0, st>>>(p);
+        } else {
+            const size_t smem = (size_t)kAdjustWarps * kAdjustBuffer<kAdjustTileBytes>;
+            const int64_t most = kSms * 3;
+            if ((rc = room(adjust_stream_kernel<DT, true>, smem)) != CADD_OK) return rc;
+            adjust_stream_kernel<DT, true><<<(unsigned)(units < most ? units : most), kAdjustThreads, smem, st>>>(p);
+        }
+        if ((rc = launched()) != CADD_OK) return rc;
     }
-    return launch_cluster(adjust_kernel<DT, kInPlace>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p);
+    if (!sparse) return CADD_OK;
+    return launch_tokens<DT, 4096>(p, st);
 }
 
 // ---------------- distillation ----------------
@@ -170,7 +223,7 @@ int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream) {
     p.V = a->V; p.in_b = a->stride_b; p.in_row = a->stride_row; p.out_b = a->out_stride_b; p.out_row = a->out_stride_row;
     p.batch = a->batch; p.R = a->R;
     p.n_bias = a->n_bias; p.history_cols = a->history_cols; p.n_allowed = a->n_allowed; p.words = (int)((a->V + 31) / 32);
-    p.in_place = in_place;
+    p.followed = false;
     p.penalised = a->repetition || a->presence || a->frequency;
     p.n_nodes = a->n_nodes; p.token_ids = a->token_ids; p.parent_idx = a->parent_idx;
     p.history = a->history; p.history_len = a->history_len; p.prompt_len = a->prompt_len; p.history_stride = a->history_stride;
@@ -178,8 +231,7 @@ int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream) {
     p.repetition = a->repetition; p.presence = a->presence; p.frequency = a->frequency;
     p.status = a->status;
     p.drop = (a->flags & CADD_FLAG_TEST_DROP_TILE) ? 1 : 0;
-    if (a->logits_dtype == CADD_DTYPE_BF16) return in_place ? launch_adjust<CADD_DTYPE_BF16, true>(p, st) : launch_adjust<CADD_DTYPE_BF16, false>(p, st);
-    return in_place ? launch_adjust<CADD_DTYPE_FP32, true>(p, st) : launch_adjust<CADD_DTYPE_FP32, false>(p, st);
+    return a->logits_dtype == CADD_DTYPE_BF16 ? launch_adjust<CADD_DTYPE_BF16>(p, in_place, st) : launch_adjust<CADD_DTYPE_FP32>(p, in_place, st);
 }
 
 int cadd_distill_loss(const cadd_distill_args* a, void* cuda_stream) { return distill(a, true, (cudaStream_t)cuda_stream); }

@@ -260,11 +260,14 @@ def test_refusals_of_the_binding():
 def test_wait_that_runs_out():
     """Copies that are never made: NaN and the status bit, and the next call is right (nothing hangs or faults)."""
     a = random_adjust(2, 9, 9000, torch.bfloat16, seed=5, dead=False)
-    x, st = a.logits.cuda(), torch.zeros(2, dtype=torch.int32, device="cuda")
-    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE, **a.args("cuda"))
+    x, st, kw = a.logits.cuda(), torch.zeros(2, dtype=torch.int32, device="cuda"), a.args("cuda")
+    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE, **kw)
     torch.cuda.synchronize()
     assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(out).all())
     both(a)
+    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE, allowed=kw["allowed"], allowed_row=kw["allowed_row"])
+    torch.cuda.synchronize()
+    assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(out).all())
 
 
 @pytest.mark.parametrize("V,history", [(4097, 1025), (40000, 3000), (2048 * 9, 5000)])
