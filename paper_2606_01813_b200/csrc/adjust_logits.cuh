@@ -23,7 +23,7 @@ constexpr int kAdjustThreads = 256;
 constexpr int kAdjustWarps = kAdjustThreads / 32;
 constexpr int kAdjustTileBytes = 8192;         // of a row: the tokens whose tables a CTA of adjust_rows_kernel has; a piece of adjust_stream_kernel
 constexpr int kAdjustPieceBytes = 4096;        // of a row: a piece of adjust_rows_kernel
-constexpr int kAdjustRows = 32;                // rows a CTA takes at most
+constexpr int kAdjustRows = 36;                // rows a CTA takes at most (trees have a power of two of nodes and the root: 65 rows are two CTAs')
 constexpr int kAdjustMaxC = 8;                 // CTAs that share a history
 constexpr int kAdjustBatch = 4;                // tokens of the history that a thread has under way
 constexpr int kMaxPath = 65;                   // nodes of a path: the deepest tree there is, and its root
@@ -233,11 +233,23 @@ __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint
         bias_of[t] = (float)s;
     }
 }
-// Places of the tokens on row j's path, the row's own first; returns how many.  One thread.
-template <typename Place>
-__device__ __forceinline__ int gather_path(const AdjustParams& p, int b, int j, uint16_t* path, Place place) {
+// Rows 0 .. n-1 of a request's tree brought to shared memory (n tokens, then n parents), where there is room: a path is a chain of
+// loads, each of them a round trip to memory otherwise.
+__device__ __forceinline__ void stage_tree(const AdjustParams& p, int b, int n, int32_t* stage, int room) {
+    if (2 * n > room) return;
     const int32_t* tok = p.token_ids + (int64_t)b * p.R;
     const int32_t* par = p.parent_idx + (int64_t)b * p.R;
+    for (int i = threadIdx.x; i < n; i += kAdjustThreads) {
+        stage[i] = tok[i];
+        stage[n + i] = par[i];
+    }
+}
+// Places of the tokens on row j's path (j < n), the row's own first; returns how many.  One thread.
+template <typename Place>
+__device__ __forceinline__ int gather_path(const AdjustParams& p, int b, int j, int n, const int32_t* stage, int room, uint16_t* path, Place place) {
+    const bool staged = 2 * n <= room;
+    const int32_t* tok = staged ? stage : p.token_ids + (int64_t)b * p.R;
+    const int32_t* par = staged ? stage + n : p.parent_idx + (int64_t)b * p.R;
     int k = 0;
     for (int step = 0; step < kMaxPath; ++step) {
         const int t = place(tok[j]), up = par[j];
@@ -487,10 +499,6 @@ __global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 4) adjust_stream_k
     }
 }
 
-__device__ __forceinline__ void adjust_cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 template <int DT>
 __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustParams p) {
     using E = Elem<DT>;
@@ -551,11 +559,15 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
     if (tid < j1 - j0) sh.path_n[tid] = 0;
     uint4* t4 = reinterpret_cast<uint4*>(table);
     for (int i = tid; i < kTile / 4; i += kAdjustThreads) t4[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (p.C > 1) adjust_cluster_sync();
-    else __syncthreads();
+    const bool paths = p.penalised && p.token_ids;
+    int32_t* stage = reinterpret_cast<int32_t*>(plain);             // (the list comes later)
+    if (paths) stage_tree(p, b, j1, stage, kTile);
+    if (p.C > 1) cluster_arrive();
+    __syncthreads();
     // (a token's place in the tile, or -1)
     auto place = [&](int tok) { return tok >= v0 && tok < v0 + n ? (int)(tok - v0) : -1; };
     if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
+    if (p.C > 1) cluster_wait();                                    // every table is clear
     const int64_t base = v0 - (int64_t)rank * kTile;                // first token of the cluster's tiles
     first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
         const int64_t t64 = (int64_t)tok - base;
@@ -563,9 +575,10 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
         const uint32_t t = (uint32_t)t64;
         count_use(&table[t % kTile], t / kTile, p.C > 1, i < first.prompt);
     });
-    if (p.penalised && p.token_ids && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, sh.path[tid], place);
-    if (p.C > 1) adjust_cluster_sync();                         // no CTA counts into another's table from here on
-    else __syncthreads();
+    if (p.C > 1) cluster_arrive();
+    if (paths && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, j1, stage, kTile, sh.path[tid], place);
+    if (p.C > 1) cluster_wait();                                    // no CTA counts into another's table from here on
+    __syncthreads();
     gather_lists<kTile, true>(table, bias_of, plain, biased, sums, sh.from);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the tables' place becomes the buffers
     __syncthreads();
@@ -663,22 +676,27 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_tokens_kernel(Adjust
     if (tid == 0) sh.twice = 0;
     if (tid < j1 - j0) sh.path_n[tid] = 0;
     for (int i = tid; i < kCards / 4; i += kAdjustThreads) reinterpret_cast<uint4*>(table)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (p.C > 1) adjust_cluster_sync();
-    else __syncthreads();
+    const bool paths = p.penalised && p.token_ids;
+    int32_t* stage = reinterpret_cast<int32_t*>(list);              // (the list comes later)
+    if (paths) stage_tree(p, b, j1, stage, kCards / 2);
+    if (p.C > 1) cluster_arrive();
+    __syncthreads();
     auto place = [&](int tok) {
         if (tok < 0 || tok >= p.V) return -1;
         const unsigned c = (unsigned)tok / S;
         return (unsigned)tok - c * S == s ? (int)c : -1;
     };
     if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
+    if (p.C > 1) cluster_wait();                                    // every table is clear
     first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
         if (tok < 0 || tok >= p.V) return;
         const unsigned c = (unsigned)tok / S, owner = (unsigned)tok - c * S - (s - (unsigned)rank);     // CTA of the cluster, if one of it
         if (owner < (unsigned)p.C) count_use(&table[c], owner, p.C > 1, i < first.prompt);
     });
-    if (p.penalised && p.token_ids && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, sh.path[tid], place);
-    if (p.C > 1) adjust_cluster_sync();                             // no CTA counts into another's table from here on
-    else __syncthreads();
+    if (p.C > 1) cluster_arrive();
+    if (paths && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, j1, stage, kCards / 2, sh.path[tid], place);
+    if (p.C > 1) cluster_wait();                                    // no CTA counts into another's table from here on
+    __syncthreads();
     gather_lists<kCards, false>(table, nullptr, list, nullptr, nullptr, sh.from);
     __syncthreads();
     const Penalty q = first.penalty();

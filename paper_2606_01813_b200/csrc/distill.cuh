@@ -69,8 +69,6 @@ __host__ __device__ inline size_t distill_first_bytes(int chunks) { return (((si
 __host__ __device__ inline size_t distill_shared_bytes() { return (sizeof(DistillShared) + 127) & ~(size_t)127; }
 inline size_t distill_smem_bytes(int chunks, int room) { return distill_shared_bytes() + distill_first_bytes(chunks) + (size_t)room * 16; }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_address(const void* p, unsigned rank) {
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
