@@ -1,18 +1,15 @@
 // Penalties, biases and grammar masks on the logits of a tree's rows (cadd_adjust_args has the definition).
 //
 // adjust_rows_kernel, into another array.  A CTA takes a tile of consecutive tokens (8 KB of logits) of some rows of one request.  It
-// first gathers what its tokens have in common over the rows: how often each stands in the history (a table in shared memory), the
-// sum of its biases, and a list of the tokens with either, in order.  A history is as long as many tiles, so the CTAs of a cluster,
-// consecutive tiles of the same rows, share it: each reads a part and counts into the tables of all (distributed shared memory).
-// Then a warp takes a row's piece of the tile at a time: it comes to shared memory by a bulk copy, the tokens that penalties or
-// biases concern are replaced there, what the mask hides is set, and a bulk copy takes it to its place; the copy of the warp's
-// first piece is under way from the start.  Tokens of a row's own path are computed before the list's and written after
-// them, from the input's value and their own count.
+// first gathers what its tokens have in common over the rows: how often each stands in the history (a table in shared memory; every
+// CTA reads the whole history, which stays in L2), the sum of its biases, and from that a list of the tokens with either, in order.  Then
+// a warp takes a row's piece of the tile at a time: it comes to shared memory by a bulk copy, the tokens that penalties or biases
+// concern are replaced there, what the mask hides is set, and a bulk copy takes it to its place.  Tokens of a row's own path are
+// computed before the list's and written after them, from the input's value and their own count.
 //
-// With few rows the table is not worth its while for every tile: then that kernel only copies and masks, and
-// adjust_tokens_kernel replaces single tokens in memory afterwards.  In place it is the same with adjust_mask_kernel, which
-// writes (and reads) only what masks change.  adjust_tokens_kernel deals the vocabulary out to its CTAs like cards (token t to CTA t % S), since the
-// tokens that come up are the frequent ones, whose numbers lie together; its tables fill while the kernel before it still runs.
+// With few rows a table for every tile is not worth its while: then adjust_stream_kernel copies and masks, and adjust_tokens_kernel
+// replaces single tokens in memory afterwards, a CTA for all tokens of a request (a hash table in shared memory, which fills
+// while the kernel before it still runs).  In place it is the same; there the former writes (and reads) only what masks change.
 #pragma once
 #include "common.cuh"
 #include "tile_ring.cuh"
@@ -24,8 +21,7 @@ constexpr int kAdjustWarps = kAdjustThreads / 32;
 constexpr int kAdjustTileBytes = 8192;         // of a row: the tokens whose tables a CTA of adjust_rows_kernel has; a piece of adjust_stream_kernel
 constexpr int kAdjustPieceBytes = 4096;        // of a row: a piece of adjust_rows_kernel
 constexpr int kAdjustRows = 36;                // rows a CTA takes at most (trees have a power of two of nodes and the root: 65 rows are two CTAs')
-constexpr int kAdjustMaxC = 8;                 // CTAs that share a history
-constexpr int kAdjustBatch = 4;                // tokens of the history that a thread has under way
+constexpr int kAdjustBatch = 8;                // tokens of the history that a thread has under way
 constexpr int kMaxPath = 65;                   // nodes of a path: the deepest tree there is, and its root
 constexpr uint32_t kInPrompt = 1u, kHasBias = 2u, kOnce = 4u;      // a token's word in the table: two flags, then n_out of the history
 
@@ -33,8 +29,8 @@ struct AdjustParams {
     const char* in;
     char* out;
     int64_t V, in_b, in_row, out_b, out_row;
-    int batch, R, tiles, groups, rows_per_cta, part_shift, C;      // pieces of a row's tile: 1 << part_shift
-    int S;                                                          // adjust_tokens_kernel: CTAs that share a request's vocabulary, a multiple of C
+    int batch, R, tiles, groups, rows_per_cta, part_shift;         // pieces of a row's tile: 1 << part_shift
+    int S, slots, slot_shift;                                       // adjust_tokens_kernel: CTAs that share a request's tokens (token t: CTA t % S); 1 << (32 - slot_shift) slots
     int n_bias, history_cols, n_allowed, words;
     bool penalised;
     bool followed;                                                  // adjust_tokens_kernel comes next
@@ -196,24 +192,16 @@ __device__ __forceinline__ void mask_piece(char* x, int n, const uint32_t* mask,
     }
 }
 
-// One use of a token more in the table of CTA `rank` of the cluster, or in this CTA's own (shared false).
-__device__ __forceinline__ void count_use(uint32_t* word, uint32_t rank, bool shared, bool in_prompt) {
-    if (!shared) {
-        if (in_prompt) atomicOr(word, kInPrompt);
-        else atomicAdd(word, kOnce);
-    } else {
-        uint32_t a;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(word)), "r"(rank));
-        if (in_prompt) asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(a), "r"(kInPrompt) : "memory");
-        else asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(a), "r"(kOnce) : "memory");
-    }
+__device__ __forceinline__ void count_use(uint32_t* word, bool in_prompt) {
+    if (in_prompt) atomicOr(word, kInPrompt);
+    else atomicAdd(word, kOnce);
 }
 // Sums of the biases of the tokens that have a place here (place(token) >= 0), marked in the table.
-template <typename Place>
+template <int kThreadsHere, typename Place>
 __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint32_t* table, float* bias_of, int* twice, Place place) {
     const int32_t* at = p.bias_token + (int64_t)b * p.n_bias;
     const float* val = p.bias + (int64_t)b * p.n_bias;
-    for (int i = threadIdx.x; i < p.n_bias; i += kAdjustThreads) {
+    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {
         const int t = place(at[i]);
         if (t < 0) continue;
         if (atomicOr(&table[t], kHasBias) & kHasBias) *twice = 1;
@@ -221,7 +209,7 @@ __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint
     }
     __syncthreads();
     if (!*twice) return;
-    for (int i = threadIdx.x; i < p.n_bias; i += kAdjustThreads) {  // a token's first entry adds up all of them, in their order
+    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {  // a token's first entry adds up all of them, in their order
         const int t = place(at[i]);
         if (t < 0) continue;
         bool once = true;
@@ -235,11 +223,12 @@ __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint
 }
 // Rows 0 .. n-1 of a request's tree brought to shared memory (n tokens, then n parents), where there is room: a path is a chain of
 // loads, each of them a round trip to memory otherwise.
+template <int kThreadsHere>
 __device__ __forceinline__ void stage_tree(const AdjustParams& p, int b, int n, int32_t* stage, int room) {
     if (2 * n > room) return;
     const int32_t* tok = p.token_ids + (int64_t)b * p.R;
     const int32_t* par = p.parent_idx + (int64_t)b * p.R;
-    for (int i = threadIdx.x; i < n; i += kAdjustThreads) {
+    for (int i = threadIdx.x; i < n; i += kThreadsHere) {
         stage[i] = tok[i];
         stage[n + i] = par[i];
     }
@@ -247,7 +236,7 @@ __device__ __forceinline__ void stage_tree(const AdjustParams& p, int b, int n, 
 // Places of the tokens on row j's path (j < n), the row's own first; returns how many.  One thread.
 template <typename Place>
 __device__ __forceinline__ int gather_path(const AdjustParams& p, int b, int j, int n, const int32_t* stage, int room, uint16_t* path, Place place) {
-    const bool staged = 2 * n <= room;
+    const bool staged = room > 0 && 2 * n <= room;
     const int32_t* tok = staged ? stage : p.token_ids + (int64_t)b * p.R;
     const int32_t* par = staged ? stage + n : p.parent_idx + (int64_t)b * p.R;
     int k = 0;
@@ -259,79 +248,68 @@ __device__ __forceinline__ int gather_path(const AdjustParams& p, int b, int j, 
     }
     return k;
 }
-// Number of set bits, over the lanes before this one, of a four-bit mask that each lane has.
-__device__ __forceinline__ int before_lane(uint32_t m) {
-    const uint32_t lower = (1u << (threadIdx.x & 31)) - 1u;
-    int n = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) n += __popc(__ballot_sync(kFullMask, (m >> j) & 1u) & lower);
-    return n;
-}
 __device__ __forceinline__ uint32_t four(const uint4& w, int j) { return j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w; }
-// The lists from the table (whole CTA; warp w has the w-th eighth of the places).  With kWords the entries are words as described at
-// kListPlace, those with a bias in a list of their own; otherwise all are places in one list.
-template <int kPlaces, bool kWords>
-__device__ __forceinline__ void gather_lists(const uint32_t* table, const float* bias_of, void* plain, uint32_t* biased, float* sums, int (*from)[kAdjustWarps + 1]) {
+// The lists from the table (whole CTA; warp w has the w-th eighth of the places); from[0], from[1]: the entries without and with a bias
+// of each eighth.
+template <int kPlaces>
+__device__ __forceinline__ void gather_lists(const uint32_t* table, const float* bias_of, uint32_t* plain, uint32_t* biased, float* sums, int (*from)[kAdjustWarps + 1]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kEighth = kPlaces / kAdjustWarps, kSteps = kEighth / 128;
-    uint4 w[kSteps];
-    int n = 0, n2 = 0;
+    // entries among a lane's four places: without a bias, and with one (from bit 16 on; at most 4096 in all: no carry)
+    auto kinds = [](const uint4& w) {
+        uint32_t n = 0;
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-        w[k] = reinterpret_cast<const uint4*>(table)[(warp * kEighth) / 4 + k * 32 + lane];
+        for (int j = 0; j < 4; ++j) n += four(w, j) == 0u ? 0u : (four(w, j) & kHasBias ? 0x10000u : 1u);
+        return n;
+    };
+    const uint4* mine = reinterpret_cast<const uint4*>(table) + warp * (kEighth / 4) + lane;
+    uint32_t all = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x = four(w[k], j);
-            const bool two = kWords && (x & kHasBias);
-            n += x != 0u && !two;
-            n2 += two;
-        }
-    }
-    n = __reduce_add_sync(kFullMask, n);
-    if (kWords) n2 = __reduce_add_sync(kFullMask, n2);
-    if (lane == 0) { from[0][warp + 1] = n; if (kWords) from[1][warp + 1] = n2; }
+    for (int k = 0; k < kSteps; ++k) all += kinds(mine[k * 32]);
+    all = __reduce_add_sync(kFullMask, all);
+    if (lane == 0) { from[0][warp + 1] = (int)(all & 0xffffu); from[1][warp + 1] = (int)(all >> 16); }
     __syncthreads();
-    int at = 0, at2 = 0, all = 0, all2 = 0;
+    uint32_t at = 0, upto = 0;
 #pragma unroll
     for (int k = 0; k < kAdjustWarps; ++k) {
-        if (k == warp) { at = all; at2 = all2; }
-        all += from[0][k + 1];
-        if (kWords) all2 += from[1][k + 1];
+        const uint32_t c = (uint32_t)from[0][k + 1] | (uint32_t)from[1][k + 1] << 16;
+        upto += k <= warp ? c : 0u;
+        at += k < warp ? c : 0u;
     }
-    __syncthreads();                                                // (everybody has read the counts, and, of the table, what becomes the lists)
+    __syncthreads();                                                // (everybody has read the counts)
     if (lane == 0) {
-        from[0][warp + 1] = at + n;
-        if (kWords) from[1][warp + 1] = at2 + n2;
-        if (warp == 0) { from[0][0] = 0; if (kWords) from[1][0] = 0; }
+        from[0][warp + 1] = (int)(upto & 0xffffu);
+        from[1][warp + 1] = (int)(upto >> 16);
+        if (warp == 0) from[0][0] = from[1][0] = 0;
     }
+#pragma unroll 1
+    for (int k = 0; k < kSteps; ++k) {                              // (rolled: code that runs once has to be fetched once)
+        const uint4 w = mine[k * 32];
+        const uint32_t n4 = kinds(w);
+        if (!__any_sync(kFullMask, n4 != 0u)) continue;
+        uint32_t to = n4;
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-        uint32_t m = 0, m2 = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x = four(w[k], j);
-            const bool two = kWords && (x & kHasBias);
-            m |= (x != 0u && !two ? 1u : 0u) << j;
-            m2 |= (two ? 1u : 0u) << j;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t up = __shfl_up_sync(kFullMask, to, o);
+            if (lane >= o) to += up;
         }
-        int to = at + before_lane(m), to2 = at2;
-        if (kWords) to2 += before_lane(m2);
+        const uint32_t total = __shfl_sync(kFullMask, to, 31);
+        to += at - n4;
+        at += total;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t x = four(w[k], j);
+            const uint32_t x = four(w, j);
+            if (x == 0u) continue;
             const int place = warp * kEighth + k * 128 + lane * 4 + j;
             const uint32_t word = (uint32_t)place | (x & kInPrompt ? kListPrompt : 0u) | (x / kOnce) << kListShift;
-            if ((m >> j) & 1u) {
-                if constexpr (kWords) ((uint32_t*)plain)[to++] = word;
-                else ((uint16_t*)plain)[to++] = (uint16_t)place;
-            }
-            if (kWords && ((m2 >> j) & 1u)) {
-                biased[to2] = word;
-                sums[to2++] = bias_of[place];
+            if (x & kHasBias) {
+                biased[to >> 16] = word;
+                sums[to >> 16] = bias_of[place];
+                to += 0x10000u;
+            } else {
+                plain[to++ & 0xffffu] = word;
             }
         }
-        at += __popc(__ballot_sync(kFullMask, m & 1u)) + __popc(__ballot_sync(kFullMask, m & 2u)) + __popc(__ballot_sync(kFullMask, m & 4u)) + __popc(__ballot_sync(kFullMask, m & 8u));
-        if (kWords) at2 += __popc(__ballot_sync(kFullMask, m2 & 1u)) + __popc(__ballot_sync(kFullMask, m2 & 2u)) + __popc(__ballot_sync(kFullMask, m2 & 4u)) + __popc(__ballot_sync(kFullMask, m2 & 8u));
     }
 }
 // Where an ordered list of words has a place between from and to, or -1.
@@ -345,11 +323,12 @@ __device__ __forceinline__ int find_place(const uint32_t* list, int from, int to
     return -1;
 }
 // What a CTA asks memory for first, all at once: each of these would cost a round trip where it is needed.
+template <int kThreadsHere>
 struct AdjustFirst {
     float rep, pres, freq;
     int live, len, prompt;
-    int tok[kAdjustBatch];                     // the thread's first tokens of the history, from `at` on, `step` apart (-1 behind its room)
-    __device__ __forceinline__ AdjustFirst(const AdjustParams& p, int b, int at, int step) {
+    int tok[kAdjustBatch];                     // the thread's first tokens of the history (-1 behind its room)
+    __device__ __forceinline__ AdjustFirst(const AdjustParams& p, int b) {
         const int32_t* h = p.history + (int64_t)b * p.history_stride;
         const bool history = p.penalised && p.history;
         rep = p.repetition ? p.repetition[b] : 1.0f;
@@ -358,30 +337,32 @@ struct AdjustFirst {
         len = prompt = 0;
         if (history) len = adjust_history(p, b, &prompt);
 #pragma unroll
-        for (int u = 0; u < kAdjustBatch; ++u) tok[u] = history && at + u * step < p.history_cols ? h[at + u * step] : -1;
+        for (int u = 0; u < kAdjustBatch; ++u) {
+            const int at = (int)threadIdx.x + u * kThreadsHere;
+            tok[u] = history && at < p.history_cols ? h[at] : -1;
+        }
         live = adjust_live(p, b);
     }
     __device__ __forceinline__ Penalty penalty() const { return Penalty{(double)rep, 1.0 / (double)rep, (double)pres, (double)freq}; }
     // count(i, token) for all of the thread's part of the history; more is asked for while a batch is counted
     template <typename Count>
-    __device__ __forceinline__ void for_history(const AdjustParams& p, int b, int at, int step, Count count) {
+    __device__ __forceinline__ void for_history(const AdjustParams& p, int b, Count count) {
         const int32_t* h = p.history + (int64_t)b * p.history_stride;
-        while (at < len) {
+#pragma unroll 1
+        for (int at = threadIdx.x; at < len; at += kAdjustBatch * kThreadsHere) {
             int now[kAdjustBatch];
 #pragma unroll
             for (int u = 0; u < kAdjustBatch; ++u) {
-                const int next = at + (kAdjustBatch + u) * step;
+                const int next = at + (kAdjustBatch + u) * kThreadsHere;
                 now[u] = tok[u];
                 tok[u] = next < len ? h[next] : -1;
             }
 #pragma unroll
             for (int u = 0; u < kAdjustBatch; ++u)
-                if (at + u * step < len) count(at + u * step, now[u]);
-            at += kAdjustBatch * step;
+                if (at + u * kThreadsHere < len) count(at + u * kThreadsHere, now[u]);
         }
     }
 };
-
 // A piece of a row that a warp takes at a time: n elements from token v on (a multiple of 32).
 struct AdjustPiece {
     char *src, *dst;
@@ -453,7 +434,7 @@ __device__ __forceinline__ void mask_words(const uint32_t* mask, const AdjustPie
 // Logits without penalties and biases, or before them: copied (kCopy) and masked.  A warp takes pieces of 8 KB, all of them dealt out to the CTAs
 // first, then to their warps, so that few pieces have SMs to themselves.
 template <int DT, bool kCopy>
-__global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 4) adjust_stream_kernel(AdjustParams p) {
+__global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 6) adjust_stream_kernel(AdjustParams p) {
     using E = Elem<DT>;
     constexpr int kTile = kAdjustTile<DT>;
     extern __shared__ __align__(128) unsigned char adjust_smem_raw[];
@@ -513,16 +494,14 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
     uint32_t* biased = reinterpret_cast<uint32_t*>(adjust_smem_raw + lay.biased);
     float* sums = reinterpret_cast<float*>(adjust_smem_raw + lay.sums);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned padded = (unsigned)((p.tiles + p.C - 1) / p.C * p.C);
-    const unsigned bg = blockIdx.x / padded;
-    const int tile = (int)(blockIdx.x - bg * padded);
+    const unsigned bg = blockIdx.x / (unsigned)p.tiles;
+    const int tile = (int)(blockIdx.x - bg * (unsigned)p.tiles);
     const int b = (int)(bg / (unsigned)p.groups), g = (int)(bg - (unsigned)b * (unsigned)p.groups);
-    const int rank = (int)((unsigned)tile % (unsigned)p.C), step = p.C * kAdjustThreads;
-    AdjustFirst first(p, b, rank * kAdjustThreads + tid, step);
+    AdjustFirst<kAdjustThreads> first(p, b);
     const int j0 = g * p.rows_per_cta, j1 = min(first.live, j0 + p.rows_per_cta);
-    if (j0 >= j1) return;                                           // the same for every CTA of a cluster
+    if (j0 >= j1) return;
     const int64_t v0 = (int64_t)tile * kTile;
-    const int n = (int)max((int64_t)0, min((int64_t)kTile, p.V - v0));     // 0: a CTA that only helps with the history
+    const int n = (int)min((int64_t)kTile, p.V - v0);
     const int parts = 1 << p.part_shift, piece = kTile >> p.part_shift;
     const int units = (j1 - j0) << p.part_shift;                   // a row's pieces one after the other
 
@@ -561,25 +540,18 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
     for (int i = tid; i < kTile / 4; i += kAdjustThreads) t4[i] = make_uint4(0u, 0u, 0u, 0u);
     const bool paths = p.penalised && p.token_ids;
     int32_t* stage = reinterpret_cast<int32_t*>(plain);             // (the list comes later)
-    if (paths) stage_tree(p, b, j1, stage, kTile);
-    if (p.C > 1) cluster_arrive();
+    if (paths) stage_tree<kAdjustThreads>(p, b, j1, stage, kTile);
     __syncthreads();
     // (a token's place in the tile, or -1)
     auto place = [&](int tok) { return tok >= v0 && tok < v0 + n ? (int)(tok - v0) : -1; };
-    if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
-    if (p.C > 1) cluster_wait();                                    // every table is clear
-    const int64_t base = v0 - (int64_t)rank * kTile;                // first token of the cluster's tiles
-    first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
-        const int64_t t64 = (int64_t)tok - base;
-        if (t64 < 0 || t64 >= (int64_t)p.C * kTile || tok >= p.V) return;
-        const uint32_t t = (uint32_t)t64;
-        count_use(&table[t % kTile], t / kTile, p.C > 1, i < first.prompt);
+    if (p.n_bias > 0) gather_biases<kAdjustThreads>(p, b, table, bias_of, &sh.twice, place);
+    first.for_history(p, b, [&](int i, int tok) {
+        const int t = place(tok);
+        if (t >= 0) count_use(&table[t], i < first.prompt);
     });
-    if (p.C > 1) cluster_arrive();
     if (paths && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, j1, stage, kTile, sh.path[tid], place);
-    if (p.C > 1) cluster_wait();                                    // no CTA counts into another's table from here on
     __syncthreads();
-    gather_lists<kTile, true>(table, bias_of, plain, biased, sums, sh.from);
+    gather_lists<kTile>(table, bias_of, plain, biased, sums, sh.from);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");    // the tables' place becomes the buffers
     __syncthreads();
     // ---- the rows ----
@@ -646,96 +618,105 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
     }
 }
 
-// Behind this: the table, the list, the sums of biases, all for kCards places.
+constexpr int kTokensThreads = 1024;
+constexpr int kTokensSlots = 16384;            // of the hash table at most
+constexpr int kTokensMost = 12288;             // tokens in it at most
+constexpr int32_t kNoToken = -1;
+// Behind this, for every slot: token, word, and the sum of its biases (where there are biases).
 struct AdjustTokensShared {
     int path_n[kAdjustRows];
-    uint16_t path[kAdjustRows][kMaxPath];      // places of each row's path
-    int from[1][kAdjustWarps + 1];
+    uint16_t path[kAdjustRows][kMaxPath];      // slots of each row's path
     int twice;
 };
 constexpr int kTokensTable = (sizeof(AdjustTokensShared) + 15) & ~15;
-template <int kCards> inline size_t adjust_tokens_smem(bool biased) { return kTokensTable + (size_t)kCards * (biased ? 10 : 6); }
+inline size_t adjust_tokens_smem(int slots, bool biased) { return kTokensTable + (size_t)slots * (biased ? 12 : 8); }
 
-// Single tokens of rows that have been copied and masked: CTA s of the S that share a request and its rows has the tokens t = place * S + s.  CTAs
-// of a cluster, neighbours among the S, share the history.
-template <int DT, int kCards>
-__global__ void __launch_bounds__(kAdjustThreads, 4) adjust_tokens_kernel(AdjustParams p) {
+// Single tokens of rows that have been copied and masked.  Every token that the history, biases or paths of the CTA's rows hold (and
+// that is this CTA's among the S) gets a slot; there are more slots than such tokens, so a search ends.
+template <int DT>
+__global__ void __launch_bounds__(kTokensThreads) adjust_tokens_kernel(AdjustParams p) {
     using E = Elem<DT>;
+    using T = typename Raw<DT>::T;
     extern __shared__ __align__(128) unsigned char adjust_smem_raw[];
     AdjustTokensShared& sh = *reinterpret_cast<AdjustTokensShared*>(adjust_smem_raw);
-    uint32_t* table = reinterpret_cast<uint32_t*>(adjust_smem_raw + kTokensTable);
-    uint16_t* list = reinterpret_cast<uint16_t*>(table + kCards);
-    float* bias_of = reinterpret_cast<float*>(list + kCards);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int32_t* token = reinterpret_cast<int32_t*>(adjust_smem_raw + kTokensTable);
+    uint32_t* table = reinterpret_cast<uint32_t*>(token + p.slots);
+    float* bias_of = reinterpret_cast<float*>(table + p.slots);
+    const int tid = threadIdx.x;
     const unsigned S = (unsigned)p.S, bg = blockIdx.x / S, s = blockIdx.x - bg * S;
     const int b = (int)(bg / (unsigned)p.groups), g = (int)(bg - (unsigned)b * (unsigned)p.groups);
-    const int rank = (int)(s % (unsigned)p.C), step = p.C * kAdjustThreads;
-    AdjustFirst first(p, b, rank * kAdjustThreads + tid, step);
+    AdjustFirst<kTokensThreads> first(p, b);
     const int j0 = g * p.rows_per_cta, j1 = min(first.live, j0 + p.rows_per_cta);
-    if (j0 >= j1) return;                                           // the same for every CTA of a cluster
+    if (j0 >= j1) return;
     if (tid == 0) sh.twice = 0;
     if (tid < j1 - j0) sh.path_n[tid] = 0;
-    for (int i = tid; i < kCards / 4; i += kAdjustThreads) reinterpret_cast<uint4*>(table)[i] = make_uint4(0u, 0u, 0u, 0u);
-    const bool paths = p.penalised && p.token_ids;
-    int32_t* stage = reinterpret_cast<int32_t*>(list);              // (the list comes later)
-    if (paths) stage_tree(p, b, j1, stage, kCards / 2);
-    if (p.C > 1) cluster_arrive();
+    for (int i = tid; i < p.slots / 4; i += kTokensThreads) {
+        reinterpret_cast<int4*>(token)[i] = make_int4(kNoToken, kNoToken, kNoToken, kNoToken);
+        reinterpret_cast<uint4*>(table)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
     __syncthreads();
     auto place = [&](int tok) {
         if (tok < 0 || tok >= p.V) return -1;
-        const unsigned c = (unsigned)tok / S;
-        return (unsigned)tok - c * S == s ? (int)c : -1;
+        if (S > 1 && (unsigned)tok % S != s) return -1;
+        for (int slot = (int)(((unsigned)tok * 2654435769u) >> p.slot_shift);; slot = (slot + 1) & (p.slots - 1)) {
+            const int32_t had = atomicCAS(&token[slot], kNoToken, tok);
+            if (had == kNoToken || had == tok) return slot;
+        }
     };
-    if (p.n_bias > 0) gather_biases(p, b, table, bias_of, &sh.twice, place);
-    if (p.C > 1) cluster_wait();                                    // every table is clear
-    first.for_history(p, b, rank * kAdjustThreads + tid, step, [&](int i, int tok) {
-        if (tok < 0 || tok >= p.V) return;
-        const unsigned c = (unsigned)tok / S, owner = (unsigned)tok - c * S - (s - (unsigned)rank);     // CTA of the cluster, if one of it
-        if (owner < (unsigned)p.C) count_use(&table[c], owner, p.C > 1, i < first.prompt);
+    if (p.n_bias > 0) gather_biases<kTokensThreads>(p, b, table, bias_of, &sh.twice, place);
+    first.for_history(p, b, [&](int i, int tok) {
+        const int t = place(tok);
+        if (t >= 0) count_use(&table[t], i < first.prompt);
     });
-    if (p.C > 1) cluster_arrive();
-    if (paths && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, j1, stage, kCards / 2, sh.path[tid], place);
-    if (p.C > 1) cluster_wait();                                    // no CTA counts into another's table from here on
-    __syncthreads();
-    gather_lists<kCards, false>(table, nullptr, list, nullptr, nullptr, sh.from);
+    if (p.penalised && p.token_ids && tid < j1 - j0) sh.path_n[tid] = gather_path(p, b, j0 + tid, 0x7fffffff, nullptr, 0, sh.path[tid], place);
     __syncthreads();
     const Penalty q = first.penalty();
-    const int parts = 1 << p.part_shift, n_list = sh.from[0][kAdjustWarps];
     grid_dependency_wait();                                         // the rows have been copied and masked
-    for (int k = warp; k < (j1 - j0) << p.part_shift; k += kAdjustWarps) {
-        const int row = k >> p.part_shift, part = k & (parts - 1);
-        const int64_t j = j0 + row;
-        const char* x = p.in + ((int64_t)b * p.in_b + j * p.in_row) * E::ES;
-        char* y = p.out + ((int64_t)b * p.out_b + j * p.out_row) * E::ES;
-        const uint32_t* mask = adjust_mask(p, b, (int)j);
-        const uint16_t* path = sh.path[row];
-        const int np = sh.path_n[row];
-        auto replace = [&](int t, uint32_t times, uint32_t uses) {
-            const int64_t v = (int64_t)t * S + s;
-            if (mask && !((mask[v >> 5] >> (v & 31)) & 1u)) return;
-            double z = penalised(q, (double)E::load(x, v), times, times > 0u || (uses & kInPrompt));
-            if (uses & kHasBias) z += (double)bias_of[t];
-            ((typename Raw<DT>::T*)y)[v] = Raw<DT>::round(z);
-        };
-        // one warp a token, in place too: the list's without those of the path, which the row's first warp takes, each once
-        const int to = (int)((int64_t)n_list * (part + 1) >> p.part_shift);
-        for (int i = (int)((int64_t)n_list * part >> p.part_shift) + lane; i < to; i += 32) {
-            const int t = list[i];
-            bool on_path = false;
-            for (int o = 0; o < np; ++o) on_path = on_path || path[o] == t;
-            if (!on_path) replace(t, table[t] / kOnce, table[t]);
-        }
-        if (part == 0)
-            for (int i = lane; i < np; i += 32) {
-                const int t = path[i];
+    for (int j = j0; j < j1; ++j) {
+        const char* x = p.in + ((int64_t)b * p.in_b + (int64_t)j * p.in_row) * E::ES;
+        T* y = (T*)(p.out + ((int64_t)b * p.out_b + (int64_t)j * p.out_row) * E::ES);
+        const uint32_t* mask = adjust_mask(p, b, j);
+        const int np = sh.path_n[j - j0];
+        const uint16_t* path = sh.path[j - j0];
+        // the path's tokens first, from the values as they are (in place, too); they are written when all others are
+        T own{};
+        int mine = -1;
+        if (tid < np) {
+            const int t = path[tid];
+            mine = token[t];
+            if (mask && !((mask[mine >> 5] >> (mine & 31)) & 1u)) mine = -1;
+            else {
                 uint32_t times = table[t] / kOnce;
-                bool once = true;
-                for (int o = 0; o < np; ++o) {
-                    times += path[o] == t;
-                    once = once && (o >= i || path[o] != t);
-                }
-                if (once) replace(t, times, table[t]);
+                for (int o = 0; o < np; ++o) times += path[o] == t;
+                const double z = penalised(q, (double)E::load(x, mine), times, true);
+                own = Raw<DT>::round(table[t] & kHasBias ? z + (double)bias_of[t] : z);
             }
+        }
+        __syncthreads();
+        constexpr int kStep = 4;                                    // slots of a thread under way
+#pragma unroll 1
+        for (int i0 = tid; i0 < p.slots; i0 += kStep * kTokensThreads) {
+            uint32_t word[kStep];
+            int v[kStep];
+            float old[kStep];
+#pragma unroll
+            for (int o = 0; o < kStep; ++o) {
+                const int i = i0 + o * kTokensThreads;
+                word[o] = i < p.slots ? table[i] : 0u;
+                v[o] = word[o] ? token[i] : 0;
+                old[o] = word[o] ? E::load(x, v[o]) : 0.0f;
+                if (mask && word[o] && !((mask[v[o] >> 5] >> (v[o] & 31)) & 1u)) word[o] = 0u;
+            }
+#pragma unroll
+            for (int o = 0; o < kStep; ++o) {
+                if (word[o] == 0u) continue;
+                const uint32_t times = word[o] / kOnce;
+                const double z = penalised(q, (double)old[o], times, times > 0u || (word[o] & kInPrompt));
+                y[v[o]] = Raw<DT>::round(word[o] & kHasBias ? z + (double)bias_of[i0 + o * kTokensThreads] : z);
+            }
+        }
+        __syncthreads();
+        if (mine >= 0) y[mine] = own;
     }
 }
 

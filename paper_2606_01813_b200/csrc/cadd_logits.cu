@@ -72,25 +72,28 @@ static void group_rows(AdjustParams& p, int64_t ctas_a_group, int part_shift) {
     while (p.part_shift < 3 && (p.rows_per_cta << p.part_shift) < kAdjustWarps) ++p.part_shift;
 }
 
-// A short history is read by every CTA, a long one shared out over a cluster of them.
-static void share_history(AdjustParams& p, int ctas) {
-    p.C = 1;
-    if (p.penalised && p.history && p.history_cols > 1024)
-        while (p.C < kAdjustMaxC && p.C < ctas) p.C *= 2;
-}
-
-template <int DT, int kCards>
+template <int DT>
 static int launch_tokens(AdjustParams& p, cudaStream_t st) {
-    p.S = (int)((p.V + kCards - 1) / kCards);
-    share_history(p, p.S);
-    p.S = (p.S + p.C - 1) / p.C * p.C;
-    group_rows(p, p.S, 0);
+    // Tokens that a CTA can meet: those of its part of the vocabulary, and no more than the history, biases and its rows' paths have.
+    p.groups = (p.R + kAdjustRows - 1) / kAdjustRows;
+    while (p.batch * p.groups < kSms && p.groups < p.R) p.groups *= 2;
+    p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
+    p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
+    int64_t most = (p.penalised && p.history ? p.history_cols : 0) + p.n_bias + (p.penalised && p.token_ids ? (int64_t)p.rows_per_cta * kMaxPath : 0);
+    p.S = 1;
+    if (most > kTokensMost) {
+        p.S = (int)((p.V + kTokensMost - 1) / kTokensMost);
+        if (most > kTokensMost) most = kTokensMost;
+    }
+    p.slots = 1024;
+    p.slot_shift = 22;
+    while (p.slots < kTokensSlots && p.slots * 3 < most * 4) { p.slots *= 2; --p.slot_shift; }
     const int64_t grid = (int64_t)p.batch * p.S * p.groups;
     if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
-    const size_t smem = adjust_tokens_smem<kCards>(p.n_bias > 0);
-    const int rc = room(adjust_tokens_kernel<DT, kCards>, smem);
+    const size_t smem = adjust_tokens_smem(p.slots, p.n_bias > 0);
+    const int rc = room(adjust_tokens_kernel<DT>, smem);
     if (rc != CADD_OK) return rc;
-    return launch_cluster(adjust_tokens_kernel<DT, kCards>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p, p.followed);
+    return launch_cluster(adjust_tokens_kernel<DT>, (unsigned)grid, kTokensThreads, 1, smem, st, p, p.followed);
 }
 
 // Rows of a request from which on the tables of adjust_rows_kernel are worth their while; where all its CTAs run at once they
@@ -108,22 +111,21 @@ static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
     }
     const bool sparse = p.penalised || p.n_bias > 0;
     if (sparse && !in_place && (!p.penalised || !p.history || p.history_cols <= kListMost) && (p.R >= kFewRows || (int64_t)p.batch * p.tiles <= 2 * kSms)) {
-        share_history(p, p.tiles);
-        const int64_t padded = (int64_t)(p.tiles + p.C - 1) / p.C * p.C;
-        group_rows(p, padded, kAdjustTileBytes / kAdjustPieceBytes == 2 ? 1 : 0);
-        const int64_t grid = p.batch * padded * p.groups;
+        group_rows(p, p.tiles, kAdjustTileBytes / kAdjustPieceBytes == 2 ? 1 : 0);
+        const int64_t grid = (int64_t)p.batch * p.tiles * p.groups;
         if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
         const size_t smem = (size_t)adjust_layout(tile, p.n_bias).bytes;
         const int rc = room(adjust_rows_kernel<DT>, smem);
         if (rc != CADD_OK) return rc;
-        return launch_cluster(adjust_rows_kernel<DT>, (unsigned)grid, kAdjustThreads, (unsigned)p.C, smem, st, p);
+        adjust_rows_kernel<DT><<<(unsigned)grid, kAdjustThreads, smem, st>>>(p);
+        return launched();
     }
     if (!in_place || p.allowed) {
         p.followed = sparse;
         const int64_t units = (int64_t)p.batch * p.R * p.tiles;
         int rc = CADD_OK;
         if (in_place) {
-            const int64_t most = kSms * 4;
+            const int64_t most = kSms * 6;
             adjust_stream_kernel<DT, false><<<(unsigned)(units < most ? units : most), kAdjustThreads, 0, st>>>(p);
         } else {
             const size_t smem = (size_t)kAdjustWarps * kAdjustBuffer<kAdjustTileBytes>;
@@ -134,7 +136,7 @@ static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
         if ((rc = launched()) != CADD_OK) return rc;
     }
     if (!sparse) return CADD_OK;
-    return launch_tokens<DT, 4096>(p, st);
+    return launch_tokens<DT>(p, st);
 }
 
 // ---------------- distillation ----------------

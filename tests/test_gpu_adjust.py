@@ -270,7 +270,9 @@ def test_wait_that_runs_out():
     assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(out).all())
 
 
-@pytest.mark.parametrize("V,history", [(4097, 1025), (40000, 3000), (2048 * 9, 5000)])
+@pytest.mark.parametrize("V,history", [(4097, 1025), (40000, 3000), (2048 * 9, 5000), (30000, 14000), (9000, 40000)])
+@pytest.mark.parametrize("R", [3, 10])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-def test_histories_that_several_ctas_share(V, history, dtype):
-    both(random_adjust(2, 3, V, dtype, seed=V, history=history, spread=V, n_bias=20))
+def test_long_histories_of_many_tokens(V, history, R, dtype):
+    """Into another array and in place; beyond 12288 tokens several CTAs share a request's."""
+    both(random_adjust(2, R, V, dtype, seed=V, history=history, spread=V, n_bias=20))
