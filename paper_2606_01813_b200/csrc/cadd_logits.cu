@@ -80,11 +80,15 @@ static int launch_tokens(AdjustParams& p, cudaStream_t st) {
     p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
     p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
     int64_t most = (p.penalised && p.history ? p.history_cols : 0) + p.n_bias + (p.penalised && p.token_ids ? (int64_t)p.rows_per_cta * kMaxPath : 0);
+    // One CTA has to hold what it meets; beyond that the tokens, single words anywhere in a row, want the load units of all SMs
+    // (64 requests of 8192 tokens: 10 us of 16 for one CTA each).
     p.S = 1;
     if (most > kTokensMost) {
         p.S = (int)((p.V + kTokensMost - 1) / kTokensMost);
-        if (most > kTokensMost) most = kTokensMost;
+        most = kTokensMost;
     }
+    const int64_t ctas = (int64_t)p.batch * p.groups;
+    while (p.S < 8 && ctas * (p.S + 1) <= kSms) ++p.S;
     p.slots = 1024;
     p.slot_shift = 22;
     while (p.slots < kTokensSlots && p.slots * 3 < most * 4) { p.slots *= 2; --p.slot_shift; }
