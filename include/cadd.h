@@ -573,7 +573,7 @@ typedef struct cadd_distill_args {
     int32_t  batch, L, R, K;       /* requests, drafter's positions, target's rows, entries of a list (1..CADD_DISTILL_MAX_K) */
     int32_t  logits_dtype;         /* CADD_DTYPE_*, of grad too */
     int32_t  path_cols;            /* columns of path */
-    int64_t  V;                    /* at most 800,000 (bf16) / 400,000 (fp32) */
+    int64_t  V;                    /* at most 2,000,000 */
     double   temperature;          /* 2^-20 .. 2^20 */
     const void* logits;            /* [batch, L, V]; element (b,i,v) at b*stride_b + i*stride_l + v */
     int64_t  stride_b, stride_l;   /* in elements, >= 0 */

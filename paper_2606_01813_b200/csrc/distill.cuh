@@ -1,13 +1,19 @@
 // Distillation of the drafter from the target's top tokens: losses and gradients (cadd_distill_args has the definition).
 //
-// A cluster of CTAs takes one row of drafter's logits, a CTA one contiguous segment of it, which comes to shared memory in tiles of
-// 16 KB (bulk copies, each with a barrier).  As the tiles land, every thread adds up the exponentials of its elements that are
-// not listed, relative to a power of two at or above its own largest; listed tokens are left out of that sum (their elements
-// count as -Inf) and go into the row's statistics one by one, in fp64: the rest's probability is therefore right even where the
-// listed tokens leave all but nothing.  The segments' (largest, sum) pairs cross the cluster through distributed shared memory.
-// Where the gradient is wanted too, all tiles of the segment have room and stay, and with the statistics known it is formed from them:
-// a row is read from memory once and written once.  The loss alone, and the gradient alone (statistics given, no exchange), need a
-// tile once, so these walk through a ring of a few tiles and give a CTA more of the row.
+// One CTA an SM walks through the rows of drafter's logits (few rows: a cluster of CTAs, each with a contiguous segment of every row), which
+// come to a ring of 40 KB tiles in shared memory by bulk copies.  The warps of a CTA have roles, so that no row waits for another's
+// small steps:
+//   producer   sends for the tiles, row after row, as stages fall free;
+//   prepare    a row's list, a row ahead: the target's probabilities, the drafter's logits of the listed tokens, where they lie in the segment;
+//   compute    (20 warps) adds up the exponentials of the tokens that are not listed, relative to a power of two at or above the
+//              largest: a listed token counts as -Inf there, and goes into the row's statistics by itself, in fp64, so the
+//              rest's probability is right even where the listed tokens leave all but nothing; then, where the gradient is
+//              wanted, forms it from the tiles: the row's last ones have stayed, as many as the ring holds, and the others come once more,
+//              from L2, where there are never more rows than SMs;
+//   finish     joins the warps' sums, exchanges them within the cluster (distributed shared memory), and makes of the statistics the
+//              loss and the two factors that the gradient needs.
+// The gradient alone (statistics given, no exchange) passes over the tiles once.
+// All waits are bounded; a CTA in which one runs out leaves NaN in its rows from there on.
 #pragma once
 #include "common.cuh"
 #include "tile_ring.cuh"
@@ -15,13 +21,16 @@
 
 namespace cadd {
 
-constexpr int kDistillThreads = 256;
-constexpr int kDistillMaxC = 8;                                     // CTAs a row at most
-constexpr int kDistillTile = 4 * kDistillThreads;                   // 16-byte chunks of one copy: four a thread
-constexpr int kDistillMaxTiles = 13;                                // that stay in shared memory: 208 KB
-constexpr int kDistillRing = 3;                                     // tiles of the ring, where they do not stay
+constexpr int kDistillWarps = 20;                                   // that compute
+constexpr int kDistillCompute = 32 * kDistillWarps;
+constexpr int kDistillThreads = kDistillCompute + 96;               // and producer, prepare, finish
+constexpr int kDistillStatusThreads = 256;
+constexpr int kDistillMaxC = 4;                                     // CTAs a row at most
+constexpr int kDistillEach = 4;                                     // 16-byte chunks of a tile that a thread has
+constexpr int kDistillTile = kDistillEach * kDistillCompute;
+constexpr int kDistillMaxStages = 216 * 1024 / (kDistillTile * 16);
+constexpr int kDistillMaxV = 2000000;
 constexpr int kDistillK = CADD_DISTILL_MAX_K;
-static_assert(kDistillK <= kDistillThreads, "one thread an entry");
 constexpr float kDistillLowest = -1.0e30f;                          // logits below count as -Inf; also the reference of an empty sum
 constexpr double kRestRounding = 0x1p-20;
 
@@ -29,8 +38,8 @@ struct DistillParams {
     const char* logits;
     char* grad;
     int64_t V, in_b, in_row, out_b, out_row;
-    int L, R, K, path_cols, rest;
-    int C, chunks_max;                            // CTAs a row; chunks of a segment at most
+    int rows, batch, L, R, K, path_cols, rest;
+    int C, clusters, chunks_max, stages;          // CTAs a row; clusters; chunks of a segment at most; tiles of the ring
     float c;                                      // log2(e) / T
     double inv_t;
     const int32_t *token, *path, *path_len, *n_rows;
@@ -41,33 +50,62 @@ struct DistillParams {
     int drop;                                     // test hook: this tile of every segment is never copied (-1: none)
 };
 
-// Behind this: int first_of[groups + 2], the first entry of the list in each group of 32 consecutive chunks (-1: none; the last
-// two groups are the row's scalar head and tail), then the segment.
-struct DistillShared {
-    alignas(8) uint64_t full[kDistillMaxTiles];
-    int sent[kDistillMaxTiles];                   // last tile sent for into each stage, -1: none
-    unsigned released[kDistillRing];              // ring: warps done with the stage's current tile
-    double value[kDistillK];                      // entries of the list: target's logit
-    double prob[kDistillK];                       // entries: p
-    double peer_sum[kDistillMaxC];
-    double warp_sum[kDistillThreads / 32];
+// A row on its way through the roles; two of them are.
+struct DistillRow {
+    double p_rest, entropy, mass, cross;          // entropy, cross: sum p log p, sum p s / T over the entries; mass: sum p
+    double z_list;                                // sum of e over tokens (not entries)
     double factor;                                // of the exponentials in the gradient of tokens that are not listed
-    float peer_max[kDistillMaxC], peer_ref[kDistillMaxC];
-    float warp_max[kDistillThreads / 32], warp_ref[kDistillThreads / 32];
-    float logit[kDistillK];                       // entries: drafter's logit
-    float g[kDistillK];                           // entries: gradient of their token
-    int token[kDistillK];                         // entries: token, -1 where there is none
-    int chunk[kDistillK];                         // entries: chunk of the segment
-    int16_t next[kDistillK];                      // next entry of the same group, -1: none
-    uint8_t elem[kDistillK], once[kDistillK];     // element of the chunk; 1: the token's first entry
-    float ref;                                    // reference exponent of the gradient's exponentials
+    double sum[kDistillWarps], peer_sum[kDistillMaxC];
+    float max[kDistillWarps], ref[kDistillWarps], peer_max[kDistillMaxC], peer_ref[kDistillMaxC];
+    float weight, upstream;                       // of the row; grad_loss
+    unsigned row;                                 // batch * L + position
+    float m_list;                                 // largest listed logit
+    float grad_ref;                               // reference exponent of the gradient's exponentials
+    int live;                                     // 0: left out from the start, nothing is read
+    int left_out;                                 // by its list, after its tiles have been sent for
     int twice;                                    // some token is listed more than once
-    int left_out;
-    int timeout;
 };
-__host__ __device__ inline size_t distill_first_bytes(int chunks) { return (((size_t)(chunks + 31) / 32 + 2) * 4 + 127) & ~(size_t)127; }
+constexpr int kDistillGroups = 512;
+struct DistillMap {
+    int before[kDistillGroups + 1];
+    int scan[kDistillThreads / 32];
+};
+// The entries of a row's list; n: K rounded up to whole warps.
+struct DistillList {
+    double *prob, *e;                             // p; exp((s - m_list) / T), 0 below kDistillLowest
+    float* g;                                     // gradient of the token
+    int* token;                                   // -1 where there is none
+    int16_t *next, *thread;                       // next entry of the same part, -1: none; the thread that has the token
+    uint8_t *where, *once;                        // which of the thread's (four) chunks of the tile, * 8 + element of the chunk; 1: the token's first entry
+    __device__ __forceinline__ DistillList(unsigned char* at, int n) {
+        prob = reinterpret_cast<double*>(at);
+        e = prob + n;
+        g = reinterpret_cast<float*>(e + n);
+        token = reinterpret_cast<int*>(g + n);
+        next = reinterpret_cast<int16_t*>(token + n);
+        thread = next + n;
+        where = reinterpret_cast<uint8_t*>(thread + n);
+        once = where + n;
+    }
+};
+constexpr int kDistillEntry = 30;                 // bytes of an entry
+// Behind this: two lists; int first_of[2][parts + 2], the first entry of each row's list in each part of the segment, what a warp has
+// of a tile (-1: none; the last two parts are the row's scalar head and tail); the ring.
+struct DistillShared {
+    alignas(8) uint64_t full[kDistillMaxStages], empty[kDistillMaxStages];
+    uint64_t listed[2], done[2], summed[2], known[2], exchanged[2];
+    int sent[kDistillMaxStages];                  // last tile sent for into each stage, -1: none
+    int error;
+    unsigned lost;                                // the first row in the cluster's order that some role has not finished
+    DistillRow row[2];
+    DistillMap map;
+};
+__host__ __device__ inline int distill_parts(int chunks) { return (chunks + kDistillTile - 1) / kDistillTile * kDistillWarps; }
+__host__ __device__ inline size_t distill_first_bytes(int chunks) { return ((size_t)(distill_parts(chunks) + 2) * 8 + 127) & ~(size_t)127; }
 __host__ __device__ inline size_t distill_shared_bytes() { return (sizeof(DistillShared) + 127) & ~(size_t)127; }
-inline size_t distill_smem_bytes(int chunks, int room) { return distill_shared_bytes() + distill_first_bytes(chunks) + (size_t)room * 16; }
+__host__ __device__ inline size_t distill_list_bytes(int K) { return (size_t)((K + 31) & ~31) * kDistillEntry; }
+__host__ __device__ inline size_t distill_ring_at(int chunks, int K) { return distill_shared_bytes() + 2 * distill_list_bytes(K) + distill_first_bytes(chunks); }
+inline size_t distill_smem_bytes(int chunks, int K, int stages) { return distill_ring_at(chunks, K) + (size_t)stages * kDistillTile * 16; }
 
 __device__ __forceinline__ uint32_t peer_address(const void* p, unsigned rank) {
     uint32_t a;
@@ -103,19 +141,52 @@ __device__ __forceinline__ void blank(uint4& w, uint32_t bits) {
         for (int i = 0; i < 4; ++i) x[i] = (bits >> i) & 1u ? 0xff800000u : x[i];
     }
 }
+// factor * 2^(x c - ref) of a chunk's elements, as a chunk.
 template <int DT>
-__device__ __forceinline__ uint4 pack_chunk(const float* f) {
-    if constexpr (DT == CADD_DTYPE_BF16) {
-        uint4 w;
-        uint32_t* x = &w.x;
+__device__ __forceinline__ uint4 gradient_chunk(const uint4& w, uint64_t c2, uint64_t nref2, uint64_t factor2) {
+    using E = Elem<DT>;
+    float f[E::EPC];
+    E::unpack(w, f);
+    uint4 r;
+    uint32_t* x = &r.x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            x[i] = *reinterpret_cast<const uint32_t*>(&h);
+    for (int q = 0; q < E::EPC; q += 2) {
+        float t0, t1;
+        unpack2(fma2(pack2(f[q], f[q + 1]), c2, nref2), t0, t1);
+        unpack2(mul2(pack2(ex2_approx(t0), ex2_approx(t1)), factor2), t0, t1);
+        if constexpr (DT == CADD_DTYPE_BF16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(t0, t1);
+            x[q / 2] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            x[q] = __float_as_uint(t0);
+            x[q + 1] = __float_as_uint(t1);
         }
-        return w;
-    } else {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    return r;
+}
+// An element's bits, and an element of a chunk replaced or read.
+template <int DT> __device__ __forceinline__ uint32_t element_bits(float x) {
+    if constexpr (DT == CADD_DTYPE_BF16) return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x));
+    else return __float_as_uint(x);
+}
+template <int DT> __device__ __forceinline__ void set_element(uint4& w, int e, uint32_t bits) {
+    uint32_t* x = &w.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == CADD_DTYPE_BF16) {
+            if (e == 2 * i) x[i] = (x[i] & 0xffff0000u) | bits;
+            if (e == 2 * i + 1) x[i] = (x[i] & 0x0000ffffu) | bits << 16;
+        } else if (e == i) x[i] = bits;
+    }
+}
+template <int DT> __device__ __forceinline__ void store_chunk(char* row, int64_t i, const uint4& w) {      // where it is not aligned
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if constexpr (DT == CADD_DTYPE_BF16) {
+            ((uint16_t*)row)[i + 2 * q] = (uint16_t)x[q];
+            ((uint16_t*)row)[i + 2 * q + 1] = (uint16_t)(x[q] >> 16);
+        } else ((uint32_t*)row)[i + q] = x[q];
     }
 }
 template <int DT> __device__ __forceinline__ void store_element(char* row, int64_t i, float x) {
@@ -168,388 +239,559 @@ __device__ __forceinline__ uint64_t chunk_terms(const uint4& w, uint64_t c2, uin
     return r;
 }
 
+
+// Where the CTA stands in a row: what all roles work out for themselves.
+template <int DT>
+struct DistillSegment {
+    using E = Elem<DT>;
+    int b, i;
+    const char* in;
+    RowSplit sp;
+    int nc, n_tiles, scalars, head;               // head: of the scalars, those before the chunks (the others are behind them)
+    int64_t e0;                                   // token of the first chunk
+    __device__ __forceinline__ DistillSegment(const DistillParams& p, unsigned row, int rank) {
+        b = (int)(row / (unsigned)p.L);
+        i = (int)(row - (unsigned)b * (unsigned)p.L);
+        in = p.logits + ((int64_t)b * p.in_b + (int64_t)i * p.in_row) * E::ES;
+        sp = split_row<DT>(in, p.V);
+        const int per = (int)((unsigned)(sp.n_chunks + p.C - 1) / (unsigned)p.C), s0 = min(sp.n_chunks, rank * per);
+        nc = min(per, sp.n_chunks - s0);
+        n_tiles = (nc + kDistillTile - 1) / kDistillTile;
+        e0 = sp.head + (int64_t)s0 * E::EPC;
+        head = rank == 0 ? sp.head : 0;
+        scalars = head + (rank == p.C - 1 ? sp.tail : 0);
+    }
+    __device__ __forceinline__ int64_t scalar(const DistillParams& p, int k) const { return k < head ? k : p.V - sp.tail + (k - head); }
+};
+// Rows in the order in which clusters take them: those that path or n_rows leave in (they cost most, and are dealt out evenly), then the
+// others.  In shared memory: how many rows the requests before each group of requests leave in.
+__device__ __forceinline__ int group_size(const DistillParams& p) { return (p.batch + kDistillGroups - 1) / kDistillGroups; }
+// The whole CTA.
+__device__ __forceinline__ void distill_map(const DistillParams& p, DistillMap& m) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, size = group_size(p), groups = (p.batch + size - 1) / size;
+    int carry = 0;
+    for (int g0 = 0; g0 < groups; g0 += kDistillThreads) {
+        const int g = g0 + tid;
+        int n = 0;
+        if (g < groups)
+            for (int b = g * size; b < min(p.batch, (g + 1) * size); ++b) n += distill_live(p, b);
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(kFullMask, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (lane == 31) m.scan[warp] = sum;
+        __syncthreads();
+        int before = carry, all = carry;
+        for (int k = 0; k < kDistillThreads / 32; ++k) {
+            before += k < warp ? m.scan[k] : 0;
+            all += m.scan[k];
+        }
+        if (g < groups) m.before[g + 1] = before + sum;
+        carry = all;
+        __syncthreads();
+    }
+    if (tid == 0) m.before[0] = 0;
+    __syncthreads();
+}
+// The k-th row that is left in (live) or out: batch * L + position.
+__device__ __forceinline__ unsigned distill_row(const DistillParams& p, const DistillMap& m, unsigned k, bool live) {
+    if (!p.path && !p.n_rows) return k;
+    const int size = group_size(p), groups = (p.batch + size - 1) / size;
+    auto before = [&](int g) { return live ? (unsigned)m.before[g] : (unsigned)min(g * size, p.batch) * (unsigned)p.L - (unsigned)m.before[g]; };
+    int lo = 0, hi = groups - 1;                                     // the last group with before(g) <= k
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (before(mid) <= k) lo = mid;
+        else hi = mid - 1;
+    }
+    unsigned left = k - before(lo);
+    for (int b = lo * size;; ++b) {
+        const unsigned in = (unsigned)distill_live(p, b), here = live ? in : (unsigned)p.L - in;
+        if (left < here) return (unsigned)b * (unsigned)p.L + (live ? left : in + left);
+        left -= here;
+    }
+}
+// The target's row for position i of request b, or -1 where the position is left out.
+__device__ __forceinline__ int distill_teacher(const DistillParams& p, unsigned row, int b, int i) {
+    const float weight = p.weight ? p.weight[row] : 1.0f;
+    int r = p.path && i > 0 && i - 1 < p.path_cols ? p.path[(int64_t)b * p.path_cols + i - 1] : (p.path ? 0 : i);
+    if (i >= distill_live(p, b) || weight == 0.0f || r < 0 || r >= p.R) r = -1;
+    return r;
+}
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
+    return x;
+}
+
 // kLoss: statistics and loss are computed here; otherwise they are given.  kGrad: the gradient is written.
 template <int DT, bool kLoss, bool kGrad>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(DistillParams p) {
+__global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillParams p) {
     using E = Elem<DT>;
     extern __shared__ __align__(128) unsigned char distill_smem_raw[];
     DistillShared& sh = *reinterpret_cast<DistillShared*>(distill_smem_raw);
-    int* first_of = reinterpret_cast<int*>(distill_smem_raw + distill_shared_bytes());
-    const uint4* seg = reinterpret_cast<const uint4*>(distill_smem_raw + distill_shared_bytes() + distill_first_bytes(p.chunks_max));
+    const int parts_max = distill_parts(p.chunks_max);
+    const int list_size = (p.K + 31) & ~31;
+    unsigned char* const list_all = distill_smem_raw + distill_shared_bytes();
+    int* const first_all = reinterpret_cast<int*>(list_all + 2 * distill_list_bytes(p.K));
+    const uint4* ring = reinterpret_cast<const uint4*>(distill_smem_raw + distill_ring_at(p.chunks_max, p.K));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr bool kRing = !(kLoss && kGrad);
-    const unsigned C = (unsigned)p.C, row = blockIdx.x / C, rank = blockIdx.x - row * C;
-    const int b = (int)(row / (unsigned)p.L), i = (int)(row - (unsigned)b * (unsigned)p.L);
+    const unsigned C = (unsigned)p.C, cluster = blockIdx.x / C;
+    const int rank = (int)(blockIdx.x - cluster * C);
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], kDistillWarps); sh.sent[s] = -1; }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&sh.listed[s], 1);
+            mbar_init(&sh.done[s], kDistillWarps + 1);
+            mbar_init(&sh.summed[s], kDistillWarps);
+            mbar_init(&sh.known[s], 1);
+            mbar_init(&sh.exchanged[s], C);
+        }
+        sh.error = 0;
+        sh.lost = 0xffffffffu;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    unsigned n_live = (unsigned)p.rows;
+    if (p.path || p.n_rows) {
+        distill_map(p, sh.map);
+        n_live = (unsigned)sh.map.before[(p.batch + group_size(p) - 1) / group_size(p)];
+    } else __syncthreads();
+    if (C > 1) { cluster_arrive(); cluster_wait(); }                 // every CTA's barriers are ready for the others
+    // Waits of one warp; false: the time is up, here or in another role (then everybody leaves).
+    volatile int* error = &sh.error;
+    const unsigned nap = warp == kDistillWarps || warp == kDistillWarps + 1 ? 200u : 32u;
+    auto wait = [&](uint64_t* bar, unsigned parity, int limit) {
+        bool ok = false;
+        for (int it = 0; it < limit && !ok; ++it) {
+            ok = mbar_try_wait_cluster(bar, parity);
+            if (ok) break;
+            if (*error) break;
+            __nanosleep(nap);                                        // a waiting warp must not take issue slots from those that compute
+        }
+        ok = __all_sync(kFullMask, ok);
+        if (!ok) *error = 1;
+        return ok;
+    };
+    auto arrive = [&](uint64_t* bar) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
+    // tile number g of the CTA (all rows' tiles in turn): its stage and the parity of that stage's barrier
+    const unsigned S = (unsigned)p.stages;
 
-    // ---- the row, and the target's row for it ----
-    const char* in = p.logits + ((int64_t)b * p.in_b + (int64_t)i * p.in_row) * E::ES;
-    char* out = kGrad ? p.grad + ((int64_t)b * p.out_b + (int64_t)i * p.out_row) * E::ES : nullptr;
-    const RowSplit sp = split_row<DT>(in, p.V);
-    const int per = (sp.n_chunks + (int)C - 1) / (int)C;
-    const int s0 = min(sp.n_chunks, (int)rank * per), nc = min(per, sp.n_chunks - s0);     // this CTA's chunks
-    const int64_t e0 = sp.head + (int64_t)s0 * E::EPC;                                      // token of its first chunk
-    const int scalars = (rank == 0 ? sp.head : 0) + (rank == C - 1 ? sp.tail : 0);
-    // token of thread tid's scalar element, tid < scalars
-    const int64_t mine_scalar = rank == 0 && tid < sp.head ? tid : p.V - sp.tail + (tid - (rank == 0 ? sp.head : 0));
-    int r = i;
-    bool left_out = i >= distill_live(p, b);
-    const float weight = p.weight ? p.weight[row] : 1.0f;
-    left_out = left_out || weight == 0.0f;
-    if (!left_out && p.path) r = i == 0 ? 0 : p.path[(int64_t)b * p.path_cols + i - 1];
-    left_out = left_out || r < 0 || r >= p.R;
-    const bool same = kGrad && ((uintptr_t)in & 15u) == ((uintptr_t)out & 15u);
-    // gradient 0 of a row that is left out
-    auto write_zeros = [&]() {
-        if constexpr (kGrad) {
-            if (tid < scalars) store_element<DT>(out, mine_scalar, 0.0f);
-            if (same) {
-                uint4* o4 = reinterpret_cast<uint4*>(out + e0 * E::ES);
-                for (int k = tid; k < nc; k += kDistillThreads) o4[k] = make_uint4(0u, 0u, 0u, 0u);
+    if (warp == kDistillWarps) {
+        // ---------------- producer ----------------
+        unsigned stage = 0, turn = 0;                                // turn: how often the ring has gone round
+        bool going = true;
+        const uint64_t keep = l2_keep(), drop_it = l2_drop();
+        for (unsigned at = cluster; going && at < n_live; at += p.clusters) {
+            const unsigned row = distill_row(p, sh.map, at, true);
+            const DistillSegment<DT> seg(p, row, rank);
+            if (distill_teacher(p, row, seg.b, seg.i) < 0) continue;
+            const int drop = p.drop < 0 ? -1 : min(p.drop, seg.n_tiles - 1);
+            // both loss and gradient: those that do not stay come twice, and are kept in L2 meanwhile
+            const int again = kLoss && kGrad ? max(0, seg.n_tiles - (int)S) : 0;
+            for (int u = 0; u < seg.n_tiles + again; ++u) {
+                const int t = u < seg.n_tiles ? u : u - seg.n_tiles;
+                if (turn > 0 && !wait(&sh.empty[stage], (turn - 1) & 1u, kSpinLimit)) { going = false; break; }
+                if (lane == 0 && u != drop) {
+                    const unsigned bytes = (unsigned)min(kDistillTile, seg.nc - t * kDistillTile) * 16u;
+                    sh.sent[stage] = (int)turn;
+                    mbar_arrive_expect_tx(&sh.full[stage], bytes);
+                    bulk_load_hint((void*)(ring + stage * kDistillTile), seg.in + seg.e0 * E::ES + (int64_t)t * kDistillTile * 16, bytes, &sh.full[stage],
+                                   u < again ? keep : drop_it);
+                }
+                if (++stage == S) { stage = 0; ++turn; }
+            }
+        }
+        // no CTA leaves with a copy of its own in flight
+        if (lane == 0)
+            for (unsigned s = 0; s < S; ++s)
+                if (sh.sent[s] >= 0) mbar_wait_bounded(&sh.full[s], (unsigned)sh.sent[s] & 1u);
+    } else if (warp == kDistillWarps + 1) {
+        // ---------------- prepare ----------------
+        unsigned n = 0;
+        for (unsigned order = cluster; order < n_live; order += p.clusters, ++n) {
+            const unsigned row = distill_row(p, sh.map, order, true);
+            DistillRow& k = sh.row[n & 1u];
+            const DistillList l(list_all + (n & 1u) * distill_list_bytes(p.K), list_size);
+            int* first_of = first_all + (n & 1u) * (parts_max + 2);
+            const DistillSegment<DT> seg(p, row, rank);
+            const int r = distill_teacher(p, row, seg.b, seg.i), parts = seg.n_tiles * kDistillWarps;
+            if (n >= 2 && !wait(&sh.done[n & 1u], (n / 2 - 1) & 1u, kSpinLimit)) break;
+            if (lane == 0) k.row = row;
+            if (r < 0) {
+                if (lane == 0) k.live = 0;
+                arrive(&sh.listed[n & 1u]);
+                continue;
+            }
+            for (int o = lane; o < parts + 2; o += 32) first_of[o] = -1;
+            const float weight = p.weight ? p.weight[row] : 1.0f, upstream = p.grad_loss ? p.grad_loss[row] : 1.0f;
+            if (lane == 0) { k.live = 1; k.weight = weight; k.upstream = upstream; }
+            const int64_t at = ((int64_t)seg.b * p.R + r) * p.K;
+            double top = p.rest && p.lse ? p.lse[(int64_t)seg.b * p.R + r] / p.inv_t : (p.rest ? 0.0 : -INFINITY);
+            float m_list = -INFINITY;
+            bool any = false, twice = false;
+            // tokens, and where they lie
+            for (int o = lane; o < p.K; o += 32) {
+                int tok = p.token[at + o];
+                if (tok < 0 || tok >= p.V) tok = -1;
+                l.token[o] = tok;
+                const double v = p.value[at + o];
+                l.prob[o] = v;
+                if (tok >= 0) {
+                    if (!p.rest) top = fmax(top, v);
+                    any = any || p.rest || !(v == -INFINITY);       // (NaN counts: it shows in the sum)
+                }
+            }
+            __syncwarp();
+            for (int o = lane; o < p.K; o += 32) {
+                const int tok = l.token[o];
+                int part = -1, thread = 0, where = 0;
+                if (tok >= seg.e0 && tok < seg.e0 + (int64_t)seg.nc * E::EPC) {
+                    const unsigned c = (unsigned)(tok - seg.e0) / E::EPC, t = c / kDistillTile, in_tile = c - t * kDistillTile;
+                    thread = (int)(in_tile % kDistillCompute);
+                    where = (int)(in_tile / kDistillCompute * 8 + (unsigned)(tok - seg.e0) % E::EPC);
+                    part = (int)t * kDistillWarps + thread / 32;
+                } else if (tok >= 0 && tok < seg.head) { thread = tok; part = parts; }
+                else if (tok >= p.V - seg.sp.tail && seg.scalars > seg.head) { thread = (int)(tok - (p.V - seg.sp.tail)) + seg.head; part = parts + 1; }
+                l.thread[o] = (int16_t)thread;
+                l.where[o] = (uint8_t)where;
+                if (part >= 0) l.next[o] = (int16_t)atomicExch(&first_of[part], o);
+                // (the gradient alone may be written over logits by the other CTAs meanwhile: only this CTA's are read)
+                float x = -INFINITY;
+                if (tok >= 0 && (kLoss || part >= 0)) x = E::load(seg.in, tok);
+                l.e[o] = (double)x;
+                m_list = fmaxf(m_list, x);
+                bool once = true;
+                for (int f = 0; f < o && tok >= 0; ++f) once = once && l.token[f] != tok;
+                l.once[o] = once;
+                twice = twice || !once;
+            }
+            m_list = warp_max(m_list);
+            if (!(m_list >= kDistillLowest)) m_list = -INFINITY;
+            any = __any_sync(kFullMask, any);
+            twice = __any_sync(kFullMask, twice);
+            if (!p.rest) {
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(kFullMask, top, o));
+            }
+            // the target's probabilities, up to their sum, and the drafter's exponentials
+            double sum = 0.0, z = 0.0, entropy = 0.0, cross = 0.0;
+#pragma unroll 1
+            for (int o = lane; o < p.K; o += 32) {
+                double q = 0.0, e = 0.0;
+                if (l.token[o] >= 0) {
+                    const double x = l.e[o], lp = (l.prob[o] - top) * p.inv_t;
+                    const bool none = x < (double)kDistillLowest;
+                    q = exp(lp);
+                    if (!none) e = exp((x - (double)m_list) * p.inv_t);
+                    if (q != 0.0) {
+                        entropy += q * lp;
+                        cross += none ? -INFINITY : q * (x * p.inv_t);
+                    }
+                    sum += q;
+                    if (l.once[o]) z += e;
+                }
+                l.prob[o] = q;
+                l.e[o] = e;
+            }
+            sum = warp_sum(sum);
+            z = warp_sum(z);
+            entropy = warp_sum(entropy);
+            cross = warp_sum(cross);
+            double mass = sum;
+            if (!p.rest) {
+                const double scale = 1.0 / sum;
+                for (int o = lane; o < p.K; o += 32) l.prob[o] *= scale;
+                mass = sum * scale;
+                entropy = entropy * scale - log(sum) * mass;
+                cross *= scale;
+            }
+            if (lane == 0) {
+                k.entropy = entropy;
+                k.mass = mass;
+                k.cross = cross;
+                k.z_list = z;
+                k.m_list = m_list;
+                k.p_rest = !p.rest ? 0.0 : (sum < 1.0 ? 1.0 - sum : (sum == sum ? 0.0 : sum));
+                k.left_out = any ? 0 : 1;
+                k.twice = twice;
+            }
+            arrive(&sh.listed[n & 1u]);
+        }
+    } else if (warp == kDistillWarps + 2) {
+        // ---------------- finish ----------------
+        unsigned n = 0, lives = 0, order = cluster;                  // lives: rows read so far, per slot, a bit each: the parity of what only they pass
+        for (; order < n_live; order += p.clusters, ++n) {
+            const unsigned slot = n & 1u;
+            DistillRow& k = sh.row[slot];
+            const DistillList l(list_all + slot * distill_list_bytes(p.K), list_size);
+            if (!wait(&sh.listed[slot], (n / 2) & 1u, kSpinLimit)) break;
+            const unsigned row = k.row;
+            float4* stats = reinterpret_cast<float4*>(p.stats) + row;
+            if (!k.live) {
+                if (kLoss && rank == 0 && lane == 0) {
+                    if (p.loss) p.loss[row] = 0.0f;
+                    if (p.stats) *stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+                arrive(&sh.done[slot]);
+                continue;
+            }
+            const unsigned phase = (lives >> slot) & 1u;
+            lives ^= 1u << slot;
+            const double nan = __longlong_as_double(0x7ff8000000000000ll);
+            float m_rest, m_all, ref = 0.0f;                         // ref: an exponential of the gradient is exp((s - m_rest) / T) * 2^(m_rest c - ref)
+            double z_rest, z_all, a_list, a_rest, up;                // up: 2^(ref - m_rest c)
+            const float m_list = k.m_list;
+            if constexpr (kLoss) {
+                if (!wait(&sh.summed[slot], phase, kSpinLimit)) break;
+                bool in_use = lane < kDistillWarps;
+                DistillSum s{in_use ? k.max[lane] : -INFINITY, in_use ? k.ref[lane] : kDistillLowest, in_use ? k.sum[lane] : 0.0};
+                distill_join(s);
+                if (C > 1) {
+                    if (lane < (int)C) {
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_max[rank], lane)), "f"(s.m) : "memory");
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_ref[rank], lane)), "f"(s.ref) : "memory");
+                        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&k.peer_sum[rank], lane)), "d"(s.acc) : "memory");
+                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_address(&sh.exchanged[slot], lane)) : "memory");
+                    }
+                    __syncwarp();
+                    if (!wait(&sh.exchanged[slot], phase, kSpinLimit)) break;
+                    in_use = lane < (int)C;
+                    s = DistillSum{in_use ? k.peer_max[lane] : -INFINITY, in_use ? k.peer_ref[lane] : kDistillLowest, in_use ? k.peer_sum[lane] : 0.0};
+                    distill_join(s);
+                }
+                m_rest = s.m >= kDistillLowest ? s.m : -INFINITY;
+                m_all = fmaxf(m_rest, m_list);
+                // three exponentials at once: of the list's and the rest's largest, and of the step from the rest's reference to its largest
+                const double x = lane == 0 ? ((double)m_list - (double)m_all) * p.inv_t : lane == 1 ? ((double)m_rest - (double)m_all) * p.inv_t
+                                                                                            : ((double)s.ref - (double)m_rest * (double)p.c) * 0.693147180559945309;
+                const double y = exp(x);
+                a_list = m_list > -INFINITY ? __shfl_sync(kFullMask, y, 0) : 0.0;
+                a_rest = __shfl_sync(kFullMask, y, 1);
+                up = __shfl_sync(kFullMask, y, 2);
+                z_rest = up * s.acc * kEx2BiasFix;
+                ref = s.ref;
+                if (!(m_rest > -INFINITY)) {
+                    a_rest = ref = 0.0f;
+                    z_rest = s.acc == s.acc ? 0.0 : s.acc;
+                }
+                z_all = k.z_list * a_list + z_rest * a_rest;
+                if (!(m_all > -INFINITY) || !(s.acc == s.acc) || !(k.z_list == k.z_list)) z_all = nan;
             } else {
-                for (int k = tid; k < nc * E::EPC; k += kDistillThreads) store_element<DT>(out, e0 + k, 0.0f);
+                const float4 st = *stats;
+                m_all = st.x; z_all = (double)st.y; m_rest = st.z; z_rest = (double)st.w;
+                if (m_rest > -INFINITY) ref = ceilf(m_rest * p.c);
+                const double x = lane == 0 ? ((double)m_list - (double)m_all) * p.inv_t : lane == 1 ? ((double)m_rest - (double)m_all) * p.inv_t
+                                                                                            : ((double)ref - (double)m_rest * (double)p.c) * 0.693147180559945309;
+                const double y = exp(x);
+                a_list = m_list > -INFINITY ? __shfl_sync(kFullMask, y, 0) : 0.0;
+                a_rest = m_rest > -INFINITY ? __shfl_sync(kFullMask, y, 1) : 0.0;
+                up = __shfl_sync(kFullMask, y, 2);
+                if (!(m_all > -INFINITY)) z_all = nan;
+            }
+            const bool empty = !(m_rest > -INFINITY);                // no token is left beside the list
+            const double total = k.mass + k.p_rest, weight = (double)k.weight;
+            if constexpr (kGrad) {
+                const double w = (double)k.upstream * weight * p.inv_t, inv = 1.0 / (lane == 1 ? z_rest : z_all);
+                const double inv_all = __shfl_sync(kFullMask, inv, 0), inv_rest = __shfl_sync(kFullMask, inv, 1);
+                if (lane == 0) {
+                    k.grad_ref = ref;
+                    k.factor = empty ? w * (0.0 * z_all) : w * (total * a_rest * inv_all - (k.p_rest != 0.0 ? k.p_rest * inv_rest : 0.0)) * up;
+                }
+                const double q = w * total * a_list * inv_all;
+                const bool twice = k.twice != 0;
+#pragma unroll 1
+                for (int o = lane; o < p.K; o += 32) {
+                    double mine = l.prob[o];
+                    if (twice)
+                        for (int f = o + 1; f < p.K; ++f)
+                            if (l.token[f] == l.token[o]) mine += l.prob[f];
+                    l.g[o] = (float)(l.e[o] * q - w * mine);
+                }
+                arrive(&sh.known[slot]);
+            }
+            if (kLoss && rank == 0) {
+                const double log_z = log(z_all);                     // of exp((s - m_all) / T)
+                // entropy - sum p log q, with log q = s / T - m_all / T - log_z
+                double loss = k.entropy - k.cross + k.mass * ((double)m_all * p.inv_t + log_z);
+                if (k.p_rest != 0.0) {
+                    if (empty) loss = k.p_rest <= kRestRounding ? loss + 0.0 * z_all : loss + k.p_rest * (double)INFINITY;
+                    else loss += k.p_rest * (log(k.p_rest) - (((double)m_rest - (double)m_all) * p.inv_t + log(z_rest) - log_z));
+                }
+                if (lane == 0) {
+                    const bool out_of_it = k.left_out != 0;
+                    if (p.loss) p.loss[row] = out_of_it ? 0.0f : (float)(weight * loss);
+                    if (p.stats) *stats = out_of_it ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(z_all == z_all ? m_all : (float)nan, (float)z_all, m_rest, (float)z_rest);
+                }
+            }
+            arrive(&sh.done[slot]);
+        }
+        if (lane == 0 && order < n_live) atomicMin(&sh.lost, order);
+    } else {
+        // ---------------- compute ----------------
+        unsigned n = 0, stage = 0, turn = 0, lives = 0;
+        const uint64_t c2 = pack2(p.c, p.c);
+        unsigned order = cluster;
+        for (; order < n_live; order += p.clusters, ++n) {
+            const unsigned slot = n & 1u;
+            DistillRow& k = sh.row[slot];
+            const DistillList l(list_all + slot * distill_list_bytes(p.K), list_size);
+            if (!wait(&sh.listed[slot], (n / 2) & 1u, kSpinLimit)) break;
+            const DistillSegment<DT> seg(p, k.row, rank);
+            const int* first_of = first_all + slot * (parts_max + 2);
+            const int nc = seg.nc, parts = seg.n_tiles * kDistillWarps;
+            char* out = kGrad ? p.grad + ((int64_t)seg.b * p.out_b + (int64_t)seg.i * p.out_row) * E::ES : nullptr;
+            const bool same = kGrad && ((uintptr_t)seg.in & 15u) == ((uintptr_t)out & 15u);
+            uint4* o4 = reinterpret_cast<uint4*>(out + seg.e0 * E::ES);
+            const bool live = k.live != 0;
+            const unsigned phase = (lives >> slot) & 1u;
+            if (live) lives ^= 1u << slot;
+            const int drop = p.drop < 0 ? -1 : min(p.drop, seg.n_tiles - 1);
+            bool ok = true;
+            const int again = kLoss && kGrad && live ? max(0, seg.n_tiles - (int)S) : seg.n_tiles;      // tiles that do not stay: the first ones
+            unsigned stay_stage = 0;                                 // of the first that does
+            if (kLoss && live) {
+                DistillSum s{-INFINITY, kDistillLowest, 0.0};
+                if (tid < seg.scalars) {
+                    float x = E::load(seg.in, seg.scalar(p, tid));
+                    for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
+                        if (l.thread[o] == tid) x = -INFINITY;
+                    distill_raise(s, x, p.c);
+                    s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
+                    if (!(x == x)) s.m = -INFINITY;
+                }
+                for (int t = 0; t < seg.n_tiles; ++t) {
+                    if (t == again) { stay_stage = stage; }
+                    if (!wait(&sh.full[stage], turn & 1u, t == drop ? kTestSpinLimit : kSpinLimit)) { ok = false; break; }
+                    const uint4* tile = ring + stage * kDistillTile;
+                    const int c0 = t * kDistillTile + tid;
+                    constexpr uint32_t ninf = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
+                    uint4 w[kDistillEach];
+#pragma unroll
+                    for (int u = 0; u < kDistillEach; ++u) w[u] = tile[u * kDistillCompute + tid];
+                    if ((t + 1) * kDistillTile > nc) {               // the last tile: what lies behind the segment's end
+#pragma unroll
+                        for (int u = 0; u < kDistillEach; ++u)
+                            if (c0 + u * kDistillCompute >= nc) w[u] = make_uint4(ninf, ninf, ninf, ninf);
+                    }
+                    const int first = first_of[t * kDistillWarps + warp];
+                    if (first >= 0) {
+                        uint32_t gone = 0;                           // bits of the thread's elements that are listed
+                        for (int o = first; o >= 0; o = l.next[o])
+                            if (l.thread[o] == tid) gone |= 1u << l.where[o];
+#pragma unroll
+                        for (int u = 0; u < kDistillEach; ++u) blank<DT>(w[u], (gone >> (8 * u)) & 255u);
+                    }
+                    if (!kGrad || t < again) arrive(&sh.empty[stage]);
+                    if (++stage == S) { stage = 0; ++turn; }
+                    if (c0 - lane >= nc) continue;                   // nothing of this tile for the warp
+                    float m;
+                    if constexpr (kDistillEach == 4) m = E::max4(w[0], w[1], w[2], w[3]);
+                    else m = fmaxf(E::chunk_max(w[0]), E::chunk_max(w[1]));
+                    if (m > s.m) distill_raise(s, m, p.c);
+                    const uint64_t nref2 = pack2(-s.ref, -s.ref);
+                    uint64_t sum2 = add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2));
+                    if constexpr (kDistillEach == 4) sum2 = add2(sum2, add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
+                    float a0, a1;
+                    unpack2(sum2, a0, a1);
+                    s.acc += (double)(a0 + a1);
+                }
+                if (!ok) break;
+                distill_join(s);
+                if (lane == 0) { k.max[warp] = s.m; k.ref[warp] = s.ref; k.sum[warp] = s.acc; }
+                arrive(&sh.summed[slot]);
+            }
+            if constexpr (kGrad) {
+                if (live && !wait(&sh.known[slot], phase, kSpinLimit)) break;
+                const bool zero = !live || k.left_out;
+                const float nref = live ? -k.grad_ref : 0.0f, factor = live ? (float)k.factor : 0.0f;
+                const uint64_t nref2 = pack2(nref, nref), factor2 = pack2(factor, factor);
+                if (tid < seg.scalars) {
+                    const int64_t v = seg.scalar(p, tid);
+                    float g = 0.0f;
+                    if (!zero) {
+                        g = factor * ex2_approx(fmaf(E::load(seg.in, v), p.c, nref));
+                        for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
+                            if (l.thread[o] == tid && l.once[o]) g = l.g[o];
+                    }
+                    store_element<DT>(out, v, g);
+                }
+                for (int o = 0; o < seg.n_tiles; ++o) {
+                    // first those that have stayed, then the others, which come again meanwhile
+                    const bool stayed = live && o < seg.n_tiles - again;
+                    const int t = stayed ? again + o : o - (seg.n_tiles - again);
+                    unsigned at = stage;
+                    if (stayed) {
+                        at = stay_stage;
+                        if (++stay_stage == S) stay_stage = 0;
+                    } else if (live) {
+                        if (!wait(&sh.full[stage], turn & 1u, !kLoss && t == drop ? kTestSpinLimit : kSpinLimit)) { ok = false; break; }
+                        if (++stage == S) { stage = 0; ++turn; }
+                    }
+                    const uint4* tile = ring + at * kDistillTile;
+                    const int first = zero ? -1 : first_of[t * kDistillWarps + warp];
+#pragma unroll
+                    for (int u = 0; u < kDistillEach; ++u) {
+                        const int c = t * kDistillTile + u * kDistillCompute + tid;
+                        if (c >= nc) break;
+                        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                        if (!zero) {
+                            w = gradient_chunk<DT>(tile[u * kDistillCompute + tid], c2, nref2, factor2);
+                            for (int o = first; o >= 0; o = l.next[o])
+                                if (l.thread[o] == tid && l.where[o] / 8 == u && l.once[o]) set_element<DT>(w, l.where[o] & 7, element_bits<DT>(l.g[o]));
+                        }
+                        if (same) o4[c] = w;
+                        else store_chunk<DT>(out, seg.e0 + (int64_t)c * E::EPC, w);
+                    }
+                    if (live) arrive(&sh.empty[at]);
+                }
+                if (!ok) break;
+            }
+            arrive(&sh.done[slot]);
+        }
+        if (lane == 0 && order < n_live) atomicMin(&sh.lost, order);
+    }
+    __syncthreads();
+    // ---- rows that path or n_rows leave out, and, where a wait ran out, NaN in all that the CTA has not finished ----
+    const unsigned lost = sh.lost;
+    auto fill = [&](unsigned row, float x) {
+        const DistillSegment<DT> seg(p, row, rank);
+        if constexpr (kGrad) {
+            char* out = p.grad + ((int64_t)seg.b * p.out_b + (int64_t)seg.i * p.out_row) * E::ES;
+            if (tid < seg.scalars) store_element<DT>(out, seg.scalar(p, tid), x);
+            const uint32_t bits = element_bits<DT>(x), two = DT == CADD_DTYPE_BF16 ? bits | bits << 16 : bits;
+            const uint4 w = make_uint4(two, two, two, two);
+            const bool same = ((uintptr_t)seg.in & 15u) == ((uintptr_t)out & 15u);
+            for (int c = tid; c < seg.nc; c += kDistillThreads) {
+                if (same) reinterpret_cast<uint4*>(out + seg.e0 * E::ES)[c] = w;
+                else store_chunk<DT>(out, seg.e0 + (int64_t)c * E::EPC, w);
             }
         }
         if (kLoss && rank == 0 && tid == 0) {
+            if (p.loss) p.loss[row] = x;
+            if (p.stats) reinterpret_cast<float4*>(p.stats)[row] = make_float4(x, x, x, x);
+        }
+        if (x != 0.0f && tid == 0 && p.status) atomicOr(&p.status[seg.b], CADD_STATUS_INTERNAL_TIMEOUT);
+    };
+    if constexpr (kGrad) {
+        for (unsigned order = cluster; order < (unsigned)p.rows - n_live; order += p.clusters) fill(distill_row(p, sh.map, order, false), 0.0f);
+    } else {
+        for (unsigned order = blockIdx.x * kDistillThreads + tid; order < (unsigned)p.rows - n_live; order += gridDim.x * kDistillThreads) {
+            const unsigned row = distill_row(p, sh.map, order, false);
             if (p.loss) p.loss[row] = 0.0f;
             if (p.stats) reinterpret_cast<float4*>(p.stats)[row] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
-    };
-    if (left_out) {                                                  // the same for every CTA of the cluster
-        write_zeros();
-        return;
     }
-    if (kLoss && C > 1) cluster_arrive();                                     // waited for before the first access to another CTA's memory
-
-    // ---- copies under way, then the list ----
-    const int n_tiles = (nc + kDistillTile - 1) / kDistillTile;
-    const int drop = p.drop < 0 ? -1 : min(p.drop, n_tiles - 1);
-    constexpr int stages = kRing ? kDistillRing : kDistillMaxTiles;
-    auto stage = [](int t) { return kRing ? t % kDistillRing : t; };
-    auto parity = [](int t) { return kRing ? (unsigned)(t / kDistillRing) & 1u : 0u; };
-    auto issue = [&](int t) {
-        if (t == drop) return;                                       // test hook: this copy is never made
-        const int c0 = t * kDistillTile, s = stage(t);
-        const unsigned bytes = (unsigned)min(kDistillTile, nc - c0) * 16u;
-        *(volatile int*)&sh.sent[s] = t;
-        mbar_arrive_expect_tx(&sh.full[s], bytes);
-        bulk_load((void*)(seg + s * kDistillTile), in + e0 * E::ES + (int64_t)c0 * 16, bytes, &sh.full[s]);
-    };
-    // a warp is done with tile t: the last one sends for the tile that takes its place
-    auto release = [&](int t) {
-        if constexpr (kRing) {
-            __syncwarp();
-            const int s = t % kDistillRing;
-            if (lane == 0 && atomicAdd(&sh.released[s], 1u) == kDistillThreads / 32 - 1) {
-                atomicExch(&sh.released[s], 0u);
-                if (t + kDistillRing < n_tiles) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    issue(t + kDistillRing);
-                }
-            }
-        }
-    };
-    auto landed = [&](int t) {
-        return __all_sync(kFullMask, mbar_wait_limited(&sh.full[stage(t)], parity(t), tile_wait_limit(t, drop))) != 0;
-    };
-    if (tid == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(&sh.full[s], 1);
-        for (int s = 0; s < stages; ++s) sh.sent[s] = -1;
-        for (int s = 0; s < kDistillRing; ++s) sh.released[s] = 0;
-        sh.timeout = 0;
-        sh.twice = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int t = 0; t < stages && t < n_tiles; ++t) issue(t);
-    }
-    const int groups = (nc + 31) / 32;
-    for (int k = tid; k < groups + 2; k += kDistillThreads) first_of[k] = -1;
-    int tok = -1;
-    if (tid < p.K) {
-        const int64_t at = ((int64_t)b * p.R + r) * p.K + tid;
-        tok = p.token[at];
-        if (tok < 0 || tok >= p.V) tok = -1;
-        sh.token[tid] = tok;
-        sh.value[tid] = p.value[at];
-        sh.logit[tid] = kLoss && tok >= 0 ? E::load(in, tok) : 0.0f;
-    }
-    __syncthreads();
-    if (tok >= 0) {
-        bool once = true;
-        for (int k = 0; k < tid; ++k) once = once && sh.token[k] != tok;
-        sh.once[tid] = once;
-        if (!once) sh.twice = 1;
-        // where in this CTA's segment the token lies
-        int group = -1, e = 0, c = 0;
-        if (tok >= e0 && tok < e0 + (int64_t)nc * E::EPC) {
-            c = (int)((tok - e0) / E::EPC);
-            e = (int)((tok - e0) % E::EPC);
-            group = c / 32;
-        } else if (rank == 0 && tok < sp.head) { c = tok; group = groups; }
-        else if (rank == C - 1 && tok >= p.V - sp.tail) { c = (int)(tok - (p.V - sp.tail)) + (rank == 0 ? sp.head : 0); group = groups + 1; }
-        sh.chunk[tid] = c;
-        sh.elem[tid] = (uint8_t)e;
-        if (group >= 0) {
-            if (!kLoss) sh.logit[tid] = E::load(in, tok);
-            sh.next[tid] = (int16_t)atomicExch(&first_of[group], tid);
-        }
-    }
-    __syncthreads();
-
-    // ---- the target's probabilities (warp 0; the others go on to the tiles) ----
-    double p_rest = 0.0, entropy = 0.0, mass = 0.0;                  // warp 0, all lanes: entropy = sum p log p of the entries
-    if (warp == 0) {
-        double top = -INFINITY;
-        bool any = false;
-        if (!p.rest) {
-            for (int k = lane; k < p.K; k += 32)
-                if (sh.token[k] >= 0) {
-                    top = fmax(top, sh.value[k]);                    // (NaN shows in the sum)
-                    any = any || !(sh.value[k] == -INFINITY);
-                }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmax(top, __shfl_xor_sync(kFullMask, top, o));
-        } else {
-            top = p.lse ? p.lse[(int64_t)b * p.R + r] / p.inv_t : 0.0;
-        }
-        double sum = 0.0;
-        for (int k = lane; k < p.K; k += 32) {
-            double q = 0.0;
-            if (sh.token[k] >= 0) {
-                q = exp((sh.value[k] - top) * p.inv_t);
-                if (p.rest) any = true;
-            }
-            sh.prob[k] = q;
-            sum += q;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
-        any = __any_sync(kFullMask, any);
-        const double scale = p.rest ? 1.0 : 1.0 / sum, log_sum = p.rest ? 0.0 : log(sum);
-        if (p.rest) p_rest = sum < 1.0 ? 1.0 - sum : (sum == sum ? 0.0 : sum);
-        for (int k = lane; k < p.K; k += 32) {
-            const double q = sh.prob[k] * scale;
-            sh.prob[k] = q;
-            if (q > 0.0) entropy += q * ((sh.value[k] - top) * p.inv_t - log_sum);
-            else if (!(q == 0.0)) entropy = q;
-            mass += q;
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            entropy += __shfl_xor_sync(kFullMask, entropy, o);
-            mass += __shfl_xor_sync(kFullMask, mass, o);
-        }
-        if (lane == 0) sh.left_out = any ? 0 : 1;
-    }
-
-    // bits of the elements of chunk c that are listed
-    auto listed = [&](int first, int c) {
-        uint32_t bits = 0;
-        for (int k = first; k >= 0; k = sh.next[k])
-            if (sh.chunk[k] == c) bits |= 1u << sh.elem[k];
-        return bits;
-    };
-    bool timeout = false;
-    float m_rest = 0.0f, m_all = 0.0f;
-    double z_rest = 0.0, z_all = 0.0;
-    if constexpr (kLoss) {
-        // ---- sum over the tokens that are not listed ----
-        DistillSum s{-INFINITY, kDistillLowest, 0.0};
-        const uint64_t c2 = pack2(p.c, p.c);
-        if (tid < scalars) {
-            float x = E::load(in, mine_scalar);
-            const int at = mine_scalar < sp.head ? groups : groups + 1;
-            if (listed(first_of[at], tid)) x = -INFINITY;
-            distill_raise(s, x, p.c);
-            s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
-            if (!(x == x)) s.m = -INFINITY;
-        }
-        for (int t = 0; t < n_tiles; ++t) {
-            if (!landed(t)) { timeout = true; break; }
-            const uint4* tile = seg + stage(t) * kDistillTile;
-            const int c0 = t * kDistillTile + tid;
-            constexpr uint32_t ninf = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
-            uint4 w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int c = c0 + u * kDistillThreads;
-                w[u] = make_uint4(ninf, ninf, ninf, ninf);
-                if (c < nc) {
-                    w[u] = tile[u * kDistillThreads + tid];
-                    const int first = first_of[c / 32];
-                    if (first >= 0) blank<DT>(w[u], listed(first, c));
-                }
-            }
-            release(t);
-            const float m = E::max4(w[0], w[1], w[2], w[3]);
-            if (m > s.m) distill_raise(s, m, p.c);
-            const uint64_t nref2 = pack2(-s.ref, -s.ref);
-            const uint64_t sum2 = add2(add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2)),
-                                       add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
-            float a0, a1;
-            unpack2(sum2, a0, a1);
-            s.acc += (double)(a0 + a1);
-        }
-        // ---- threads, warps, CTAs ----
-        distill_join(s);
-        if (lane == 0) { sh.warp_max[warp] = s.m; sh.warp_ref[warp] = s.ref; sh.warp_sum[warp] = s.acc; }
-        if (timeout) sh.timeout = 1;
-        __syncthreads();
-        timeout = sh.timeout != 0;
-        if (warp == 0) {
-            const bool in_use = lane < kDistillThreads / 32;
-            s = DistillSum{in_use ? sh.warp_max[lane] : -INFINITY, in_use ? sh.warp_ref[lane] : kDistillLowest, in_use ? sh.warp_sum[lane] : 0.0};
-            distill_join(s);
-            if (timeout) s.acc = __longlong_as_double(0x7ff8000000000000ll);
-        }
-        if (C > 1) {
-            cluster_wait();
-            if (warp == 0 && lane < (int)C) {
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&sh.peer_max[rank], lane)), "f"(s.m) : "memory");
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&sh.peer_ref[rank], lane)), "f"(s.ref) : "memory");
-                asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&sh.peer_sum[rank], lane)), "d"(s.acc) : "memory");
-            }
-            __syncwarp();
-            cluster_arrive();
-            cluster_wait();
-            if (warp == 0) {
-                const bool in_use = lane < (int)C;
-                s = DistillSum{in_use ? sh.peer_max[lane] : -INFINITY, in_use ? sh.peer_ref[lane] : kDistillLowest, in_use ? sh.peer_sum[lane] : 0.0};
-                distill_join(s);
-            }
-        }
-        if (warp == 0) {
-            m_rest = s.m >= kDistillLowest ? s.m : -INFINITY;
-            z_rest = m_rest > -INFINITY ? s.acc * kEx2BiasFix * exp2((double)s.ref - (double)m_rest * (double)p.c) : (s.acc == s.acc ? 0.0 : s.acc);
-            m_all = m_rest;
-            bool bad = !(s.acc == s.acc);
-            for (int k = lane; k < p.K; k += 32)
-                if (sh.token[k] >= 0) {
-                    const float x = sh.logit[k];
-                    if (!(x == x)) bad = true;
-                    if (x >= kDistillLowest) m_all = fmaxf(m_all, x);
-                }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(kFullMask, m_all, o));
-            double z = 0.0;
-            for (int k = lane; k < p.K; k += 32)
-                if (sh.token[k] >= 0 && sh.once[k] && sh.logit[k] >= kDistillLowest) z += exp(((double)sh.logit[k] - (double)m_all) * p.inv_t);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(kFullMask, z, o);
-            if (m_rest > -INFINITY) z += z_rest * exp(((double)m_rest - (double)m_all) * p.inv_t);
-            z_all = __any_sync(kFullMask, bad) ? __longlong_as_double(0x7ff8000000000000ll) : z;
-        }
-    } else if (warp == 0) {
-        const float4 st = reinterpret_cast<const float4*>(p.stats)[row];
-        m_all = st.x; z_all = (double)st.y; m_rest = st.z; z_rest = (double)st.w;
-    }
-
-    // ---- loss and the gradient's factors (warp 0) ----
-    if (warp == 0) {
-        const double nan = __longlong_as_double(0x7ff8000000000000ll);
-        if (!(m_all > -INFINITY)) z_all = nan;                       // a row without a finite logit
-        const bool empty = !(m_rest > -INFINITY);                    // no token is left beside the list
-        const double log_z = log(z_all), total = mass + p_rest;
-        const double w = (p.grad_loss ? (double)p.grad_loss[row] : 1.0) * (double)weight * p.inv_t;
-        double cross = 0.0;                                          // sum p log q
-        for (int k = lane; k < p.K; k += 32) {
-            if (sh.token[k] < 0) continue;
-            const double x = sh.logit[k] < kDistillLowest ? -INFINITY : (double)sh.logit[k];
-            const double log_q = (x - (double)m_all) * p.inv_t - log_z;
-            if (sh.prob[k] != 0.0) cross += sh.prob[k] * log_q;
-            double mine = sh.prob[k];
-            if (sh.twice)
-                for (int n = k + 1; n < p.K; ++n)
-                    if (sh.token[n] == sh.token[k]) mine += sh.prob[n];
-            if (kGrad) sh.g[k] = (float)(w * (total * exp(log_q) - mine));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) cross += __shfl_xor_sync(kFullMask, cross, o);
-        if (kLoss && rank == 0 && lane == 0) {
-            double loss = entropy - cross;
-            if (p_rest != 0.0) {
-                if (empty) loss = p_rest <= kRestRounding ? loss + 0.0 * z_all : loss + p_rest * (double)INFINITY;
-                else loss += p_rest * (log(p_rest) - (((double)m_rest - (double)m_all) * p.inv_t + log(z_rest) - log_z));
-            }
-            const bool out_of_it = sh.left_out != 0;
-            if (p.loss) p.loss[row] = out_of_it ? 0.0f : (float)((double)weight * loss);
-            if (p.stats) reinterpret_cast<float4*>(p.stats)[row] =
-                out_of_it ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(z_all == z_all ? m_all : (float)nan, (float)z_all, m_rest, (float)z_rest);
-        }
-        if (kGrad && lane == 0) {
-            // an exponential below is exp((s - m_rest) / T) * 2^(m_rest c - ref)
-            const float ref = empty ? 0.0f : ceilf(m_rest * p.c);
-            double f = empty ? 0.0 * z_all : total * exp(((double)m_rest - (double)m_all) * p.inv_t) / z_all - (p_rest != 0.0 ? p_rest / z_rest : 0.0);
-            if (!empty) f *= exp2((double)ref - (double)m_rest * (double)p.c);
-            sh.ref = ref;
-            sh.factor = w * f;
-        }
-    }
-    if constexpr (kGrad) {
-        __syncthreads();
-        if (sh.left_out) write_zeros();
-        else {
-            // ---- the gradient ----
-            const float nref = -sh.ref;
-            float factor = (float)sh.factor;
-            if (timeout) factor = __int_as_float(0x7fc00000);
-            if (tid < scalars) {
-                const int at = mine_scalar < sp.head ? groups : groups + 1;
-                float g = factor * ex2_approx(fmaf(E::load(in, mine_scalar), p.c, nref));
-                for (int k = first_of[at]; k >= 0; k = sh.next[k])
-                    if (sh.chunk[k] == tid && sh.once[k]) g = sh.g[k];
-                store_element<DT>(out, mine_scalar, g);
-            }
-            const uint64_t c2 = pack2(p.c, p.c), nref2 = pack2(nref, nref);
-            uint4* o4 = reinterpret_cast<uint4*>(out + e0 * E::ES);
-            for (int t = 0; t < n_tiles; ++t) {
-                if (!kLoss && !timeout && !landed(t)) timeout = true;
-                if (!kLoss && timeout) factor = __int_as_float(0x7fc00000);
-                const uint4* tile = seg + stage(t) * kDistillTile;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int c = t * kDistillTile + u * kDistillThreads + tid;
-                    if (c >= nc) break;
-                    float f[E::EPC];
-                    E::unpack(tile[u * kDistillThreads + tid], f);
-#pragma unroll
-                    for (int q = 0; q < E::EPC; q += 2) {
-                        float t0, t1;
-                        unpack2(fma2(pack2(f[q], f[q + 1]), c2, nref2), t0, t1);
-                        f[q] = factor * ex2_approx(t0);
-                        f[q + 1] = factor * ex2_approx(t1);
-                    }
-                    const int first = first_of[c / 32];
-                    if (first >= 0)
-                        for (int k = first; k >= 0; k = sh.next[k])
-                            if (sh.chunk[k] == c && sh.once[k]) {
-#pragma unroll
-                                for (int q = 0; q < E::EPC; ++q)
-                                    if (q == sh.elem[k]) f[q] = sh.g[k];
-                            }
-                    if (same) o4[c] = pack_chunk<DT>(f);
-                    else {
-#pragma unroll
-                        for (int q = 0; q < E::EPC; ++q) store_element<DT>(out, e0 + (int64_t)c * E::EPC + q, f[q]);
-                    }
-                }
-                if (!timeout) release(t);
-            }
-        }
-    }
-    // No CTA leaves with a copy of its own in flight.  All tiles have been waited for, but where a wait ran out or the list left the
-    // row out before its first tile: then the last tile sent for in each stage is, once no warp can send for another.
-    if constexpr (!kLoss) {
-        if (timeout) sh.timeout = 1;
-        __syncthreads();
-    }
-    if (tid == 0 && (sh.timeout || (!kLoss && sh.left_out))) {
-        for (int s = 0; s < stages; ++s)
-            if (sh.sent[s] >= 0) mbar_wait_bounded(&sh.full[s], parity(sh.sent[s]));
-        if (sh.timeout && p.status) atomicOr(&p.status[b], CADD_STATUS_INTERNAL_TIMEOUT);
-    }
+    for (unsigned order = lost; order < n_live; order += p.clusters) fill(distill_row(p, sh.map, order, true), __int_as_float(0x7fc00000));
+    if (C > 1) { cluster_arrive(); cluster_wait(); }                 // nobody writes to a CTA that has left
 }
 
 // Status of one request, where it is asked for.
-__global__ void __launch_bounds__(kDistillThreads) distill_status_kernel(DistillParams p) {
+__global__ void __launch_bounds__(kDistillStatusThreads) distill_status_kernel(DistillParams p) {
     __shared__ int bits;
     const int b = blockIdx.x, tid = threadIdx.x;
     if (tid == 0) bits = 0;
@@ -557,7 +799,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_status_kernel(Distill
     int st = 0;
     if (p.path ? p.path_len[b] < 0 || p.path_len[b] > min(p.L - 1, p.path_cols) : p.n_rows && (p.n_rows[b] < 0 || p.n_rows[b] > p.L)) st |= CADD_STATUS_BAD_LENGTH;
     const int live = distill_live(p, b);
-    for (int64_t n = tid; n < (int64_t)live * p.K; n += kDistillThreads) {
+    for (int64_t n = tid; n < (int64_t)live * p.K; n += kDistillStatusThreads) {
         const int i = (int)(n / p.K), k = (int)(n - (int64_t)i * p.K);
         const int r = !p.path ? i : (i == 0 ? 0 : p.path[(int64_t)b * p.path_cols + i - 1]);
         if (r < 0 || r >= p.R) { st |= CADD_STATUS_BAD_PATH; continue; }

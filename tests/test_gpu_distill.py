@@ -47,7 +47,7 @@ def test_sizes(dtype, rest, B, L, V, K):
     every(random_distill(B, L, V, K, dtype, seed=B + V + K, rest=rest))
 
 
-@pytest.mark.parametrize("V", [2048 * 8 - 3, 2048 * 8, 131072 + 5, 300007, 800000])
+@pytest.mark.parametrize("V", [2048 * 8 - 3, 2048 * 8, 131072 + 5, 300007, 2000000])
 def test_segments_of_every_size(V):
     every(random_distill(1, 2, V, 32, torch.bfloat16, seed=V, rest=True))
 

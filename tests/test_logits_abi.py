@@ -38,8 +38,8 @@ def loss():
 
 CALLS = {"adjust": (adjust, "cadd_adjust_logits"), "loss": (loss, "cadd_distill_loss"), "grad": (loss, "cadd_distill_grad")}
 DISTILL = [
-    (dict(batch=0), G.ERR_SHAPE), (dict(L=0), G.ERR_SHAPE), (dict(V=0), G.ERR_SHAPE), (dict(V=800001, grad_stride_l=1 << 20, grad_stride_b=1 << 24), G.ERR_SHAPE),
-    (dict(logits_dtype=1, V=400001, grad_stride_l=1 << 20, grad_stride_b=1 << 24), G.ERR_SHAPE), (dict(K=0), G.ERR_SHAPE), (dict(K=257), G.ERR_SHAPE), (dict(R=0), G.ERR_SHAPE),
+    (dict(batch=0), G.ERR_SHAPE), (dict(L=0), G.ERR_SHAPE), (dict(V=0), G.ERR_SHAPE), (dict(V=2000001, grad_stride_l=1 << 21, grad_stride_b=1 << 25), G.ERR_SHAPE),
+    (dict(K=0), G.ERR_SHAPE), (dict(K=257), G.ERR_SHAPE), (dict(R=0), G.ERR_SHAPE),
     (dict(path=None, path_len=None, R=3), G.ERR_SHAPE), (dict(path_cols=0), G.ERR_SHAPE), (dict(temperature=0.0), G.ERR_SHAPE), (dict(temperature=-1.0), G.ERR_SHAPE),
     (dict(temperature=float("nan")), G.ERR_SHAPE), (dict(temperature=float("inf")), G.ERR_SHAPE), (dict(temperature=2.0 ** 21), G.ERR_SHAPE),
     (dict(logits_dtype=2), G.ERR_DTYPE), (dict(logits=None), G.ERR_NULL), (dict(teacher_token=None), G.ERR_NULL), (dict(teacher_logit=None), G.ERR_NULL),
