@@ -93,7 +93,7 @@ constexpr int kDistillEntry = 30;                 // bytes of an entry
 // of a tile (-1: none; the last two parts are the row's scalar head and tail); the ring.
 struct DistillShared {
     alignas(8) uint64_t full[kDistillMaxStages], empty[kDistillMaxStages];
-    uint64_t listed[2], done[2], summed[2], known[2], exchanged[2];
+    uint64_t listed[2], ready[2], done[2], summed[2], known[2], exchanged[2];
     int sent[kDistillMaxStages];                  // last tile sent for into each stage, -1: none
     int error;
     unsigned lost;                                // the first row in the cluster's order that some role has not finished
@@ -126,20 +126,11 @@ __device__ __forceinline__ int distill_live(const DistillParams& p, int b) {
     return p.n_rows ? max(0, min(p.n_rows[b], p.L)) : p.L;
 }
 
-// -Inf in the elements of a chunk whose bit is set.
+// -Inf in an element of a chunk in shared memory.
 template <int DT>
-__device__ __forceinline__ void blank(uint4& w, uint32_t bits) {
-    uint32_t* x = &w.x;
-    if constexpr (DT == CADD_DTYPE_BF16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t gone = ((bits >> (2 * i)) & 1u ? 0x0000ffffu : 0u) | ((bits >> (2 * i + 1)) & 1u ? 0xffff0000u : 0u);
-            x[i] = (x[i] & ~gone) | (0xff80ff80u & gone);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (bits >> i) & 1u ? 0xff800000u : x[i];
-    }
+__device__ __forceinline__ void hide_element(uint4* chunk, int e) {
+    if constexpr (DT == CADD_DTYPE_BF16) reinterpret_cast<volatile uint16_t*>(chunk)[e] = 0xff80u;
+    else reinterpret_cast<volatile uint32_t*>(chunk)[e] = 0xff800000u;
 }
 // factor * 2^(x c - ref) of a chunk's elements, as a chunk.
 template <int DT>
@@ -164,20 +155,10 @@ __device__ __forceinline__ uint4 gradient_chunk(const uint4& w, uint64_t c2, uin
     }
     return r;
 }
-// An element's bits, and an element of a chunk replaced or read.
+// An element's bits.
 template <int DT> __device__ __forceinline__ uint32_t element_bits(float x) {
     if constexpr (DT == CADD_DTYPE_BF16) return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(x));
     else return __float_as_uint(x);
-}
-template <int DT> __device__ __forceinline__ void set_element(uint4& w, int e, uint32_t bits) {
-    uint32_t* x = &w.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (DT == CADD_DTYPE_BF16) {
-            if (e == 2 * i) x[i] = (x[i] & 0xffff0000u) | bits;
-            if (e == 2 * i + 1) x[i] = (x[i] & 0x0000ffffu) | bits << 16;
-        } else if (e == i) x[i] = bits;
-    }
 }
 template <int DT> __device__ __forceinline__ void store_chunk(char* row, int64_t i, const uint4& w) {      // where it is not aligned
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
@@ -336,7 +317,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
     const int list_size = (p.K + 31) & ~31;
     unsigned char* const list_all = distill_smem_raw + distill_shared_bytes();
     int* const first_all = reinterpret_cast<int*>(list_all + 2 * distill_list_bytes(p.K));
-    const uint4* ring = reinterpret_cast<const uint4*>(distill_smem_raw + distill_ring_at(p.chunks_max, p.K));
+    uint4* ring = reinterpret_cast<uint4*>(distill_smem_raw + distill_ring_at(p.chunks_max, p.K));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned C = (unsigned)p.C, cluster = blockIdx.x / C;
     const int rank = (int)(blockIdx.x - cluster * C);
@@ -344,6 +325,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
         for (int s = 0; s < p.stages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], kDistillWarps); sh.sent[s] = -1; }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&sh.listed[s], 1);
+            mbar_init(&sh.ready[s], 1);
             mbar_init(&sh.done[s], kDistillWarps + 1);
             mbar_init(&sh.summed[s], kDistillWarps);
             mbar_init(&sh.known[s], 1);
@@ -425,6 +407,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             if (r < 0) {
                 if (lane == 0) k.live = 0;
                 arrive(&sh.listed[n & 1u]);
+                arrive(&sh.ready[n & 1u]);
                 continue;
             }
             for (int o = lane; o < parts + 2; o += 32) first_of[o] = -1;
@@ -434,21 +417,11 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             double top = p.rest && p.lse ? p.lse[(int64_t)seg.b * p.R + r] / p.inv_t : (p.rest ? 0.0 : -INFINITY);
             float m_list = -INFINITY;
             bool any = false, twice = false;
-            // tokens, and where they lie
-            for (int o = lane; o < p.K; o += 32) {
-                int tok = p.token[at + o];
+            // tokens, and where they lie: all that the sums need
+            for (int o = lane; o < list_size; o += 32) {
+                int tok = o < p.K ? p.token[at + o] : -1;
                 if (tok < 0 || tok >= p.V) tok = -1;
                 l.token[o] = tok;
-                const double v = p.value[at + o];
-                l.prob[o] = v;
-                if (tok >= 0) {
-                    if (!p.rest) top = fmax(top, v);
-                    any = any || p.rest || !(v == -INFINITY);       // (NaN counts: it shows in the sum)
-                }
-            }
-            __syncwarp();
-            for (int o = lane; o < p.K; o += 32) {
-                const int tok = l.token[o];
                 int part = -1, thread = 0, where = 0;
                 if (tok >= seg.e0 && tok < seg.e0 + (int64_t)seg.nc * E::EPC) {
                     const unsigned c = (unsigned)(tok - seg.e0) / E::EPC, t = c / kDistillTile, in_tile = c - t * kDistillTile;
@@ -456,19 +429,36 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     where = (int)(in_tile / kDistillCompute * 8 + (unsigned)(tok - seg.e0) % E::EPC);
                     part = (int)t * kDistillWarps + thread / 32;
                 } else if (tok >= 0 && tok < seg.head) { thread = tok; part = parts; }
-                else if (tok >= p.V - seg.sp.tail && seg.scalars > seg.head) { thread = (int)(tok - (p.V - seg.sp.tail)) + seg.head; part = parts + 1; }
+                else if (tok >= 0 && tok >= p.V - seg.sp.tail && seg.scalars > seg.head) { thread = (int)(tok - (p.V - seg.sp.tail)) + seg.head; part = parts + 1; }
                 l.thread[o] = (int16_t)thread;
                 l.where[o] = (uint8_t)where;
                 if (part >= 0) l.next[o] = (int16_t)atomicExch(&first_of[part], o);
+                // a token's first entry: none before it among the 32 of this turn, nor in the turns before
+                const unsigned same = __match_any_sync(kFullMask, tok);
+                bool once = tok >= 0 && __ffs(same) - 1 == lane;
+                for (int f = 0; f < o - lane; f += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(&l.token[f]);
+                    once = once && x.x != tok && x.y != tok && x.z != tok && x.w != tok;
+                }
+                l.once[o] = once;
+                twice = twice || (tok >= 0 && !once);
                 // (the gradient alone may be written over logits by the other CTAs meanwhile: only this CTA's are read)
-                float x = -INFINITY;
-                if (tok >= 0 && (kLoss || part >= 0)) x = E::load(seg.in, tok);
+                l.e[o] = tok >= 0 && (kLoss || part >= 0) ? 1.0 : 0.0;
+                __syncwarp();
+            }
+            arrive(&sh.listed[n & 1u]);
+            // the target's and the drafter's logits
+            for (int o = lane; o < p.K; o += 32) {
+                const int tok = l.token[o];
+                const double v = p.value[at + o];
+                const float x = l.e[o] != 0.0 ? E::load(seg.in, tok) : -INFINITY;
+                l.prob[o] = v;
                 l.e[o] = (double)x;
                 m_list = fmaxf(m_list, x);
-                bool once = true;
-                for (int f = 0; f < o && tok >= 0; ++f) once = once && l.token[f] != tok;
-                l.once[o] = once;
-                twice = twice || !once;
+                if (tok >= 0) {
+                    if (!p.rest) top = fmax(top, v);
+                    any = any || p.rest || !(v == -INFINITY);       // (NaN counts: it shows in the sum)
+                }
             }
             m_list = warp_max(m_list);
             if (!(m_list >= kDistillLowest)) m_list = -INFINITY;
@@ -520,7 +510,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 k.left_out = any ? 0 : 1;
                 k.twice = twice;
             }
-            arrive(&sh.listed[n & 1u]);
+            arrive(&sh.ready[n & 1u]);
         }
     } else if (warp == kDistillWarps + 2) {
         // ---------------- finish ----------------
@@ -529,7 +519,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             const unsigned slot = n & 1u;
             DistillRow& k = sh.row[slot];
             const DistillList l(list_all + slot * distill_list_bytes(p.K), list_size);
-            if (!wait(&sh.listed[slot], (n / 2) & 1u, kSpinLimit)) break;
+            if (!wait(&sh.ready[slot], (n / 2) & 1u, kSpinLimit)) break;
             const unsigned row = k.row;
             float4* stats = reinterpret_cast<float4*>(p.stats) + row;
             if (!k.live) {
@@ -667,9 +657,18 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 for (int t = 0; t < seg.n_tiles; ++t) {
                     if (t == again) { stay_stage = stage; }
                     if (!wait(&sh.full[stage], turn & 1u, t == drop ? kTestSpinLimit : kSpinLimit)) { ok = false; break; }
-                    const uint4* tile = ring + stage * kDistillTile;
+                    uint4* tile = ring + stage * kDistillTile;
                     const int c0 = t * kDistillTile + tid;
                     constexpr uint32_t ninf = E::ES == 2 ? 0xff80ff80u : 0xff800000u;
+                    const int first = first_of[t * kDistillWarps + warp];
+                    if (first >= 0) {
+                        // listed tokens of this warp's part: each becomes -Inf where it lies (its gradient does not come from there)
+                        for (int o = first; o >= 0; o = l.next[o])
+                            if (l.thread[o] == tid) {
+                                hide_element<DT>(tile + (l.where[o] / 8) * kDistillCompute + tid, l.where[o] & 7);
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (the stage's next tile comes after this)
+                            }
+                    }
                     uint4 w[kDistillEach];
 #pragma unroll
                     for (int u = 0; u < kDistillEach; ++u) w[u] = tile[u * kDistillCompute + tid];
@@ -677,14 +676,6 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
 #pragma unroll
                         for (int u = 0; u < kDistillEach; ++u)
                             if (c0 + u * kDistillCompute >= nc) w[u] = make_uint4(ninf, ninf, ninf, ninf);
-                    }
-                    const int first = first_of[t * kDistillWarps + warp];
-                    if (first >= 0) {
-                        uint32_t gone = 0;                           // bits of the thread's elements that are listed
-                        for (int o = first; o >= 0; o = l.next[o])
-                            if (l.thread[o] == tid) gone |= 1u << l.where[o];
-#pragma unroll
-                        for (int u = 0; u < kDistillEach; ++u) blank<DT>(w[u], (gone >> (8 * u)) & 255u);
                     }
                     if (!kGrad || t < again) arrive(&sh.empty[stage]);
                     if (++stage == S) { stage = 0; ++turn; }
@@ -739,14 +730,14 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                         const int c = t * kDistillTile + u * kDistillCompute + tid;
                         if (c >= nc) break;
                         uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                        if (!zero) {
-                            w = gradient_chunk<DT>(tile[u * kDistillCompute + tid], c2, nref2, factor2);
-                            for (int o = first; o >= 0; o = l.next[o])
-                                if (l.thread[o] == tid && l.where[o] / 8 == u && l.once[o]) set_element<DT>(w, l.where[o] & 7, element_bits<DT>(l.g[o]));
-                        }
+                        if (!zero) w = gradient_chunk<DT>(tile[u * kDistillCompute + tid], c2, nref2, factor2);
                         if (same) o4[c] = w;
                         else store_chunk<DT>(out, seg.e0 + (int64_t)c * E::EPC, w);
                     }
+                    // listed tokens, over what this thread has written
+                    for (int o = first; o >= 0; o = l.next[o])
+                        if (l.thread[o] == tid && l.once[o])
+                            store_element<DT>(out, seg.e0 + (int64_t)(t * kDistillTile + (l.where[o] / 8) * kDistillCompute + tid) * E::EPC + (l.where[o] & 7), l.g[o]);
                     if (live) arrive(&sh.empty[at]);
                 }
                 if (!ok) break;
