@@ -999,29 +999,34 @@ def cadd_cache_evict(cache: KvCache, weights: torch.Tensor, new_block_table: tor
 
 # ---- the logits of a round: penalties, biases, masks; distillation ----
 
-def _need_logits(t: torch.Tensor, shape, dtype, dev, name: str):
+def _need_logits(t: torch.Tensor, shape, dtype, index: int, name: str):
     """Pointer and (batch, row) strides of logits [batch, rows, V]."""
-    if t.dim() != 3 or t.dtype != dtype or t.device != dev or t.shape != shape or t.stride(2) != 1:
-        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {dev} with a contiguous vocabulary axis")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on cuda:{index}")
+    sb, sr, sv = t.stride()
+    if sv != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have a contiguous vocabulary axis")
     # an axis of length one may carry any stride; it is never stepped along
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else 0
+    return t.data_ptr(), sb if shape[0] > 1 else 0, sr if shape[1] > 1 else 0
 
 
-def _need_like(t: Optional[torch.Tensor], dtype, shape, dev, name: str) -> Optional[int]:
+def _need_like(t: Optional[torch.Tensor], dtype, shape, index: int, name: str) -> Optional[int]:
     """Pointer of a contiguous input or output of the given dtype and shape on the call's device (None passes)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != dev or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {dev}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{index}")
     return t.data_ptr()
 
 
 def _logits_of(t: torch.Tensor, name: str):
-    if t.device.type != "cuda":
+    """Device, its index, and dtype code of the logits of a call."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError(f"{name} must be a CUDA tensor (there is no CPU path)")
-    if t.dim() != 3 or t.shape[2] > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name} must be [batch, rows, V] with a contiguous vocabulary axis")
-    return t.device, _dtype_code(t)
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [batch, rows, V]")
+    return t.device, index, _dtype_code(t)
 
 
 def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, parent_idx=None, history=None, history_len=None,
@@ -1036,24 +1041,23 @@ def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, pa
     the first prompt_len tokens count for repetition alone.  repetition, presence, frequency fp32 [batch].  bias_token int32,
     bias fp32 [batch, n_bias].  allowed int32 [n_masks, ceil(V / 32)] (bit v % 32 of word v / 32), allowed_row int32 [batch, R],
     -1 for rows without a mask.  status int32 [batch]."""
-    dev, code = _logits_of(logits, "logits")
+    dev, index, code = _logits_of(logits, "logits")
     B, R, V = shape = logits.shape
-    lp, sb, sr = _need_logits(logits, shape, logits.dtype, dev, "logits")
+    lp, sb, sr = _need_logits(logits, shape, logits.dtype, index, "logits")
     if out is None or out is logits:
         out, op, ob, orow = logits, lp, sb, sr
     else:
-        op, ob, orow = _need_logits(out, shape, logits.dtype, dev, "out")
+        op, ob, orow = _need_logits(out, shape, logits.dtype, index, "out")
     hp, hs, hc = None, 0, 0
     if history is not None:
-        _need(history.dim() == 2 and history.shape[0] == B and history.dtype == torch.int32 and history.device == dev
+        _need(history.dim() == 2 and history.shape[0] == B and history.dtype is torch.int32 and history.get_device() == index
               and (history.shape[1] <= 1 or history.stride(1) == 1), "history must be an int32 tensor [batch, n] on the call's device with contiguous rows")
         hc = history.shape[1]
         hp, hs = (history.data_ptr(), history.stride(0) if B > 1 else 0) if hc else (None, 0)
     else:
         _need(history_len is None and prompt_len is None, "history_len and prompt_len come with history")
-    _need((bias_token is None) == (bias is None), "bias comes with bias_token")
-    _need((allowed is None) == (allowed_row is None), "allowed comes with allowed_row")
-    _need((token_ids is None) == (parent_idx is None), "token_ids comes with parent_idx")
+    if (bias_token is None) != (bias is None) or (allowed is None) != (allowed_row is None) or (token_ids is None) != (parent_idx is None):
+        raise ValueError("bias comes with bias_token, allowed with allowed_row, token_ids with parent_idx")
     n_bias, n_allowed, f32, i32 = 0, 0, torch.float32, torch.int32
     if bias is not None:
         _need(bias.dim() == 2, "bias must be [batch, n_bias]")
@@ -1062,13 +1066,13 @@ def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, pa
         _need(allowed.dim() == 2, "allowed must be [n_masks, ceil(V / 32)]")
         n_allowed = allowed.shape[0]
     a = AdjustArgs(C.sizeof(AdjustArgs), flags, B, R, code, n_bias, V, lp, sb, sr, op, ob, orow,
-                   _need_like(n_nodes, i32, (B,), dev, "n_nodes"), _need_like(token_ids, i32, (B, R), dev, "token_ids"),
-                   _need_like(parent_idx, i32, (B, R), dev, "parent_idx"), hp, hs, hc, n_allowed,
-                   _need_like(history_len, i32, (B,), dev, "history_len"), _need_like(prompt_len, i32, (B,), dev, "prompt_len"),
-                   _need_like(repetition, f32, (B,), dev, "repetition"), _need_like(presence, f32, (B,), dev, "presence"),
-                   _need_like(frequency, f32, (B,), dev, "frequency"), _need_like(bias_token, i32, (B, n_bias), dev, "bias_token"),
-                   _need_like(bias, f32, (B, n_bias), dev, "bias"), _need_like(allowed, i32, (n_allowed, (V + 31) // 32), dev, "allowed"),
-                   _need_like(allowed_row, i32, (B, R), dev, "allowed_row"), _need_like(status, i32, (B,), dev, "status"))
+                   _need_like(n_nodes, i32, (B,), index, "n_nodes"), _need_like(token_ids, i32, (B, R), index, "token_ids"),
+                   _need_like(parent_idx, i32, (B, R), index, "parent_idx"), hp, hs, hc, n_allowed,
+                   _need_like(history_len, i32, (B,), index, "history_len"), _need_like(prompt_len, i32, (B,), index, "prompt_len"),
+                   _need_like(repetition, f32, (B,), index, "repetition"), _need_like(presence, f32, (B,), index, "presence"),
+                   _need_like(frequency, f32, (B,), index, "frequency"), _need_like(bias_token, i32, (B, n_bias), index, "bias_token"),
+                   _need_like(bias, f32, (B, n_bias), index, "bias"), _need_like(allowed, i32, (n_allowed, (V + 31) // 32), index, "allowed"),
+                   _need_like(allowed_row, i32, (B, R), index, "allowed_row"), _need_like(status, i32, (B,), index, "status"))
     _enqueue(lib().cadd_adjust_logits, a, dev, stream)
     return out
 
@@ -1084,7 +1088,7 @@ class Distilled:
 
 
 def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags):
-    dev, code = _logits_of(x, "draft_logits")
+    dev, index, code = _logits_of(x, "draft_logits")
     B, L, V = shape = x.shape
     _need(teacher_token.dim() == 3 and teacher_token.shape[0] == B, "teacher_token must be [batch, R, K]")
     R, K = teacher_token.shape[1:]
@@ -1096,13 +1100,13 @@ def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperatur
         P = path.shape[1]
     else:
         _need(path_len is None, "path_len comes with path")
-    gp, gb, gl = (None, 0, 0) if out.grad is None else _need_logits(out.grad, shape, x.dtype, dev, "grad")
+    gp, gb, gl = (None, 0, 0) if out.grad is None else _need_logits(out.grad, shape, x.dtype, index, "grad")
     return dev, DistillArgs(
-        C.sizeof(DistillArgs), flags | (DISTILL_REST if rest else 0), B, L, R, K, code, P, V, float(temperature), *_need_logits(x, shape, x.dtype, dev, "draft_logits"),
-        _need_like(teacher_token, i32, (B, R, K), dev, "teacher_token"), _need_like(teacher_logit, f64, (B, R, K), dev, "teacher_logit"),
-        _need_like(teacher_lse, f64, (B, R), dev, "teacher_lse"), _need_like(path, i32, (B, P), dev, "path"), _need_like(path_len, i32, (B,), dev, "path_len"),
-        _need_like(n_rows, i32, (B,), dev, "n_rows"), _need_like(weight, f32, (B, L), dev, "weight"), _need_like(grad_loss, f32, (B, L), dev, "grad_loss"),
-        _need_like(out.loss, f32, (B, L), dev, "loss"), _need_like(out.stats, f32, (B, L, 4), dev, "stats"), gp, gb, gl, _need_like(out.status, i32, (B,), dev, "status"))
+        C.sizeof(DistillArgs), flags | (DISTILL_REST if rest else 0), B, L, R, K, code, P, V, float(temperature), *_need_logits(x, shape, x.dtype, index, "draft_logits"),
+        _need_like(teacher_token, i32, (B, R, K), index, "teacher_token"), _need_like(teacher_logit, f64, (B, R, K), index, "teacher_logit"),
+        _need_like(teacher_lse, f64, (B, R), index, "teacher_lse"), _need_like(path, i32, (B, P), index, "path"), _need_like(path_len, i32, (B,), index, "path_len"),
+        _need_like(n_rows, i32, (B,), index, "n_rows"), _need_like(weight, f32, (B, L), index, "weight"), _need_like(grad_loss, f32, (B, L), index, "grad_loss"),
+        _need_like(out.loss, f32, (B, L), index, "loss"), _need_like(out.stats, f32, (B, L, 4), index, "stats"), gp, gb, gl, _need_like(out.status, i32, (B,), index, "status"))
 
 
 def cadd_distill_loss(draft_logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor, *, teacher_lse=None,
