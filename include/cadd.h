@@ -71,7 +71,8 @@ extern "C" {
 #define CADD_STATUS_BAD_TOKEN        32768   /* distill: teacher_token held a number outside [-1, V); that entry was left out */
 #define CADD_STATUS_INTERNAL_TIMEOUT   128   /* a bounded wait on an asynchronous copy ran out; build returns the empty tree, verify leaves -2 in node_argmax,
                                                 attention leaves NaN in out and lse of the rows concerned and sets the bit for every request of the call,
-                                                distill leaves NaN in loss, stats and grad, adjust in out of the rows concerned */
+                                                distill leaves NaN in loss, stats and grad of the rows that the CTA has not finished, adjust in the pieces of out
+                                                that the warp has not (single tokens may still be replaced there); both set the bit for those rows' requests */
 
 #define CADD_DTYPE_BF16 0
 #define CADD_DTYPE_FP32 1

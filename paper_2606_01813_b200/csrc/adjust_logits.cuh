@@ -443,6 +443,7 @@ __global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 6) adjust_stream_k
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned char* buffer = adjust_smem_raw + warp * kAdjustBuffer<kAdjustTileBytes>;
     unsigned phase = 0;
+    bool lost = false;                                              // a copy did not come: this piece and all that the warp would have taken after it
     if constexpr (kCopy) {
         if (lane == 0) {
             mbar_init(&full[warp], 1);
@@ -461,16 +462,21 @@ __global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 6) adjust_stream_k
         u.src = const_cast<char*>(p.in) + ((int64_t)b * p.in_b + (int64_t)j * p.in_row + u.v) * E::ES;
         u.dst = p.out + ((int64_t)b * p.out_b + (int64_t)j * p.out_row + u.v) * E::ES;
         bool coming = false;
-        if constexpr (kCopy) coming = fetch_piece<DT>(u, buffer, &full[warp], p.drop != 0);
+        if constexpr (kCopy) {
+            if (lost) {
+                lose_piece<DT>(p, u, b);
+                continue;
+            }
+            coming = fetch_piece<DT>(u, buffer, &full[warp], p.drop != 0);
+        }
         const uint32_t* mask = adjust_mask(p, b, j);
         uint32_t word[kMaskRegs<DT, kAdjustTileBytes>];
         if (mask) mask_words(mask, u, word);
         if constexpr (kCopy) {
             if (coming && !__all_sync(kFullMask, mbar_wait_limited(&full[warp], phase, p.drop ? kTestSpinLimit : kSpinLimit))) {
                 lose_piece<DT>(p, u, b);
-                if (p.drop) continue;
-                if (lane == 0) mbar_wait_bounded(&full[warp], phase);      // not to leave with a copy in flight
-                return;
+                lost = true;
+                continue;
             }
             if (coming) phase ^= 1u;
             __syncwarp();
@@ -478,6 +484,8 @@ __global__ void __launch_bounds__(kAdjustThreads, kCopy ? 3 : 6) adjust_stream_k
             deliver_piece<DT>(u, buffer);
         } else if (mask) mask_piece<DT, kAdjustTileBytes>(u.dst, u.n, mask, p.words, u.v, word);
     }
+    if constexpr (kCopy)
+        if (lost && !p.drop && lane == 0) mbar_wait_bounded(&full[warp], phase);      // not to leave with a copy in flight
 }
 
 template <int DT>

@@ -276,3 +276,13 @@ def test_wait_that_runs_out():
 def test_long_histories_of_many_tokens(V, history, R, dtype):
     """Into another array and in place; beyond 12288 tokens several CTAs share a request's."""
     both(random_adjust(2, R, V, dtype, seed=V, history=history, spread=V, n_bias=20))
+
+
+def test_wait_that_runs_out_with_more_pieces_to_come():
+    """A warp whose copy never comes loses the pieces it would have taken after it, too: no request is left as it was without its bit."""
+    B, V = 100, 40 * 4096                                                      # 4000 pieces for 3552 warps
+    x, st = torch.zeros(B, 1, V, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE)
+    torch.cuda.synchronize()
+    assert bool((st == G.STATUS_INTERNAL_TIMEOUT).all()) and bool(torch.isnan(out).all())
+    assert torch.equal(G.cadd_adjust_logits(x, out=out, status=st), x) and not bool(st.any())
