@@ -655,7 +655,10 @@ __global__ void __launch_bounds__(kTokensThreads) adjust_tokens_kernel(AdjustPar
     const int b = (int)(bg / (unsigned)p.groups), g = (int)(bg - (unsigned)b * (unsigned)p.groups);
     AdjustFirst<kTokensThreads> first(p, b);
     const int j0 = g * p.rows_per_cta, j1 = min(first.live, j0 + p.rows_per_cta);
-    if (j0 >= j1) return;
+    if (j0 >= j1) {
+        grid_dependency_wait();                                     // (what comes after this kernel comes after the one before it, too)
+        return;
+    }
     if (tid == 0) sh.twice = 0;
     if (tid < j1 - j0) sh.path_n[tid] = 0;
     for (int i = tid; i < p.slots / 4; i += kTokensThreads) {
