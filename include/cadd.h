@@ -507,7 +507,8 @@ typedef struct cadd_evict_args {
  *     if n_out(v) > 0:   x = x - frequency * n_out(v) - presence
  *     x = x + every bias listed for v
  *     x = -Inf           where the row's mask has bit v clear, whatever x is
- * computed in 64 bits for tokens that penalties or biases concern and rounded once; all others keep their bits.  Tokens outside
+ * computed in 64 bits for tokens that penalties or biases concern and rounded once (several biases of a token: their sum first, to
+ * fp32); all others keep their bits.  Tokens outside
  * [0, V) in the history, on a path or in bias_token have no effect.  Rows above n_nodes[b] are left as they were in out.
  * A row whose mask allows nothing becomes -Inf throughout (CADD_STATUS_NOTHING_ALLOWED); verification then takes token 0 there.
  * Greedy and sampled verification and tree construction take the result as it is.
@@ -537,7 +538,7 @@ typedef struct cadd_adjust_args {
     const float* repetition;       /* [batch], above 0; NULL => 1.  Where all three are NULL, history and paths are not read */
     const float* presence;         /* [batch]; NULL => 0 */
     const float* frequency;        /* [batch]; NULL => 0 */
-    const int32_t* bias_token;     /* [batch, n_bias], in any order, a token more than once gets the sum; negative: unused entry */
+    const int32_t* bias_token;     /* [batch, n_bias], in any order, a token more than once gets the sum (added in 64 bits, rounded to fp32); negative: unused entry */
     const float* bias;             /* [batch, n_bias] */
     const uint32_t* allowed;       /* [n_allowed, ceil(V/32)] bit v % 32 of word v / 32: token v may follow; NULL: no masks */
     const int32_t* allowed_row;    /* [batch,R] row of allowed for each row of the request, -1: no mask; rows may share one.  Required with allowed */

@@ -196,7 +196,8 @@ __device__ __forceinline__ void count_use(uint32_t* word, bool in_prompt) {
     if (in_prompt) atomicOr(word, kInPrompt);
     else atomicAdd(word, kOnce);
 }
-// Sums of the biases of the tokens that have a place here (place(token) >= 0), marked in the table.
+// Sums of the biases of the tokens that have a place here (place(token) >= 0), marked in the table, which holds nothing else yet.  A sum of several
+// is taken in 64 bits and kept in 32, as the biases come.
 template <int kThreadsHere, typename Place>
 __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint32_t* table, float* bias_of, int* twice, Place place) {
     const int32_t* at = p.bias_token + (int64_t)b * p.n_bias;
@@ -209,17 +210,45 @@ __device__ __forceinline__ void gather_biases(const AdjustParams& p, int b, uint
     }
     __syncthreads();
     if (!*twice) return;
-    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {  // a token's first entry adds up all of them, in their order
+    // Some token is listed more than once.  Its word becomes the place of its first entry (counted from behind, from bit 2 on) and a top bit;
+    // a warp adds up its entries: lane l the l-th of every 32, and then the lanes' sums, so the order is always the same.
+    constexpr uint32_t kMore = 0x80000000u;
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {
         const int t = place(at[i]);
-        if (t < 0) continue;
-        bool once = true;
-        for (int k = 0; k < i && once; ++k) once = at[k] != at[i];
-        if (!once) continue;
-        double s = 0.0;
-        for (int k = i; k < p.n_bias; ++k)
-            if (at[k] == at[i]) s += (double)val[k];
-        bias_of[t] = (float)s;
+        if (t >= 0) atomicMax(&table[t], (uint32_t)(p.n_bias - i) << 2 | kHasBias);
     }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {
+        const int t = place(at[i]);
+        if (t >= 0 && (table[t] & ~kMore) >> 2 != (uint32_t)(p.n_bias - i)) atomicOr(&table[t], kMore);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i0 = (int)(threadIdx.x - lane); i0 < p.n_bias; i0 += kThreadsHere) {
+        const int i = i0 + (int)lane, tok = i < p.n_bias ? at[i] : -1, t = i < p.n_bias ? place(tok) : -1;
+        unsigned firsts = __ballot_sync(kFullMask, t >= 0 && table[t] == ((uint32_t)(p.n_bias - i) << 2 | kHasBias | kMore));
+        while (firsts) {
+            const int from = __ffs(firsts) - 1, want = __shfl_sync(kFullMask, tok, from), to = __shfl_sync(kFullMask, t, from);
+            firsts &= firsts - 1u;
+            double s = 0.0;
+#pragma unroll 4
+            for (int k = i0 + (int)lane; k < p.n_bias; k += 32)
+                if (at[k] == want) s += (double)val[k];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFullMask, s, o);
+            if (lane == 0) bias_of[to] = (float)s;
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < p.n_bias; i += kThreadsHere) {
+        const int t = place(at[i]);
+        if (t >= 0) table[t] = kHasBias;
+    }
+    __syncthreads();
 }
 // Rows 0 .. n-1 of a request's tree brought to shared memory (n tokens, then n parents), where there is room: a path is a chain of
 // loads, each of them a round trip to memory otherwise.

@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 bool in_use = lane < kDistillWarps;
                 DistillSum s{in_use ? k.max[lane] : -INFINITY, in_use ? k.ref[lane] : kDistillLowest, in_use ? k.sum[lane] : 0.0};
                 distill_join(s);
-                if (C > 1) {
+                if (C > 1) {                                         // (the cluster's only row: there are at least as many clusters as rows)
                     if (lane < (int)C) {
                         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_max[rank], lane)), "f"(s.m) : "memory");
                         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_ref[rank], lane)), "f"(s.ref) : "memory");

@@ -286,3 +286,19 @@ def test_wait_that_runs_out_with_more_pieces_to_come():
     torch.cuda.synchronize()
     assert bool((st == G.STATUS_INTERNAL_TIMEOUT).all()) and bool(torch.isnan(out).all())
     assert torch.equal(G.cadd_adjust_logits(x, out=out, status=st), x) and not bool(st.any())
+
+
+@pytest.mark.parametrize("n_bias,spread", [(31, 1), (33, 2), (1024, 3), (4096, 2000), (65536, 65536), (65536, 20000)])
+@pytest.mark.parametrize("R", [1, 8])
+def test_biases_listed_many_times(n_bias, spread, R):
+    both(random_adjust(1, R, 70000, torch.float32, seed=n_bias + R, spread=spread, n_bias=n_bias, history=20, masks=False))
+
+
+def test_unused_biases_filled_with_one_token():
+    """Lists padded with a token and nothing to add, as well as with none."""
+    a = random_adjust(2, 9, 9000, torch.float32, seed=4, n_bias=300)
+    a.bias_token[:, 100:], a.bias[:, 100:] = 17, 0.0
+    a.bias_token[1, 50:], a.bias[1, 50:] = -1, math.nan
+    both(a)
+    a.bias_token[0, :3], a.bias[0, :3] = 17, torch.tensor([1e8, -1e8, 1.0])      # a sum that 32 bits would lose on the way
+    both(a)
