@@ -302,3 +302,64 @@ def test_unused_biases_filled_with_one_token():
     both(a)
     a.bias_token[0, :3], a.bias[0, :3] = 17, torch.tensor([1e8, -1e8, 1.0])      # a sum that 32 bits would lose on the way
     both(a)
+
+
+@pytest.mark.parametrize("R,batch", [(1, 2), (1, 40), (9, 3), (65, 2)])
+def test_calls_on_two_streams_and_graphs_of_both(R, batch):
+    """Calls share nothing: two at once, captured and not, into other arrays and in place."""
+    sets = [random_adjust(batch, R, 30000, torch.bfloat16, seed=s, history=500, tree=R > 1) for s in (3, 4)]
+    xs, kws = [a.logits.cuda() for a in sets], [a.args("cuda") for a in sets]
+    alone = [G.cadd_adjust_logits(x, out=x.clone(), **kw) for x, kw in zip(xs, kws)]
+    outs, placed, streams, graphs = [x.clone() for x in xs], [x.clone() for x in xs], [torch.cuda.Stream() for _ in xs], []
+    torch.cuda.synchronize()
+    for x, kw, out, y in zip(xs, kws, outs, placed):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            G.cadd_adjust_logits(x, out=out, **kw)
+            y.copy_(x)
+            G.cadd_adjust_logits(y, **kw)
+        graphs.append(g)
+    for again in range(3):
+        for out, x in zip(outs, xs):
+            out.copy_(x)
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for r, out, y in zip(alone, outs, placed):
+            assert torch.equal(r, out) and torch.equal(r, y)
+
+
+def test_results_are_there_for_the_next_kernel():
+    """What reads the rows next on the stream reads them as they are when the call is done, with and without live rows."""
+    for batch, live in ((64, 0), (64, -1)):
+        x = torch.zeros(batch, 1, 151936, dtype=torch.bfloat16, device="cuda")
+        n = torch.full((batch,), live, dtype=torch.int32, device="cuda")
+        n[0] = 0
+        hist = torch.arange(1000, dtype=torch.int32, device="cuda").repeat(batch, 1)
+        kw = dict(history=hist, presence=torch.full((batch,), 2.0, device="cuda"), n_nodes=n)
+        for _ in range(20):
+            out = torch.full_like(x, 1.0)
+            total = G.cadd_adjust_logits(x, out=out, **kw).float().sum(-1)[:, 0]
+            assert total.tolist() == [-2000.0 if live == 0 or b == 0 else 151936.0 for b in range(batch)]
+
+
+def test_many_rows():
+    """As many rows as a call can have: a tree whose nodes all follow the root."""
+    R, V = 65536, 40
+    a = Adjust(torch.randn(1, R, V).bfloat16(), token_ids=(torch.arange(R) % 50).int()[None], parent_idx=torch.zeros(1, R, dtype=torch.int32),
+               presence=torch.ones(1), history=i32([[3, 3, 7]]), bias_token=i32([[5]]), bias=torch.tensor([[0.5]]))
+    a.parent_idx[0, 0] = -1
+    x = a.logits.double()
+    for t, n in ((0, 1), (3, 1), (7, 1)):
+        x[0, :, t] -= n
+    at = torch.arange(R)
+    own = (at % 50 < V) & (at > 0)
+    for t in (0, 3, 7):
+        own &= at % 50 != t
+    x[0, at[own], (at % 50)[own]] -= 1
+    x[0, :, 5] += 0.5
+    y = a.logits.cuda()
+    assert torch.equal(G.cadd_adjust_logits(y, out=torch.zeros_like(y), **a.args("cuda")).cpu(), x.bfloat16())
+    assert torch.equal(G.cadd_adjust_logits(y, **a.args("cuda")).cpu(), x.bfloat16())

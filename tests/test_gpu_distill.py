@@ -7,7 +7,7 @@ import torch
 
 from paper_2606_01813_b200 import binding as G
 from paper_2606_01813_b200 import synth
-from logits_util import Adjust, Distill, check_adjust, check_grad, check_loss, pack_bits, plain_distill, random_distill
+from logits_util import Adjust, Distill, check_adjust, check_grad, check_loss, pack_bits, plain_distill, random_distill, row_loss, teacher_rows
 
 pytestmark = pytest.mark.gpu
 i32 = lambda x: torch.tensor(x, dtype=torch.int32)
@@ -331,3 +331,86 @@ def test_refusals_of_the_binding():
     for bad, kw in ((t[:, :2].contiguous(), {}), (t, dict(temperature=0.0)), (t, dict(out=G.Distilled()))):
         with pytest.raises(G.CaddError):
             G.cadd_distill_loss(x, bad, torch.zeros(bad.shape, dtype=torch.float64, device="cuda"), **kw)
+
+
+@pytest.mark.parametrize("rest,T", [(False, 1.0), (True, 1.0), (True, 1.7), (False, 0.5)])
+def test_gradient_against_differences(rest, T):
+    """Central differences of the plain loss in 64 bits, step h: their error is h^2 / 6 times a third derivative of at most w / T^3 (a
+    softmax's is at most 1, and with p_rest / q_rest it has the rest's own softmax besides: 2), and 2^-50 / h of rounding."""
+    d = random_distill(2, 3, 40, 6, torch.float32, seed=21, rest=rest, temperature=T, lse=rest)
+    (x, t, v), kw = put(d)
+    got = G.cadd_distill_loss(x, t, v, grad=True, **kw).grad.double().cpu()
+    tol, h, rows = plain_distill(d)[4], 2.0 ** -14, teacher_rows(d)
+    for b in range(2):
+        for i in range(3):
+            r = int(rows[b, i])
+            if r < 0:
+                assert int(got[b, i].count_nonzero()) == 0
+                continue
+            f = lambda s: float(row_loss(s, d.teacher_token[b, r], d.teacher_logit[b, r], float(d.teacher_lse[b, r]) if rest else 0.0, rest, T))
+            s, w = d.logits[b, i].double(), float(d.weight[b, i]) * float(d.grad_loss[b, i])
+            for k in range(40):
+                step = torch.zeros(40, dtype=torch.float64)
+                step[k] = h
+                want = w * (f(s + step) - f(s - step)) / (2 * h)
+                assert abs(float(got[b, i, k]) - want) <= float(tol[b, i, k]) + abs(w) * (3 * h * h / (6 * T ** 3) + 2.0 ** -46 / h), (b, i, k)
+
+
+@pytest.mark.parametrize("B,L,V,path", [(700, 3, 130, False), (3000, 2, 64, True), (1025, 2, 9000, False)])
+def test_many_requests_of_few_rows(B, L, V, path):
+    """More requests than the map of live rows has groups, some of them without any."""
+    d = random_distill(B, L, V, 3, torch.bfloat16, seed=B, rest=True, path=path)
+    if not path:
+        d.n_rows[100:400] = 0
+    every(d)
+
+
+def test_no_row_is_left():
+    d = random_distill(3, 4, 5000, 3, torch.float32, seed=1)
+    d.n_rows[:] = 0
+    r = every(d)
+    assert int(r.grad.count_nonzero()) == 0
+
+
+def test_calls_on_two_streams_and_graphs_of_both():
+    """Calls share nothing: two at once, captured and not, each with its own answers."""
+    sets = [random_distill(20, 8, 40000, 16, torch.bfloat16, seed=s, rest=True) for s in (5, 6)]
+    args = [put(d) for d in sets]
+    alone = [G.cadd_distill_loss(*a, grad=True, **kw) for a, kw in args]
+    outs = [G.Distilled(loss=torch.zeros_like(r.loss), stats=torch.zeros_like(r.stats), grad=torch.zeros_like(r.grad)) for r in alone]
+    streams, graphs = [torch.cuda.Stream() for _ in args], []
+    torch.cuda.synchronize()
+    for (a, kw), out in zip(args, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            G.cadd_distill_loss(*a, out=out, **kw)
+        graphs.append(g)
+    for again in range(3):
+        for out in outs:
+            out.loss.zero_(), out.grad.zero_()
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        plain = [G.cadd_distill_loss(*a, grad=True, stream=s, **kw) for (a, kw), s in zip(args, reversed(streams))]
+        torch.cuda.synchronize()
+        for r, out, p in zip(alone, outs, plain):
+            for f in ("loss", "stats", "grad"):
+                assert torch.equal(getattr(r, f), getattr(out, f)) and torch.equal(getattr(r, f), getattr(p, f))
+
+
+def test_listed_tokens_at_every_place():
+    """Lists of 256 neighbouring tokens: over the head, the boundaries of chunks, warps and tiles, the tail."""
+    V = 2 * 20480 + 37
+    d = random_distill(1, 12, V, 256, torch.bfloat16, seed=9, rest=True)
+    d.n_rows = None
+    starts = [0, 1, 7, 250, 5100, 20480 - 128, 20480 - 255, 20480, 2 * 20480 - 100, V - 256, V - 300, 10000]
+    for i, s in enumerate(starts):
+        d.teacher_token[0, i] = torch.randperm(256).int() + s
+    d.teacher_logit = torch.log_softmax(torch.randn(1, 12, 256, dtype=torch.float64), -1) - 0.1
+    every(d)
+    (x, t, v), kw = put(d)
+    big = torch.zeros(12 * V + 3, dtype=torch.bfloat16, device="cuda")
+    y = big[3:].view(1, 12, V)                                             # rows that start anywhere
+    y.copy_(x)
+    check_grad(G.cadd_distill_loss(y, t, v, grad=True, **kw).grad, plain_distill(d))
