@@ -20,7 +20,7 @@ constexpr int kAdjustThreads = 256;
 constexpr int kAdjustWarps = kAdjustThreads / 32;
 constexpr int kAdjustTileBytes = 8192;         // of a row: the tokens whose tables a CTA of adjust_rows_kernel has; a piece of adjust_stream_kernel
 constexpr int kAdjustPieceBytes = 4096;        // of a row: a piece of adjust_rows_kernel
-constexpr int kAdjustRows = 36;                // rows a CTA takes at most (trees have a power of two of nodes and the root: 65 rows are two CTAs')
+constexpr int kAdjustRows = 24;                // rows a CTA takes at most (trees of 65 rows 147 us with 36, 144 with 24, 146 with 20; of 257 rows 127, 114, 116)
 constexpr int kAdjustBatch = 8;                // tokens of the history that a thread has under way
 constexpr int kMaxPath = 65;                   // nodes of a path: the deepest tree there is, and its root
 constexpr uint32_t kInPrompt = 1u, kHasBias = 2u, kOnce = 4u;      // a token's word in the table: two flags, then n_out of the history
@@ -125,9 +125,11 @@ template <> struct Raw<CADD_DTYPE_FP32> {
 struct Penalty {
     double rep, inv, pres, freq;
 };
-__device__ __forceinline__ double penalised(const Penalty& q, double x, uint32_t times, bool seen) {
-    if (seen) x *= x > 0.0 ? q.inv : q.rep;    // (x / rep to 2^-52, long before the rounding to fp32 or bf16)
-    if (times > 0u) x -= q.freq * (double)times + q.pres;
+__device__ __forceinline__ double penalised(const Penalty& q, float logit, uint32_t times, bool seen) {
+    double x = (double)logit;
+    if (seen) x *= logit > 0.0f ? q.inv : q.rep;      // (x / rep to 2^-52, long before the rounding to fp32 or bf16)
+    // (times as a double: the low word of 2^52's, less 2^52; four times the rate of a conversion)
+    if (times > 0u) x -= q.freq * (__hiloint2double(0x43300000, (int)times) - 0x1p52) + q.pres;
     return x;
 }
 
@@ -618,28 +620,21 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_rows_kernel(AdjustPa
                 const int a = find_place(plain, sh.from[0][eighth], sh.from[0][eighth + 1], t), c = find_place(biased, sh.from[1][eighth], sh.from[1][eighth + 1], t);
                 uint32_t times = a >= 0 ? plain[a] >> kListShift : (c >= 0 ? biased[c] >> kListShift : 0u);
                 for (int o = 0; o < np; ++o) times += path[o] == t;
-                own[s] = Raw<DT>::round(penalised(q, (double)E::load(x, t - e0), times, true) + (c >= 0 ? (double)sums[c] : 0.0));
+                own[s] = Raw<DT>::round(penalised(q, E::load(x, t - e0), times, true) + (c >= 0 ? (double)sums[c] : 0.0));
             }
         }
         __syncwarp();
         // the lists' entries in [e0, e0 + piece): pieces are whole eighths
         const int part0 = e0 / (kTile / kAdjustWarps), part1 = part0 + (kAdjustWarps >> p.part_shift);
-        for (int i = sh.from[0][part0] + lane, to = sh.from[0][part1]; i < to; i += 64) {      // two at a time
-            uint32_t e[2];
-            float y[2];
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                e[o] = plain[min(i + 32 * o, to - 1)];
-                y[o] = E::load(x, (int)(e[o] & kListPlace) - e0);
-            }
-#pragma unroll
-            for (int o = 0; o < 2; ++o)
-                if (i + 32 * o < to) ((T*)x)[(int)(e[o] & kListPlace) - e0] = Raw<DT>::round(penalised(q, (double)y[o], e[o] >> kListShift, true));
+        for (int i = sh.from[0][part0] + lane, to = sh.from[0][part1]; i < to; i += 32) {
+            const uint32_t e = plain[i];
+            const int at = (int)(e & kListPlace) - e0;
+            ((T*)x)[at] = Raw<DT>::round(penalised(q, E::load(x, at), e >> kListShift, true));
         }
         for (int i = sh.from[1][part0] + lane, to = sh.from[1][part1]; i < to; i += 32) {
             const uint32_t e = biased[i], times = e >> kListShift;
             const int at = (int)(e & kListPlace) - e0;
-            ((T*)x)[at] = Raw<DT>::round(penalised(q, (double)E::load(x, at), times, times > 0u || (e & kListPrompt)) + (double)sums[i]);
+            ((T*)x)[at] = Raw<DT>::round(penalised(q, E::load(x, at), times, times > 0u || (e & kListPrompt)) + (double)sums[i]);
         }
         __syncwarp();
 #pragma unroll
@@ -728,7 +723,7 @@ __global__ void __launch_bounds__(kTokensThreads) adjust_tokens_kernel(AdjustPar
             else {
                 uint32_t times = table[t] / kOnce;
                 for (int o = 0; o < np; ++o) times += path[o] == t;
-                const double z = penalised(q, (double)E::load(x, mine), times, true);
+                const double z = penalised(q, E::load(x, mine), times, true);
                 own = Raw<DT>::round(table[t] & kHasBias ? z + (double)bias_of[t] : z);
             }
         }
@@ -751,7 +746,7 @@ __global__ void __launch_bounds__(kTokensThreads) adjust_tokens_kernel(AdjustPar
             for (int o = 0; o < kStep; ++o) {
                 if (word[o] == 0u) continue;
                 const uint32_t times = word[o] / kOnce;
-                const double z = penalised(q, (double)old[o], times, times > 0u || (word[o] & kInPrompt));
+                const double z = penalised(q, old[o], times, times > 0u || (word[o] & kInPrompt));
                 y[v[o]] = Raw<DT>::round(word[o] & kHasBias ? z + (double)bias_of[i0 + o * kTokensThreads] : z);
             }
         }
