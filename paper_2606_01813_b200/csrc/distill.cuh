@@ -175,18 +175,18 @@ template <int DT> __device__ __forceinline__ void store_element(char* row, int64
     else ((float*)row)[i] = x;
 }
 
-// A thread's running sum of 2^(x c - ref) over the elements it has seen, ref an integer at or above the largest x c.
+// A thread's running sum of 2^(x c - ref) over the elements it has seen, ref an integer at or above the largest x c.  It is raised by
+// kDistillSpare more than it has to be, so that a row's first elements mostly raise it for all others: with the least reference nearly every
+// tile had a larger element for one of a warp's 32 threads (training step of 2048 rows 247 us against 241, losses of 1728 rows 103 against 99).
+constexpr float kDistillSpare = 16.0f;
 struct DistillSum {
     float m, ref;
     double acc;
 };
-__device__ __forceinline__ void distill_raise(DistillSum& s, float m, float c) {
-    s.m = m;
-    const float ref = fmaxf(ceilf(m * c), kDistillLowest);
-    if (ref > s.ref) {
-        s.acc *= pow2_down(s.ref - ref);
-        s.ref = ref;
-    }
+__device__ __forceinline__ void distill_raise(DistillSum& s, float top) {       // top = m c, above ref
+    const float ref = ceilf(top) + kDistillSpare;
+    s.acc *= pow2_down(s.ref - ref);
+    s.ref = ref;
 }
 __device__ __forceinline__ float warp_max(float x) {                // NaN ignored
     float r;
@@ -564,7 +564,8 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 a_rest = __shfl_sync(kFullMask, y, 1);
                 up = __shfl_sync(kFullMask, y, 2);
                 z_rest = up * s.acc * kEx2BiasFix;
-                ref = s.ref;
+                ref = ceilf(m_rest * p.c);                           // the least that serves, so that small gradients stay
+                up *= pow2_down(ref - s.ref);
                 if (!(m_rest > -INFINITY)) {
                     a_rest = ref = 0.0f;
                     z_rest = s.acc == s.acc ? 0.0 : s.acc;
@@ -650,9 +651,9 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     float x = E::load(seg.in, seg.scalar(p, tid));
                     for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
                         if (l.thread[o] == tid) x = -INFINITY;
-                    distill_raise(s, x, p.c);
+                    s.m = fmaxf(s.m, x);
+                    if (x * p.c > s.ref) distill_raise(s, x * p.c);
                     s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
-                    if (!(x == x)) s.m = -INFINITY;
                 }
                 for (int t = 0; t < seg.n_tiles; ++t) {
                     if (t == again) { stay_stage = stage; }
@@ -683,7 +684,8 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     float m;
                     if constexpr (kDistillEach == 4) m = E::max4(w[0], w[1], w[2], w[3]);
                     else m = fmaxf(E::chunk_max(w[0]), E::chunk_max(w[1]));
-                    if (m > s.m) distill_raise(s, m, p.c);
+                    s.m = fmaxf(s.m, m);
+                    if (m * p.c > s.ref) distill_raise(s, m * p.c);
                     const uint64_t nref2 = pack2(-s.ref, -s.ref);
                     uint64_t sum2 = add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2));
                     if constexpr (kDistillEach == 4) sum2 = add2(sum2, add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
