@@ -110,7 +110,7 @@ extern "C" {
    exercises the library's bounded-wait exit (copies already in flight are waited for, then the CTA leaves) and every
    request reports CADD_STATUS_INTERNAL_TIMEOUT with the empty tree (build) or accepted_len 0 (verify).  For tests only.
    cadd_distill_loss and cadd_distill_grad take it too (each CTA's second tile of a row, or its first; NaN), and cadd_adjust_logits
-   into another array (the first piece of every warp; NaN).
+   where rows pass through shared memory, as they do into another array (all pieces of every warp; NaN).
    cadd_tree_attention takes it too: in its tiled kernel the keys of each CTA's second unit (its first, if its first item has
    only one there) are never announced, and every wait gives up after some 16 ms. */
 #define CADD_FLAG_TEST_DROP_TILE  0x80000000u
@@ -522,7 +522,7 @@ typedef struct cadd_adjust_args {
     int64_t  V;
     const void* logits;            /* [batch, R, V]; element (b,j,v) at b*stride_b + j*stride_row + v */
     int64_t  stride_b, stride_row; /* in elements, >= 0 */
-    void*    out;                  /* the same shape; may be logits with the same strides (in place: only what changes is written),
+    void*    out;                  /* the same shape; may be logits with the same strides (in place),
                                       otherwise overlaps no input.  No two of its rows may overlap.  Fastest where the rows of logits and out
                                       start equally far behind a 16-byte boundary */
     int64_t  out_stride_b, out_stride_row;
@@ -670,8 +670,9 @@ int cadd_cache_weights(const cadd_weights_args* a, void* cuda_stream);
  * (choice, copy; a third, tiny one where new_length is cache.length). */
 int cadd_cache_evict(const cadd_evict_args* a, void* cuda_stream);
 
-/* Penalties, biases and grammar masks on the logits of a tree's rows (see cadd_adjust_args).  Asynchronous on `cuda_stream`:
- * one kernel (a second, small one where status is given).  The same inputs give the same bits. */
+/* Penalties, biases and grammar masks on the logits of a tree's rows (see cadd_adjust_args).  Asynchronous on `cuda_stream`: one
+ * kernel or two (few rows of many requests, histories of more than 524,287 tokens), and a small one before them where status is
+ * given.  The same inputs give the same bits. */
 int cadd_adjust_logits(const cadd_adjust_args* a, void* cuda_stream);
 
 /* Divergence of the drafter's distribution from the target's top tokens and, where `grad` is given, its gradient in the same pass

@@ -62,33 +62,34 @@ static int room(K kernel, size_t smem) {
     cudaGetLastError();
     return CADD_ERR_LAUNCH;
 }
-// Rows a CTA: what they have in common is gathered once for all of them, but the device wants CTAs enough.
+// Rows a CTA: what they have in common is gathered once for all of them, but the device wants CTAs enough.  Few rows are cut in more pieces,
+// as long as each warp has one at most.
 static void group_rows(AdjustParams& p, int64_t ctas_a_group, int part_shift) {
     p.groups = (p.R + kAdjustRows - 1) / kAdjustRows;
     while (p.batch * ctas_a_group * p.groups < 4 * kSms && (p.R + p.groups - 1) / p.groups > kAdjustWarps) p.groups *= 2;
     p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
     p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
     p.part_shift = part_shift;
-    while (p.part_shift < 3 && (p.rows_per_cta << p.part_shift) < kAdjustWarps) ++p.part_shift;
+    while (p.part_shift < 3 && (p.rows_per_cta << (p.part_shift + 1)) <= kAdjustWarps) ++p.part_shift;
 }
 
 template <int DT>
 static int launch_tokens(AdjustParams& p, cudaStream_t st) {
-    // Tokens that a CTA can meet: those of its part of the vocabulary, and no more than the history, biases and its rows' paths have.
+    // Rows that share a table; CTAs that share a request's tokens, as many as find room at once (single words anywhere in a row want the
+    // load units of all SMs: 64 requests of 8192 tokens 32 us with one CTA each, 20 with two); and fewer rows a CTA where there is room still.
     p.groups = (p.R + kAdjustRows - 1) / kAdjustRows;
-    while (p.batch * p.groups < kSms && p.groups < p.R) p.groups *= 2;
+    p.S = 1;
+    while (p.S < 8 && (int64_t)p.batch * p.groups * (p.S + 1) <= kSms) ++p.S;
+    while ((int64_t)p.batch * p.groups * p.S * 2 <= kSms && p.groups < p.R) p.groups *= 2;
     p.rows_per_cta = (p.R + p.groups - 1) / p.groups;
     p.groups = (p.R + p.rows_per_cta - 1) / p.rows_per_cta;
+    // Tokens that a CTA can meet: those of its part of the vocabulary, and no more than the history, biases and its rows' paths have.
     int64_t most = (p.penalised && p.history ? p.history_cols : 0) + p.n_bias + (p.penalised && p.token_ids ? (int64_t)p.rows_per_cta * kMaxPath : 0);
-    // One CTA has to hold what it meets; beyond that the tokens, single words anywhere in a row, want the load units of all SMs
-    // (64 requests of 8192 tokens: 10 us of 16 for one CTA each).
-    p.S = 1;
     if (most > kTokensMost) {
-        p.S = (int)((p.V + kTokensMost - 1) / kTokensMost);
+        const int parts = (int)((p.V + kTokensMost - 1) / kTokensMost);
+        if (p.S < parts) p.S = parts;
         most = kTokensMost;
     }
-    const int64_t ctas = (int64_t)p.batch * p.groups;
-    while (p.S < 8 && ctas * (p.S + 1) <= kSms) ++p.S;
     p.slots = 1024;
     p.slot_shift = 22;
     while (p.slots < kTokensSlots && p.slots * 3 < most * 4) { p.slots *= 2; --p.slot_shift; }
@@ -100,9 +101,18 @@ static int launch_tokens(AdjustParams& p, cudaStream_t st) {
     return launch_cluster(adjust_tokens_kernel<DT>, (unsigned)grid, kTokensThreads, 1, smem, st, p, p.followed);
 }
 
-// Rows of a request from which on the tables of adjust_rows_kernel are worth their while; where all its CTAs run at once they
-// always are, since one launch is less than two (one token over 151936: 5.8 us on the device and 15 on the host, against 6.2 and 25).
-constexpr int kFewRows = 8;
+// Whether adjust_rows_kernel takes the call (us a call on the device, tables against single tokens; 151936 tokens, bf16).  Where all its CTAs
+// run at once: one launch is less than two (one token, 5.8 against 6.2; 65 rows of one request in place 13 against 28).  Otherwise from
+// four rows a request on (32 requests, histories of 4000: one row 26 against 14, two 26 / 19, three 28 / 25, four 30 / 32, six 40 / 50).
+// In place without masks, when it has to write all that it reads, also not where few tokens can be concerned (32 requests of 65 rows: histories
+// of 100 tokens 202 against 51, of 4000 211 / 256; with masks 226 / 452).
+constexpr int kFewRows = 4, kFewTokens = 40;              // one token of so many
+static bool by_tables(const AdjustParams& p, bool in_place) {
+    const int64_t history = p.penalised && p.history ? p.history_cols : 0;
+    if (history > kListMost) return false;
+    if ((int64_t)p.batch * p.tiles * ((p.R + kAdjustRows - 1) / kAdjustRows) <= 4 * kSms) return true;
+    return p.R >= kFewRows && (!in_place || p.allowed || (history + p.n_bias) * kFewTokens >= p.V);
+}
 
 template <int DT>
 static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
@@ -114,7 +124,7 @@ static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
         if (rc != CADD_OK) return rc;
     }
     const bool sparse = p.penalised || p.n_bias > 0;
-    if (sparse && !in_place && (!p.penalised || !p.history || p.history_cols <= kListMost) && (p.R >= kFewRows || (int64_t)p.batch * p.tiles <= 2 * kSms)) {
+    if (sparse && by_tables(p, in_place)) {
         group_rows(p, p.tiles, kAdjustTileBytes / kAdjustPieceBytes == 2 ? 1 : 0);
         const int64_t grid = (int64_t)p.batch * p.tiles * p.groups;
         if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;

@@ -13,6 +13,13 @@
 //   finish     joins the warps' sums, exchanges them within the cluster (distributed shared memory), and makes of the statistics the
 //              loss and the two factors that the gradient needs.
 // The gradient alone (statistics given, no exchange) passes over the tiles once.
+//
+// What bounds it.  Losses alone: 1728 rows of 151936 in bf16 (526 MB) take 98 us, 5.4 TB/s; the exponential unit has 16 ex2 a clock of an SM, which
+// is 68 % busy over the whole launch (DRAM 60 % of nominal).  Doing an eighth of them or more on the FMA pipes instead, as polynomials
+// in packed fp32, was slower (103 -> 111: packed operations have only half of those pipes), and so was more CTAs an SM.  With the gradient:
+// 2048 rows, 1245 MB, 242 us, 5.1 TB/s; the unit 61 % busy, and writes, which alone reach 3.8 to 4.0 TB/s here.  Both exponentials of an element
+// are computed: kept ones would need fp32 tiles twice as large.  512 rows of 100003 in fp32: 91 us, 4.5 TB/s, of which a sixth
+// is that 512 rows are not a multiple of the SMs.  Few rows: chains of loads and 64-bit steps, 9 us.
 // All waits are bounded; a CTA in which one runs out leaves NaN in its rows from there on.
 #pragma once
 #include "common.cuh"
@@ -21,7 +28,7 @@
 
 namespace cadd {
 
-constexpr int kDistillWarps = 20;                                   // that compute
+constexpr int kDistillWarps = 20;                                   // that compute (step of 2048 rows: 281 us with 20, 292 with 24 of half as many chunks, 305 with 16, 293 with 28)
 constexpr int kDistillCompute = 32 * kDistillWarps;
 constexpr int kDistillThreads = kDistillCompute + 96;               // and producer, prepare, finish
 constexpr int kDistillStatusThreads = 256;
@@ -93,7 +100,7 @@ constexpr int kDistillEntry = 30;                 // bytes of an entry
 // of a tile (-1: none; the last two parts are the row's scalar head and tail); the ring.
 struct DistillShared {
     alignas(8) uint64_t full[kDistillMaxStages], empty[kDistillMaxStages];
-    uint64_t listed[2], ready[2], done[2], summed[2], known[2], exchanged[2];
+    uint64_t listed[2], ready[2], done[2], summed[2], known[2], exchanged;
     int sent[kDistillMaxStages];                  // last tile sent for into each stage, -1: none
     int error;
     unsigned lost;                                // the first row in the cluster's order that some role has not finished
@@ -329,8 +336,8 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             mbar_init(&sh.done[s], kDistillWarps + 1);
             mbar_init(&sh.summed[s], kDistillWarps);
             mbar_init(&sh.known[s], 1);
-            mbar_init(&sh.exchanged[s], C);
         }
+        mbar_init(&sh.exchanged, C);
         sh.error = 0;
         sh.lost = 0xffffffffu;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -546,10 +553,10 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_max[rank], lane)), "f"(s.m) : "memory");
                         asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_ref[rank], lane)), "f"(s.ref) : "memory");
                         asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&k.peer_sum[rank], lane)), "d"(s.acc) : "memory");
-                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_address(&sh.exchanged[slot], lane)) : "memory");
+                        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_address(&sh.exchanged, lane)) : "memory");
                     }
                     __syncwarp();
-                    if (!wait(&sh.exchanged[slot], phase, kSpinLimit)) break;
+                    if (!wait(&sh.exchanged, 0u, kSpinLimit)) break;
                     in_use = lane < (int)C;
                     s = DistillSum{in_use ? k.peer_max[lane] : -INFINITY, in_use ? k.peer_ref[lane] : kDistillLowest, in_use ? k.peer_sum[lane] : 0.0};
                     distill_join(s);
@@ -656,7 +663,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
                 }
                 for (int t = 0; t < seg.n_tiles; ++t) {
-                    if (t == again) { stay_stage = stage; }
+                    if (t == again) stay_stage = stage;
                     if (!wait(&sh.full[stage], turn & 1u, t == drop ? kTestSpinLimit : kSpinLimit)) { ok = false; break; }
                     uint4* tile = ring + stage * kDistillTile;
                     const int c0 = t * kDistillTile + tid;
@@ -681,14 +688,12 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     if (!kGrad || t < again) arrive(&sh.empty[stage]);
                     if (++stage == S) { stage = 0; ++turn; }
                     if (c0 - lane >= nc) continue;                   // nothing of this tile for the warp
-                    float m;
-                    if constexpr (kDistillEach == 4) m = E::max4(w[0], w[1], w[2], w[3]);
-                    else m = fmaxf(E::chunk_max(w[0]), E::chunk_max(w[1]));
+                    const float m = E::max4(w[0], w[1], w[2], w[3]);
                     s.m = fmaxf(s.m, m);
                     if (m * p.c > s.ref) distill_raise(s, m * p.c);
                     const uint64_t nref2 = pack2(-s.ref, -s.ref);
-                    uint64_t sum2 = add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2));
-                    if constexpr (kDistillEach == 4) sum2 = add2(sum2, add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
+                    const uint64_t sum2 = add2(add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2)),
+                                               add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
                     float a0, a1;
                     unpack2(sum2, a0, a1);
                     s.acc += (double)(a0 + a1);

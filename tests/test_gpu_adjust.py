@@ -363,3 +363,34 @@ def test_many_rows():
     y = a.logits.cuda()
     assert torch.equal(G.cadd_adjust_logits(y, out=torch.zeros_like(y), **a.args("cuda")).cpu(), x.bfloat16())
     assert torch.equal(G.cadd_adjust_logits(y, **a.args("cuda")).cpu(), x.bfloat16())
+
+
+@pytest.mark.parametrize("B,R,V,dtype,history,n_bias", [(40, 1, 70001, torch.bfloat16, 50, 7), (40, 3, 70000, torch.bfloat16, 3000, 40), (70, 2, 20000, torch.float32, 14000, 20),
+                                                        (30, 3, 65000, torch.float32, 500, 0), (700, 1, 5000, torch.float32, 5, 3)])
+@pytest.mark.parametrize("masks", [False, True])
+def test_few_rows_of_many_requests(B, R, V, dtype, history, n_bias, masks):
+    """More tiles than the device has room for at once: copied and masked first, then token by token."""
+    both(random_adjust(B, R, V, dtype, seed=B + R, history=history, n_bias=n_bias, tree=R > 1, masks=masks, spread=V if history > 1000 else None))
+
+
+def test_many_rows_in_place_with_few_tokens():
+    both(random_adjust(40, 25, 40000, torch.bfloat16, seed=2, history=50, masks=False))
+
+
+@pytest.mark.parametrize("R", [1, 5])
+def test_a_history_of_more_uses_than_a_word_counts(R):
+    a = random_adjust(1, R, 6000, torch.float32, seed=R, history=600000, spread=6000, tree=R > 1)
+    a.history[:, 100000:] = 7                                                  # half a million uses of one token
+    a.prompt_len[0] = 1000
+    both(a)
+
+
+def test_one_history_for_all_requests():
+    a = random_adjust(5, 3, 9000, torch.bfloat16, seed=6, history=300)
+    a.history = a.history[:1].expand(5, -1)
+    want = plain_adjust(a)
+    kw = a.args("cuda")
+    kw["history"] = kw["history"][:1].expand(5, -1)
+    assert kw["history"].stride(0) == 0
+    x = a.logits.cuda()
+    check_adjust(G.cadd_adjust_logits(x, out=x.clone(), **kw), a, want)
