@@ -304,7 +304,7 @@ def test_unused_biases_filled_with_one_token():
     both(a)
 
 
-@pytest.mark.parametrize("R,batch", [(1, 2), (1, 40), (9, 3), (65, 2)])
+@pytest.mark.parametrize("R,batch", [(1, 2), (1, 40), (2, 90), (9, 3), (65, 2)])
 def test_calls_on_two_streams_and_graphs_of_both(R, batch):
     """Calls share nothing: two at once, captured and not, into other arrays and in place."""
     sets = [random_adjust(batch, R, 30000, torch.bfloat16, seed=s, history=500, tree=R > 1) for s in (3, 4)]
@@ -394,3 +394,15 @@ def test_one_history_for_all_requests():
     assert kw["history"].stride(0) == 0
     x = a.logits.cuda()
     check_adjust(G.cadd_adjust_logits(x, out=x.clone(), **kw), a, want)
+
+
+def test_wait_that_runs_out_before_single_tokens():
+    """Rows whose copies never come hold NaN but where single tokens are replaced afterwards, and every request has its bit."""
+    a = random_adjust(50, 1, 70000, torch.bfloat16, seed=7, tree=False, dead=False, history=40, masks=False)
+    x, st, kw = a.logits.cuda(), torch.zeros(50, dtype=torch.int32, device="cuda"), a.args("cuda")
+    out = G.cadd_adjust_logits(x, out=torch.zeros_like(x), status=st, flags=G.FLAG_TEST_DROP_TILE, **kw)
+    torch.cuda.synchronize()
+    assert bool((st == G.STATUS_INTERNAL_TIMEOUT).all())
+    _, touched, _ = plain_adjust(a)
+    assert bool(torch.isnan(out.cpu()[~touched]).all())
+    both(a)
