@@ -564,7 +564,8 @@ typedef struct cadd_adjust_args {
  * token (without CADD_DISTILL_REST: no mass): loss 0, stats 0, gradient 0, whatever the logits hold.
  * stats[b,i] = (m, Z, m', Z'): m the largest logit of the row, Z = sum_v exp((s_v - m) / T); m' and Z' the same over the tokens that
  * are not listed (-Inf and 0 where there are none).  cadd_distill_grad reads them instead of passing over the logits twice.
- * Logits of -Inf (and below -1e30) have probability 0; a row without any other gives NaN, as do NaN and +Inf in the logits or entries.
+ * Logits of -Inf (and below -1e30) have probability 0; a row without any other gives NaN, as do NaN and +Inf in the logits or entries, and as a
+ * row may whose largest logit over T is beyond 5e29 in magnitude.
  * Exponentials of the logits are fp32, their sums fp64, list and loss are fp64; the gradient is rounded once.
  */
 #define CADD_DISTILL_REST 1u
