@@ -418,6 +418,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 continue;
             }
             for (int o = lane; o < parts + 2; o += 32) first_of[o] = -1;
+            __syncwarp();                                            // (below, any lane's token may lie in any part)
             const float weight = p.weight ? p.weight[row] : 1.0f, upstream = p.grad_loss ? p.grad_loss[row] : 1.0f;
             if (lane == 0) { k.live = 1; k.weight = weight; k.upstream = upstream; }
             const int64_t at = ((int64_t)seg.b * p.R + r) * p.K;

@@ -414,3 +414,20 @@ def test_listed_tokens_at_every_place():
     y = big[3:].view(1, 12, V)                                             # rows that start anywhere
     y.copy_(x)
     check_grad(G.cadd_distill_loss(y, t, v, grad=True, **kw).grad, plain_distill(d))
+
+
+def test_lists_over_all_parts_of_rows_in_turn():
+    """Several rows a CTA, each with a list in every part of it: what a list leaves in its place is not seen by the row two behind it, and
+    all of a row's entries are found, call after call."""
+    B, L, V, K = 40, 9, 60000, 256
+    d = random_distill(B, L, V, K, torch.bfloat16, seed=31, rest=True)
+    d.n_rows = None
+    g = torch.Generator().manual_seed(31)
+    d.teacher_token = (torch.arange(K) * (V // K) + torch.randint(0, V // K, (B, L, K), generator=g)).int()
+    d.teacher_logit = torch.log_softmax(torch.randn(B, L, K, generator=g, dtype=torch.float64), -1) - 0.2
+    first = every(d)
+    (x, t, v), kw = put(d)
+    for _ in range(20):
+        r = G.cadd_distill_loss(x, t, v, grad=True, **kw)
+        for f in ("loss", "stats", "grad"):
+            assert torch.equal(getattr(r, f), getattr(first, f))
