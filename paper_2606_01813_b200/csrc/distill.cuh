@@ -119,7 +119,7 @@ __device__ __forceinline__ uint32_t peer_address(const void* p, unsigned rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
     return a;
 }
-// 2^n for integer-valued n <= 0, 0 below the normal range.
+// 2^n for an integer n that is small or negative, 0 below the normal range.
 __device__ __forceinline__ double pow2_down(float n) {
     return n > -1000.0f ? __hiloint2double((1023 + (int)n) << 20, 0) : (n == n ? 0.0 : (double)n);
 }
@@ -182,15 +182,17 @@ template <int DT> __device__ __forceinline__ void store_element(char* row, int64
     else ((float*)row)[i] = x;
 }
 
-// A thread's running sum of 2^(x c - ref) over the elements it has seen, ref an integer at or above the largest x c.  It is raised by
-// kDistillSpare more than it has to be, so that a row's first elements mostly raise it for all others: with the least reference nearly every
-// tile had a larger element for one of a warp's 32 threads (training step of 2048 rows 247 us against 241, losses of 1728 rows 103 against 99).
-constexpr float kDistillSpare = 16.0f;
+// A thread's running sum of 2^(x c - ref) over the elements it has seen, ref an integer between 3 above and 4 below the largest x c.  Rounding x c - ref
+// then moves a term by 2^-23 ln 2 of the largest at most (between 2^-24 and 2^-23 below 4 in magnitude; further down terms get smaller as fast as their
+// roundings grow), which is less than ex2's own error.  The room on either side is for speed: it saves most steps to another reference, one of which
+// halts a warp's 32 threads (training step of 2048 rows 242.0 us, losses of 1728 rows 99.9; with the least reference always 247 and 103, with 16 more 241.4 and
+// 98.2 and roundings of 2^-20).
+constexpr float kDistillSpare = 2.0f, kDistillAbove = 4.0f;
 struct DistillSum {
     float m, ref;
     double acc;
 };
-__device__ __forceinline__ void distill_raise(DistillSum& s, float top) {       // top = m c, above ref
+__device__ __forceinline__ void distill_raise(DistillSum& s, float top) {       // top = m c, more than kDistillAbove above ref
     const float ref = ceilf(top) + kDistillSpare;
     s.acc *= pow2_down(s.ref - ref);
     s.ref = ref;
@@ -660,7 +662,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
                         if (l.thread[o] == tid) x = -INFINITY;
                     s.m = fmaxf(s.m, x);
-                    if (x * p.c > s.ref) distill_raise(s, x * p.c);
+                    if (fmaf(x, p.c, -kDistillAbove) > s.ref) distill_raise(s, x * p.c);
                     s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
                 }
                 for (int t = 0; t < seg.n_tiles; ++t) {
@@ -691,7 +693,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     if (c0 - lane >= nc) continue;                   // nothing of this tile for the warp
                     const float m = E::max4(w[0], w[1], w[2], w[3]);
                     s.m = fmaxf(s.m, m);
-                    if (m * p.c > s.ref) distill_raise(s, m * p.c);
+                    if (fmaf(m, p.c, -kDistillAbove) > s.ref) distill_raise(s, m * p.c);
                     const uint64_t nref2 = pack2(-s.ref, -s.ref);
                     const uint64_t sum2 = add2(add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2)),
                                                add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));

@@ -431,3 +431,33 @@ def test_lists_over_all_parts_of_rows_in_turn():
         r = G.cadd_distill_loss(x, t, v, grad=True, **kw)
         for f in ("loss", "stats", "grad"):
             assert torch.equal(getattr(r, f), getattr(first, f))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("equal", [False, True])
+def test_sums_of_few_large_terms(dtype, equal):
+    """Rows of which one token beside the list, or equal ones, make up the sum: nothing averages out.  The argument of the exponential of a large
+    term is at most 4 in magnitude, in log2 units, so that its rounding is off by 2^-23 at most (ln 2 of that relative); ex2 by 2^-22; the factor that
+    centres ex2, the statistics' fp32 and two roundings of a sum of up to eight equal terms by 2^-24 each."""
+    tol = math.log(2.0) * 2.0 ** -23 + 2.0 ** -22 + 4 * 2.0 ** -24
+    B, L, V = 30, 8, 4096 if equal else 45056
+    g = torch.Generator().manual_seed(17)
+    top = (6 * torch.randn(B, L, 1, generator=g)).to(dtype)
+    if equal:
+        x = top.expand(-1, -1, V).clone()
+    else:                                                                  # and one below it that its thread meets first
+        x = ((torch.randn(B, L, V, generator=g) - 60.0).to(dtype) + top).to(dtype)
+        x[:, :, 1234], x[:, :, 1234 + 20480] = top[:, :, 0] - 2.5, top[:, :, 0]
+    t, v = torch.zeros(B, L, 1, dtype=torch.int32), torch.full((B, L, 1), math.log(0.25), dtype=torch.float64)
+    x[:, :, 0] = top[:, :, 0] - 8
+    for T in (1.0, 0.7):
+        r = G.cadd_distill_loss(x.cuda(), t.cuda(), v.cuda(), rest=True, temperature=T)
+        z, m = x[..., 1:].double(), top.double()
+        want = torch.exp((z - m) / T).sum(-1)
+        assert torch.equal(r.stats[..., 2].cpu(), top[..., 0].float())
+        err = (r.stats[..., 3].double().cpu() / want - 1.0).abs()
+        assert float(err.max()) <= tol, float(err.max())
+        logq = torch.log_softmax(x.double() / T, -1)
+        p = 0.25 ** (1.0 / T)                                              # (the target's entries are logits, too)
+        loss = p * (math.log(p) - logq[..., 0]) + (1.0 - p) * (math.log(1.0 - p) - torch.logsumexp(logq[..., 1:], -1))
+        assert bool(((r.loss.double().cpu() - loss).abs() <= 2 * tol + 2.0 ** -24 * loss.abs()).all())
