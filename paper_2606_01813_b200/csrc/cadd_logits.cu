@@ -190,6 +190,7 @@ static int distill(const cadd_distill_args* a, bool loss, cudaStream_t st) {
     p.V = a->V; p.in_b = a->stride_b; p.in_row = a->stride_l; p.out_b = a->grad_stride_b; p.out_row = a->grad_stride_l;
     p.L = a->L; p.R = a->R; p.K = a->K; p.path_cols = a->path_cols; p.rest = (a->flags & CADD_DISTILL_REST) ? 1 : 0;
     p.c = (float)(1.4426950408889634 / a->temperature);
+    p.over_c = (float)(a->temperature / 1.4426950408889634);
     p.inv_t = 1.0 / a->temperature;
     p.token = a->teacher_token; p.path = a->path; p.path_len = a->path_len; p.n_rows = a->n_rows;
     p.value = a->teacher_logit; p.lse = a->teacher_lse; p.weight = a->weight; p.grad_loss = a->grad_loss;

@@ -38,7 +38,9 @@ constexpr int kDistillTile = kDistillEach * kDistillCompute;
 constexpr int kDistillMaxStages = 216 * 1024 / (kDistillTile * 16);
 constexpr int kDistillMaxV = 2000000;
 constexpr int kDistillK = CADD_DISTILL_MAX_K;
-constexpr float kDistillLowest = -1.0e30f;                          // logits below count as -Inf; also the reference of an empty sum
+constexpr float kDistillLowest = -1.0e30f;                          // logits below count as -Inf
+constexpr float kDistillUnder = -0x1.93e596p+99f;                   // the next float below that
+constexpr float kDistillNear = 262144.0f;                           // see DistillSum
 constexpr double kRestRounding = 0x1p-20;
 
 struct DistillParams {
@@ -47,7 +49,7 @@ struct DistillParams {
     int64_t V, in_b, in_row, out_b, out_row;
     int rows, batch, L, R, K, path_cols, rest;
     int C, clusters, chunks_max, stages;          // CTAs a row; clusters; chunks of a segment at most; tiles of the ring
-    float c;                                      // log2(e) / T
+    float c, over_c;                              // log2(e) / T and its inverse
     double inv_t;
     const int32_t *token, *path, *path_len, *n_rows;
     const double *value, *lse;
@@ -59,7 +61,7 @@ struct DistillParams {
 
 // A row on its way through the roles; two of them are.
 struct DistillRow {
-    double p_rest, entropy, mass, cross;          // entropy, cross: sum p log p, sum p s / T over the entries; mass: sum p
+    double p_rest, entropy, mass, cross;          // entropy, cross: sum p log p, sum p (s - m_list) / T over the entries; mass: sum p
     double z_list;                                // sum of e over tokens (not entries)
     double factor;                                // of the exponentials in the gradient of tokens that are not listed
     double sum[kDistillWarps], peer_sum[kDistillMaxC];
@@ -67,7 +69,7 @@ struct DistillRow {
     float weight, upstream;                       // of the row; grad_loss
     unsigned row;                                 // batch * L + position
     float m_list;                                 // largest listed logit
-    float grad_ref;                               // reference exponent of the gradient's exponentials
+    float grad_base, grad_ref;                    // reference of the gradient's exponentials
     int live;                                     // 0: left out from the start, nothing is read
     int left_out;                                 // by its list, after its tiles have been sent for
     int twice;                                    // some token is listed more than once
@@ -124,6 +126,12 @@ __device__ __forceinline__ double pow2_down(float n) {
     return n > -1000.0f ? __hiloint2double((1023 + (int)n) << 20, 0) : (n == n ? 0.0 : (double)n);
 }
 
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
+    return x;
+}
+
 // Positions of request b that are learnt from.
 __device__ __forceinline__ int distill_live(const DistillParams& p, int b) {
     if (p.path) {
@@ -139,12 +147,16 @@ __device__ __forceinline__ void hide_element(uint4* chunk, int e) {
     if constexpr (DT == CADD_DTYPE_BF16) reinterpret_cast<volatile uint16_t*>(chunk)[e] = 0xff80u;
     else reinterpret_cast<volatile uint32_t*>(chunk)[e] = 0xff800000u;
 }
-// factor * 2^(x c - ref) of a chunk's elements, as a chunk.
-template <int DT>
-__device__ __forceinline__ uint4 gradient_chunk(const uint4& w, uint64_t c2, uint64_t nref2, uint64_t factor2) {
+// factor * 2^((x - base) c - ref) of a chunk's elements, as a chunk; without kFar, base is 0.
+template <int DT, bool kFar>
+__device__ __forceinline__ uint4 gradient_chunk(const uint4& w, uint64_t c2, float nbase, uint64_t nref2, uint64_t factor2) {
     using E = Elem<DT>;
     float f[E::EPC];
     E::unpack(w, f);
+    if constexpr (kFar) {
+#pragma unroll
+        for (int q = 0; q < E::EPC; ++q) f[q] += nbase;
+    }
     uint4 r;
     uint32_t* x = &r.x;
 #pragma unroll
@@ -182,38 +194,64 @@ template <int DT> __device__ __forceinline__ void store_element(char* row, int64
     else ((float*)row)[i] = x;
 }
 
-// A thread's running sum of 2^(x c - ref) over the elements it has seen, ref an integer between 3 above and 4 below the largest x c.  Rounding x c - ref
-// then moves a term by 2^-23 ln 2 of the largest at most (between 2^-24 and 2^-23 below 4 in magnitude; further down terms get smaller as fast as their
-// roundings grow), which is less than ex2's own error.  The room on either side is for speed: it saves most steps to another reference, one of which
-// halts a warp's 32 threads (training step of 2048 rows 242.0 us, losses of 1728 rows 99.9; with the least reference always 247 and 103, with 16 more 241.4 and
-// 98.2 and roundings of 2^-20).
-constexpr float kDistillSpare = 2.0f, kDistillAbove = 4.0f;
+// A thread's running sum of 2^((x - base) c - ref) over the elements it has seen.
+// While the largest x c is within kDistillNear, base is 0 and ref an integer between 3 above and 4 below it, so that x c - ref is rounded once, and a step from
+// one reference to another is a power of two.  The rounding then moves a term by 2^-23 ln 2 of the largest at most (between 2^-24 and 2^-23 below 4 in
+// magnitude; further down terms get smaller as fast as their roundings grow), which is less than ex2's own error.  The room on either side is for
+// speed: it saves most steps to another reference, one of which halts a warp's 32 threads (training step of 2048 rows 242.0 us, losses of 1728 rows 99.9; with the
+// least reference always 247 and 103, with 16 more 241.4 and 98.2 and roundings of 2^-20).
+// Beyond, fp32 has no integers fine enough to tell x c from ref by: then base is the largest logit itself and ref 0, the difference of two logits being
+// as exact as a product.  Every tile then goes the long way (top is -Inf).
+constexpr float kDistillSpare = 2.0f, kDistillAbove = 3.75f;
 struct DistillSum {
-    float m, ref;
+    float m;                                      // the largest logit
+    float base, ref;
+    float top;                                    // the largest logit that the reference serves
     double acc;
+    __device__ __forceinline__ DistillSum() : m(-INFINITY), base(0.0f), ref(0.0f), top(kDistillUnder), acc(0.0) {}
 };
-__device__ __forceinline__ void distill_raise(DistillSum& s, float top) {       // top = m c, more than kDistillAbove above ref
-    const float ref = ceilf(top) + kDistillSpare;
-    s.acc *= pow2_down(s.ref - ref);
-    s.ref = ref;
-}
 __device__ __forceinline__ float warp_max(float x) {                // NaN ignored
     float r;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-// The warp's sums together, in every lane.
-__device__ __forceinline__ void distill_join(DistillSum& s) {
-    const float m = warp_max(s.m), ref = warp_max(s.ref);
-    s.acc *= pow2_down(s.ref - ref);
-    s.m = m;
-    s.ref = ref;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s.acc += __shfl_xor_sync(kFullMask, s.acc, o);
+__device__ __forceinline__ bool is_far(float x, float c) { return !(fabsf(x * c) <= kDistillNear); }
+// s.m is above s.top: the reference follows.
+__device__ __forceinline__ void distill_raise(const DistillParams& p, DistillSum& s) {
+    const bool far = is_far(s.m, p.c), none = s.base == 0.0f && s.top < kDistillLowest;      // (none: acc is 0, or NaN)
+    if (!far && s.base == 0.0f) {
+        const float ref = ceilf(s.m * p.c) + kDistillSpare;
+        s.acc *= none ? 0.0 : pow2_down(s.ref - ref);
+        s.ref = ref;
+        s.top = fmaxf(s.m, (ref + kDistillAbove) * p.over_c);
+    } else if (s.base != s.m) {
+        const float base = far ? s.m : 0.0f, ref = far ? 0.0f : ceilf(s.m * p.c) + kDistillSpare;
+        s.acc *= none ? 0.0 : exp2(((double)s.base * (double)p.c + (double)s.ref) - ((double)base * (double)p.c + (double)ref));
+        s.base = base;
+        s.ref = ref;
+        s.top = far ? -INFINITY : fmaxf(s.m, (ref + kDistillAbove) * p.over_c);
+    }
+}
+// A sum's reference for others: the integer; +-Inf where it is the largest logit; -Inf where there is nothing.
+__device__ __forceinline__ float told_reference(const DistillSum& s) {
+    return s.base != 0.0f ? copysignf(INFINITY, s.base) : (s.top < kDistillLowest ? -INFINITY : s.ref);
+}
+__device__ __forceinline__ double whole_reference(float m, float told, float c) { return isinf(told) ? (double)m * (double)c : (double)told; }
+// The step from one reference to another where the latter is far out, or so near that it is not far from others that are.
+__device__ __noinline__ double far_step(float m, float told, float m_all, float all, float c) {
+    return m >= kDistillLowest ? exp2(whole_reference(m, told, c) - whole_reference(m_all, all, c)) : 0.0;
+}
+// Sums of the lanes together, in every lane: m the largest logit of a lane's sum, told its reference.
+__device__ __forceinline__ void distill_join(float c, float& m, float& told, double& acc) {
+    const float m_all = warp_max(m), all = warp_max(told);
+    acc *= fabsf(all) <= kDistillNear - 200.0f ? pow2_down(told - all) : far_step(m, told, m_all, all, c);      // (told -Inf: 0)
+    m = m_all;
+    told = all;
+    acc = warp_sum(acc);
 }
 // Packed sums of the exponentials of a chunk's even and odd elements.
-template <int DT>
-__device__ __forceinline__ uint64_t chunk_terms(const uint4& w, uint64_t c2, uint64_t nref2) {
+template <int DT, bool kFar>
+__device__ __forceinline__ uint64_t chunk_terms(const uint4& w, uint64_t c2, float nbase, uint64_t nref2) {
     using E = Elem<DT>;
     float f[E::EPC];
     E::unpack(w, f);
@@ -221,14 +259,23 @@ __device__ __forceinline__ uint64_t chunk_terms(const uint4& w, uint64_t c2, uin
 #pragma unroll
     for (int q = 0; q < E::EPC; q += 2) {
         float t0, t1;
-        unpack2(fma2(pack2(f[q], f[q + 1]), c2, nref2), t0, t1);
+        if (kFar) unpack2(mul2(pack2(f[q] + nbase, f[q + 1] + nbase), c2), t0, t1);
+        else unpack2(fma2(pack2(f[q], f[q + 1]), c2, nref2), t0, t1);
         pr[q / 2] = pack2(ex2_approx(t0), ex2_approx(t1));
     }
     uint64_t r = add2(pr[0], pr[1]);
     if constexpr (E::EPC == 8) r = add2(r, add2(pr[2], pr[3]));
     return r;
 }
-
+template <int DT, bool kFar>
+__device__ __forceinline__ double tile_terms(const uint4 (&w)[kDistillEach], uint64_t c2, const DistillSum& s) {
+    const uint64_t nref2 = pack2(-s.ref, -s.ref);
+    const uint64_t sum2 = add2(add2(chunk_terms<DT, kFar>(w[0], c2, -s.base, nref2), chunk_terms<DT, kFar>(w[1], c2, -s.base, nref2)),
+                               add2(chunk_terms<DT, kFar>(w[2], c2, -s.base, nref2), chunk_terms<DT, kFar>(w[3], c2, -s.base, nref2)));
+    float a0, a1;
+    unpack2(sum2, a0, a1);
+    return (double)(a0 + a1);
+}
 
 // Where the CTA stands in a row: what all roles work out for themselves.
 template <int DT>
@@ -309,11 +356,6 @@ __device__ __forceinline__ int distill_teacher(const DistillParams& p, unsigned 
     int r = p.path && i > 0 && i - 1 < p.path_cols ? p.path[(int64_t)b * p.path_cols + i - 1] : (p.path ? 0 : i);
     if (i >= distill_live(p, b) || weight == 0.0f || r < 0 || r >= p.R) r = -1;
     return r;
-}
-__device__ __forceinline__ double warp_sum(double x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
-    return x;
 }
 
 // kLoss: statistics and loss are computed here; otherwise they are given.  kGrad: the gradient is written.
@@ -487,10 +529,11 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     const double x = l.e[o], lp = (l.prob[o] - top) * p.inv_t;
                     const bool none = x < (double)kDistillLowest;
                     q = exp(lp);
-                    if (!none) e = exp((x - (double)m_list) * p.inv_t);
+                    const double below = (x - (double)m_list) * p.inv_t;
+                    if (!none) e = exp(below);
                     if (q != 0.0) {
                         entropy += q * lp;
-                        cross += none ? -INFINITY : q * (x * p.inv_t);
+                        cross += none ? -INFINITY : q * below;
                     }
                     sum += q;
                     if (l.once[o]) z += e;
@@ -543,51 +586,59 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             const unsigned phase = (lives >> slot) & 1u;
             lives ^= 1u << slot;
             const double nan = __longlong_as_double(0x7ff8000000000000ll);
-            float m_rest, m_all, ref = 0.0f;                         // ref: an exponential of the gradient is exp((s - m_rest) / T) * 2^(m_rest c - ref)
-            double z_rest, z_all, a_list, a_rest, up;                // up: 2^(ref - m_rest c)
+            float m_rest, m_all, ref = 0.0f;                         // an exponential of the gradient is exp((s - m_rest) / T) / up, where up is 2^(ref - m_rest c),
+            double z_rest, z_all, a_list, a_rest, up;                // or, far out, 1
+            bool far;
             const float m_list = k.m_list;
             if constexpr (kLoss) {
                 if (!wait(&sh.summed[slot], phase, kSpinLimit)) break;
                 bool in_use = lane < kDistillWarps;
-                DistillSum s{in_use ? k.max[lane] : -INFINITY, in_use ? k.ref[lane] : kDistillLowest, in_use ? k.sum[lane] : 0.0};
-                distill_join(s);
+                float m = in_use ? k.max[lane] : -INFINITY, told = in_use ? k.ref[lane] : -INFINITY;
+                double acc = in_use ? k.sum[lane] : 0.0;
+                distill_join(p.c, m, told, acc);
                 if (C > 1) {                                         // (the cluster's only row: there are at least as many clusters as rows)
                     if (lane < (int)C) {
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_max[rank], lane)), "f"(s.m) : "memory");
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_ref[rank], lane)), "f"(s.ref) : "memory");
-                        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&k.peer_sum[rank], lane)), "d"(s.acc) : "memory");
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_max[rank], lane)), "f"(m) : "memory");
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_address(&k.peer_ref[rank], lane)), "f"(told) : "memory");
+                        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(peer_address(&k.peer_sum[rank], lane)), "d"(acc) : "memory");
                         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(peer_address(&sh.exchanged, lane)) : "memory");
                     }
                     __syncwarp();
                     if (!wait(&sh.exchanged, 0u, kSpinLimit)) break;
                     in_use = lane < (int)C;
-                    s = DistillSum{in_use ? k.peer_max[lane] : -INFINITY, in_use ? k.peer_ref[lane] : kDistillLowest, in_use ? k.peer_sum[lane] : 0.0};
-                    distill_join(s);
+                    m = in_use ? k.peer_max[lane] : -INFINITY;
+                    told = in_use ? k.peer_ref[lane] : -INFINITY;
+                    acc = in_use ? k.peer_sum[lane] : 0.0;
+                    distill_join(p.c, m, told, acc);
                 }
-                m_rest = s.m >= kDistillLowest ? s.m : -INFINITY;
+                m_rest = m >= kDistillLowest ? m : -INFINITY;
                 m_all = fmaxf(m_rest, m_list);
                 // three exponentials at once: of the list's and the rest's largest, and of the step from the rest's reference to its largest
                 const double x = lane == 0 ? ((double)m_list - (double)m_all) * p.inv_t : lane == 1 ? ((double)m_rest - (double)m_all) * p.inv_t
-                                                                                            : ((double)s.ref - (double)m_rest * (double)p.c) * 0.693147180559945309;
+                                                                                            : (whole_reference(m_rest, told, p.c) - (double)m_rest * (double)p.c) * 0.693147180559945309;
                 const double y = exp(x);
                 a_list = m_list > -INFINITY ? __shfl_sync(kFullMask, y, 0) : 0.0;
                 a_rest = __shfl_sync(kFullMask, y, 1);
                 up = __shfl_sync(kFullMask, y, 2);
-                z_rest = up * s.acc * kEx2BiasFix;
-                ref = ceilf(m_rest * p.c);                           // the least that serves, so that small gradients stay
-                up *= pow2_down(ref - s.ref);
+                z_rest = up * acc * kEx2BiasFix;
+                far = m_rest > -INFINITY && is_far(m_rest, p.c);
                 if (!(m_rest > -INFINITY)) {
-                    a_rest = ref = 0.0f;
-                    z_rest = s.acc == s.acc ? 0.0 : s.acc;
+                    a_rest = 0.0;
+                    z_rest = acc == acc ? 0.0 : acc;
+                } else if (far) up = 1.0;
+                else {
+                    ref = ceilf(m_rest * p.c);                       // the least that serves, so that small gradients stay
+                    up *= pow2_down(ref - told);
                 }
                 z_all = k.z_list * a_list + z_rest * a_rest;
-                if (!(m_all > -INFINITY) || !(s.acc == s.acc) || !(k.z_list == k.z_list)) z_all = nan;
+                if (!(m_all > -INFINITY) || !(acc == acc) || !(k.z_list == k.z_list)) z_all = nan;
             } else {
                 const float4 st = *stats;
                 m_all = st.x; z_all = (double)st.y; m_rest = st.z; z_rest = (double)st.w;
-                if (m_rest > -INFINITY) ref = ceilf(m_rest * p.c);
+                far = m_rest > -INFINITY && is_far(m_rest, p.c);
+                if (m_rest > -INFINITY && !far) ref = ceilf(m_rest * p.c);
                 const double x = lane == 0 ? ((double)m_list - (double)m_all) * p.inv_t : lane == 1 ? ((double)m_rest - (double)m_all) * p.inv_t
-                                                                                            : ((double)ref - (double)m_rest * (double)p.c) * 0.693147180559945309;
+                                                                                            : (far ? 0.0 : ((double)ref - (double)m_rest * (double)p.c) * 0.693147180559945309);
                 const double y = exp(x);
                 a_list = m_list > -INFINITY ? __shfl_sync(kFullMask, y, 0) : 0.0;
                 a_rest = m_rest > -INFINITY ? __shfl_sync(kFullMask, y, 1) : 0.0;
@@ -600,6 +651,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                 const double w = (double)k.upstream * weight * p.inv_t, inv = 1.0 / (lane == 1 ? z_rest : z_all);
                 const double inv_all = __shfl_sync(kFullMask, inv, 0), inv_rest = __shfl_sync(kFullMask, inv, 1);
                 if (lane == 0) {
+                    k.grad_base = far ? m_rest : 0.0f;
                     k.grad_ref = ref;
                     k.factor = empty ? w * (0.0 * z_all) : w * (total * a_rest * inv_all - (k.p_rest != 0.0 ? k.p_rest * inv_rest : 0.0)) * up;
                 }
@@ -617,8 +669,8 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             }
             if (kLoss && rank == 0) {
                 const double log_z = log(z_all);                     // of exp((s - m_all) / T)
-                // entropy - sum p log q, with log q = s / T - m_all / T - log_z
-                double loss = k.entropy - k.cross + k.mass * ((double)m_all * p.inv_t + log_z);
+                // entropy - sum p log q, with log q = s / T - m_all / T - log_z  (without a logit in the list, cross says all)
+                double loss = k.entropy - k.cross + k.mass * ((m_list > -INFINITY ? ((double)m_all - (double)m_list) * p.inv_t : 0.0) + log_z);
                 if (k.p_rest != 0.0) {
                     if (empty) loss = k.p_rest <= kRestRounding ? loss + 0.0 * z_all : loss + k.p_rest * (double)INFINITY;
                     else loss += k.p_rest * (log(k.p_rest) - (((double)m_rest - (double)m_all) * p.inv_t + log(z_rest) - log_z));
@@ -656,14 +708,14 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             const int again = kLoss && kGrad && live ? max(0, seg.n_tiles - (int)S) : seg.n_tiles;      // tiles that do not stay: the first ones
             unsigned stay_stage = 0;                                 // of the first that does
             if (kLoss && live) {
-                DistillSum s{-INFINITY, kDistillLowest, 0.0};
+                DistillSum s;
                 if (tid < seg.scalars) {
                     float x = E::load(seg.in, seg.scalar(p, tid));
                     for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
                         if (l.thread[o] == tid) x = -INFINITY;
                     s.m = fmaxf(s.m, x);
-                    if (fmaf(x, p.c, -kDistillAbove) > s.ref) distill_raise(s, x * p.c);
-                    s.acc += (double)ex2_approx(fmaf(x, p.c, -s.ref));
+                    if (x > s.top) distill_raise(p, s);
+                    s.acc += (double)ex2_approx(fmaf(x - s.base, p.c, -s.ref));
                 }
                 for (int t = 0; t < seg.n_tiles; ++t) {
                     if (t == again) stay_stage = stage;
@@ -693,29 +745,32 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     if (c0 - lane >= nc) continue;                   // nothing of this tile for the warp
                     const float m = E::max4(w[0], w[1], w[2], w[3]);
                     s.m = fmaxf(s.m, m);
-                    if (fmaf(m, p.c, -kDistillAbove) > s.ref) distill_raise(s, m * p.c);
-                    const uint64_t nref2 = pack2(-s.ref, -s.ref);
-                    const uint64_t sum2 = add2(add2(chunk_terms<DT>(w[0], c2, nref2), chunk_terms<DT>(w[1], c2, nref2)),
-                                               add2(chunk_terms<DT>(w[2], c2, nref2), chunk_terms<DT>(w[3], c2, nref2)));
-                    float a0, a1;
-                    unpack2(sum2, a0, a1);
-                    s.acc += (double)(a0 + a1);
+                    bool near = true;
+                    if (m > s.top) {
+                        distill_raise(p, s);
+                        near = s.base == 0.0f;
+                        if (!near) s.acc += tile_terms<DT, true>(w, c2, s);
+                    }
+                    if (near) s.acc += tile_terms<DT, false>(w, c2, s);
                 }
                 if (!ok) break;
-                distill_join(s);
-                if (lane == 0) { k.max[warp] = s.m; k.ref[warp] = s.ref; k.sum[warp] = s.acc; }
+                float m = s.m, told = told_reference(s);
+                double acc = s.acc;
+                distill_join(p.c, m, told, acc);
+                if (lane == 0) { k.max[warp] = m; k.ref[warp] = told; k.sum[warp] = acc; }
                 arrive(&sh.summed[slot]);
             }
             if constexpr (kGrad) {
                 if (live && !wait(&sh.known[slot], phase, kSpinLimit)) break;
                 const bool zero = !live || k.left_out;
-                const float nref = live ? -k.grad_ref : 0.0f, factor = live ? (float)k.factor : 0.0f;
+                const float nbase = live ? -k.grad_base : 0.0f, nref = live ? -k.grad_ref : 0.0f, factor = live ? (float)k.factor : 0.0f;
+                const bool far = nbase != 0.0f;
                 const uint64_t nref2 = pack2(nref, nref), factor2 = pack2(factor, factor);
                 if (tid < seg.scalars) {
                     const int64_t v = seg.scalar(p, tid);
                     float g = 0.0f;
                     if (!zero) {
-                        g = factor * ex2_approx(fmaf(E::load(seg.in, v), p.c, nref));
+                        g = factor * ex2_approx(fmaf(E::load(seg.in, v) + nbase, p.c, nref));
                         for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
                             if (l.thread[o] == tid && l.once[o]) g = l.g[o];
                     }
@@ -740,7 +795,8 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                         const int c = t * kDistillTile + u * kDistillCompute + tid;
                         if (c >= nc) break;
                         uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                        if (!zero) w = gradient_chunk<DT>(tile[u * kDistillCompute + tid], c2, nref2, factor2);
+                        if (!zero && far) w = gradient_chunk<DT, true>(tile[u * kDistillCompute + tid], c2, nbase, nref2, factor2);
+                        else if (!zero) w = gradient_chunk<DT, false>(tile[u * kDistillCompute + tid], c2, 0.0f, nref2, factor2);
                         if (same) o4[c] = w;
                         else store_chunk<DT>(out, seg.e0 + (int64_t)c * E::EPC, w);
                     }
