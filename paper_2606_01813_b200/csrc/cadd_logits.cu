@@ -56,9 +56,11 @@ static int check_output(int batch, int rows, int64_t V, int dtype, const void* x
 
 // ---------------- penalties, biases, masks ----------------
 
+// Dynamic shared memory that a kernel may have.  `most` is what any call of it can want: the limit belongs to the process, and a call that set its
+// own size would have another thread's larger launch refused.
 template <typename K>
-static int room(K kernel, size_t smem) {
-    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) == cudaSuccess) return CADD_OK;
+static int room(K kernel, size_t most) {
+    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) == cudaSuccess) return CADD_OK;
     cudaGetLastError();
     return CADD_ERR_LAUNCH;
 }
@@ -96,7 +98,7 @@ static int launch_tokens(AdjustParams& p, cudaStream_t st) {
     const int64_t grid = (int64_t)p.batch * p.S * p.groups;
     if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
     const size_t smem = adjust_tokens_smem(p.slots, p.n_bias > 0);
-    const int rc = room(adjust_tokens_kernel<DT>, smem);
+    const int rc = room(adjust_tokens_kernel<DT>, adjust_tokens_smem(kTokensSlots, true));
     if (rc != CADD_OK) return rc;
     return launch_cluster(adjust_tokens_kernel<DT>, (unsigned)grid, kTokensThreads, 1, smem, st, p, p.followed);
 }
@@ -129,7 +131,7 @@ static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
         const int64_t grid = (int64_t)p.batch * p.tiles * p.groups;
         if (grid >= ((int64_t)1 << 31)) return CADD_ERR_SHAPE;
         const size_t smem = (size_t)adjust_layout(tile, p.n_bias).bytes;
-        const int rc = room(adjust_rows_kernel<DT>, smem);
+        const int rc = room(adjust_rows_kernel<DT>, (size_t)adjust_layout(tile, tile).bytes);
         if (rc != CADD_OK) return rc;
         adjust_rows_kernel<DT><<<(unsigned)grid, kAdjustThreads, smem, st>>>(p);
         return launched();
@@ -158,15 +160,15 @@ static int launch_adjust(AdjustParams& p, bool in_place, cudaStream_t st) {
 // Chunks of a row at most: its whole 16-byte chunks where it starts on a boundary.
 static int64_t row_chunks(int dtype, int64_t V) { return V / (dtype == CADD_DTYPE_BF16 ? 8 : 4); }
 
+constexpr size_t kDistillRoom = 227 * 1024;               // shared memory of a CTA
+
 template <int DT, bool kLoss, bool kGrad>
 static int launch_distill(DistillParams& p, cudaStream_t st) {
     const size_t smem = distill_smem_bytes(p.chunks_max, p.K, p.stages);
-    const int rc = room(distill_kernel<DT, kLoss, kGrad>, smem);
+    const int rc = room(distill_kernel<DT, kLoss, kGrad>, kDistillRoom);
     if (rc != CADD_OK) return rc;
     return launch_cluster(distill_kernel<DT, kLoss, kGrad>, (unsigned)(p.clusters * p.C), kDistillThreads, (unsigned)p.C, smem, st, p);
 }
-
-constexpr size_t kDistillRoom = 227 * 1024;               // shared memory of a CTA
 
 static int distill(const cadd_distill_args* a, bool loss, cudaStream_t st) {
     if (!a) return CADD_ERR_NULL;
