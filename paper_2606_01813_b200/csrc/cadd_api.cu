@@ -145,7 +145,10 @@ static int launch_expand(const cadd_build_args* a, int KP, int S, int rec_fmt, c
     ep.topk_logprob = a->topk_logprob; ep.status = a->status;
     void (*kernel)(ExpandParams) = rec_fmt == kRecDirect ? expand_emit_kernel<true> : expand_emit_kernel<false>;
     if (lay.total > 48 * 1024) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lay.total) != cudaSuccess) {
+        // (all that an SM has beside the kernel's own 64 bytes: the limit belongs to the process, and a call that set its own size would have another
+        // thread's larger launch refused)
+        constexpr int kMost = 227 * 1024 - 64;
+        if (lay.total > (size_t)kMost || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) {
             cudaGetLastError();
             return CADD_ERR_LAUNCH;
         }

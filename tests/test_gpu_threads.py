@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2606_01813_b200 import binding as G
+from paper_2606_01813_b200 import synth
 from logits_util import random_adjust, random_distill
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +65,32 @@ def test_adjustment(R, batch, V):
     torch.cuda.synchronize()
     for r, want in zip(together(large, small), (a, b)):
         assert torch.equal(r, want)
+
+
+def build_call(L, K, B_max):
+    """The C call alone, so that threads are in it most of the time."""
+    cfg = synth.scaled(synth.CONFIGS["c2"], batch=2, V=2000, L=L, B_max=B_max, K=K)
+    x, coef = synth.make_draft_inputs(cfg, 3).logits.cuda(), synth.make_cost_inputs(cfg, 3).coef.double().cuda().contiguous()
+    call, given = G.lib().cadd_build_tree, []
+    want, out = (G.cadd_build_tree(x, K, B_max, cost_coef=coef) for _ in range(2))
+    ws = torch.empty(G.cadd_build_workspace_bytes(2, L, 2000, K, B_max, B_max + 1, x.dtype), dtype=torch.uint8, device="cuda")
+    G.lib().cadd_build_tree = lambda args, stream: given.append(args) or call(args, stream)
+    try:
+        G.cadd_build_tree(x, K, B_max, cost_coef=coef, out=out, workspace=ws)
+    finally:
+        G.lib().cadd_build_tree = call
+    assert given[0]._obj.cost_coef == coef.data_ptr()
+
+    def again(s):
+        for _ in range(5):
+            if call(given[0], s.cuda_stream) != G.OK:
+                raise G.CaddError(G.ERR_LAUNCH)
+        return x, coef, ws, out
+    return again, want
+
+
+def test_construction():
+    calls = [build_call(32, 32, b) for b in (2048, 1400, 2048, 1400)]
+    torch.cuda.synchronize()
+    for (*_, r), (_, want) in zip(together(*(c for c, _ in calls)), calls):
+        assert torch.equal(r.token_ids, want.token_ids) and torch.equal(r.parent_idx, want.parent_idx) and torch.equal(r.n_nodes, want.n_nodes)
