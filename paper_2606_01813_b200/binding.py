@@ -1087,7 +1087,7 @@ class Distilled:
     status: Optional[torch.Tensor] = None
 
 
-def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags):
+def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags, stream):
     dev, index, code = _logits_of(x, "draft_logits")
     B, L, V = shape = x.shape
     _need(teacher_token.dim() == 3 and teacher_token.shape[0] == B, "teacher_token must be [batch, R, K]")
@@ -1097,6 +1097,10 @@ def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperatur
     if path is not None:
         _need(path_len is not None and n_rows is None, "path comes with path_len and without n_rows")
         _need(path.dim() == 2, "path must be [batch, columns]")
+        if path.shape[1] == 0 and path.shape[0] == B:                 # (its pointer is NULL, which would mean no path) a column of no row: row 0 alone
+            _need_like(path, i32, (B, 0), index, "path")
+            with torch.cuda.stream(_stream_of(stream, dev)):
+                path = torch.full((B, 1), -1, dtype=i32, device=dev)
         P = path.shape[1]
     else:
         _need(path_len is None, "path_len comes with path")
@@ -1117,7 +1121,7 @@ def cadd_distill_loss(draft_logits: torch.Tensor, teacher_token: torch.Tensor, t
     target's top tokens, teacher_token int32 and teacher_logit fp64 [batch, R, K] (cadd_build_tree's topk_token and topk_logprob fit),
     and with `grad` (or out.grad, which may be draft_logits itself) the gradient of its sum in the same pass: go on with
     draft_logits.backward(result.grad).  Position i learns from row i of the lists, with path / path_len (a verification's
-    accepted_nodes / accepted_len) from row 0, then from the accepted nodes, as far as they go.  `rest`: all tokens that are not
+    accepted_nodes / accepted_len) from row 0, then from the accepted nodes, as far as they go (a path without a column: from row 0 alone).  `rest`: all tokens that are not
     listed are one more class (teacher_logit are then log-probabilities, or logits with teacher_lse fp64 [batch, R]).
     weight and grad_loss fp32 [batch, L]; n_rows int32 [batch]."""
     dev = draft_logits.device
@@ -1128,7 +1132,7 @@ def cadd_distill_loss(draft_logits: torch.Tensor, teacher_token: torch.Tensor, t
             out = Distilled(loss=torch.empty(B, L, device=dev), stats=torch.empty(B, L, 4, device=dev),
                             grad=torch.empty(draft_logits.shape, dtype=draft_logits.dtype, device=dev) if grad else None,
                             status=torch.empty(B, dtype=torch.int32, device=dev))
-    dev, a = _distill_args(draft_logits, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags)
+    dev, a = _distill_args(draft_logits, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss, out, flags, stream)
     _enqueue(lib().cadd_distill_loss, a, dev, stream)
     return out
 
@@ -1145,6 +1149,6 @@ def cadd_distill_grad(draft_logits: torch.Tensor, teacher_token: torch.Tensor, t
         with torch.cuda.stream(_stream_of(stream, dev)):
             grad = torch.empty(draft_logits.shape, dtype=draft_logits.dtype, device=dev)
     dev, a = _distill_args(draft_logits, teacher_token, teacher_logit, teacher_lse, rest, temperature, path, path_len, n_rows, weight, grad_loss,
-                           Distilled(stats=stats, grad=grad, status=status), flags)
+                           Distilled(stats=stats, grad=grad, status=status), flags, stream)
     _enqueue(lib().cadd_distill_grad, a, dev, stream)
     return grad

@@ -461,3 +461,17 @@ def test_sums_of_few_large_terms(dtype, equal):
         p = 0.25 ** (1.0 / T)                                              # (the target's entries are logits, too)
         loss = p * (math.log(p) - logq[..., 0]) + (1.0 - p) * (math.log(1.0 - p) - torch.logsumexp(logq[..., 1:], -1))
         assert bool(((r.loss.double().cpu() - loss).abs() <= 2 * tol + 2.0 ** -24 * loss.abs()).all())
+
+
+@pytest.mark.parametrize("rest", [False, True])
+def test_a_path_without_columns(rest):
+    """Accepted nodes cut to the longest accepted length, of a batch in which nothing was accepted: only the first position is learnt from."""
+    for L in (1, 5):
+        d = random_distill(3, L, 2000, 6, torch.float32, seed=19, rest=rest, path=True)
+        d.path, d.path_len = d.path[:, :0].contiguous(), i32([0, 0, 0])
+        assert d.teacher_token.shape[1] >= L                               # (rows of lists for all positions are there)
+        r = every(d)
+        assert r.status.tolist() == [0, 0, 0] and int(r.loss[:, 1:].count_nonzero()) == 0 and int(r.grad[:, 1:].count_nonzero()) == 0
+        assert int((r.loss[:, 0] != 0).sum()) == 3
+    d.teacher_token, d.teacher_logit = d.teacher_token[:, :2].contiguous(), d.teacher_logit[:, :2].contiguous()      # fewer rows than positions
+    every(d)
