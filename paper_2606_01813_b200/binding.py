@@ -1119,12 +1119,13 @@ def cadd_distill_loss(draft_logits: torch.Tensor, teacher_token: torch.Tensor, t
                       stream: Optional[torch.cuda.Stream] = None) -> Distilled:
     """Distillation: the divergence of the drafter's distribution at each position of draft_logits [batch, L, V] from the
     target's top tokens, teacher_token int32 and teacher_logit fp64 [batch, R, K] (cadd_build_tree's topk_token and topk_logprob fit),
-    and with `grad` (or out.grad, which may be draft_logits itself) the gradient of its sum in the same pass: go on with
+    and with `grad` (with `out`: where it has a grad, which may be draft_logits itself) the gradient of its sum in the same pass: go on with
     draft_logits.backward(result.grad).  Position i learns from row i of the lists, with path / path_len (a verification's
     accepted_nodes / accepted_len) from row 0, then from the accepted nodes, as far as they go (a path without a column: from row 0 alone).  `rest`: all tokens that are not
     listed are one more class (teacher_logit are then log-probabilities, or logits with teacher_lse fp64 [batch, R]).
     weight and grad_loss fp32 [batch, L]; n_rows int32 [batch]."""
     dev = draft_logits.device
+    _need(out is None or not grad or out.grad is not None, "grad goes with out.grad, where out is given")
     if out is None:
         _need(dev.type == "cuda" and draft_logits.dim() == 3, "draft_logits must be a CUDA tensor [batch, L, V] (there is no CPU path)")
         B, L = draft_logits.shape[:2]

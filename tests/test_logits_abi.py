@@ -123,3 +123,9 @@ def test_plain_gradient_by_formula_and_by_differences(rest, T, twice):
                 e[v] = 1e-5
                 diff = (row_loss(s + e, tok, val, lse, rest, T) - row_loss(s - e, tok, val, lse, rest, T)) / 2e-5
                 assert abs(float(diff) * w - float(grad[b, i, v])) < 1e-7
+
+
+def test_a_gradient_that_has_no_place_is_refused():
+    x, t = torch.zeros(1, 2, 8), torch.zeros(1, 2, 3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="out.grad"):
+        G.cadd_distill_loss(x, t, torch.zeros(1, 2, 3, dtype=torch.float64), grad=True, out=G.Distilled(loss=torch.zeros(1, 2)))
