@@ -830,6 +830,15 @@ class Evicted:
     status: Optional[torch.Tensor] = None
 
 
+def _some_column(path: Optional[torch.Tensor], B: int, dev, stream) -> Optional[torch.Tensor]:
+    """A path without columns has a NULL pointer, which would mean no path: one column of no row instead, so that the root is left."""
+    if path is None or path.dim() != 2 or path.shape[1] != 0 or path.shape[0] != B:
+        return path
+    _need_like(path, torch.int32, (B, 0), dev.index, "path")
+    with torch.cuda.stream(_stream_of(stream, dev)):
+        return torch.full((B, 1), -1, dtype=torch.int32, device=dev)
+
+
 def _row_list(cache: KvCache, n_rows, path, path_len):
     """L and the pointers of n_rows, path and path_len, of the calls that take a path or leading rows.  (The caller keeps its
     own names bound to the tensors until the call is enqueued: a temporary would otherwise be freed, and its memory given out.)"""
@@ -851,7 +860,7 @@ def cadd_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, n_row
                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Write rows of k and v (bf16 [batch, R, heads, head_dim]) behind each request's cached tokens: rows 0..n_rows[b]-1
     (all R without n_rows), or with path / path_len (a verification's accepted_nodes / accepted_len) the root and the accepted
-    path.  Returns new_length (which may be given, cache.length itself included: the cache then goes on from there)."""
+    path (without a column: the root alone).  Returns new_length (which may be given, cache.length itself included: the cache then goes on from there)."""
     B, dev = cache.batch, cache.device
     _need(k.dim() == 4 and k.shape[0] == B, "k must be [batch, R, heads, head_dim]")
     R = k.shape[1]
@@ -859,6 +868,7 @@ def cadd_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, *, n_row
     kp, *strides = _need_rows(k, shape, dev, "k")
     vp, *vs = _need_rows(v, shape, dev, "v")
     _need(strides == vs, "k and v must have the same strides")
+    path = _some_column(path, B, dev, stream)
     L, *rows = _row_list(cache, n_rows, path, path_len)
     if new_length is None:
         with torch.cuda.stream(_stream_of(stream, dev)):
@@ -958,6 +968,7 @@ def cadd_cache_weights(q: torch.Tensor, lse: torch.Tensor, cache: KvCache, base_
     B, dev, D = cache.batch, cache.device, cache.head_dim
     _need(q.dim() == 4, "q must be [batch, R, heads_q, head_dim]")
     R, hq = q.shape[1], q.shape[2]
+    path = _some_column(path, B, dev, stream)
     L, *rows = _row_list(cache, n_rows, path, path_len)
     _need(lse.dtype == torch.float32 and lse.device == dev and lse.shape == (B, R, hq) and lse.is_contiguous(),
           "lse must be a contiguous float32 tensor [batch, R, heads_q]")
@@ -1097,10 +1108,7 @@ def _distill_args(x, teacher_token, teacher_logit, teacher_lse, rest, temperatur
     if path is not None:
         _need(path_len is not None and n_rows is None, "path comes with path_len and without n_rows")
         _need(path.dim() == 2, "path must be [batch, columns]")
-        if path.shape[1] == 0 and path.shape[0] == B:                 # (its pointer is NULL, which would mean no path) a column of no row: row 0 alone
-            _need_like(path, i32, (B, 0), index, "path")
-            with torch.cuda.stream(_stream_of(stream, dev)):
-                path = torch.full((B, 1), -1, dtype=i32, device=dev)
+        path = _some_column(path, B, dev, stream)
         P = path.shape[1]
     else:
         _need(path_len is None, "path_len comes with path")

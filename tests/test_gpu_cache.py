@@ -638,3 +638,19 @@ def test_weights_of_warps_that_go_through_many_steps(fp4, page, window):
     case = weights_case(fp4=fp4, heads=8, group=2, page=page, R=9, base=[16000, 9000, 12345, 100], path_lens=[3, 8, 0, 5], window=window, sinks=40 if window else 0)
     check_weights(case)
     check_weights(case, in_place=True)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_a_path_without_columns_is_the_root_alone(fp4):
+    p = problem(fp4=fp4, batch=3, lens=[10, 31, 0], R=6, live=[6] * 3, heads=1, page=16)
+    none, some = (torch.zeros(3, m, dtype=torch.int32, device=DEV) for m in (0, 1))
+    a, b = p.cache(G), p.cache(G)
+    n = G.cadd_cache_append(a, p.k.to(DEV), p.v.to(DEV), path=none, path_len=i32([0, 0, 0]))
+    assert n.tolist() == [11, 32, 1]
+    assert torch.equal(n, G.cadd_cache_append(b, p.k.to(DEV), p.v.to(DEV), path=some, path_len=i32([0, 0, 0])))
+    for x, y in zip((a.k, a.v, a.k_scale, a.v_scale), (b.k, b.v, b.k_scale, b.v_scale)):
+        assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    lse, w = torch.zeros(3, 6, p.heads * p.group, device=DEV), torch.zeros(3, p.heads, a.capacity, device=DEV)
+    got, want = (G.cadd_cache_weights(p.q.to(DEV), lse, at_length(a, n), i32(p.lens), w, path=path, path_len=i32([0, 0, 0]), out=torch.zeros_like(w))
+                 for path in (none, some))
+    assert int(want.count_nonzero()) > 0 and torch.equal(got, want)
