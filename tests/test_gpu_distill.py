@@ -475,3 +475,14 @@ def test_a_path_without_columns(rest):
         assert int((r.loss[:, 0] != 0).sum()) == 3
     d.teacher_token, d.teacher_logit = d.teacher_token[:, :2].contiguous(), d.teacher_logit[:, :2].contiguous()      # fewer rows than positions
     every(d)
+
+
+@pytest.mark.parametrize("V", [60000, 3000])
+def test_gradient_alone_when_a_wait_runs_out(V):
+    """All of its rows are lost."""
+    d = random_distill(2, 3, V, 5, torch.bfloat16, seed=2, rest=True)
+    d.n_rows = None
+    (x, t, v), kw = put(d)
+    stats, st = G.cadd_distill_loss(x, t, v, **kw).stats, torch.zeros(2, dtype=torch.int32, device="cuda")
+    g = G.cadd_distill_grad(x, t, v, stats, status=st, flags=G.FLAG_TEST_DROP_TILE, grad=torch.zeros_like(x), **kw)
+    assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(g).all())
