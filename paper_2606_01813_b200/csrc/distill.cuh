@@ -73,6 +73,7 @@ struct DistillRow {
     int live;                                     // 0: left out from the start, nothing is read
     int left_out;                                 // by its list, after its tiles have been sent for
     int twice;                                    // some token is listed more than once
+    int near;                                     // some logit beside the list is far above those that are far out below
 };
 constexpr int kDistillGroups = 512;
 struct DistillMap {
@@ -201,14 +202,16 @@ template <int DT> __device__ __forceinline__ void store_element(char* row, int64
 // speed: it saves most steps to another reference, one of which halts a warp's 32 threads (training step of 2048 rows 242.0 us, losses of 1728 rows 99.9; with the
 // least reference always 247 and 103, with 16 more 241.4 and 98.2 and roundings of 2^-20).
 // Beyond, fp32 has no integers fine enough to tell x c from ref by: then base is the largest logit itself and ref 0, the difference of two logits being
-// as exact as a product.  Every tile then goes the long way (top is -Inf).
+// as exact as a product.  Every tile then goes the long way (top is -Inf), unless the row has been seen to hold logits so far above (DistillRow::near) that
+// these add exactly nothing: such a thread goes on as one that has seen nothing yet (rows with a finite mask: 2048 rows 347 us without that).
+// A sum of nothing has ref Inf, from which all terms are 0.
 constexpr float kDistillSpare = 2.0f, kDistillAbove = 3.75f;
 struct DistillSum {
     float m;                                      // the largest logit
     float base, ref;
     float top;                                    // the largest logit that the reference serves
     double acc;
-    __device__ __forceinline__ DistillSum() : m(-INFINITY), base(0.0f), ref(0.0f), top(kDistillUnder), acc(0.0) {}
+    __device__ __forceinline__ DistillSum() : m(-INFINITY), base(0.0f), ref(INFINITY), top(kDistillUnder), acc(0.0) {}
 };
 __device__ __forceinline__ float warp_max(float x) {                // NaN ignored
     float r;
@@ -217,16 +220,24 @@ __device__ __forceinline__ float warp_max(float x) {                // NaN ignor
 }
 __device__ __forceinline__ bool is_far(float x, float c) { return !(fabsf(x * c) <= kDistillNear); }
 // s.m is above s.top: the reference follows.
-__device__ __forceinline__ void distill_raise(const DistillParams& p, DistillSum& s) {
-    const bool far = is_far(s.m, p.c), none = s.base == 0.0f && s.top < kDistillLowest;      // (none: acc is 0, or NaN)
+__device__ __forceinline__ void distill_raise(const DistillParams& p, DistillSum& s, volatile int* near) {
+    const float at = s.m * p.c;
+    const bool far = is_far(s.m, p.c), none = s.base == 0.0f && s.ref == INFINITY;         // (none: acc is 0, or NaN)
+    if (at >= 1200.0f - kDistillNear) *near = 1;                    // (2^-1000 and less count as 0)
     if (!far && s.base == 0.0f) {
-        const float ref = ceilf(s.m * p.c) + kDistillSpare;
+        const float ref = ceilf(at) + kDistillSpare;
         s.acc *= none ? 0.0 : pow2_down(s.ref - ref);
         s.ref = ref;
         s.top = fmaxf(s.m, (ref + kDistillAbove) * p.over_c);
+    } else if (far && at < 0.0f && *near) {
+        s.acc *= 0.0;
+        s.base = 0.0f;
+        s.ref = INFINITY;
+        s.top = -kDistillNear * p.over_c;
     } else if (s.base != s.m) {
-        const float base = far ? s.m : 0.0f, ref = far ? 0.0f : ceilf(s.m * p.c) + kDistillSpare;
-        s.acc *= none ? 0.0 : exp2(((double)s.base * (double)p.c + (double)s.ref) - ((double)base * (double)p.c + (double)ref));
+        const float base = far ? s.m : 0.0f, ref = far ? 0.0f : ceilf(at) + kDistillSpare;
+        const double step = ((double)s.base * (double)p.c + (double)s.ref) - ((double)base * (double)p.c + (double)ref);
+        s.acc *= none || step < -1000.0 ? 0.0 : exp2(step);
         s.base = base;
         s.ref = ref;
         s.top = far ? -INFINITY : fmaxf(s.m, (ref + kDistillAbove) * p.over_c);
@@ -234,17 +245,19 @@ __device__ __forceinline__ void distill_raise(const DistillParams& p, DistillSum
 }
 // A sum's reference for others: the integer; +-Inf where it is the largest logit; -Inf where there is nothing.
 __device__ __forceinline__ float told_reference(const DistillSum& s) {
-    return s.base != 0.0f ? copysignf(INFINITY, s.base) : (s.top < kDistillLowest ? -INFINITY : s.ref);
+    return s.base != 0.0f ? copysignf(INFINITY, s.base) : (s.ref == INFINITY ? -INFINITY : s.ref);
 }
 __device__ __forceinline__ double whole_reference(float m, float told, float c) { return isinf(told) ? (double)m * (double)c : (double)told; }
 // The step from one reference to another where the latter is far out, or so near that it is not far from others that are.
 __device__ __noinline__ double far_step(float m, float told, float m_all, float all, float c) {
-    return m >= kDistillLowest ? exp2(whole_reference(m, told, c) - whole_reference(m_all, all, c)) : 0.0;
+    if (!(m >= kDistillLowest)) return 0.0;
+    const double step = whole_reference(m, told, c) - whole_reference(m_all, all, c);
+    return step < -1000.0 ? 0.0 : exp2(step);
 }
 // Sums of the lanes together, in every lane: m the largest logit of a lane's sum, told its reference.
 __device__ __forceinline__ void distill_join(float c, float& m, float& told, double& acc) {
     const float m_all = warp_max(m), all = warp_max(told);
-    acc *= fabsf(all) <= kDistillNear - 200.0f ? pow2_down(told - all) : far_step(m, told, m_all, all, c);      // (told -Inf: 0)
+    acc *= fabsf(all) <= kDistillNear - 1200.0f ? pow2_down(told - all) : far_step(m, told, m_all, all, c);      // (told -Inf: 0)
     m = m_all;
     told = all;
     acc = warp_sum(acc);
@@ -464,7 +477,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
             for (int o = lane; o < parts + 2; o += 32) first_of[o] = -1;
             __syncwarp();                                            // (below, any lane's token may lie in any part)
             const float weight = p.weight ? p.weight[row] : 1.0f, upstream = p.grad_loss ? p.grad_loss[row] : 1.0f;
-            if (lane == 0) { k.live = 1; k.weight = weight; k.upstream = upstream; }
+            if (lane == 0) { k.live = 1; k.near = 0; k.weight = weight; k.upstream = upstream; }
             const int64_t at = ((int64_t)seg.b * p.R + r) * p.K;
             double top = p.rest && p.lse ? p.lse[(int64_t)seg.b * p.R + r] / p.inv_t : (p.rest ? 0.0 : -INFINITY);
             float m_list = -INFINITY;
@@ -714,7 +727,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     for (int o = first_of[tid < seg.head ? parts : parts + 1]; o >= 0; o = l.next[o])
                         if (l.thread[o] == tid) x = -INFINITY;
                     s.m = fmaxf(s.m, x);
-                    if (x > s.top) distill_raise(p, s);
+                    if (x > s.top) distill_raise(p, s, &k.near);
                     s.acc += (double)ex2_approx(fmaf(x - s.base, p.c, -s.ref));
                 }
                 for (int t = 0; t < seg.n_tiles; ++t) {
@@ -747,7 +760,7 @@ __global__ void __launch_bounds__(kDistillThreads, 1) distill_kernel(DistillPara
                     s.m = fmaxf(s.m, m);
                     bool near = true;
                     if (m > s.top) {
-                        distill_raise(p, s);
+                        distill_raise(p, s, &k.near);
                         near = s.base == 0.0f;
                         if (!near) s.acc += tile_terms<DT, true>(w, c2, s);
                     }

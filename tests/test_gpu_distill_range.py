@@ -5,6 +5,8 @@ The expected gradient of rows with a rest is the formula itself, w / T (S q - p)
 passes by log q, which in 64 bits has no digits left for log q_rest once the rest is some 1e12 T below the list.  The tolerances are logits_util's, whose share of
 the rest, q p_rest / q_rest, is 0 / 0 there, and is r p_rest here, with its own distances from the rest's largest logit:
 |g w / T| r p_rest (2 Z_TOL + |s - m'| / T * 2 * 2^-24)."""
+import math
+
 import pytest
 import torch
 
@@ -129,3 +131,32 @@ def test_single_logits_far_above_all_others():
                 ids = d.teacher_token[0, i]
                 d.logits[0, i, ids[ids >= 0][0].long()] = high
             every(d)
+
+
+def test_masked_rows_repeat_bit_for_bit_and_keep_nan():
+    """Which of a row's threads have met a mask before they learn of larger logits is not the same from call to call; what they give is."""
+    for dtype, fill in ((torch.bfloat16, -1e9), (torch.float32, -1e12)):
+        d = random_distill(20, 12, 45000, 6, dtype, seed=41, rest=True)
+        d.n_rows = None
+        kept = torch.rand(45000, generator=torch.Generator().manual_seed(2)) < 0.01
+        ids = d.teacher_token.clamp(min=0).long()
+        listed = torch.gather(d.logits, 2, ids)
+        d.logits[:, :, ~kept] = fill
+        d.logits.scatter_(2, ids, listed)
+        d.logits[3, 4] = fill                                              # a row of nothing else
+        x, t, v, kw = d.logits.cuda(), d.teacher_token.cuda(), d.teacher_logit.cuda(), d.args("cuda")
+        first = G.cadd_distill_loss(x, t, v, grad=True, **kw)
+        for _ in range(30):
+            r = G.cadd_distill_loss(x, t, v, grad=True, **kw)
+            for f in ("loss", "stats", "grad"):
+                assert torch.equal(getattr(r, f), getattr(first, f))
+        check = Distill(d.logits[:3], d.teacher_token[:3], d.teacher_logit[:3], rest=True, weight=d.weight[:3], grad_loss=d.grad_loss[:3])
+        expected = expected_of(check)
+        check_loss(first.loss[:3], first.stats[:3], check, expected)
+        check_grad(first.grad[:3], expected)
+        masked = [v for v in torch.nonzero(~kept)[:, 0].tolist() if not bool((ids == v).any())]
+        for i, at in enumerate((masked[0], masked[len(masked) // 2], masked[-1])):
+            x[5, i, at] = math.nan
+        r = G.cadd_distill_loss(x, t, v, grad=True, **kw)
+        assert torch.isnan(r.loss[5]).tolist() == [True] * 3 + [False] * 9 and bool(torch.isnan(r.grad[5, :3]).all())
+        assert torch.equal(r.loss[:5], first.loss[:5]) and torch.equal(r.grad[6:], first.grad[6:])
