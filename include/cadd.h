@@ -527,11 +527,13 @@ typedef struct cadd_adjust_args {
                                       start equally far behind a 16-byte boundary */
     int64_t  out_stride_b, out_stride_row;
     const int32_t* n_nodes;        /* [batch]: rows 0..n_nodes[b] are live; NULL => R-1; -1: none.  Outside [-1, R-1]: clamped, CADD_STATUS_BAD_N_NODES */
-    const int32_t* token_ids;      /* [batch,R] from cadd_build_tree, NULL: no paths */
+    const int32_t* token_ids;      /* [batch,R] from cadd_build_tree, NULL: no paths.  Row 0's token, the last one put out, counts where the tree was built
+                                      with bonus_token (without, it is -1 there and counts for nothing) */
     const int32_t* parent_idx;     /* [batch,R] from cadd_build_tree, required with token_ids */
     const int32_t* history;        /* [batch, history_cols], rows history_stride apart; NULL: none.  What came before row 0's token */
     int64_t  history_stride;       /* in elements, >= 0 */
-    int32_t  history_cols;         /* >= 1 with history, < 2^30 */
+    int32_t  history_cols;         /* >= 1 with history, < 2^30.  Which kernels take the call, and how large their tables are, goes by this and not by
+                                      the lengths: room far beyond the longest history costs time */
     int32_t  n_allowed;            /* rows of allowed, >= 1 with it */
     const int32_t* history_len;    /* [batch], NULL => history_cols; clamped to [0, history_cols] */
     const int32_t* prompt_len;     /* [batch], NULL => 0; clamped to [0, history_len] */
@@ -564,9 +566,10 @@ typedef struct cadd_adjust_args {
  * token (without CADD_DISTILL_REST: no mass): loss 0, stats 0, gradient 0, whatever the logits hold.
  * stats[b,i] = (m, Z, m', Z'): m the largest logit of the row, Z = sum_v exp((s_v - m) / T); m' and Z' the same over the tokens that
  * are not listed (-Inf and 0 where there are none).  cadd_distill_grad reads them instead of passing over the logits twice.
- * Logits of -Inf (and below -1e30) have probability 0; a row without any other gives NaN, as do NaN and +Inf in the logits or entries, and as a
+ * Logits of -Inf (and below -1e30 as an fp32 number) have probability 0; a row without any other gives NaN, as do NaN and +Inf in the logits or entries, and as a
  * row may whose largest logit over T is beyond 5e29 in magnitude.
- * Exponentials of the logits are fp32, their sums fp64, list and loss are fp64; the gradient is rounded once.
+ * Exponentials of the logits are fp32 (arguments good to 2^-23 of a log2 unit where a term is large; partial sums of up to 32 terms, too), their sums
+ * fp64: Z and Z' are right to 2^-20.  List and loss are fp64; the gradient is rounded once.
  */
 #define CADD_DISTILL_REST 1u
 #define CADD_DISTILL_MAX_K 256

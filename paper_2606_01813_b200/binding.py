@@ -1048,10 +1048,10 @@ def cadd_adjust_logits(logits: torch.Tensor, *, n_nodes=None, token_ids=None, pa
     cadd_verify_tree_sampled or cadd_build_tree: each row by its own context, the history and, with token_ids / parent_idx
     (and n_nodes) of cadd_build_tree, the row's path.  Works in place unless `out` is given; rows above n_nodes keep what `out` held.
 
-    history int32 [batch, n] (rows may be strided) with history_len and prompt_len int32 [batch]: what stands before row 0's token;
-    the first prompt_len tokens count for repetition alone.  repetition, presence, frequency fp32 [batch].  bias_token int32,
+    history int32 [batch, n] (rows may be strided) with history_len and prompt_len int32 [batch]: what stands before row 0's token
+    (which counts itself where the tree was built with bonus_token); the first prompt_len tokens count for repetition alone.  repetition, presence, frequency fp32 [batch].  bias_token int32,
     bias fp32 [batch, n_bias].  allowed int32 [n_masks, ceil(V / 32)] (bit v % 32 of word v / 32), allowed_row int32 [batch, R],
-    -1 for rows without a mask.  status int32 [batch]."""
+    -1 for rows without a mask (of no masks at all, n_masks 0, it is not looked at).  status int32 [batch]."""
     dev, index, code = _logits_of(logits, "logits")
     B, R, V = shape = logits.shape
     lp, sb, sr = _need_logits(logits, shape, logits.dtype, index, "logits")

@@ -486,3 +486,32 @@ def test_gradient_alone_when_a_wait_runs_out(V):
     stats, st = G.cadd_distill_loss(x, t, v, **kw).stats, torch.zeros(2, dtype=torch.int32, device="cuda")
     g = G.cadd_distill_grad(x, t, v, stats, status=st, flags=G.FLAG_TEST_DROP_TILE, grad=torch.zeros_like(x), **kw)
     assert st.tolist() == [G.STATUS_INTERNAL_TIMEOUT] * 2 and bool(torch.isnan(g).all())
+
+
+def test_lists_of_the_accepted_rows_alone():
+    """The target's rows along the accepted path gathered first, and their lists made: the same tokens as in the lists of all rows by the path (log-probabilities
+    differ in how a row's sum was cut), and the loss and gradient that they stand for."""
+    batch, R, L, V, K = 5, 17, 6, 4001, 7
+    g = torch.Generator().manual_seed(23)
+    target, draft = torch.randn(batch, R, V, generator=g).cuda(), torch.randn(batch, L, V, generator=g).cuda().requires_grad_(True)
+    nodes, lens = torch.full((batch, L), -1, dtype=torch.int32, device="cuda"), i32([0, 1, 4, 6, 5]).cuda()
+    for b, n in enumerate(lens.tolist()):
+        nodes[b, :n] = torch.randperm(R - 1, generator=g)[:n].sort().values.int().cuda() + 1
+    rows = torch.cat([nodes.new_zeros(batch, 1), nodes[:, :L - 1].clamp(min=0)], 1).long()
+    accepted = target[torch.arange(batch, device=rows.device)[:, None], rows]
+    lists = G.cadd_build_tree(accepted.view(batch * L, 1, V), K, 0, cost_coef=torch.ones(batch * L, 4), flags=G.FLAG_EMIT_TOPK)
+    tok, logp, n_rows = lists.topk_token.view(batch, L, K), lists.topk_logprob.view(batch, L, K), (lens + 1).clamp(max=L)
+    d = G.cadd_distill_loss(draft.detach(), tok, logp, rest=True, n_rows=n_rows, grad=True)
+    q = Distill(draft.detach().cpu(), tok.cpu(), logp.cpu(), rest=True, n_rows=n_rows.cpu())
+    expected = plain_distill(q)
+    check_loss(d.loss, d.stats, q, expected)
+    check_grad(d.grad, expected)
+    assert d.status.tolist() == [0] * batch and int((d.loss != 0).sum()) == int(n_rows.sum())
+    draft.backward(d.grad)
+    assert torch.equal(draft.grad, d.grad)
+    every_row = G.cadd_build_tree(target.view(batch * R, 1, V), K, 0, cost_coef=torch.ones(batch * R, 4), flags=G.FLAG_EMIT_TOPK)
+    all_tok, all_logp = every_row.topk_token.view(batch, R, K), every_row.topk_logprob.view(batch, R, K)
+    assert torch.equal(torch.gather(all_tok, 1, rows[..., None].expand(-1, -1, K)), tok)
+    by_path = G.cadd_distill_loss(draft.detach(), all_tok, all_logp, rest=True, path=nodes, path_len=lens, grad=True)
+    check_grad(by_path.grad, plain_distill(Distill(draft.detach().cpu(), all_tok.cpu(), all_logp.cpu(), rest=True, path=nodes.cpu(), path_len=lens.cpu())))
+    assert torch.equal(by_path.loss != 0, d.loss != 0)
