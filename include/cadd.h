@@ -587,7 +587,8 @@ typedef struct cadd_distill_args {
     const double*  teacher_logit;  /* [batch, R, K] logits or log-probabilities */
     const double*  teacher_lse;    /* [batch, R], CADD_DISTILL_REST only; may be NULL */
     const int32_t* path;           /* [batch, path_cols] or NULL (then R >= L) */
-    const int32_t* path_len;       /* [batch], required with path; clamped to [0, min(L-1, path_cols)] */
+    const int32_t* path_len;       /* [batch], required with path; clamped to [0, min(L-1, path_cols)] (an accepted_len of L as well: its last node predicts
+                                      behind the drafter's positions; it is flagged like any other) */
     const int32_t* n_rows;         /* [batch] without path; NULL => L; clamped to [0, L] */
     const float* weight;           /* [batch, L], NULL => 1 */
     const float* grad_loss;        /* [batch, L], NULL => 1 */

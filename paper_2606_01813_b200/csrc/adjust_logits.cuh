@@ -8,8 +8,9 @@
 // computed before the list's and written after them, from the input's value and their own count.
 //
 // With few rows a table for every tile is not worth its while: then adjust_stream_kernel copies and masks, and adjust_tokens_kernel
-// replaces single tokens in memory afterwards, a CTA for all tokens of a request (a hash table in shared memory, which fills
-// while the kernel before it still runs).  In place the former writes (and reads) only what masks change: masks alone are its, too.
+// replaces single tokens in memory afterwards, a CTA for all tokens of a request (a hash table in shared memory).  Its launch is under way
+// while the kernel before it still runs, no more: a CTA wants an SM's whole register file and up to 200 KB of shared memory, and begins where the copying
+// CTAs have left.  In place the former writes (and reads) only what masks change: masks alone are its, too (six CTAs an SM, for which it spills 56 bytes).
 //
 // What bounds it.  32 trees of up to 65 rows of 151936, bf16, histories of 4000 (779 MB): 141 us, 5.5 TB/s; issue 64 % (logic 55 %: masks), DRAM 64 % of
 // nominal.  8 trees of up to 257 rows of 32001 in fp32, histories of 32768 (382 MB): 108 us, 3.5 TB/s; half of all tokens are replaced, in 64 bits, and

@@ -107,7 +107,8 @@ static int launch_tokens(AdjustParams& p, cudaStream_t st) {
 // run at once: one launch is less than two (one token, 5.8 against 6.2; 65 rows of one request in place 13 against 28).  Otherwise from
 // four rows a request on (32 requests, histories of 4000: one row 26 against 14, two 26 / 19, three 28 / 25, four 30 / 32, six 40 / 50).
 // In place without masks, when it has to write all that it reads, also not where few tokens can be concerned (32 requests of 65 rows: histories
-// of 100 tokens 202 against 51, of 4000 211 / 256; with masks 226 / 452).
+// of 100 tokens 202 against 51, of 4000 211 / 256; with masks 226 / 452).  That border lies somewhere between these two histories, of one vocabulary and
+// one tree size; it leaves out that single tokens take longer with more rows.  All goes by the room for a history: its lengths are on the device.
 constexpr int kFewRows = 4, kFewTokens = 40;              // one token of so many
 static bool by_tables(const AdjustParams& p, bool in_place) {
     const int64_t history = p.penalised && p.history ? p.history_cols : 0;

@@ -5,8 +5,8 @@
 // small steps:
 //   producer   sends for the tiles, row after row, as stages fall free;
 //   prepare    a row's list, a row ahead: the target's probabilities, the drafter's logits of the listed tokens, where they lie in the segment;
-//   compute    (20 warps) adds up the exponentials of the tokens that are not listed, relative to a power of two at or above the
-//              largest: a listed token counts as -Inf there, and goes into the row's statistics by itself, in fp64, so the
+//   compute    (20 warps) adds up the exponentials of the tokens that are not listed, relative to a power of two near the
+//              largest (see DistillSum): a listed token counts as -Inf there, and goes into the row's statistics by itself, in fp64, so the
 //              rest's probability is right even where the listed tokens leave all but nothing; then, where the gradient is
 //              wanted, forms it from the tiles: the row's last ones have stayed, as many as the ring holds, and the others come once more,
 //              from L2, where there are never more rows than SMs;
@@ -14,12 +14,13 @@
 //              loss and the two factors that the gradient needs.
 // The gradient alone (statistics given, no exchange) passes over the tiles once.
 //
-// What bounds it.  Losses alone: 1728 rows of 151936 in bf16 (526 MB) take 98 us, 5.4 TB/s; the exponential unit has 16 ex2 a clock of an SM, which
-// is 68 % busy over the whole launch (DRAM 60 % of nominal).  Doing an eighth of them or more on the FMA pipes instead, as polynomials
+// What bounds it.  Losses alone: 1728 rows of 151936 in bf16 (526 MB) take 102 us, 5.2 TB/s; the exponential unit has 16 ex2 a clock of an SM, which
+// is 66 % busy over the whole launch (DRAM 59 % of nominal).  Doing an eighth of them or more on the FMA pipes instead, as polynomials
 // in packed fp32, was slower (103 -> 111: packed operations have only half of those pipes), and so was more CTAs an SM.  With the gradient:
-// 2048 rows, 1245 MB, 242 us, 5.1 TB/s; the unit 61 % busy, and writes, which alone reach 3.8 to 4.0 TB/s here.  Both exponentials of an element
-// are computed: kept ones would need fp32 tiles twice as large.  512 rows of 100003 in fp32: 91 us, 4.5 TB/s, of which a sixth
-// is that 512 rows are not a multiple of the SMs.  Few rows: chains of loads and 64-bit steps, 9 us.
+// 2048 rows, 1245 MB, 246 us, 5.1 TB/s; the unit 60 % busy, and writes, which alone reach 3.8 to 4.0 TB/s here.  Both exponentials of an element
+// are computed: kept ones would need fp32 tiles twice as large.  512 rows of 100003 in fp32: 88 to 93 us, 4.5 TB/s, of which a sixth
+// is that 512 rows are not a multiple of the SMs.  Few rows: chains of loads and 64-bit steps, 9.4 us.  (All as replayed from a graph; called one
+// after another with other inputs each time, 103 to 108 and 249 to 259 us for the first two.)
 // All waits are bounded; a CTA in which one runs out leaves NaN in its rows from there on.
 #pragma once
 #include "common.cuh"
